@@ -336,6 +336,95 @@ adaspark_status_t adaspark_attn_set_prefill_kernel(adaspark_attn_t *handle, int3
 adaspark_status_t adaspark_attn_set_gather(adaspark_attn_t *handle, float pairs_per_block,
                                            uint64_t budget_bytes);
 
+/* ---- Text beside the video ------------------------------------------------------------------------------------------
+ * Requests, or turns of a conversation, that are text only: causal attention of whole prompts packed one behind the other, a
+ * paged cache of their keys and values (bf16 or 8 bits), and a decode step over its pages.  Of the handle they use the heads,
+ * head_dim, softmax_scale and device; no _partition is needed.  Query head h uses KV head h / (Hq/Hkv).
+ *
+ * Conventions of these calls
+ *   - Rows (q, k, v, q_new, ...) are bf16 [tokens][heads][head_dim] at any token and head stride (in elements, multiples of 8, at
+ *     least head_dim; 0: dense), so that slices of a fused projection or head-major tensors are read where they are; 16-byte
+ *     aligned.  Outputs are dense.
+ *   - Packed sequences: cu is device int32 [batch + 1], not decreasing; sequence b is the rows cu[b] .. cu[b+1] - 1 and may be
+ *     empty.  Rows of the tensors that belong to no sequence (in front of cu[0], behind cu[batch]) are neither read nor written.
+ *   - kv_len is device int32 [batch]: tokens of each sequence INCLUDING those of this call.  block_table is device int32
+ *     [batch][table_width]: the page of tokens [c * page_size, (c + 1) * page_size) in column c; columns behind the last
+ *     token are not read.
+ *   - status (nullable) is a device int32 that a call sets when it finds something wrong on the device, and leaves alone
+ *     otherwise (clear it yourself): 1 = a cu, kv_len or page number out of range; 6 = a bounded wait expired.  What
+ *     is out of range is never read or written; each call says what it yields instead.
+ *   - The caller's current device is current again when a call returns.  workspace: 256-byte aligned device scratch of
+ *     adaspark_attn_text_workspace_bytes; nothing in it has to be initialised, nothing is kept in it between calls, and calls
+ *     that may overlap on the GPU (also captured ones) need one each.
+ *   - batch = 0 or no rows: the call does nothing. */
+typedef enum { ADASPARK_PAGES_BF16 = 0, ADASPARK_PAGES_E4M3 = 1 } adaspark_page_format_t;
+
+/* A paged cache: n_pages pages of page_size tokens (16, 32, 64, 128 or 256), keys and values
+ * [n_pages][n_kv_heads][page_size][head_dim] in bf16, or in e4m3 with a byte s per token and head in
+ * [n_pages][n_kv_heads][page_size]: a stored code c stands for c * 2^(s - 127).  Writing takes the smallest s (0 .. 247) with
+ * max|x| <= 448 * 2^(s - 127) over the finite values of the row and rounds to nearest (ties to even): off by at most 2^-4 of a value, or by
+ * 2^(s - 137) of the smallest.  An infinite value is stored as NaN (e4m3 has no infinity). */
+typedef struct {
+    void *k_pages, *v_pages;  /* 16-byte aligned                                                       */
+    uint8_t *k_scale, *v_scale; /* e4m3: 16-byte aligned; bf16: ignored                                */
+    int64_t page_stride;      /* elements from page to page of k_pages and v_pages (0: dense)          */
+    int64_t scale_stride;     /* bytes from page to page of k_scale and v_scale (0: dense)             */
+    int32_t n_pages, page_size;
+    int32_t format;           /* adaspark_page_format_t                                                */
+    int32_t reserved;
+} adaspark_attn_pages_t;
+
+/* Bytes of workspace for adaspark_attn_prompt and adaspark_attn_paged_decode with this handle (of any batch and length). */
+int64_t adaspark_attn_text_workspace_bytes(const adaspark_attn_t *handle);
+
+/* Causal attention over whole prompts.  Sequence b has n_q = cu_q[b+1] - cu_q[b] query rows and n_k = cu_k[b+1] - cu_k[b]
+ * keys; its row i sees the keys 0 .. n_k - n_q + i (cu_k = cu_q: a prompt from its first token; n_k > n_q: a prompt that
+ * continues tokens whose keys and values are given too, e.g. by adaspark_attn_paged_read; n_k < n_q: the first rows see nothing).
+ *   q, k, v      in : n_q, n_k: rows of q / out and of k / v that the tensors hold.
+ *   out          out: bf16 [n_q][Hq][head_dim]; zeros for a row that sees nothing.
+ *   lse          out, nullable: fp32 [n_q][Hq], the natural logarithm of the sum of the exponentials of the row's scaled
+ *                     scores; -infinity for a row that sees nothing.
+ * Keys and values that a row does not see do not reach it, whatever they hold (infinities and NaN included). */
+adaspark_status_t adaspark_attn_prompt(adaspark_attn_t *handle, const void *q, int64_t q_token_stride, int64_t q_head_stride,
+                                       const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v,
+                                       int64_t v_token_stride, int64_t v_head_stride, const int32_t *cu_q,
+                                       const int32_t *cu_k, int32_t batch, int32_t n_q, int32_t n_k, void *out, float *lse,
+                                       void *workspace, size_t workspace_bytes, int32_t *status, void *cuda_stream);
+
+/* Writes the keys and values of packed rows into their pages: row cu[b] + i of sequence b becomes token
+ * kv_len[b] - (cu[b+1] - cu[b]) + i.  n: rows that k and v hold.  A row without a place (before token 0, behind the table, page number
+ * outside [0, n_pages)) is not written and sets status 1.  Two rows with the same place in one call: either may win. */
+adaspark_status_t adaspark_attn_paged_write(adaspark_attn_t *handle, const adaspark_attn_pages_t *pages, const void *k,
+                                            int64_t k_token_stride, int64_t k_head_stride, const void *v,
+                                            int64_t v_token_stride, int64_t v_head_stride, const int32_t *cu, int32_t batch,
+                                            int32_t n, const int32_t *block_table, int32_t table_width, const int32_t *kv_len,
+                                            int32_t *status, void *cuda_stream);
+
+/* Reads the last cu[b+1] - cu[b] tokens of every sequence back: k_out, v_out dense bf16 [n][Hkv][head_dim], laid out as the rows of
+ * adaspark_attn_paged_write.  Exact: every value that a page holds is a bf16 number.  A row without a place reads zeros and
+ * sets status 1. */
+adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t *handle, const adaspark_attn_pages_t *pages, const int32_t *cu,
+                                           int32_t batch, int32_t n, const int32_t *block_table, int32_t table_width,
+                                           const int32_t *kv_len, void *k_out, void *v_out, int32_t *status,
+                                           void *cuda_stream);
+
+/* One new token per sequence: the row q of sequence b attends the tokens 0 .. kv_len[b] - 1 of its pages.
+ *   q            in : bf16 [batch][Hq][head_dim].
+ *   k_new, v_new in, nullable: bf16 [batch][Hkv][head_dim], the new token's; written as token kv_len[b] - 1 and attended as
+ *                     the pages hold them.  NULL: they are there already.
+ *   kv_len       in : 0 marks a slot of the batch without a sequence (nothing is appended).
+ *   out, lse     out: as adaspark_attn_prompt, [batch][Hq]; zeros and -infinity where kv_len is 0, where kv_len is negative
+ *                     or more than the table holds, and where a page number among the tokens is outside [0, n_pages) (the last two set
+ *                     status 1 and append nothing into a place that is not there).
+ * Two sequences may share pages that neither of them appends to. */
+adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t *handle, const void *q, int64_t q_token_stride,
+                                             int64_t q_head_stride, const void *k_new, int64_t k_token_stride,
+                                             int64_t k_head_stride, const void *v_new, int64_t v_token_stride,
+                                             int64_t v_head_stride, const adaspark_attn_pages_t *pages,
+                                             const int32_t *block_table, int32_t table_width, const int32_t *kv_len,
+                                             int32_t batch, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                                             int32_t *status, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

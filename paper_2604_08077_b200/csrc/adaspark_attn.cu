@@ -1012,6 +1012,8 @@ extern "C" adaspark_status_t adaspark_attn_decode_static(adaspark_attn_t* h, con
                                 (size_t)ADASPARK_ATTN_STATIC_SCRATCH_BYTES, cuda_stream);
 }
 
+#include "text_entry.cuh"
+
 // ---------------------------------------------------------------------------------------------
 // Diagnostics (include/adaspark_attn_debug.h)
 // ---------------------------------------------------------------------------------------------
