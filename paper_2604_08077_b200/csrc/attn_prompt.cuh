@@ -1,48 +1,662 @@
-// Causal attention of whole prompts, packed one behind the other: a warp per (row, query head).
+// Causal attention over whole prompts, packed one behind the other, on the 5th-generation tensor cores.
+//
+//   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = 2^(scale_log2 q_i.k_j - m_i),  j <= n_k - n_q + i
+//
+// One pass over the keys with a running reference m_i and sum, scores and weights in tensor memory alone.  Work is dealt out in
+// tiles of 256 rows, a CTA pair (cta_group::2) each: the rows are (token, head of the group) pairs, 128 / G tokens per CTA, so that
+// K and V are read once for all heads of a group, a sequence of a few tokens fills rows that it would leave empty head by head, and
+// the diagonal wastes little (256 rows of a group of 7 are 36 tokens: 2 % of the scores of 8192 tokens lie above it, 256 tokens of one head: 4.7 %).
+//
+// Roles of a CTA (512 threads), coupled by barriers alone, so that set-up, loads and first scores of the next tile overlap the end of
+// the present one:
+//   warps 0-11  softmax, three warpgroups that take the steps of 128 keys in turn (thread = row = TMEM lane)
+//   warp  12    TMA producer of K
+//   warp  13    MMA issuer (CTA 0): S = Q K^T, O += P V (P in TMEM, V with its rows along d); CTA 1: passes on that its Q is there
+//   warp  14    producer of V
+//   warp  15    planner: the next tile and its Q
+// TMEM (512 columns): three score tiles of 128 columns, the weights (bf16 pairs) over the first 64 of each, and O.  The waits are
+// those of the prefill kernel (attn_prefill_tc.cuh): the issuer never waits for a tile that it has not begun while a product of an
+// earlier one is still to be issued.
+//
+// Tiles are dealt longest first and back and forth over the pairs of CTAs.  Every planner works the order out for itself from cu_q and
+// cu_k, level by level of the number of steps: no list in memory, no counter, one launch, and nothing to be cleared before it.
+//
+// A weight of zero does not hide a value that is no number: 0 * inf is one too.  Steps in which a row of the tile does not see a key
+// (the last one to three of a tile) therefore go over V in shared memory before the tensor core reads it: what is infinite or no
+// number is replaced by zero, and if it belongs to the sequence, the rows that do see it get it added at the end.
 #pragma once
-#include "common.cuh"
+#include <type_traits>
+
+#include "tc_common.cuh"
 
 namespace adaspark {
 
-// Row i of a sequence with n_q rows and n_k keys sees the keys 0 .. n_k - n_q + i.
+constexpr int kPromptGroups = 3;                              // softmax warpgroups
+constexpr int kPromptThreads = (kPromptGroups + 1) * 128;
+constexpr int kPromptSoftmaxRegs = 144, kPromptHelperRegs = 80;
+static_assert(kPromptGroups * 128 * kPromptSoftmaxRegs + 128 * kPromptHelperRegs <= kPromptThreads * 128, "setmaxnreg must stay inside the CTA's launch allocation");
+constexpr int kPromptBufs = 3;                                // score tiles in TMEM, one per warpgroup
+constexpr int kPromptRefSlots = 4;
+constexpr int kPromptOddSlots = 8;                            // more than tiles whose V can be under way at once (a step each)
+__host__ __device__ constexpr int prompt_stages(int D) { return D == 64 ? 6 : 3; }
+static_assert(prompt_stages(64) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
+
+// 2^x on the FMA pipe (every 8th exponential of steps without a mask; MUFU gives 16 a cycle and is the busier pipe): 2^f on
+// [-0.5, 0.5] by a minimax polynomial of degree 4 (relative error 2.6e-6), n through a multiplication, so that what is no number stays
+// one.  x is clamped at -125: a weight that would vanish is 2^-125 beside a largest one of at least 2^-8.
+__device__ __forceinline__ float poly_exp2(float x) {
+    float xc;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(xc) : "f"(x), "f"(-125.f));
+    const float xr = xc + 12582912.f;                         // 1.5 * 2^23: the low mantissa bits hold n = round(x)
+    const float f = xc - (xr - 12582912.f);
+    const float p = fmaf(fmaf(fmaf(fmaf(0.0095701f, f, 0.05591786f), f, 0.24024745f), f, 0.69312181f), f, 0.99999926f);
+    return p * __uint_as_float((__float_as_uint(xr) << 23) + 0x3f800000u);
+}
+
+// What one call works on.
+struct PromptGeom {
+    const int32_t *cu_q, *cu_k;
+    int batch, n_q, n_k;
+    int Hq, Hkv, G;
+    int T;                      // tokens of a CTA: 128 / G
+    FastDiv div_w, div_g, div_kv;   // by 2 T, G, Hkv
+    float scale_log2;
+    const __nv_bfloat16* v;     // for values that are no numbers
+    long long v_ts, v_hs;
+};
+
+struct PromptTile {
+    int q0, n_tok;              // this CTA's first row of q and its tokens (the pair's first CTA may have all)
+    int k0;                     // first key row of the sequence
+    int last0;                  // last key that this CTA's first token sees (-1 and less: none)
+    int gk;
+    int n_steps, first_masked;  // steps of 128 keys; from this one on rows are masked
+};
+
+// A sequence as a planner sees it; one that leaves the tensors has no tiles.
+struct PromptSeq {
+    int q0, k0, nq, nk, off, nt;
+    __device__ __forceinline__ bool load(const PromptGeom& g, int b) {
+        const int a0 = g.cu_q[b], a1 = g.cu_q[b + 1], b0 = g.cu_k[b], b1 = g.cu_k[b + 1];
+        const bool valid = 0 <= a0 && a0 <= a1 && a1 <= g.n_q && 0 <= b0 && b0 <= b1 && b1 <= g.n_k;
+        q0 = a0;
+        k0 = b0;
+        nq = valid ? a1 - a0 : 0;
+        nk = valid ? b1 - b0 : 0;
+        off = nk - nq;
+        nt = nq > 0 ? g.div_w.div(nq + 2 * g.T - 1) : 0;
+        return valid;
+    }
+    // tiles whose last row sees at most x keys
+    __device__ __forceinline__ int tiles_up_to(const PromptGeom& g, int x) const {
+        return x >= nk ? nt : x <= off ? 0 : min(g.div_w.div(x - off), nt);
+    }
+};
+
 template <int D>
-__global__ void __launch_bounds__(128) attn_prompt_kernel(const __nv_bfloat16* q, long long q_ts, long long q_hs, const __nv_bfloat16* k, long long k_ts,
-                                                          long long k_hs, const __nv_bfloat16* v, long long v_ts, long long v_hs, const int32_t* cu_q,
-                                                          const int32_t* cu_k, int batch, int n_q, int n_k, int Hq, int G, float scale_log2,
-                                                          __nv_bfloat16* out, float* lse, int32_t* status) {
-    constexpr int kPer = D / 32;
+struct PromptSmem {
+    __nv_bfloat16 q[2][D / 64][128][64];                      // [tile & 1][d panel][row][64 d]
+    __nv_bfloat16 kv[2 * prompt_stages(D)][64 * D];           // K: [d panel][this CTA's 64 keys][64 d]; V: [128 keys][this CTA's half of d]
+    unsigned char out[128][2 * D + 16];
+    float ref[kPromptRefSlots][128];
+    float part_l[2][kPromptGroups][128], part_m[2][kPromptGroups][128];
+    uint64_t q_full[2], q_peer[2], q_empty[2], k_full[prompt_stages(D)], k_empty[prompt_stages(D)], v_full[prompt_stages(D)], v_empty[prompt_stages(D)];
+    uint64_t v_raw, s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], o_full, o_free;
+    uint64_t plan_full[2], plan_empty[2], part_full[2], part_free[2], out_free;
+    PromptTile tile[2];
+    int odd_tile[kPromptOddSlots];                            // number + 1 of a tile with masked values that are no numbers
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+template <int D>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) attn_prompt_kernel(
+    PromptGeom g, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+    __nv_bfloat16* out, float* lse, int32_t* status) {
+    extern __shared__ unsigned char prompt_smem_raw[];
+    PromptSmem<D>& sm = *reinterpret_cast<PromptSmem<D>*>((reinterpret_cast<uintptr_t>(prompt_smem_raw) + 1023) & ~(uintptr_t)1023);
+    constexpr int kPanels = D / 64, kQKSteps = D / 16, kStages = prompt_stages(D);
+    constexpr uint32_t kIdescS = tc::make_idesc_bf16(256, 128);
+    constexpr uint32_t kIdescO = tc::make_idesc_bf16(256, D) | (1u << 16);   // B = V: rows along N
+    constexpr uint32_t kTileBytes = 64 * D * 2;               // a CTA's share of the K or V of a step
+    constexpr int kVRow = D;                                  // bytes of a key in a CTA's share of V (half of d)
+    constexpr int kKWarp = kPromptGroups * 4, kMmaWarp = kKWarp + 1, kVWarp = kKWarp + 2, kPlanWarp = kKWarp + 3;
+    constexpr uint32_t kOCol = kPromptBufs * 128;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = (int)(blockIdx.x & 1u), n_pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
+
+    // ---------------------------------------------------------------- set-up
     launch_dependents();
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(&sm.q_full[i], 1);
+            tc::mbar_init(&sm.q_peer[i], 1);
+            tc::mbar_init(&sm.q_empty[i], 1);
+            tc::mbar_init(&sm.plan_full[i], 1);
+            tc::mbar_init(&sm.plan_empty[i], 3 + kPromptGroups * 4);
+            tc::mbar_init(&sm.part_full[i], (kPromptGroups - 1) * 4);
+            tc::mbar_init(&sm.part_free[i], 4);
+        }
+        for (int i = 0; i < kStages; ++i) {
+            tc::mbar_init(&sm.k_full[i], 1);
+            tc::mbar_init(&sm.k_empty[i], 1);
+            tc::mbar_init(&sm.v_full[i], 2);                  // the V warps of both CTAs
+            tc::mbar_init(&sm.v_empty[i], 1);
+        }
+        for (int i = 0; i < kPromptBufs; ++i) {
+            tc::mbar_init(&sm.s_full[i], 1);
+            tc::mbar_init(&sm.p_full[i], 8);
+        }
+        for (int i = 0; i < kPromptRefSlots; ++i)
+            for (int w = 0; w < 4; ++w) tc::mbar_init(&sm.ref_done[i][w], 1);
+        for (int i = 0; i < kPromptOddSlots; ++i) sm.odd_tile[i] = 0;
+        tc::mbar_init(&sm.v_raw, 1);
+        tc::mbar_init(&sm.o_full, 1);
+        tc::mbar_init(&sm.o_free, 8);
+        tc::mbar_init(&sm.out_free, 4);
+        sm.abort_flag = 0;
+        tc::fence_barrier_init();
+        tc::prefetch_tensormap(&tmQ);
+        tc::prefetch_tensormap(&tmK);
+        tc::prefetch_tensormap(&tmV);
+    }
+    __syncwarp();
     wait_for_previous_kernel();
-    const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31, row = (int)(w / Hq), h = (int)(w % Hq), gk = h / G;
-    if (row >= n_q) return;
-    int seq = -1;
-    for (int i = 0; i < batch; ++i) {
-        const bool valid = 0 <= cu_q[i] && cu_q[i] <= cu_q[i + 1] && cu_q[i + 1] <= n_q && 0 <= cu_k[i] && cu_k[i] <= cu_k[i + 1] && cu_k[i + 1] <= n_k;
-        if (!valid && status != nullptr) atomicExch(status, 1);
-        if (valid && row >= cu_q[i] && row < cu_q[i + 1]) seq = i;
+    // (not before the wait: a CTA of the previous kernel that is still to allocate would wait for this one)
+    if (warp == kMmaWarp) tc::tmem_alloc_pair<512>(&sm.tmem_base);
+    tc::tc_fence_before_sync();
+    cluster_sync();
+    tc::tc_fence_after_sync();
+    const uint32_t tbase = sm.tmem_base;
+    volatile int* abort_flag = &sm.abort_flag;
+
+    if (warp >= kKWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kPromptHelperRegs));
+    if (warp == kPlanWarp) {
+        // ------------------------------------------------------------ planner
+        const int W = 2 * g.T;
+        // the most steps of a tile; sequences that leave the tensors are reported
+        int level = 0;
+        for (int b0 = 0; b0 < g.batch; b0 += 32) {
+            PromptSeq s;
+            bool bad = false;
+            if (b0 + lane < g.batch) {
+                bad = !s.load(g, b0 + lane);
+                if (s.nt > 0) level = max(level, max(1, (s.nk + 127) >> 7));
+            }
+            if (bad && blockIdx.x == 0 && status != nullptr) atomicExch(status, 1);
+        }
+        level = (int)__reduce_max_sync(0xffffffffu, (unsigned)level);
+        int chunk = 0, base = 0;                              // number of the first item of (level, chunk)
+        for (int k = 0;; ++k) {
+            const int slot = k & 1;
+            const int rank_of = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
+            if (!tc::mbar_wait(&sm.plan_empty[slot], ((k >> 1) & 1) ^ 1u, abort_flag)) break;
+            // ---- item `rank_of`: levels from many steps to few, sequences in order, tiles, kv heads
+            bool found = false;
+            PromptTile t;
+            while (level > 0) {
+                PromptSeq s;
+                int first = 0, n = 0;
+                const int b = chunk * 32 + lane;
+                if (b < g.batch) {
+                    s.load(g, b);
+                    first = level == 1 ? 0 : s.tiles_up_to(g, 128 * (level - 1));
+                    n = (s.tiles_up_to(g, 128 * level) - first) * g.Hkv;
+                }
+                int upto = n;
+#pragma unroll
+                for (int x = 1; x < 32; x <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, upto, x);
+                    if (lane >= x) upto += y;
+                }
+                const int total = __shfl_sync(0xffffffffu, upto, 31);
+                if (rank_of < base + total) {
+                    const int who = __ffs(__ballot_sync(0xffffffffu, base + upto > rank_of)) - 1;
+                    const int mine = rank_of - base - (upto - n);      // the owner's own count
+                    int tt, gk;
+                    g.div_kv.divmod(max(mine, 0), tt, gk);
+                    tt += first;
+                    const int tok = tt * W + rank * g.T, see = s.off + tt * W;   // see: the last key of the pair's first token
+                    t.q0 = s.q0 + tok;
+                    t.n_tok = min(max(s.nq - tok, 0), g.T);
+                    t.k0 = s.k0;
+                    t.last0 = s.off + tok;
+                    t.gk = gk;
+                    t.n_steps = level;
+                    t.first_masked = max(see + 1, 0) >> 7;
+                    if (lane == who) sm.tile[slot] = t;
+                    t.q0 = __shfl_sync(0xffffffffu, t.q0, who);
+                    t.gk = __shfl_sync(0xffffffffu, t.gk, who);
+                    found = true;
+                    break;
+                }
+                base += total;
+                if (++chunk * 32 >= g.batch) {
+                    chunk = 0;
+                    --level;
+                }
+            }
+            if (!found) {
+                if (lane == 0) {
+                    sm.tile[slot].n_steps = 0;                // no more
+                    tc::mbar_arrive(&sm.plan_full[slot]);
+                }
+                break;
+            }
+            if (!tc::mbar_wait(&sm.q_empty[slot], ((k >> 1) & 1) ^ 1, abort_flag)) break;
+            __syncwarp();
+            if (lane == 0) {
+                // rows (token, head of the group); tokens behind the tensor read zeros, those of the next sequence are not stored
+                tc::mbar_arrive_expect_tx(&sm.q_full[slot], (uint32_t)(g.T * g.G) * D * 2);
+                for (int p = 0; p < kPanels; ++p) tc::tma_load_3d(&sm.q[slot][p][0][0], &tmQ, p * 64, t.gk * g.G, t.q0, &sm.q_full[slot]);
+                tc::mbar_arrive(&sm.plan_full[slot]);
+            }
+            __syncwarp();
+        }
+    } else if (warp == kKWarp) {
+        // ------------------------------------------------------------ K: CTA r fetches the keys r * 64 .. of a step
+        if (tc::elect_one()) {
+            const uint32_t bar0 = cluster_address(sm.k_full, 0);
+            int st = 0, ph = 1;
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                const int slot = k & 1;
+                if (!(ok = tc::mbar_wait(&sm.plan_full[slot], (k >> 1) & 1, abort_flag))) break;
+                const int n_steps = sm.tile[slot].n_steps, row0 = sm.tile[slot].k0 + rank * 64, gk = sm.tile[slot].gk;
+                if (n_steps == 0) break;
+                for (int j = 0; j < n_steps; ++j) {
+                    if (!(ok = tc::mbar_wait(&sm.k_empty[st], ph, abort_flag))) break;
+                    if (rank == 0) tc::mbar_arrive_expect_tx(&sm.k_full[st], 2 * kTileBytes);
+                    for (int p = 0; p < kPanels; ++p)
+                        tc::tma_load_3d_pair(&sm.kv[st][p * 64 * 64], &tmK, p * 64, gk, row0 + j * 128, bar0 + st * 8);
+                    if (++st == kStages) { st = 0; ph ^= 1; }
+                }
+                tc::mbar_arrive(&sm.plan_empty[slot]);
+            }
+        }
+    } else if (warp == kVWarp) {
+        // ------------------------------------------------------------ V: CTA r fetches half r of d of a step's 128 keys
+        const uint32_t bar0 = cluster_address(sm.v_full, 0), odd0 = cluster_address(sm.odd_tile, 0), odd1 = cluster_address(sm.odd_tile, 1);
+        int st = 0, ph = 1, raw_ph = 0;
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            const int slot = k & 1;
+            if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k >> 1) & 1, abort_flag))) break;
+            const int n_steps = sm.tile[slot].n_steps, k0 = sm.tile[slot].k0, gk = sm.tile[slot].gk, first_masked = sm.tile[slot].first_masked;
+            if (n_steps == 0) break;
+            for (int j = 0; j < n_steps; ++j) {
+                if (!(ok = tc::mbar_wait_warp(&sm.v_empty[st], ph, abort_flag))) break;
+                unsigned char* tile = reinterpret_cast<unsigned char*>(&sm.kv[kStages + st][0]);
+                if (j < first_masked) {
+                    if (tc::elect_one()) {
+                        if (rank == 0) tc::mbar_arrive_expect_tx(&sm.v_full[st], 2 * kTileBytes);
+                        else tc::mbar_arrive_cluster(bar0 + st * 8);
+                        tc::tma_load_3d_pair(tile, &tmV, rank * (D / 2), gk, k0 + j * 128, bar0 + st * 8);
+                    }
+                } else {
+                    if (tc::elect_one()) {
+                        tc::mbar_arrive_expect_tx(&sm.v_raw, kTileBytes);
+                        tc::tma_load_3d(tile, &tmV, rank * (D / 2), gk, k0 + j * 128, &sm.v_raw);
+                    }
+                    if (!(ok = tc::mbar_wait_warp(&sm.v_raw, raw_ph, abort_flag))) break;
+                    raw_ph ^= 1;
+                    // exponents of all ones: adding 0x80 to (x & 0x7f80) carries into bit 15
+                    uint4* chunks = reinterpret_cast<uint4*>(tile);
+                    uint32_t any = 0;
+#pragma unroll 8
+                    for (int i = lane; i < (int)kTileBytes / 16; i += 32) {
+                        const uint4 x = chunks[i];
+                        any |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) | ((x.z & 0x7f807f80u) + 0x00800080u) |
+                               ((x.w & 0x7f807f80u) + 0x00800080u);
+                    }
+                    if (__any_sync(0xffffffffu, (any & 0x80008000u) != 0u)) {
+                        for (int i = lane; i < (int)kTileBytes / 16; i += 32) {
+                            uint32_t x[4] = {chunks[i].x, chunks[i].y, chunks[i].z, chunks[i].w};
+                            for (int e = 0; e < 4; ++e) {
+                                if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+                                if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
+                            }
+                            chunks[i] = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
+                        if (lane < 2)                         // (keys of other sequences among them: the rows look for themselves)
+                            asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"((lane ? odd1 : odd0) + (k % kPromptOddSlots) * 4), "r"(k + 1) : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
+                        tc::mbar_arrive_release_cluster(bar0 + st * 8);
+                    }
+                    __syncwarp();
+                }
+                if (++st == kStages) { st = 0; ph ^= 1; }
+            }
+            if (!ok) break;
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
+        }
+    } else if (warp == kMmaWarp && rank == 1) {
+        // ------------------------------------------------------------ CTA 1: Q is there, said to the issuing warp of CTA 0
+        if (lane == 0) {
+            for (int k = 0;; ++k) {
+                if (!tc::mbar_wait(&sm.plan_full[k & 1], (k >> 1) & 1, abort_flag) || sm.tile[k & 1].n_steps == 0) break;
+                if (!tc::mbar_wait(&sm.q_full[k & 1], (k >> 1) & 1, abort_flag)) break;
+                asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
+                tc::mbar_arrive_cluster(cluster_address(&sm.q_peer[k & 1], 0));
+                tc::mbar_arrive(&sm.plan_empty[k & 1]);
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------ MMA issuer
+        constexpr uint32_t kKStep = 32 >> 4;                                        // 16 elements of a 128-byte row
+        constexpr uint32_t kQPanelStep = (128 * 128) >> 4, kKPanelStep = (64 * 128) >> 4, kVStep = (16 * kVRow) >> 4;
+        constexpr uint32_t kQSlotStep = (uint32_t)sizeof(sm.q[0]) >> 4, kStageStep = (uint32_t)sizeof(sm.kv[0]) >> 4;
+        // V: rows of a key's 64 (D = 64: 32) values with the 128- (64-) byte swizzle, groups of 8 keys kVRow * 8 bytes apart
+        constexpr uint32_t kVDescHi = (uint32_t)((8 * kVRow) >> 4) | (1u << 14) | ((D == 128 ? 2u : 4u) << 29);
+        const uint32_t q_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.q[0][0][0][0])), 0);
+        const uint32_t k_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.kv[0][0])), 0);
+        const uint32_t v_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.kv[kStages][0])), 0);
+        const uint32_t tb = __shfl_sync(0xffffffffu, tbase, 0);
+        if (tc::elect_one()) {
+            bool ok = true, ended = false;
+            int ks = -1, s_left = 0, sbuf = 0, kst = 0, kph = 0, ahead = 0;
+            int n_steps0 = 0, n_steps1 = 0, n_steps2 = 0;         // steps of tiles ks, ks - 1, ks - 2
+            // S of the next step, if there is one (must: nothing else is left to issue, so the next tile is waited for)
+            auto next_scores = [&](bool must) -> bool {
+                if (s_left == 0) {
+                    if (ended) return false;
+                    const int kn = ks + 1, slot = kn & 1;
+                    auto there = [&](uint64_t* bar, uint32_t phase) -> bool { return must ? (ok = tc::mbar_wait(bar, phase, abort_flag)) : tc::mbar_test(bar, phase); };
+                    if (!there(&sm.plan_full[slot], (kn >> 1) & 1)) return false;
+                    if ((ended = sm.tile[slot].n_steps == 0)) return false;
+                    if (!there(&sm.q_full[slot], (kn >> 1) & 1) || !there(&sm.q_peer[slot], (kn >> 1) & 1)) return false;
+                    ks = kn;
+                    n_steps2 = n_steps1;
+                    n_steps1 = n_steps0;
+                    s_left = n_steps0 = sm.tile[slot].n_steps;
+                    tc::mbar_arrive(&sm.plan_empty[slot]);
+                }
+                if (!(ok = tc::mbar_wait(&sm.k_full[kst], kph, abort_flag))) return false;
+                tc::tc_fence_after_sync();
+                const uint32_t qa = q_lo0 + (ks & 1) * kQSlotStep, kb = k_lo0 + kst * kStageStep, dst = tb + sbuf * 128;
+#pragma unroll
+                for (int x = 0; x < kQKSteps; ++x)
+                    tc::umma_ss_pair(dst, tc::smem_desc_from_halves(qa + (x >> 2) * kQPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128),
+                                     tc::smem_desc_from_halves(kb + (x >> 2) * kKPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128), kIdescS, x > 0);
+                tc::umma_commit_pair(&sm.s_full[sbuf]);
+                tc::umma_commit_pair(&sm.k_empty[kst]);
+                if (--s_left == 0) tc::umma_commit_pair(&sm.q_empty[ks & 1]);
+                if (++sbuf == kPromptBufs) sbuf = 0;
+                if (++kst == kStages) { kst = 0; kph ^= 1; }
+                ++ahead;
+                return true;
+            };
+            int buf = 0, buf_ph = 0, vst = 0, vph = 0;
+            for (int k = 0; ok; ++k) {
+                int steps = 1;
+                for (int j = 0; j < steps; ++j) {
+                    while (ahead < kPromptBufs && next_scores(ahead == 0)) {}
+                    if (!ok || ahead == 0) { ok = false; break; }  // no more
+                    if (j == 0) steps = ks == k ? n_steps0 : ks == k + 1 ? n_steps1 : n_steps2;
+                    if (!(ok = tc::mbar_wait(&sm.v_full[vst], vph, abort_flag))) break;
+                    if (j == 0 && k > 0 && !(ok = tc::mbar_wait(&sm.o_free, (k - 1) & 1, abort_flag))) break;
+                    if (!(ok = tc::mbar_wait(&sm.p_full[buf], buf_ph, abort_flag))) break;
+                    tc::tc_fence_after_sync();
+                    const uint32_t vb = v_lo0 + vst * kStageStep, src = tb + buf * 128;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        tc::umma_ts_pair(tb + kOCol, src + x * 8, tc::smem_desc_from_halves(vb + x * kVStep, kVDescHi), kIdescO, x > 0 || j > 0);
+                    tc::umma_commit_pair(&sm.v_empty[vst]);
+                    if (j == steps - 1) tc::umma_commit_pair(&sm.o_full);
+                    if (++vst == kStages) { vst = 0; vph ^= 1; }
+                    if (++buf == kPromptBufs) { buf = 0; buf_ph ^= 1; }
+                    --ahead;
+                }
+            }
+        }
+    } else if (warp < kKWarp) {
+        // ------------------------------------------------------------ softmax warps
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kPromptSoftmaxRegs));
+        const int wg = warp >> 2, quad = warp & 3;
+        const int row = quad * 32 + lane;
+        const uint32_t lane_addr = tbase + ((uint32_t)(quad * 32) << 16);
+        const uint32_t s_addr = lane_addr + wg * 128;
+        const uint32_t p_bar = cluster_address(&sm.p_full[wg], 0), o_free_bar = cluster_address(&sm.o_free, 0);
+        const float scale_log2 = g.scale_log2;
+        const unsigned long long scale2 = pack_f32x2(scale_log2, scale_log2);
+        int tok, head;                                        // of the row
+        g.div_g.divmod(row, tok, head);
+        bool ok = true;
+        int g0 = 0;                                           // steps of the tiles before this one
+        uint32_t s_ph = 0;
+        bool out_pending = false;                             // the rows of an epilogue leave shared memory while this warpgroup goes on
+        auto release_out = [&]() {
+            if (out_pending) {
+                asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.out_free);
+                out_pending = false;
+            }
+        };
+        for (int k = 0;; ++k) {
+            const int slot = k & 1;
+            if (!(ok = tc::mbar_wait(&sm.plan_full[slot], (k >> 1) & 1, abort_flag))) break;
+            const PromptTile t = sm.tile[slot];
+            if (t.n_steps == 0) break;
+            const int last = t.last0 + tok;                   // the last key that the row sees
+            const int j0 = (wg + kPromptGroups - g0 % kPromptGroups) % kPromptGroups;
+            const bool last_wg = (g0 + t.n_steps - 1) % kPromptGroups == wg;
+            float m_ref = -INFINITY, l_sum = 0.f;
+            for (int j = j0; j < t.n_steps; j += kPromptGroups) {
+                const int gs = g0 + j, rs = gs & (kPromptRefSlots - 1);
+                const bool masked = j >= t.first_masked;
+                const int n_vis = masked ? min(max(last + 1 - j * 128, 0), 128) : 128;    // keys of the step that the row sees
+                if (!(ok = tc::mbar_wait(&sm.s_full[wg], s_ph, abort_flag))) break;
+                s_ph ^= 1u;
+                tc::tc_fence_after_sync();
+                // ---- the row's largest score; the reference moves through the warpgroups step by step
+                float mx = -INFINITY;
+                {
+                    auto fold = [&](const uint32_t (&s)[32], int c) {
+                        float a0 = -INFINITY, a1 = -INFINITY;
+                        if (masked) {
+                            const int n = n_vis - c * 32;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                a0 = fmaxf(a0, 2 * i < n ? __uint_as_float(s[2 * i]) : -INFINITY);
+                                a1 = fmaxf(a1, 2 * i + 1 < n ? __uint_as_float(s[2 * i + 1]) : -INFINITY);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                a0 = fmax3(a0, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+                                a1 = fmax3(a1, __uint_as_float(s[16 + 2 * i]), __uint_as_float(s[17 + 2 * i]));
+                            }
+                        }
+                        mx = fmax3(mx, a0, a1);
+                    };
+                    uint32_t s0[32], s1[32];                  // the next chunk is requested before the present one is looked at
+                    tc::tmem_ld_32x32(s_addr, s0);
+                    tc::tmem_wait_ld_for(s0);
+                    tc::tmem_ld_32x32(s_addr + 32, s1);
+                    fold(s0, 0);
+                    tc::tmem_wait_ld_for(s1);
+                    tc::tmem_ld_32x32(s_addr + 64, s0);
+                    fold(s1, 1);
+                    tc::tmem_wait_ld_for(s0);
+                    tc::tmem_ld_32x32(s_addr + 96, s1);
+                    fold(s0, 2);
+                    tc::tmem_wait_ld_for(s1);
+                    fold(s1, 3);
+                }
+                const float mx_x = mx * scale_log2;           // scale > 0
+                float m_prev = -INFINITY;
+                if (gs > 0 && !(ok = tc::mbar_wait(&sm.ref_done[(gs - 1) & (kPromptRefSlots - 1)][quad], ((gs - 1) / kPromptRefSlots) & 1, abort_flag))) break;
+                if (j > 0) m_prev = sm.ref[(gs - 1) & (kPromptRefSlots - 1)][row];
+                // the reference moves only when it grows by more than 2^8 (weights up to 2^8 stay exact enough: fp32 sums, bf16 weights)
+                const bool need = mx_x > m_prev + 8.f;
+                const float m_new = need ? mx_x : m_prev;
+                sm.ref[rs][row] = m_new;
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.ref_done[rs][quad]);
+                const bool rescale = j > 0 && __any_sync(0xffffffffu, need);
+                const float factor = need ? fast_exp2(m_prev - mx_x) : 1.f;   // 0 where nothing was visible before
+                l_sum = m_ref == -INFINITY ? 0.f : l_sum * fast_exp2(m_ref - m_new);
+                m_ref = m_new;
+                // ---- weights, 32 keys at a time over the scores
+                const unsigned long long add2 = pack_f32x2(-m_ref, -m_ref);
+                unsigned long long psA = 0ull, psB = 0ull;
+                {
+                    auto emit = [&](const uint32_t (&s)[32], int c) {
+                        uint32_t pk[16];
+                        if (masked) {
+                            const int n = n_vis - c * 32;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                float x0, x1;
+                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, add2), x0, x1);
+                                const float p0 = fast_exp2(2 * i < n ? x0 : -INFINITY), p1 = fast_exp2(2 * i + 1 < n ? x1 : -INFINITY);
+                                psA = add_f32x2(psA, pack_f32x2(p0, p1));
+                                pk[i] = pack_bf16x2(p0, p1);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const unsigned long long x01 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), scale2, add2);
+                                const unsigned long long x23 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), scale2, add2);
+                                float x0, x1, x2, x3;
+                                unpack_f32x2(x01, x0, x1);
+                                unpack_f32x2(x23, x2, x3);
+                                const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = (i & 1) ? poly_exp2(x3) : fast_exp2(x3);
+                                psA = add_f32x2(psA, pack_f32x2(p0, p1));
+                                psB = add_f32x2(psB, pack_f32x2(p2, p3));
+                                pk[2 * i] = pack_bf16x2(p0, p1);
+                                pk[2 * i + 1] = pack_bf16x2(p2, p3);
+                            }
+                        }
+                        tc::tmem_st_32x16(s_addr + c * 16, pk);
+                    };
+                    uint32_t s0[32], s1[32];
+                    tc::tmem_ld_32x32(s_addr, s0);
+                    tc::tmem_wait_ld_for(s0);
+                    tc::tmem_ld_32x32(s_addr + 32, s1);
+                    emit(s0, 0);
+                    tc::tmem_wait_ld_for(s1);
+                    tc::tmem_ld_32x32(s_addr + 64, s0);
+                    emit(s1, 1);
+                    tc::tmem_wait_ld_for(s0);
+                    tc::tmem_ld_32x32(s_addr + 96, s1);
+                    emit(s0, 2);
+                    tc::tmem_wait_ld_for(s1);
+                    emit(s1, 3);
+                }
+                if (rescale) {
+                    // O holds the products of all steps up to the last one, and no later one starts before this step's weights are reported
+                    if (!(ok = tc::mbar_wait(&sm.v_empty[(gs - 1) % kStages], ((gs - 1) / kStages) & 1, abort_flag))) break;
+                    tc::tc_fence_after_sync();
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; c += 2) {
+                        uint32_t o0[32], o1[32];
+                        tc::tmem_ld_32x32(lane_addr + kOCol + c * 32, o0);
+                        tc::tmem_wait_ld_for(o0);
+                        tc::tmem_ld_32x32(lane_addr + kOCol + c * 32 + 32, o1);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o0[e] = __float_as_uint(__uint_as_float(o0[e]) * factor);
+                        tc::tmem_st_32x32(lane_addr + kOCol + c * 32, o0);
+                        tc::tmem_wait_ld_for(o1);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o1[e] = __float_as_uint(__uint_as_float(o1[e]) * factor);
+                        tc::tmem_st_32x32(lane_addr + kOCol + c * 32 + 32, o1);
+                    }
+                }
+                tc::tmem_wait_st();
+                tc::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive_cluster(p_bar);
+                float a0, a1, b0, b1;
+                unpack_f32x2(psA, a0, a1);
+                unpack_f32x2(psB, b0, b1);
+                l_sum += (a0 + a1) + (b0 + b1);
+            }
+            if (!ok) break;
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
+            // ---- the sums of the three warpgroups meet in the one that took the last step; the others go on to the next tile
+            release_out();
+            const int ps = k & 1, p_ph = (k >> 1) & 1;
+            if (!last_wg) {
+                if (!(ok = tc::mbar_wait(&sm.part_free[ps], p_ph ^ 1, abort_flag))) break;
+                sm.part_l[ps][wg][row] = l_sum;
+                sm.part_m[ps][wg][row] = m_ref;
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.part_full[ps]);
+            } else {
+                if (!(ok = tc::mbar_wait(&sm.part_full[ps], p_ph, abort_flag))) break;
+                float l_fin = 0.f;                            // the reference only grows: the last step's is the largest
+#pragma unroll
+                for (int r = 0; r < kPromptGroups; ++r) {     // in the order of the steps
+                    int w = g0 % kPromptGroups + r;
+                    w = w >= kPromptGroups ? w - kPromptGroups : w;
+                    const float l = w == wg ? l_sum : sm.part_l[ps][w][row], m = w == wg ? m_ref : sm.part_m[ps][w][row];
+                    if (l != 0.f) l_fin += l * fast_exp2(m - m_ref);
+                }
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.part_free[ps]);
+                const float inv = l_fin != 0.f ? 1.f / l_fin : 0.f;
+                const bool mine = tok < t.n_tok;              // (the tile's last rows may be none, tokens behind the sequence not its own)
+                const long long at = (long long)(t.q0 + tok) * g.Hq + t.gk * g.G + head;
+                if (mine && lse != nullptr) lse[at] = (m_ref + log2f(l_fin)) * 0.6931471805599453f;
+                if (k > 0 && !(ok = tc::mbar_wait(&sm.out_free, (k - 1) & 1, abort_flag))) break;
+                if (!(ok = tc::mbar_wait(&sm.o_full, k & 1, abort_flag))) break;
+                tc::tc_fence_after_sync();
+                const bool odd = *(volatile int*)&sm.odd_tile[k % kPromptOddSlots] == k + 1;
+                unsigned char* srow = sm.out[row];
+#pragma unroll 1
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    tc::tmem_ld_32x32(lane_addr + kOCol + c * 32, o);
+                    tc::tmem_wait_ld_for(o);
+                    if (c == D / 32 - 1) {
+                        tc::tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive_cluster(o_free_bar);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint4 val;
+                        val.x = pack_bf16x2(__uint_as_float(o[8 * e + 0]) * inv, __uint_as_float(o[8 * e + 1]) * inv);
+                        val.y = pack_bf16x2(__uint_as_float(o[8 * e + 2]) * inv, __uint_as_float(o[8 * e + 3]) * inv);
+                        val.z = pack_bf16x2(__uint_as_float(o[8 * e + 4]) * inv, __uint_as_float(o[8 * e + 5]) * inv);
+                        val.w = pack_bf16x2(__uint_as_float(o[8 * e + 6]) * inv, __uint_as_float(o[8 * e + 7]) * inv);
+                        *reinterpret_cast<uint4*>(srow + (c * 4 + e) * 16) = val;
+                    }
+                }
+                if (odd && mine) {                            // rare: values that are no numbers and that this row sees
+                    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(srow);
+                    for (int key = t.first_masked * 128; key <= last; ++key) {
+                        const __nv_bfloat16* vr = g.v + (long long)(t.k0 + key) * g.v_ts + t.gk * g.v_hs;
+                        for (int d = 0; d < D; ++d) {
+                            const float x = __bfloat162float(vr[d]);
+                            if (!(fabsf(x) < INFINITY)) o[d] = __float2bfloat16(__bfloat162float(o[d]) + x);
+                        }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                if (mine) asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(out + at * D), "r"(smem_u32(srow)), "n"(2 * D) : "memory");
+                asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
+                out_pending = true;
+            }
+            g0 += t.n_steps;
+        }
+        release_out();
     }
-    if (seq < 0) return;
-    const int k0 = cu_k[seq], last = (cu_k[seq + 1] - k0) - (cu_q[seq + 1] - cu_q[seq]) + (row - cu_q[seq]);
-    float qv[kPer], o[kPer], m = -INFINITY, l = 0.f;
-    for (int e = 0; e < kPer; ++e) {
-        qv[e] = __bfloat162float(q[row * q_ts + h * q_hs + lane * kPer + e]);
-        o[e] = 0.f;
-    }
-    for (int j = 0; j <= last; ++j) {
-        const __nv_bfloat16* kr = k + (long long)(k0 + j) * k_ts + gk * k_hs + lane * kPer;
-        const __nv_bfloat16* vr = v + (long long)(k0 + j) * v_ts + gk * v_hs + lane * kPer;
-        float s = 0.f;
-        for (int e = 0; e < kPer; ++e) s = fmaf(qv[e], __bfloat162float(kr[e]), s);
-        for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-        s *= scale_log2;
-        const float m_new = fmaxf(m, s), corr = exp2f(m - m_new), p = exp2f(s - m_new);
-        l = l * corr + p;
-        for (int e = 0; e < kPer; ++e) o[e] = o[e] * corr + p * __bfloat162float(vr[e]);
-        m = m_new;
-    }
-    for (int e = 0; e < kPer; ++e) out[((long long)row * Hq + h) * D + lane * kPer + e] = __float2bfloat16(last >= 0 ? o[e] / l : 0.f);
-    if (lse != nullptr && lane == 0) lse[(long long)row * Hq + h] = last >= 0 ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
+    // ---------------------------------------------------------------- teardown
+    __syncwarp();
+    tc::tc_fence_before_sync();
+    cluster_sync();                                           // nothing of the other CTA reaches this one any more
+    if (tid == 0 && sm.abort_flag && status != nullptr) atomicExch(status, 6);   // a bounded wait expired
+    if (warp == kMmaWarp) tc::tmem_dealloc_pair<512>(tbase);
 }
 
 }  // namespace adaspark

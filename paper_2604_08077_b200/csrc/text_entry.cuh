@@ -17,6 +17,7 @@ struct DeviceScope {
             e = cudaSetDevice(h->cfg.device);
             changed = e == cudaSuccess;
         }
+        if (e == cudaSuccess && h->sm_count <= 0) e = cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->cfg.device);
         return e == cudaSuccess ? ADASPARK_OK : fail(h, ADASPARK_ERR_CUDA, "%s: device %d: %s", who, h->cfg.device, cudaGetErrorString(e));
     }
     ~DeviceScope() { if (changed) (void)cudaSetDevice(before); }
@@ -99,26 +100,49 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const void* q, int64_
     if (batch == 0 || n_q == 0) return ADASPARK_OK;
     Rows rq, rk, rv;
     ADASPARK_TRY(check_rows(h, who, "q", q, q_token_stride, q_head_stride, h->cfg.n_q_heads, rq));
-    // (no keys at all: nothing is read through k and v, which may be NULL then)
-    ADASPARK_TRY(check_rows(h, who, "k", n_k ? k : q, k_token_stride, k_head_stride, h->cfg.n_kv_heads, rk));
-    ADASPARK_TRY(check_rows(h, who, "v", n_k ? v : q, v_token_stride, v_head_stride, h->cfg.n_kv_heads, rv));
+    if (n_k) {
+        ADASPARK_TRY(check_rows(h, who, "k", k, k_token_stride, k_head_stride, h->cfg.n_kv_heads, rk));
+        ADASPARK_TRY(check_rows(h, who, "v", v, v_token_stride, v_head_stride, h->cfg.n_kv_heads, rv));
+    } else {                                       // no keys at all: k and v may be NULL; the tensor maps need some row, which no row sees
+        rk = rv = {rq.p, (long long)h->cfg.n_kv_heads * h->cfg.head_dim, h->cfg.head_dim};
+    }
     if (!cu_q || !cu_k || !out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL pointer", who);
     if ((uintptr_t)out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: out is not 16-byte aligned", who);
     if (!workspace || (uintptr_t)workspace % kAlign) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", who);
     if (workspace_bytes < (size_t)adaspark_attn_text_workspace_bytes(h)) return fail(h, ADASPARK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes", who, workspace_bytes);
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));
-    const int Hq = h->cfg.n_q_heads, G = Hq / h->cfg.n_kv_heads;
-    const float scale_log2 = text_scale(h) * 1.4426950408889634f;
-    const dim3 grid((unsigned)(((long long)n_q * Hq + 3) / 4));
-    cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (h->cfg.head_dim == 128)
-        launch_kernel(true, attn_prompt_kernel<128>, grid, dim3(128), 0, st, rq.p, rq.ts, rq.hs, rk.p, rk.ts, rk.hs, rv.p, rv.ts, rv.hs, cu_q, cu_k, batch, n_q, n_k, Hq, G,
-                      scale_log2, (__nv_bfloat16*)out, lse, status);
-    else
-        launch_kernel(true, attn_prompt_kernel<64>, grid, dim3(128), 0, st, rq.p, rq.ts, rq.hs, rk.p, rk.ts, rk.hs, rv.p, rv.ts, rv.hs, cu_q, cu_k, batch, n_q, n_k, Hq, G,
-                      scale_log2, (__nv_bfloat16*)out, lse, status);
-    return launch_ok(h, "attn_prompt_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+    PromptGeom g;
+    g.cu_q = cu_q;
+    g.cu_k = cu_k;
+    g.batch = batch;
+    g.n_q = n_q;
+    g.n_k = n_k;
+    g.Hq = h->cfg.n_q_heads;
+    g.Hkv = h->cfg.n_kv_heads;
+    g.G = g.Hq / g.Hkv;
+    g.T = 128 / g.G;
+    g.div_w.init(2 * g.T);
+    g.div_g.init(g.G);
+    g.div_kv.init(g.Hkv);
+    g.scale_log2 = text_scale(h) * 1.4426950408889634f;
+    g.v = rv.p;
+    g.v_ts = rv.ts;
+    g.v_hs = rv.hs;
+    const int D = h->cfg.head_dim, n_rows = n_k ? n_k : 1;
+    CUtensorMap tmQ, tmK, tmV;
+    if (!encode_bf16_rows(&tmQ, rq.p, n_q, g.Hq, D, rq.ts, rq.hs, 64, g.G, g.T) || !encode_bf16_rows(&tmK, rk.p, n_rows, g.Hkv, D, rk.ts, rk.hs, 64, 1, 64) ||
+        !encode_bf16_rows(&tmV, rv.p, n_rows, g.Hkv, D, rv.ts, rv.hs, D / 2, 1, 128))
+        return fail(h, ADASPARK_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
+    // a pair of CTAs per tile, at most as many as there are SMs: 2 T tokens a tile, at most one tile of each sequence not full
+    const long long most = ((long long)n_q / (2 * g.T) + batch) * g.Hkv;
+    const int pairs = (int)(most < h->sm_count / 2 ? most : h->sm_count / 2);
+    auto launch = [&](auto kernel, size_t bytes) -> adaspark_status_t {
+        if (!set_smem(h, kernel, bytes, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
+        launch_kernel(true, kernel, dim3(2 * pairs), dim3(kPromptThreads), bytes, (cudaStream_t)cuda_stream, g, tmQ, tmK, tmV, (__nv_bfloat16*)out, lse, status);
+        return launch_ok(h, "attn_prompt_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+    };
+    return D == 128 ? launch(attn_prompt_kernel<128>, sizeof(PromptSmem<128>) + 1024) : launch(attn_prompt_kernel<64>, sizeof(PromptSmem<64>) + 1024);
 }
 
 adaspark_status_t adaspark_attn_paged_write(adaspark_attn_t* h, const adaspark_attn_pages_t* pages, const void* k, int64_t k_token_stride, int64_t k_head_stride,
