@@ -87,7 +87,9 @@ adaspark_status_t check_pages(adaspark_attn* h, const char* who, const adaspark_
 
 extern "C" {
 
-int64_t adaspark_attn_text_workspace_bytes(const adaspark_attn_t* h) { return h ? 256 : 0; }
+int64_t adaspark_attn_text_workspace_bytes(const adaspark_attn_t* h) {
+    return h ? (int64_t)align_up(paged_partial_bytes(h->cfg.head_dim, h->cfg.n_q_heads / h->cfg.n_kv_heads)) : 0;
+}
 
 adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
                                        int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride, const int32_t* cu_q,
@@ -225,20 +227,42 @@ adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t* h, const void* q, 
     if (workspace_bytes < (size_t)adaspark_attn_text_workspace_bytes(h)) return fail(h, ADASPARK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes", who, workspace_bytes);
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));
-    const int Hq = h->cfg.n_q_heads, G = Hq / g.Hkv;
-    const float scale_log2 = text_scale(h) * 1.4426950408889634f;
-    cudaStream_t st = (cudaStream_t)cuda_stream;
-    auto launch = [&](auto append, auto kernel) -> adaspark_status_t {
-        if (rk.p) {
-            launch_kernel(true, append, dim3(g.Hkv, batch), dim3(64), 0, st, g, rk.p, rk.ts, rk.hs, rv.p, rv.ts, rv.hs, kv_len, status);
-            if (!launch_ok(h, "paged_append_kernel")) return ADASPARK_ERR_CUDA;
-        }
-        launch_kernel(true, kernel, dim3(Hq, batch), dim3(32), 0, st, g, rq.p, rq.ts, rq.hs, kv_len, Hq, G, scale_log2, (__nv_bfloat16*)out, lse, status);
-        return launch_ok(h, "paged_decode_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
-    };
+    const int D = h->cfg.head_dim, Hq = h->cfg.n_q_heads;
     const bool e4m3 = pages->format == ADASPARK_PAGES_E4M3;
-    if (h->cfg.head_dim == 128) return e4m3 ? launch(paged_append_kernel<128, true>, paged_decode_kernel<128, true>) : launch(paged_append_kernel<128, false>, paged_decode_kernel<128, false>);
-    return e4m3 ? launch(paged_append_kernel<64, true>, paged_decode_kernel<64, true>) : launch(paged_append_kernel<64, false>, paged_decode_kernel<64, false>);
+    const int tile = paged_tile(e4m3), page_size = pages->page_size;
+    PagedCall a;
+    a.kv_len = kv_len;
+    a.batch = batch;
+    a.Hq = Hq;
+    a.G = Hq / g.Hkv;
+    a.q = rq.p; a.q_ts = rq.ts; a.q_hs = rq.hs;
+    a.k_new = rk.p; a.k_ts = rk.ts; a.k_hs = rk.hs;
+    a.v_new = rv.p; a.v_ts = rv.ts; a.v_hs = rv.hs;
+    a.scale_log2 = text_scale(h) * 1.4426950408889634f;
+    a.out = (__nv_bfloat16*)out;
+    a.lse = lse;
+    a.partial = (float*)workspace;
+    a.status = status;
+    CUtensorMap tmK, tmV;
+    if (!encode_pages(&tmK, g.k, e4m3, g.n_pages, g.Hkv, page_size, D, g.page_stride, page_size < tile ? page_size : tile) ||
+        !encode_pages(&tmV, g.v, e4m3, g.n_pages, g.Hkv, page_size, D, g.page_stride, page_size < tile ? page_size : tile))
+        return fail(h, ADASPARK_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
+    // two CTAs per SM, or as many as the tables have tiles
+    const long long most = (long long)batch * g.Hkv * (((long long)table_width * page_size + tile - 1) / tile);
+    const int n_ctas = (int)(most < kPagedCtas ? most : kPagedCtas);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    auto launch = [&](auto kernel, auto join, size_t bytes) -> adaspark_status_t {
+        if (!set_smem(h, kernel, bytes, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
+        launch_kernel(true, kernel, dim3(n_ctas), dim3(kPagedThreads), bytes, st, g, a, tmK, tmV);
+        if (!launch_ok(h, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
+        launch_kernel(true, join, dim3(Hq, batch), dim3(512), 0, st, g, a, n_ctas);
+        return launch_ok(h, "paged_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+    };
+    if (D == 128)
+        return e4m3 ? launch(paged_decode_kernel<128, true>, paged_join_kernel<128, true>, sizeof(PagedSmem<128, true>))
+                    : launch(paged_decode_kernel<128, false>, paged_join_kernel<128, false>, sizeof(PagedSmem<128, false>));
+    return e4m3 ? launch(paged_decode_kernel<64, true>, paged_join_kernel<64, true>, sizeof(PagedSmem<64, true>))
+                : launch(paged_decode_kernel<64, false>, paged_join_kernel<64, false>, sizeof(PagedSmem<64, false>));
 }
 
 }  // extern "C"
