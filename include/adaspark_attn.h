@@ -374,56 +374,69 @@ typedef struct {
     int32_t reserved;
 } adaspark_attn_pages_t;
 
+/* Rows of bf16 [tokens][heads][head_dim]; strides in elements, 0: dense. */
+typedef struct {
+    void *data;
+    int64_t token_stride, head_stride;
+} adaspark_attn_rows_t;
+
 /* Bytes of workspace for adaspark_attn_prompt and adaspark_attn_paged_decode with this handle (of any batch and length). */
 int64_t adaspark_attn_text_workspace_bytes(const adaspark_attn_t *handle);
 
 /* Causal attention over whole prompts.  Sequence b has n_q = cu_q[b+1] - cu_q[b] query rows and n_k = cu_k[b+1] - cu_k[b]
  * keys; its row i sees the keys 0 .. n_k - n_q + i (cu_k = cu_q: a prompt from its first token; n_k > n_q: a prompt that
  * continues tokens whose keys and values are given too, e.g. by adaspark_attn_paged_read; n_k < n_q: the first rows see nothing).
- *   q, k, v      in : n_q, n_k: rows of q / out and of k / v that the tensors hold.
- *   out          out: bf16 [n_q][Hq][head_dim]; zeros for a row that sees nothing.
- *   lse          out, nullable: fp32 [n_q][Hq], the natural logarithm of the sum of the exponentials of the row's scaled
- *                     scores; -infinity for a row that sees nothing.
+ * A sequence whose rows leave the tensors sets status 1 and is left out; the others are worked on.
  * Keys and values that a row does not see do not reach it, whatever they hold (infinities and NaN included). */
-adaspark_status_t adaspark_attn_prompt(adaspark_attn_t *handle, const void *q, int64_t q_token_stride, int64_t q_head_stride,
-                                       const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v,
-                                       int64_t v_token_stride, int64_t v_head_stride, const int32_t *cu_q,
-                                       const int32_t *cu_k, int32_t batch, int32_t n_q, int32_t n_k, void *out, float *lse,
-                                       void *workspace, size_t workspace_bytes, int32_t *status, void *cuda_stream);
+typedef struct {
+    adaspark_attn_rows_t q, k, v; /* in: n_q rows of Hq heads, n_k rows of Hkv heads                   */
+    const int32_t *cu_q, *cu_k;
+    void *out;                    /* bf16 [n_q][Hq][head_dim]; zeros for a row that sees nothing       */
+    float *lse;                   /* nullable: fp32 [n_q][Hq], natural logarithm of the sum of the exponentials of the row's
+                                     scaled scores; -infinity for a row that sees nothing              */
+    void *workspace;
+    int64_t workspace_bytes;
+    int32_t *status;
+    int32_t batch, n_q, n_k;      /* sequences; rows that the tensors hold                             */
+    int32_t reserved;
+} adaspark_attn_prompt_t;
+adaspark_status_t adaspark_attn_prompt(adaspark_attn_t *handle, const adaspark_attn_prompt_t *call, void *cuda_stream);
 
-/* Writes the keys and values of packed rows into their pages: row cu[b] + i of sequence b becomes token
- * kv_len[b] - (cu[b+1] - cu[b]) + i.  n: rows that k and v hold.  A row without a place (before token 0, behind the table, page number
- * outside [0, n_pages)) is not written and sets status 1.  Two rows with the same place in one call: either may win. */
-adaspark_status_t adaspark_attn_paged_write(adaspark_attn_t *handle, const adaspark_attn_pages_t *pages, const void *k,
-                                            int64_t k_token_stride, int64_t k_head_stride, const void *v,
-                                            int64_t v_token_stride, int64_t v_head_stride, const int32_t *cu, int32_t batch,
-                                            int32_t n, const int32_t *block_table, int32_t table_width, const int32_t *kv_len,
-                                            int32_t *status, void *cuda_stream);
-
-/* Reads the last cu[b+1] - cu[b] tokens of every sequence back: k_out, v_out dense bf16 [n][Hkv][head_dim], laid out as the rows of
- * adaspark_attn_paged_write.  Exact: every value that a page holds is a bf16 number.  A row without a place reads zeros and
- * sets status 1. */
-adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t *handle, const adaspark_attn_pages_t *pages, const int32_t *cu,
-                                           int32_t batch, int32_t n, const int32_t *block_table, int32_t table_width,
-                                           const int32_t *kv_len, void *k_out, void *v_out, int32_t *status,
-                                           void *cuda_stream);
+/* Keys and values of packed rows and their places in the pages: row cu[b] + i of sequence b is token
+ * kv_len[b] - (cu[b+1] - cu[b]) + i.
+ * _write puts the rows k, v into their places.  A row without a place (before token 0, behind the table, page number outside
+ * [0, n_pages)) is not written and sets status 1.  Two rows with the same place in one call: either may win.
+ * _read gets the last cu[b+1] - cu[b] tokens of every sequence back into the rows k, v.  Exact: every value that a page holds
+ * is a bf16 number.  A row without a place becomes zeros and sets status 1. */
+typedef struct {
+    adaspark_attn_pages_t pages;
+    adaspark_attn_rows_t k, v;    /* n rows of Hkv heads                                               */
+    const int32_t *cu, *kv_len, *block_table;
+    int32_t *status;
+    int32_t batch, n, table_width, reserved;
+} adaspark_attn_paged_rows_t;
+adaspark_status_t adaspark_attn_paged_write(adaspark_attn_t *handle, const adaspark_attn_paged_rows_t *call, void *cuda_stream);
+adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t *handle, const adaspark_attn_paged_rows_t *call, void *cuda_stream);
 
 /* One new token per sequence: the row q of sequence b attends the tokens 0 .. kv_len[b] - 1 of its pages.
- *   q            in : bf16 [batch][Hq][head_dim].
- *   k_new, v_new in, nullable: bf16 [batch][Hkv][head_dim], the new token's; written as token kv_len[b] - 1 and attended as
- *                     the pages hold them.  NULL: they are there already.
- *   kv_len       in : 0 marks a slot of the batch without a sequence (nothing is appended).
- *   out, lse     out: as adaspark_attn_prompt, [batch][Hq]; zeros and -infinity where kv_len is 0, where kv_len is negative
- *                     or more than the table holds, and where a page number among the tokens is outside [0, n_pages) (the last two set
- *                     status 1 and append nothing into a place that is not there).
+ * kv_len 0 marks a slot of the batch without a sequence (nothing is appended).  Where kv_len is negative or more than the table
+ * holds, or a page number among the tokens is outside [0, n_pages), status is set to 1 and nothing is appended into a place that is
+ * not there; the row becomes zeros (lse: -infinity), as it does with kv_len 0.
  * Two sequences may share pages that neither of them appends to. */
-adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t *handle, const void *q, int64_t q_token_stride,
-                                             int64_t q_head_stride, const void *k_new, int64_t k_token_stride,
-                                             int64_t k_head_stride, const void *v_new, int64_t v_token_stride,
-                                             int64_t v_head_stride, const adaspark_attn_pages_t *pages,
-                                             const int32_t *block_table, int32_t table_width, const int32_t *kv_len,
-                                             int32_t batch, void *out, float *lse, void *workspace, size_t workspace_bytes,
-                                             int32_t *status, void *cuda_stream);
+typedef struct {
+    adaspark_attn_pages_t pages;
+    adaspark_attn_rows_t q;            /* batch rows of Hq heads                                       */
+    adaspark_attn_rows_t k_new, v_new; /* batch rows of Hkv heads: the new tokens', written as token kv_len[b] - 1 and attended as
+                                          the pages hold them; data NULL: they are there already       */
+    const int32_t *kv_len, *block_table;
+    void *out;                         /* bf16 [batch][Hq][head_dim]                                   */
+    float *lse;                        /* nullable: fp32 [batch][Hq], as adaspark_attn_prompt          */
+    void *workspace;
+    int64_t workspace_bytes;
+    int32_t *status;
+    int32_t batch, table_width;
+} adaspark_attn_paged_decode_t;
+adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t *handle, const adaspark_attn_paged_decode_t *call, void *cuda_stream);
 
 #ifdef __cplusplus
 }

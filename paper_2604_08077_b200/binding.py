@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -34,14 +35,14 @@ class Layout(ctypes.Structure):
         "v_cube_bytes", "cube_keys_bytes", "forward_workspace_bytes", "decode_workspace_bytes")]
 
 
-class Pages(ctypes.Structure):
-    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
-                ("v_scale", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
-                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("format", ctypes.c_int32),
-                ("reserved", ctypes.c_int32)]
-
-
 PAGES_BF16, PAGES_E4M3 = 0, 1
+
+# The arguments of the text calls, packed as the header's structs lay them out (one bytes object per call: a quarter of the time that
+# ctypes takes for two dozen arguments).  A row argument is (pointer, token stride, head stride).
+_PAGES = struct.Struct("4Q2q4i")          # adaspark_attn_pages_t
+_PROMPT = struct.Struct("QqqQqqQqq5QqQ4i")  # adaspark_attn_prompt_t
+_PAGED_ROWS = struct.Struct("QqqQqq4Q4i")   # adaspark_attn_paged_rows_t behind its pages
+_PAGED_DECODE = struct.Struct("QqqQqqQqq5QqQ2i")   # adaspark_attn_paged_decode_t behind its pages
 
 
 class AdasparkError(RuntimeError):
@@ -97,14 +98,10 @@ def load() -> ctypes.CDLL:
     lib.adaspark_attn_enable_stage_timing.argtypes = [vp, i32]
     lib.adaspark_attn_get_stage_times.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
     lib.adaspark_attn_get_attention_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
-    i64, pages = ctypes.c_int64, ctypes.POINTER(Pages)
-    rows = [vp, i64, i64]                                       # pointer, token stride, head stride
     lib.adaspark_attn_text_workspace_bytes.argtypes = [vp]
-    lib.adaspark_attn_text_workspace_bytes.restype = i64
-    lib.adaspark_attn_prompt.argtypes = [vp, *rows, *rows, *rows, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp, vp]
-    lib.adaspark_attn_paged_write.argtypes = [vp, pages, *rows, *rows, vp, i32, i32, vp, i32, vp, vp, vp]
-    lib.adaspark_attn_paged_read.argtypes = [vp, pages, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp]
-    lib.adaspark_attn_paged_decode.argtypes = [vp, *rows, *rows, *rows, pages, vp, i32, vp, i32, vp, vp, vp, sz, vp, vp]
+    lib.adaspark_attn_text_workspace_bytes.restype = ctypes.c_int64
+    for name in ("prompt", "paged_write", "paged_read", "paged_decode"):
+        getattr(lib, "adaspark_attn_" + name).argtypes = [vp, ctypes.c_char_p, vp]
     for name in EXPORTS:
         if name not in ("adaspark_attn_last_error", "adaspark_attn_last_launch_count", "adaspark_attn_text_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_int
@@ -270,38 +267,49 @@ def adaspark_attn_get_attention_kernel_ms(handle: int) -> float:
     return float(ms[0])
 
 
-# ---- text beside the video (tensors: a row argument is (tensor or pointer, token stride, head stride)) ----
+# ---- text beside the video: pointers (None: NULL), rows as (pointer, token stride, head stride), pages from pages_struct() ----
+
+_NO_ROWS = (0, 0, 0)
+
 
 def adaspark_attn_text_workspace_bytes(handle: int) -> int:
     return int(load().adaspark_attn_text_workspace_bytes(handle))
 
 
+def pages_struct(k_pages, v_pages, k_scale, v_scale, page_stride: int, scale_stride: int, n_pages: int, page_size: int,
+                 page_format: int) -> bytes:
+    """adaspark_attn_pages_t."""
+    return _PAGES.pack(k_pages or 0, v_pages or 0, k_scale or 0, v_scale or 0, page_stride, scale_stride, n_pages, page_size, page_format, 0)
+
+
 def adaspark_attn_prompt(handle: int, q, k, v, cu_q, cu_k, batch: int, n_q: int, n_k: int, out, lse, workspace,
                          workspace_bytes: int, status, stream: Optional[int]):
-    """q, k, v: (pointer, token stride, head stride); the others pointers or None."""
-    st = load().adaspark_attn_prompt(handle, *q, *k, *v, cu_q, cu_k, batch, n_q, n_k, out, lse, workspace, workspace_bytes, status, stream)
+    st = (_lib or load()).adaspark_attn_prompt(handle, _PROMPT.pack(*q, *k, *v, cu_q or 0, cu_k or 0, out or 0, lse or 0, workspace or 0, workspace_bytes,
+                                                                    status or 0, batch, n_q, n_k, 0), stream)
     if st != OK:
         _check(handle, st)
 
 
-def adaspark_attn_paged_write(handle: int, pages: Pages, k, v, cu, batch: int, n: int, block_table, table_width: int, kv_len,
+def adaspark_attn_paged_write(handle: int, pages: bytes, k, v, cu, batch: int, n: int, block_table, table_width: int, kv_len,
                               status, stream: Optional[int]):
-    st = load().adaspark_attn_paged_write(handle, pages, *k, *v, cu, batch, n, block_table, table_width, kv_len, status, stream)
+    st = (_lib or load()).adaspark_attn_paged_write(handle, pages + _PAGED_ROWS.pack(*k, *v, cu or 0, kv_len or 0, block_table or 0, status or 0, batch, n,
+                                                                                     table_width, 0), stream)
     if st != OK:
         _check(handle, st)
 
 
-def adaspark_attn_paged_read(handle: int, pages: Pages, cu, batch: int, n: int, block_table, table_width: int, kv_len, k_out, v_out,
+def adaspark_attn_paged_read(handle: int, pages: bytes, k, v, cu, batch: int, n: int, block_table, table_width: int, kv_len,
                              status, stream: Optional[int]):
-    st = load().adaspark_attn_paged_read(handle, pages, cu, batch, n, block_table, table_width, kv_len, k_out, v_out, status, stream)
+    st = (_lib or load()).adaspark_attn_paged_read(handle, pages + _PAGED_ROWS.pack(*k, *v, cu or 0, kv_len or 0, block_table or 0, status or 0, batch, n,
+                                                                                    table_width, 0), stream)
     if st != OK:
         _check(handle, st)
 
 
-def adaspark_attn_paged_decode(handle: int, q, k_new, v_new, pages: Pages, block_table, table_width: int, kv_len, batch: int, out, lse,
+def adaspark_attn_paged_decode(handle: int, q, k_new, v_new, pages: bytes, block_table, table_width: int, kv_len, batch: int, out, lse,
                                workspace, workspace_bytes: int, status, stream: Optional[int]):
-    st = load().adaspark_attn_paged_decode(handle, *q, *k_new, *v_new, pages, block_table, table_width, kv_len, batch, out, lse, workspace,
-                                           workspace_bytes, status, stream)
+    st = (_lib or load()).adaspark_attn_paged_decode(handle, pages + _PAGED_DECODE.pack(*q, *k_new, *v_new, kv_len or 0, block_table or 0, out or 0, lse or 0,
+                                                                                        workspace or 0, workspace_bytes, status or 0, batch, table_width), stream)
     if st != OK:
         _check(handle, st)
 
@@ -315,6 +323,11 @@ class WorkspaceHeader(ctypes.Structure):
 
 
 # ---- a small convenience owner of the handle and of the caller-side buffers --------------------
+
+def _raw_stream(index: int) -> int:
+    """The current stream of a device, as torch hands it to its own generated code: 0.1 us instead of 2 for the stream object."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
 
 def _refuse(message: str):
     raise AdasparkError(ERR_INVALID_ARG, message)
@@ -354,11 +367,12 @@ class PagedCache:
         if k_pages.shape[0] == 0:
             _refuse("PagedCache: no pages")
         self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
-        self.device = k_pages.device
+        self.device, self.index = k_pages.device, k_pages.get_device()
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
-        self.pages = Pages(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if fmt else None,
-                           v_scale.data_ptr() if fmt else None, stride_of(k_pages, v_pages),
-                           stride_of(k_scale, v_scale) if fmt else 0, self.n_pages, self.page_size, fmt, 0)
+        self.page_stride = stride_of(k_pages, v_pages)
+        self.pages = pages_struct(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if fmt else None,
+                                  v_scale.data_ptr() if fmt else None, self.page_stride, stride_of(k_scale, v_scale) if fmt else 0,
+                                  self.n_pages, self.page_size, fmt)
 
 class AdaSAttn:
     """Owns a handle plus the torch-allocated caches and workspace for one partition."""
@@ -371,6 +385,7 @@ class AdaSAttn:
         self.device = torch.device("cuda", device)
         self.layout: Optional[Layout] = None
         self._text = None
+        self._index, self._n_q_heads, self._n_kv_heads, self._head_dim = device, n_q_heads, n_kv_heads, head_dim
 
     def set_gather(self, pairs_per_block: float, budget_bytes: int = 24 << 30):
         """Threshold and workspace budget of the query-gather path (budget: before partition())."""
@@ -459,130 +474,125 @@ class AdaSAttn:
         return PagedCache(*pages, *scales)
 
     def _text_buffers(self):
-        """Workspace and status word of the text calls, made once."""
-        if self._text is None:
-            n = adaspark_attn_text_workspace_bytes(self.handle)
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-            self._text = (ws, n, ws.data_ptr(), torch.zeros(1, dtype=torch.int32, device=self.device))
-            self._text = (*self._text, self._text[3].data_ptr())
+        """(status pointer, workspace pointer, workspace bytes) of the text calls, made once."""
+        n = adaspark_attn_text_workspace_bytes(self.handle)
+        self._text_ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self._text_flag = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._text = (self._text_flag.data_ptr(), self._text_ws.data_ptr(), n)
         return self._text
 
     def text_status(self) -> int:
         """What the text calls of this object found wrong on the device since the last look: 0 = nothing (waits for the device)."""
         if self._text is None:
             return 0
-        got = int(self._text[3].item())
+        got = int(self._text_flag.item())
         if got:
-            self._text[3].zero_()
+            self._text_flag.zero_()
         return got
 
     def _stream(self, stream):
-        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream or None
+        return (_raw_stream(self._index) if stream is None else stream.cuda_stream) or None
 
     def _rows(self, t, heads: int, what: str):
-        """(pointer, token stride, head stride) of a bf16 tensor [rows, heads, head_dim] on this device."""
+        """(pointer, token stride, head stride) of a bf16 tensor [rows, heads, head_dim] on this device, and its rows."""
         shape, strides = t.shape, t.stride()
-        if len(shape) != 3 or shape[1] != heads or shape[2] != self.cfg.head_dim or t.dtype != torch.bfloat16:
-            _refuse(f"{what}: {t.dtype} {tuple(shape)} is not bfloat16 [rows, {heads}, {self.cfg.head_dim}]")
+        if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[1] != heads or shape[2] != self._head_dim:
+            _refuse(f"{what}: {t.dtype} {tuple(shape)} is not bfloat16 [rows, {heads}, {self._head_dim}]")
         if strides[2] != 1:
             _refuse(f"{what}: the values of a row have to lie side by side")
-        if t.device != self.device:
+        if t.get_device() != self._index:
             _refuse(f"{what} is on {t.device}, not on {self.device}")
+        n = shape[0]
         # (the stride of an axis of one entry says nothing)
-        return t.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1] if heads > 1 else 0
+        return (t.data_ptr(), strides[0] if n > 1 else 0, strides[1] if heads > 1 else 0), n
 
     def _dense(self, t, shape, dtype, what: str) -> int:
-        if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
-            _refuse(f"{what}: {t.dtype} {tuple(t.shape)} is not dense {dtype} {tuple(shape)}")
-        if t.device != self.device:
-            _refuse(f"{what} is on {t.device}, not on {self.device}")
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != self._index:
+            _refuse(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device} is not dense {dtype} {tuple(shape)} on {self.device}")
         return t.data_ptr()
 
-    def _ints(self, t, what: str, dims: int = 1) -> int:
-        if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() or t.device != self.device:
-            _refuse(f"{what}: dense int32 with {dims} axes on {self.device} is needed")
+    def _ints(self, t, n: int, what: str) -> int:
+        if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous() or t.get_device() != self._index:
+            _refuse(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device} is not dense int32 [{n}] on {self.device}")
         return t.data_ptr()
 
-    def _cache(self, cache: PagedCache) -> Pages:
-        if cache.n_kv_heads != self.cfg.n_kv_heads or cache.head_dim != self.cfg.head_dim or cache.device != self.device:
+    def _tables(self, block_table, kv_len):
+        """(batch, pointer of the block table, its width, pointer of kv_len)."""
+        shape = block_table.shape
+        if block_table.dtype is not torch.int32 or len(shape) != 2 or not block_table.is_contiguous() or block_table.get_device() != self._index:
+            _refuse(f"block_table: {block_table.dtype} {tuple(shape)} on {block_table.device} is not dense int32 [batch, pages] on {self.device}")
+        return shape[0], block_table.data_ptr(), shape[1], self._ints(kv_len, shape[0], "kv_len")
+
+    def _cache(self, cache: PagedCache) -> bytes:
+        if cache.n_kv_heads != self._n_kv_heads or cache.head_dim != self._head_dim or cache.index != self._index:
             _refuse(f"cache of {cache.n_kv_heads} heads of {cache.head_dim} on {cache.device}: not this handle's")
         return cache.pages
 
     def prompt(self, q, k, v, cu_q, cu_k=None, *, out=None, lse=None, want_lse=False, stream=None):
         """Causal attention of packed prompts: q [n_q, Hq, D], k and v [n_k, Hkv, D] bf16, cu_q (and cu_k, if the keys of a sequence
-        are more than its queries) int32 [batch + 1].  Returns (out, lse); lse is None unless given or wanted."""
-        c = self.cfg
-        ws, ws_bytes, ws_ptr, status, status_ptr = self._text_buffers()
-        qr, kr, vr = self._rows(q, c.n_q_heads, "q"), self._rows(k, c.n_kv_heads, "k"), self._rows(v, c.n_kv_heads, "v")
-        n_q, n_k = q.shape[0], k.shape[0]
-        if v.shape[0] != n_k:
-            _refuse(f"v has {v.shape[0]} rows, k {n_k}")
-        cq = self._ints(cu_q, "cu_q")
-        ck = cq if cu_k is None else self._ints(cu_k, "cu_k")
-        batch = cu_q.shape[0] - 1
-        if batch < 0 or (cu_k is not None and cu_k.shape[0] != batch + 1):
-            _refuse("cu_q and cu_k hold batch + 1 entries each")
+        are more than its queries) int32 [batch + 1].  Returns (out, lse); lse is None unless given or wanted.  The text calls of one
+        object share a workspace: calls that may overlap on the GPU (other streams, graphs replayed side by side) need an object each."""
+        status, ws, ws_bytes = self._text or self._text_buffers()
+        Hq, D = self._n_q_heads, self._head_dim
+        (qr, n_q), (kr, n_k), (vr, n_v) = self._rows(q, Hq, "q"), self._rows(k, self._n_kv_heads, "k"), self._rows(v, self._n_kv_heads, "v")
+        if n_v != n_k:
+            _refuse(f"v has {n_v} rows, k {n_k}")
+        n_cu = cu_q.numel()
+        cq = self._ints(cu_q, n_cu, "cu_q")
+        if n_cu == 0:
+            _refuse("cu_q: batch + 1 entries are needed")
         if out is None:
-            out = torch.empty(n_q, c.n_q_heads, c.head_dim, dtype=torch.bfloat16, device=self.device)
+            out = torch.empty(n_q, Hq, D, dtype=torch.bfloat16, device=self.device)
         if lse is None and want_lse:
-            lse = torch.empty(n_q, c.n_q_heads, dtype=torch.float32, device=self.device)
-        adaspark_attn_prompt(self.handle, qr, kr, vr, cq, ck, batch, n_q, n_k,
-                             self._dense(out, (n_q, c.n_q_heads, c.head_dim), torch.bfloat16, "out"),
-                             None if lse is None else self._dense(lse, (n_q, c.n_q_heads), torch.float32, "lse"),
-                             ws_ptr, ws_bytes, status_ptr, self._stream(stream))
+            lse = torch.empty(n_q, Hq, dtype=torch.float32, device=self.device)
+        adaspark_attn_prompt(self.handle, qr, kr, vr, cq, cq if cu_k is None else self._ints(cu_k, n_cu, "cu_k"), n_cu - 1, n_q, n_k,
+                             self._dense(out, (n_q, Hq, D), torch.bfloat16, "out"),
+                             None if lse is None else self._dense(lse, (n_q, Hq), torch.float32, "lse"), ws, ws_bytes, status,
+                             self._stream(stream))
         return out, lse
 
     def paged_write(self, cache: PagedCache, k, v, cu, block_table, kv_len, *, stream=None):
         """Packed keys and values into the pages: the rows cu[b] .. cu[b + 1] - 1 become the last tokens of sequence b, which
         then holds kv_len[b].  block_table int32 [batch, width]."""
-        status_ptr = self._text_buffers()[4]
-        kr, vr = self._rows(k, self.cfg.n_kv_heads, "k"), self._rows(v, self.cfg.n_kv_heads, "v")
-        if k.shape[0] != v.shape[0]:
-            _refuse(f"v has {v.shape[0]} rows, k {k.shape[0]}")
-        batch = self._batch(cu, block_table, kv_len)
-        adaspark_attn_paged_write(self.handle, self._cache(cache), kr, vr, self._ints(cu, "cu"), batch, k.shape[0],
-                                  self._ints(block_table, "block_table", 2), block_table.shape[1], self._ints(kv_len, "kv_len"),
-                                  status_ptr, self._stream(stream))
+        self._paged_rows(adaspark_attn_paged_write, cache, k, v, cu, block_table, kv_len, stream)
 
     def paged_read(self, cache: PagedCache, cu, block_table, kv_len, k_out, v_out, *, stream=None):
         """The last cu[b + 1] - cu[b] tokens of every sequence from the pages into k_out, v_out: bf16 [n, Hkv, D].  Returns them."""
-        c = self.cfg
-        status_ptr = self._text_buffers()[4]
-        n = k_out.shape[0]
-        batch = self._batch(cu, block_table, kv_len)
-        adaspark_attn_paged_read(self.handle, self._cache(cache), self._ints(cu, "cu"), batch, n,
-                                 self._ints(block_table, "block_table", 2), block_table.shape[1], self._ints(kv_len, "kv_len"),
-                                 self._dense(k_out, (n, c.n_kv_heads, c.head_dim), torch.bfloat16, "k_out"),
-                                 self._dense(v_out, (n, c.n_kv_heads, c.head_dim), torch.bfloat16, "v_out"), status_ptr, self._stream(stream))
+        self._paged_rows(adaspark_attn_paged_read, cache, k_out, v_out, cu, block_table, kv_len, stream)
         return k_out, v_out
 
-    @staticmethod
-    def _batch(cu, block_table, kv_len) -> int:
-        batch = kv_len.shape[0]
-        if block_table.dim() != 2 or block_table.shape[0] != batch or (cu is not None and cu.shape[0] != batch + 1):
-            _refuse(f"kv_len of {batch} sequences, block table {tuple(block_table.shape)}, cu {None if cu is None else tuple(cu.shape)}")
-        return batch
+    def _paged_rows(self, call, cache, k, v, cu, block_table, kv_len, stream):
+        status = (self._text or self._text_buffers())[0]
+        (kr, n), (vr, n_v) = self._rows(k, self._n_kv_heads, "k"), self._rows(v, self._n_kv_heads, "v")
+        if n_v != n:
+            _refuse(f"v has {n_v} rows, k {n}")
+        batch, table, width, lens = self._tables(block_table, kv_len)
+        call(self.handle, self._cache(cache), kr, vr, self._ints(cu, batch + 1, "cu"), batch, n, table, width, lens, status, self._stream(stream))
 
     def paged_decode(self, q, k_new, v_new, cache: PagedCache, block_table, kv_len, *, out=None, lse=None, want_lse=False,
                      stream=None):
         """One new token per sequence against its pages.  q [batch, Hq, D]; k_new, v_new [batch, Hkv, D] are stored as token
         kv_len[b] - 1 first (None: they are there).  kv_len 0: a slot without a sequence.  Returns (out, lse)."""
-        c = self.cfg
-        ws, ws_bytes, ws_ptr, status, status_ptr = self._text_buffers()
-        batch = self._batch(None, block_table, kv_len)
-        if q.shape[0] != batch or (k_new is None) != (v_new is None) or (k_new is not None and (k_new.shape[0] != batch or v_new.shape[0] != batch)):
-            _refuse("q, k_new and v_new hold a row for each entry of kv_len (k_new and v_new both or neither)")
-        none = (None, 0, 0)
+        status, ws, ws_bytes = self._text or self._text_buffers()
+        Hq, D = self._n_q_heads, self._head_dim
+        batch, table, width, lens = self._tables(block_table, kv_len)
+        qr, n = self._rows(q, Hq, "q")
+        kr = vr = _NO_ROWS
+        n_k = n_v = batch
+        if k_new is not None and v_new is not None:
+            (kr, n_k), (vr, n_v) = self._rows(k_new, self._n_kv_heads, "k_new"), self._rows(v_new, self._n_kv_heads, "v_new")
+        elif k_new is not None or v_new is not None:
+            _refuse("k_new and v_new come together")
+        if n != batch or n_k != batch or n_v != batch:
+            _refuse(f"q, k_new and v_new hold a row for each of the {batch} entries of kv_len")
         if out is None:
-            out = torch.empty(batch, c.n_q_heads, c.head_dim, dtype=torch.bfloat16, device=self.device)
+            out = torch.empty(batch, Hq, D, dtype=torch.bfloat16, device=self.device)
         if lse is None and want_lse:
-            lse = torch.empty(batch, c.n_q_heads, dtype=torch.float32, device=self.device)
-        adaspark_attn_paged_decode(self.handle, self._rows(q, c.n_q_heads, "q"), none if k_new is None else self._rows(k_new, c.n_kv_heads, "k_new"),
-                                   none if v_new is None else self._rows(v_new, c.n_kv_heads, "v_new"), self._cache(cache),
-                                   self._ints(block_table, "block_table", 2), block_table.shape[1], self._ints(kv_len, "kv_len"), batch,
-                                   self._dense(out, (batch, c.n_q_heads, c.head_dim), torch.bfloat16, "out"),
-                                   None if lse is None else self._dense(lse, (batch, c.n_q_heads), torch.float32, "lse"),
-                                   ws_ptr, ws_bytes, status_ptr, self._stream(stream))
+            lse = torch.empty(batch, Hq, dtype=torch.float32, device=self.device)
+        adaspark_attn_paged_decode(self.handle, qr, kr, vr, self._cache(cache), table, width, lens, batch,
+                                   self._dense(out, (batch, Hq, D), torch.bfloat16, "out"),
+                                   None if lse is None else self._dense(lse, (batch, Hq), torch.float32, "lse"), ws, ws_bytes, status,
+                                   self._stream(stream))
         return out, lse
 
     def header(self) -> WorkspaceHeader:

@@ -203,12 +203,12 @@ __global__ void __launch_bounds__(kCacheThreads) paged_write_kernel(
     }
 }
 
-// pages -> k_out, v_out [n][Hkv][D] bf16.  Rows of no sequence are left as they are; rows of a sequence that have no place in
+// pages -> k_out, v_out [n][Hkv][D] bf16 (row and head strides in elements).  Rows of no sequence are left as they are; rows of a sequence that have no place in
 // its pages read as zeros.
 template <int D, bool kE4m3>
-__global__ void __launch_bounds__(kCacheThreads) paged_read_kernel(PageGeom p, const int32_t* cu, const int32_t* kv_len, int batch, int n,
-                                                                   FastDiv div_rows, FastDiv div_heads, __nv_bfloat16* k_out,
-                                                                   __nv_bfloat16* v_out, int32_t* status) {
+__global__ void __launch_bounds__(kCacheThreads) paged_read_kernel(
+    PageGeom p, __nv_bfloat16* k_out, long long k_ts, long long k_hs, __nv_bfloat16* v_out, long long v_ts, long long v_hs, const int32_t* cu,
+    const int32_t* kv_len, int batch, int n, FastDiv div_rows, FastDiv div_heads, int32_t* status) {
     constexpr int kLanes = D / 8, kBatch = 4;
     __shared__ int page[kCacheTokens], place[kCacheTokens];
     const int t0 = blockIdx.x * kCacheTokens;
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kCacheThreads) paged_read_kernel(PageGeom p, c
             dst[i] = nullptr;
             if (c < n_chunks && page[r] != -1) {
                 const int pg = page[r];
-                dst[i] = (w ? v_out : k_out) + ((long long)(t0 + r) * p.Hkv + h) * D + part * 8;
+                dst[i] = (w ? v_out + (long long)(t0 + r) * v_ts + h * v_hs : k_out + (long long)(t0 + r) * k_ts + h * k_hs) + part * 8;
                 if (pg >= 0) {
                     const long long at = ((long long)h << p.page_shift) + place[r];
                     if (kE4m3) {

@@ -1,6 +1,9 @@
 // Entry points of the text operators (include/adaspark_attn.h, "Text beside the video"): argument checks and launches.
 // Included by adaspark_attn.cu, whose handle and launch helpers they use.
 #pragma once
+#include <atomic>
+#include <type_traits>
+
 #include "attn_prompt.cuh"
 #include "paged_cache.cuh"
 #include "paged_decode.cuh"
@@ -29,14 +32,15 @@ float text_scale(const adaspark_attn* h) {
 
 // bf16 rows [n][heads][D] with strides in elements, 0 standing for the dense ones
 struct Rows {
-    const __nv_bfloat16* p;
+    __nv_bfloat16* p;
     long long ts, hs;
 };
-adaspark_status_t check_rows(adaspark_attn* h, const char* who, const char* what, const void* p, int64_t ts, int64_t hs, int heads, Rows& r) {
+adaspark_status_t check_rows(adaspark_attn* h, const char* who, const char* what, const adaspark_attn_rows_t& rows, int heads, Rows& r) {
     const int D = h->cfg.head_dim;
-    r.p = (const __nv_bfloat16*)p;
-    r.hs = hs ? hs : D;
-    r.ts = ts ? ts : (long long)heads * D;
+    const void* p = rows.data;
+    r.p = (__nv_bfloat16*)p;
+    r.hs = rows.head_stride ? rows.head_stride : D;
+    r.ts = rows.token_stride ? rows.token_stride : (long long)heads * D;
     if (!p) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL %s", who, what);
     if ((uintptr_t)p % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: %s is not 16-byte aligned", who, what);
     if (r.hs < D || r.ts < D || r.hs % 8 || r.ts % 8 || r.hs >= (1ll << 38) || r.ts >= (1ll << 38))
@@ -77,11 +81,59 @@ adaspark_status_t check_pages(adaspark_attn* h, const char* who, const adaspark_
     return ADASPARK_OK;
 }
 
+adaspark_status_t check_workspace(adaspark_attn* h, const char* who, const void* ws, int64_t bytes) {
+    if (!ws || (uintptr_t)ws % kAlign) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", who);
+    const int64_t need = adaspark_attn_text_workspace_bytes(h);
+    return bytes >= need ? ADASPARK_OK : fail(h, ADASPARK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %lld < %lld bytes", who, (long long)bytes, (long long)need);
+}
+
+// Room for a kernel's dynamic shared memory, asked for once per kernel and device.
+template <auto kKernel>
+bool text_smem(adaspark_attn* h, size_t bytes, const char* what) {
+    static std::atomic<uint64_t> done{0};
+    const uint64_t bit = 1ull << (h->cfg.device & 63);
+    if (h->cfg.device < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (!set_smem(h, kKernel, bytes, what)) return false;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
 #define ADASPARK_TRY(expr)                       \
     do {                                         \
         const adaspark_status_t st_ = (expr);    \
         if (st_ != ADASPARK_OK) return st_;      \
     } while (0)
+
+adaspark_status_t paged_rows_impl(adaspark_attn* h, const char* who, const adaspark_attn_paged_rows_t* c, bool write, void* cuda_stream) {
+    if (!h) return ADASPARK_ERR_INVALID_ARG;
+    if (!c || c->batch < 0 || c->n < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call or negative size", who);
+    h->launches = 0;
+    if (c->batch == 0 || c->n == 0) return ADASPARK_OK;
+    PageGeom g;
+    Rows rk, rv;
+    ADASPARK_TRY(check_pages(h, who, &c->pages, c->block_table, c->table_width, g));
+    ADASPARK_TRY(check_rows(h, who, "k", c->k, h->cfg.n_kv_heads, rk));
+    ADASPARK_TRY(check_rows(h, who, "v", c->v, h->cfg.n_kv_heads, rv));
+    if (!c->cu || !c->kv_len) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL cu or kv_len", who);
+    DeviceScope scope;
+    ADASPARK_TRY(scope.enter(h, who));
+    FastDiv rows, heads;
+    rows.init(2 * g.Hkv);
+    heads.init(g.Hkv);
+    auto launch = [&](auto kernel) {
+        launch_kernel(true, kernel, dim3((unsigned)((c->n + kCacheTokens - 1) / kCacheTokens)), dim3(kCacheThreads), 0, (cudaStream_t)cuda_stream, g, rk.p, rk.ts, rk.hs, rv.p, rv.ts,
+                      rv.hs, c->cu, c->kv_len, c->batch, c->n, rows, heads, c->status);
+    };
+    const bool e4m3 = c->pages.format == ADASPARK_PAGES_E4M3, wide = h->cfg.head_dim == 128;
+    if (write) {
+        if (wide) e4m3 ? launch(paged_write_kernel<128, true>) : launch(paged_write_kernel<128, false>);
+        else e4m3 ? launch(paged_write_kernel<64, true>) : launch(paged_write_kernel<64, false>);
+    } else {
+        if (wide) e4m3 ? launch(paged_read_kernel<128, true>) : launch(paged_read_kernel<128, false>);
+        else e4m3 ? launch(paged_read_kernel<64, true>) : launch(paged_read_kernel<64, false>);
+    }
+    return launch_ok(h, write ? "paged_write_kernel" : "paged_read_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+}
 
 }  // namespace
 
@@ -91,32 +143,29 @@ int64_t adaspark_attn_text_workspace_bytes(const adaspark_attn_t* h) {
     return h ? (int64_t)align_up(paged_partial_bytes(h->cfg.head_dim, h->cfg.n_q_heads / h->cfg.n_kv_heads)) : 0;
 }
 
-adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
-                                       int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride, const int32_t* cu_q,
-                                       const int32_t* cu_k, int32_t batch, int32_t n_q, int32_t n_k, void* out, float* lse, void* workspace,
-                                       size_t workspace_bytes, int32_t* status, void* cuda_stream) {
+adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_prompt_t* c, void* cuda_stream) {
     if (!h) return ADASPARK_ERR_INVALID_ARG;
     const char* who = "prompt";
-    if (batch < 0 || n_q < 0 || n_k < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: negative size", who);
+    if (!c || c->batch < 0 || c->n_q < 0 || c->n_k < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call or negative size", who);
+    const int batch = c->batch, n_q = c->n_q, n_k = c->n_k;
     h->launches = 0;
     if (batch == 0 || n_q == 0) return ADASPARK_OK;
     Rows rq, rk, rv;
-    ADASPARK_TRY(check_rows(h, who, "q", q, q_token_stride, q_head_stride, h->cfg.n_q_heads, rq));
+    ADASPARK_TRY(check_rows(h, who, "q", c->q, h->cfg.n_q_heads, rq));
     if (n_k) {
-        ADASPARK_TRY(check_rows(h, who, "k", k, k_token_stride, k_head_stride, h->cfg.n_kv_heads, rk));
-        ADASPARK_TRY(check_rows(h, who, "v", v, v_token_stride, v_head_stride, h->cfg.n_kv_heads, rv));
+        ADASPARK_TRY(check_rows(h, who, "k", c->k, h->cfg.n_kv_heads, rk));
+        ADASPARK_TRY(check_rows(h, who, "v", c->v, h->cfg.n_kv_heads, rv));
     } else {                                       // no keys at all: k and v may be NULL; the tensor maps need some row, which no row sees
         rk = rv = {rq.p, (long long)h->cfg.n_kv_heads * h->cfg.head_dim, h->cfg.head_dim};
     }
-    if (!cu_q || !cu_k || !out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL pointer", who);
-    if ((uintptr_t)out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: out is not 16-byte aligned", who);
-    if (!workspace || (uintptr_t)workspace % kAlign) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", who);
-    if (workspace_bytes < (size_t)adaspark_attn_text_workspace_bytes(h)) return fail(h, ADASPARK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes", who, workspace_bytes);
+    if (!c->cu_q || !c->cu_k || !c->out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL pointer", who);
+    if ((uintptr_t)c->out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: out is not 16-byte aligned", who);
+    ADASPARK_TRY(check_workspace(h, who, c->workspace, c->workspace_bytes));
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));
     PromptGeom g;
-    g.cu_q = cu_q;
-    g.cu_k = cu_k;
+    g.cu_q = c->cu_q;
+    g.cu_k = c->cu_k;
     g.batch = batch;
     g.n_q = n_q;
     g.n_k = n_k;
@@ -139,99 +188,51 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const void* q, int64_
     // a pair of CTAs per tile, at most as many as there are SMs: 2 T tokens a tile, at most one tile of each sequence not full
     const long long most = ((long long)n_q / (2 * g.T) + batch) * g.Hkv;
     const int pairs = (int)(most < h->sm_count / 2 ? most : h->sm_count / 2);
-    auto launch = [&](auto kernel, size_t bytes) -> adaspark_status_t {
-        if (!set_smem(h, kernel, bytes, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
-        launch_kernel(true, kernel, dim3(2 * pairs), dim3(kPromptThreads), bytes, (cudaStream_t)cuda_stream, g, tmQ, tmK, tmV, (__nv_bfloat16*)out, lse, status);
+    auto launch = [&](auto d) -> adaspark_status_t {
+        constexpr auto kernel = attn_prompt_kernel<d.value>;
+        const size_t bytes = sizeof(PromptSmem<d.value>) + 1024;
+        if (!text_smem<kernel>(h, bytes, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
+        launch_kernel(true, kernel, dim3(2 * pairs), dim3(kPromptThreads), bytes, (cudaStream_t)cuda_stream, g, tmQ, tmK, tmV, (__nv_bfloat16*)c->out, c->lse, c->status);
         return launch_ok(h, "attn_prompt_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
     };
-    return D == 128 ? launch(attn_prompt_kernel<128>, sizeof(PromptSmem<128>) + 1024) : launch(attn_prompt_kernel<64>, sizeof(PromptSmem<64>) + 1024);
+    return D == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>());
 }
 
-adaspark_status_t adaspark_attn_paged_write(adaspark_attn_t* h, const adaspark_attn_pages_t* pages, const void* k, int64_t k_token_stride, int64_t k_head_stride,
-                                            const void* v, int64_t v_token_stride, int64_t v_head_stride, const int32_t* cu, int32_t batch, int32_t n,
-                                            const int32_t* block_table, int32_t table_width, const int32_t* kv_len, int32_t* status, void* cuda_stream) {
-    if (!h) return ADASPARK_ERR_INVALID_ARG;
-    const char* who = "paged_write";
-    if (batch < 0 || n < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: negative size", who);
-    h->launches = 0;
-    if (batch == 0 || n == 0) return ADASPARK_OK;
-    PageGeom g;
-    Rows rk, rv;
-    ADASPARK_TRY(check_pages(h, who, pages, block_table, table_width, g));
-    ADASPARK_TRY(check_rows(h, who, "k", k, k_token_stride, k_head_stride, h->cfg.n_kv_heads, rk));
-    ADASPARK_TRY(check_rows(h, who, "v", v, v_token_stride, v_head_stride, h->cfg.n_kv_heads, rv));
-    if (!cu || !kv_len) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL cu or kv_len", who);
-    DeviceScope scope;
-    ADASPARK_TRY(scope.enter(h, who));
-    FastDiv rows, heads;
-    rows.init(2 * g.Hkv);
-    heads.init(g.Hkv);
-    auto launch = [&](auto kernel) {
-        launch_kernel(true, kernel, dim3((unsigned)((n + kCacheTokens - 1) / kCacheTokens)), dim3(kCacheThreads), 0, (cudaStream_t)cuda_stream, g, rk.p, rk.ts, rk.hs, rv.p, rv.ts, rv.hs,
-                      cu, kv_len, batch, n, rows, heads, status);
-    };
-    const bool e4m3 = pages->format == ADASPARK_PAGES_E4M3;
-    if (h->cfg.head_dim == 128) e4m3 ? launch(paged_write_kernel<128, true>) : launch(paged_write_kernel<128, false>);
-    else e4m3 ? launch(paged_write_kernel<64, true>) : launch(paged_write_kernel<64, false>);
-    return launch_ok(h, "paged_write_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+adaspark_status_t adaspark_attn_paged_write(adaspark_attn_t* h, const adaspark_attn_paged_rows_t* c, void* cuda_stream) {
+    return paged_rows_impl(h, "paged_write", c, true, cuda_stream);
 }
 
-adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t* h, const adaspark_attn_pages_t* pages, const int32_t* cu, int32_t batch, int32_t n,
-                                           const int32_t* block_table, int32_t table_width, const int32_t* kv_len, void* k_out, void* v_out, int32_t* status,
-                                           void* cuda_stream) {
-    if (!h) return ADASPARK_ERR_INVALID_ARG;
-    const char* who = "paged_read";
-    if (batch < 0 || n < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: negative size", who);
-    h->launches = 0;
-    if (batch == 0 || n == 0) return ADASPARK_OK;
-    PageGeom g;
-    ADASPARK_TRY(check_pages(h, who, pages, block_table, table_width, g));
-    if (!cu || !kv_len || !k_out || !v_out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL pointer", who);
-    if ((uintptr_t)k_out % 16 || (uintptr_t)v_out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: outputs are not 16-byte aligned", who);
-    DeviceScope scope;
-    ADASPARK_TRY(scope.enter(h, who));
-    FastDiv rows, heads;
-    rows.init(2 * g.Hkv);
-    heads.init(g.Hkv);
-    auto launch = [&](auto kernel) {
-        launch_kernel(true, kernel, dim3((unsigned)((n + kCacheTokens - 1) / kCacheTokens)), dim3(kCacheThreads), 0, (cudaStream_t)cuda_stream, g, cu, kv_len, batch, n, rows, heads,
-                      (__nv_bfloat16*)k_out, (__nv_bfloat16*)v_out, status);
-    };
-    const bool e4m3 = pages->format == ADASPARK_PAGES_E4M3;
-    if (h->cfg.head_dim == 128) e4m3 ? launch(paged_read_kernel<128, true>) : launch(paged_read_kernel<128, false>);
-    else e4m3 ? launch(paged_read_kernel<64, true>) : launch(paged_read_kernel<64, false>);
-    return launch_ok(h, "paged_read_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t* h, const adaspark_attn_paged_rows_t* c, void* cuda_stream) {
+    return paged_rows_impl(h, "paged_read", c, false, cuda_stream);
 }
 
-adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t* h, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k_new,
-                                             int64_t k_token_stride, int64_t k_head_stride, const void* v_new, int64_t v_token_stride, int64_t v_head_stride,
-                                             const adaspark_attn_pages_t* pages, const int32_t* block_table, int32_t table_width, const int32_t* kv_len,
-                                             int32_t batch, void* out, float* lse, void* workspace, size_t workspace_bytes, int32_t* status, void* cuda_stream) {
+adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t* h, const adaspark_attn_paged_decode_t* c, void* cuda_stream) {
     if (!h) return ADASPARK_ERR_INVALID_ARG;
     const char* who = "paged_decode";
-    if (batch < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: negative batch", who);
+    if (!c || c->batch < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call or negative batch", who);
+    const int batch = c->batch, table_width = c->table_width;
     h->launches = 0;
     if (batch == 0) return ADASPARK_OK;
+    const adaspark_attn_pages_t* pages = &c->pages;
     PageGeom g;
     Rows rq, rk = {nullptr, 0, 0}, rv = {nullptr, 0, 0};
-    if ((k_new == nullptr) != (v_new == nullptr)) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: k_new and v_new must both be given or both be NULL", who);
-    ADASPARK_TRY(check_pages(h, who, pages, block_table, table_width, g));
-    ADASPARK_TRY(check_rows(h, who, "q", q, q_token_stride, q_head_stride, h->cfg.n_q_heads, rq));
-    if (k_new) {
-        ADASPARK_TRY(check_rows(h, who, "k_new", k_new, k_token_stride, k_head_stride, h->cfg.n_kv_heads, rk));
-        ADASPARK_TRY(check_rows(h, who, "v_new", v_new, v_token_stride, v_head_stride, h->cfg.n_kv_heads, rv));
+    if ((c->k_new.data == nullptr) != (c->v_new.data == nullptr)) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: k_new and v_new must both be given or both be NULL", who);
+    ADASPARK_TRY(check_pages(h, who, pages, c->block_table, table_width, g));
+    ADASPARK_TRY(check_rows(h, who, "q", c->q, h->cfg.n_q_heads, rq));
+    if (c->k_new.data) {
+        ADASPARK_TRY(check_rows(h, who, "k_new", c->k_new, h->cfg.n_kv_heads, rk));
+        ADASPARK_TRY(check_rows(h, who, "v_new", c->v_new, h->cfg.n_kv_heads, rv));
     }
-    if (!kv_len || !out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL kv_len or out", who);
-    if ((uintptr_t)out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: out is not 16-byte aligned", who);
-    if (!workspace || (uintptr_t)workspace % kAlign) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: workspace NULL or not 256-byte aligned", who);
-    if (workspace_bytes < (size_t)adaspark_attn_text_workspace_bytes(h)) return fail(h, ADASPARK_ERR_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes", who, workspace_bytes);
+    if (!c->kv_len || !c->out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL kv_len or out", who);
+    if ((uintptr_t)c->out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: out is not 16-byte aligned", who);
+    ADASPARK_TRY(check_workspace(h, who, c->workspace, c->workspace_bytes));
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));
     const int D = h->cfg.head_dim, Hq = h->cfg.n_q_heads;
     const bool e4m3 = pages->format == ADASPARK_PAGES_E4M3;
     const int tile = paged_tile(e4m3), page_size = pages->page_size;
     PagedCall a;
-    a.kv_len = kv_len;
+    a.kv_len = c->kv_len;
     a.batch = batch;
     a.Hq = Hq;
     a.G = Hq / g.Hkv;
@@ -239,10 +240,10 @@ adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t* h, const void* q, 
     a.k_new = rk.p; a.k_ts = rk.ts; a.k_hs = rk.hs;
     a.v_new = rv.p; a.v_ts = rv.ts; a.v_hs = rv.hs;
     a.scale_log2 = text_scale(h) * 1.4426950408889634f;
-    a.out = (__nv_bfloat16*)out;
-    a.lse = lse;
-    a.partial = (float*)workspace;
-    a.status = status;
+    a.out = (__nv_bfloat16*)c->out;
+    a.lse = c->lse;
+    a.partial = (float*)c->workspace;
+    a.status = c->status;
     CUtensorMap tmK, tmV;
     if (!encode_pages(&tmK, g.k, e4m3, g.n_pages, g.Hkv, page_size, D, g.page_stride, page_size < tile ? page_size : tile) ||
         !encode_pages(&tmV, g.v, e4m3, g.n_pages, g.Hkv, page_size, D, g.page_stride, page_size < tile ? page_size : tile))
@@ -251,18 +252,20 @@ adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t* h, const void* q, 
     const long long most = (long long)batch * g.Hkv * (((long long)table_width * page_size + tile - 1) / tile);
     const int n_ctas = (int)(most < kPagedCtas ? most : kPagedCtas);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    auto launch = [&](auto kernel, auto join, size_t bytes) -> adaspark_status_t {
-        if (!set_smem(h, kernel, bytes, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
-        launch_kernel(true, kernel, dim3(n_ctas), dim3(kPagedThreads), bytes, st, g, a, tmK, tmV);
+    auto launch = [&](auto d, auto bytes_held) -> adaspark_status_t {
+        constexpr int kD = d.value;
+        constexpr bool kE4m3 = bytes_held.value;
+        constexpr size_t bytes = sizeof(PagedSmem<kD, kE4m3>);
+        if (!text_smem<paged_decode_kernel<kD, kE4m3>>(h, bytes, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
+        launch_kernel(true, paged_decode_kernel<kD, kE4m3>, dim3(n_ctas), dim3(kPagedThreads), bytes, st, g, a, tmK, tmV);
         if (!launch_ok(h, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
-        launch_kernel(true, join, dim3(Hq, batch), dim3(512), 0, st, g, a, n_ctas);
+        launch_kernel(true, paged_join_kernel<kD, kE4m3>, dim3(Hq, batch), dim3(512), 0, st, g, a, n_ctas);
         return launch_ok(h, "paged_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
     };
-    if (D == 128)
-        return e4m3 ? launch(paged_decode_kernel<128, true>, paged_join_kernel<128, true>, sizeof(PagedSmem<128, true>))
-                    : launch(paged_decode_kernel<128, false>, paged_join_kernel<128, false>, sizeof(PagedSmem<128, false>));
-    return e4m3 ? launch(paged_decode_kernel<64, true>, paged_join_kernel<64, true>, sizeof(PagedSmem<64, true>))
-                : launch(paged_decode_kernel<64, false>, paged_join_kernel<64, false>, sizeof(PagedSmem<64, false>));
+    const std::integral_constant<int, 128> wide;
+    const std::integral_constant<int, 64> narrow;
+    if (D == 128) return e4m3 ? launch(wide, std::true_type()) : launch(wide, std::false_type());
+    return e4m3 ? launch(narrow, std::true_type()) : launch(narrow, std::false_type());
 }
 
 }  // extern "C"

@@ -1,5 +1,5 @@
 """CPU-only checks of the text operators' argument checks: every refusal is found on the host, before any launch."""
-import ctypes
+import os
 
 import pytest
 import torch
@@ -22,7 +22,9 @@ ROW = (P, 0, 0)
 def pages(**kw):
     f = dict(k_pages=P, v_pages=P, k_scale=P, v_scale=P, page_stride=0, scale_stride=0, n_pages=8, page_size=16, format=binding.PAGES_E4M3, reserved=0)
     f.update(kw)
-    return binding.Pages(*[f[n] for n, _ in binding.Pages._fields_])
+    f.pop("reserved")
+    f["page_format"] = f.pop("format")
+    return binding.pages_struct(**f)
 
 
 def code(fn, *a):
@@ -44,7 +46,7 @@ def test_workspace_size_is_known_without_a_partition(handle):
 
 
 @pytest.mark.parametrize("bad,status", [
-    (dict(q=(None, 0, 0)), binding.ERR_INVALID_ARG), (dict(k=(None, 0, 0)), binding.ERR_INVALID_ARG), (dict(out=None), binding.ERR_INVALID_ARG),
+    (dict(q=(0, 0, 0)), binding.ERR_INVALID_ARG), (dict(k=(0, 0, 0)), binding.ERR_INVALID_ARG), (dict(out=None), binding.ERR_INVALID_ARG),
     (dict(cu_q=None), binding.ERR_INVALID_ARG), (dict(cu_k=None), binding.ERR_INVALID_ARG), (dict(batch=-1), binding.ERR_INVALID_ARG),
     (dict(n_q=-1), binding.ERR_INVALID_ARG), (dict(n_k=-4), binding.ERR_INVALID_ARG), (dict(q=(P + 8, 0, 0)), binding.ERR_INVALID_ARG),
     (dict(v=(P, 130, 0)), binding.ERR_INVALID_ARG), (dict(k=(P, 0, 64)), binding.ERR_INVALID_ARG), (dict(q=(P, -256, 0)), binding.ERR_INVALID_ARG),
@@ -57,11 +59,11 @@ def test_prompt_refusals(handle, bad, status):
 
 def test_nothing_to_do_is_no_error(handle):
     prompt(handle, batch=0)
-    prompt(handle, n_q=0, q=(None, 0, 0))
+    prompt(handle, n_q=0, q=(0, 0, 0))
     assert binding.adaspark_attn_last_launch_count(handle) == 0
     binding.adaspark_attn_paged_write(handle, pages(), ROW, ROW, P, 2, 0, P, 4, P, None, None)
-    binding.adaspark_attn_paged_read(handle, pages(), P, 0, 5, P, 4, P, P, P, None, None)
-    binding.adaspark_attn_paged_decode(handle, ROW, (None, 0, 0), (None, 0, 0), pages(), P, 4, P, 0, P, None, P, 0, None, None)
+    binding.adaspark_attn_paged_read(handle, pages(), ROW, ROW, P, 0, 5, P, 4, P, None, None)
+    binding.adaspark_attn_paged_decode(handle, ROW, (0, 0, 0), (0, 0, 0), pages(), P, 4, P, 0, P, None, P, 0, None, None)
 
 
 @pytest.mark.parametrize("bad,status", [
@@ -73,13 +75,25 @@ def test_page_refusals(handle, bad, status):
     p = pages(**bad)
     ws = binding.adaspark_attn_text_workspace_bytes(handle)
     assert code(binding.adaspark_attn_paged_write, handle, p, ROW, ROW, P, 2, 5, P, 4, P, None, None) == status
-    assert code(binding.adaspark_attn_paged_read, handle, p, P, 2, 5, P, 4, P, P, P, None, None) == status
+    assert code(binding.adaspark_attn_paged_read, handle, p, ROW, ROW, P, 2, 5, P, 4, P, None, None) == status
     assert code(binding.adaspark_attn_paged_decode, handle, ROW, ROW, ROW, p, P, 4, P, 2, P, None, P, ws, None, None) == status
+
+
+def test_packed_structs_are_the_headers(tmp_path):
+    """The sizes that the binding packs are the compiler's."""
+    import subprocess
+    src = tmp_path / "sizes.c"
+    names = ["adaspark_attn_pages_t", "adaspark_attn_prompt_t", "adaspark_attn_paged_rows_t", "adaspark_attn_paged_decode_t"]
+    src.write_text('#include "adaspark_attn.h"\n#include <stdio.h>\nint main(void) { printf("' + "%zu " * 4 + '", ' + ", ".join(f"sizeof({n})" for n in names) + "); return 0; }")
+    subprocess.run(["gcc", "-I", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include"), "-o", str(tmp_path / "sizes"), str(src)], check=True)
+    got = [int(x) for x in subprocess.run([str(tmp_path / "sizes")], capture_output=True, text=True, check=True).stdout.split()]
+    p = binding._PAGES.size
+    assert got == [p, binding._PROMPT.size, p + binding._PAGED_ROWS.size, p + binding._PAGED_DECODE.size]
 
 
 def test_other_paged_refusals(handle):
     ws = binding.adaspark_attn_text_workspace_bytes(handle)
-    none = (None, 0, 0)
+    none = (0, 0, 0)
     dec = binding.adaspark_attn_paged_decode
     assert code(dec, handle, ROW, ROW, none, pages(), P, 4, P, 2, P, None, P, ws, None, None) == binding.ERR_INVALID_ARG
     assert code(dec, handle, none, none, none, pages(), P, 4, P, 2, P, None, P, ws, None, None) == binding.ERR_INVALID_ARG
@@ -90,8 +104,10 @@ def test_other_paged_refusals(handle):
     assert code(dec, handle, ROW, none, none, pages(), P, 4, P, -2, P, None, P, ws, None, None) == binding.ERR_INVALID_ARG
     assert code(binding.adaspark_attn_paged_write, handle, pages(), ROW, ROW, None, 2, 5, P, 4, P, None, None) == binding.ERR_INVALID_ARG
     assert code(binding.adaspark_attn_paged_write, handle, pages(), ROW, ROW, P, 2, 5, None, 4, P, None, None) == binding.ERR_INVALID_ARG
-    assert code(binding.adaspark_attn_paged_read, handle, pages(), P, 2, 5, P, 4, P, P + 4, P, None, None) == binding.ERR_INVALID_ARG
-    assert binding.load().adaspark_attn_prompt(None, *[0] * 9, None, None, 1, 1, 1, None, None, None, 0, None, None) == binding.ERR_INVALID_ARG
+    assert code(binding.adaspark_attn_paged_read, handle, pages(), ROW, (P + 4, 0, 0), P, 2, 5, P, 4, P, None, None) == binding.ERR_INVALID_ARG
+    for name in ("prompt", "paged_write", "paged_read", "paged_decode"):
+        assert getattr(binding.load(), "adaspark_attn_" + name)(None, b"", None) == binding.ERR_INVALID_ARG
+        assert getattr(binding.load(), "adaspark_attn_" + name)(handle, None, None) == binding.ERR_INVALID_ARG
 
 
 def test_without_a_gpu_the_calls_fail_loudly(handle):
@@ -111,5 +127,5 @@ def test_paged_cache_refusals():
     pool = torch.zeros(6, 2, 16, 64, dtype=torch.bfloat16)
     assert refused(pool[::2], k)
     c = binding.PagedCache(pool[::2], pool[1::2])                # keys and values of a page beside each other
-    assert c.pages.page_stride == 2 * 2 * 16 * 64 and c.n_pages == 3 and c.page_size == 16
-    assert binding.PagedCache(q, q.clone(), s, s.clone()).pages.format == binding.PAGES_E4M3
+    assert c.page_stride == 2 * 2 * 16 * 64 and c.n_pages == 3 and c.page_size == 16
+    assert binding.PagedCache(q, q.clone(), s, s.clone()).pages[-8:] == binding.PAGES_E4M3.to_bytes(8, "little")
