@@ -12,10 +12,15 @@
 //               their pages and the bytes of the powers of two into a ring, the next (sequence, head)'s q; the new token into its page
 //   warps 0-3   each a quarter of a tile's keys: S = Q K^T, softmax, O += P V, with a state of its own, merged at the end of a run's part
 //
-// 8-bit pages go through the tensor cores as f16, which holds every e4m3 value.  q is brought to f16 by a power of two per row (largest
-// magnitude 2^14 ..: what falls below 2^-29 of it loses bits, 2^-39 of it at most); a key's power of two multiplies its score.  A
-// value's power of two e_j joins its weight: the weights of the product are 2^(x_j + e_j - m') with their own maximum m', so that they stay within f16
-// whatever the rows' sizes, and beside them the sum of 2^(x_j - m) is kept.
+// The scores are S = q K^T with the heads as rows (an 8-row half of the m16 tile where the group has at most 8), the outputs
+// O^T = V^T P^T with the heads as columns: S's accumulators are P^T's operand as they stand, and O takes half the registers and products.
+//
+// 8-bit pages: the scores take K as it is (e4m3 products): q is brought to 2^7 .. by a power of two per row and split into two
+// e4m3 parts, q = hi + lo, exact for every element down to 2^-9 of the row's largest and off by at most 2^-17 of that largest below; with up to 8 heads hi
+// and lo are the two halves of one tile.  A key's power of two multiplies its score.  V goes through the tensor cores as f16, which holds every
+// e4m3 value (8-bit weights would lose a long tail beside one large weight).  A value's power of two e_j joins its
+// weight: the weights of the product are 2^(x_j + e_j - m') with their own maximum m', so that they stay within f16 whatever the
+// rows' sizes, and beside them the sum of 2^(x_j - m) is kept.
 #pragma once
 #include "common.cuh"
 #include "paged_cache.cuh"
@@ -26,6 +31,7 @@ namespace adaspark {
 constexpr int kPagedThreads = 160;
 constexpr int kPagedCtas = 296;              // two per SM of a B200
 constexpr int kPagedRing = 96 * 1024;        // bytes of a CTA's ring
+constexpr int kPartCost = 1;                 // what a part costs beside its tiles, in tiles
 constexpr float kPagedBias = 14.f;           // f16 weights are at most 2^14: 2^-28 of the largest one is still a normal number
 
 __host__ __device__ constexpr int paged_tile(bool e4m3) { return e4m3 ? 128 : 64; }   // keys of a tile
@@ -65,77 +71,96 @@ struct PagedCall {
     int32_t* status;
 };
 
-// The line of tiles: sequence by sequence, kv head by kv head.  Held by a whole warp, which has the tile counts of 32 sequences in its lanes.
+// The line of tiles: sequence by sequence, kv head by kv head, in front of each (sequence, kv head) kPartCost places for what a part costs
+// beside its tiles (q, the merge of the warps, the output).  Held by a whole warp, which has the lengths of 32 sequences in its lanes.
 template <int kTile>
-struct TileLine {
+struct PageLine {
     const PageGeom* p;
     const int32_t* kv_len;
     int batch, lane;
-    int chunk, tiles;                        // first sequence of the lanes' 32, tiles of this lane's sequence (0: none, or out of range)
-    __device__ __forceinline__ int count(int n) const { return n > 0 && n <= (p->table_width << p->page_shift) ? (n + kTile - 1) / kTile : 0; }
+    int chunk, len;                          // first sequence of the lanes' 32, tokens of this lane's sequence (0: none, or out of range)
+    __device__ __forceinline__ bool in_range(int n) const { return n >= 0 && n <= (p->table_width << p->page_shift); }
     __device__ __forceinline__ void load(int c) {
         chunk = c;
-        tiles = c + lane < batch ? count(kv_len[c + lane]) : 0;
+        const int n = c + lane < batch ? kv_len[c + lane] : 0;
+        len = in_range(n) ? n : 0;
     }
+    // places of one (sequence, kv head) of n tokens
+    static __device__ __forceinline__ int places(int n) { return n > 0 ? (n + kTile - 1) / kTile + kPartCost : 0; }
     __device__ __forceinline__ long long total() {
         long long sum = 0;
         for (int c = 0; c < batch; c += 32) {
             load(c);
-            sum += (long long)__reduce_add_sync(0xffffffffu, (unsigned)(tiles & 0xffff)) + ((long long)__reduce_add_sync(0xffffffffu, (unsigned)(tiles >> 16)) << 16);
+            const unsigned x = (unsigned)places(len);
+            sum += (long long)__reduce_add_sync(0xffffffffu, x & 0xffffu) + ((long long)__reduce_add_sync(0xffffffffu, x >> 16) << 16);
         }
         return sum * p->Hkv;
     }
 };
 
-// The line's total tiles are cut into runs of at least one tile: how many, the first tile of run c, and the run that holds tile x.
+// The line's places are cut into runs of at least one: how many, the first place of run c, and the run that holds place x.
 __device__ __forceinline__ int run_count(long long total, int n_ctas) { return (int)min(total, (long long)n_ctas); }
 __device__ __forceinline__ long long run_begin(long long total, int n_runs, int c) { return total * c / n_runs; }
 __device__ __forceinline__ int run_of(long long total, int n_runs, long long x) { return (int)(((x + 1) * n_runs - 1) / total); }
 
-// A place on the line: tile `tile` of `tiles` of (sequence b, kv head gk).
+// A walk along a run, part by part: the tiles [tile, end) of (sequence b, kv head gk), which has n tokens in `tiles` tiles.
 template <int kTile>
-struct LineWalk {
-    TileLine<kTile> line;
-    int b, gk, tile, tiles;
-    // to position x < total
-    __device__ __forceinline__ void seek(long long x) {
+struct RunWalk {
+    PageLine<kTile> line;
+    long long place, stop;                   // first place of the (sequence, kv head); first place behind the run
+    int b, gk, n, tiles, tile, end;
+    // to place x < total; false: no tile there (only the places in front of one)
+    __device__ __forceinline__ bool seek(long long x, long long run_end) {
+        stop = run_end;
+        long long before = 0;
         for (int c = 0; c < line.batch; c += 32) {
             line.load(c);
-            long long upto = (long long)line.tiles * line.p->Hkv;
-            const long long mine = upto;
+            const long long mine = (long long)line.places(line.len) * line.p->Hkv;
+            long long upto = mine;
 #pragma unroll
             for (int s = 1; s < 32; s <<= 1) {
                 const long long y = __shfl_up_sync(0xffffffffu, upto, s);
                 if (line.lane >= s) upto += y;
             }
             const long long all = __shfl_sync(0xffffffffu, upto, 31);
-            if (x < all) {
-                const int who = __ffs(__ballot_sync(0xffffffffu, upto > x)) - 1;
-                const int rest = (int)(x - __shfl_sync(0xffffffffu, upto - mine, who));
+            if (x < before + all) {
+                const int who = __ffs(__ballot_sync(0xffffffffu, before + upto > x)) - 1;
+                const long long first = before + __shfl_sync(0xffffffffu, upto - mine, who);
                 b = c + who;
-                tiles = __shfl_sync(0xffffffffu, line.tiles, who);
-                gk = rest / tiles;
-                tile = rest - gk * tiles;
-                return;
+                n = __shfl_sync(0xffffffffu, line.len, who);
+                tiles = (n + kTile - 1) / kTile;
+                const int per = tiles + kPartCost, rest = (int)(x - first);
+                gk = rest / per;
+                place = first + (long long)gk * per;
+                return begin(max(rest - gk * per - kPartCost, 0));
             }
-            x -= all;
+            before += all;
         }
+        return false;
     }
-    // to the first tile of the next (sequence, kv head); there has to be one
-    __device__ __forceinline__ void next() {
-        tile = 0;
-        if (++gk < line.p->Hkv) return;
+    // the part that begins with tile t; false: the run ends in front of it
+    __device__ __forceinline__ bool begin(int t) {
+        tile = t;
+        end = (int)min((long long)tiles, max(stop - place - kPartCost, 0ll));
+        return end > tile;
+    }
+    // the next part
+    __device__ __forceinline__ bool next() {
+        place += tiles + kPartCost;
+        if (place >= stop) return false;
+        if (++gk < line.p->Hkv) return begin(0);
         gk = 0;
         int from = b + 1 - line.chunk;
         while (true) {
-            const uint32_t there = from < 32 ? __ballot_sync(0xffffffffu, line.tiles > 0) >> from << from : 0u;
+            const uint32_t there = from < 32 ? __ballot_sync(0xffffffffu, line.len > 0) >> from << from : 0u;
             if (there) {
                 const int who = __ffs(there) - 1;
                 b = line.chunk + who;
-                tiles = __shfl_sync(0xffffffffu, line.tiles, who);
-                return;
+                n = __shfl_sync(0xffffffffu, line.len, who);
+                tiles = (n + kTile - 1) / kTile;
+                return begin(0);
             }
-            if (line.chunk + 32 >= line.batch) return;
+            if (line.chunk + 32 >= line.batch) return false;
             line.load(line.chunk + 32);
             from = 0;
         }
@@ -148,15 +173,14 @@ struct PagedSmem {
     static constexpr int kTileBytes = kTile * kRowBytes;       // of K, and of V
     static constexpr int kStages = kPagedRing / (2 * kTileBytes);
     unsigned char kv[kStages][2][kTileBytes];                 // bf16: [panel of 64 d][key][128 bytes]; e4m3: [key][D bytes]; swizzled by TMA
-    float red[16][D];
-    __nv_bfloat16 q[16][D + 8];                               // of one part at a time (read into registers when it begins)
+    float red[16][D + 4];                                     // outputs of a part: 16 heads, or 8 of two halves
+    __nv_bfloat16 q[16][D + 8];                               // of one part (16 heads), or two (8 heads)
     unsigned char scale[kStages][2][kE4m3 ? kTile : 16];
     float stat[4][16][4];
-    uint64_t full[kStages], empty[kStages], q_full, q_empty;
-    int bad[2];                                               // number + 1 of a part with a page that is not there
+    uint64_t full[kStages], empty[kStages], q_full[2], q_empty[2];
+    int bad[4];                                               // number + 1 of a part with a page that is not there
     int abort_flag;
 };
-
 static_assert(sizeof(PagedSmem<128, true>) <= 115712 && sizeof(PagedSmem<128, false>) <= 115712, "two CTAs share an SM");
 
 __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3, const void* smem_ptr) {
@@ -166,6 +190,31 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// D = A(16x32, row) * B(32x8, col) + D, e4m3 inputs, fp32 accumulate.
+__device__ __forceinline__ void mma_e4m3_16832(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 4 bf16 (two words) times f -> 4 codes of the values and 4 of what is left
+__device__ __forceinline__ void split_codes(const uint2& x, float f, uint32_t& hi, uint32_t& lo) {
+    const float v[4] = {__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f, __uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f};
+    hi = lo = 0u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint16_t h2, l2;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(h2) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
+        const uint32_t back = codes_to_f16x2(h2);
+        const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&back));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(l2) : "f"(v[2 * i + 1] - b.y), "f"(v[2 * i] - b.x));
+        hi |= (uint32_t)h2 << (16 * i);
+        lo |= (uint32_t)l2 << (16 * i);
+    }
+}
+// four codes -> two f16 pairs
+__device__ __forceinline__ void codes_to_f16x4(uint32_t c, uint32_t& a, uint32_t& b) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}\n" : "=r"(a), "=r"(b) : "r"(c));
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
@@ -178,13 +227,18 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint3
 }
 __device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 128;\n" ::: "memory"); }
 
-template <int D, bool kE4m3>
+// kGroups: groups of 8 heads, (G + 7) / 8.
+template <int D, bool kE4m3, int kGroups>
 __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom p, PagedCall a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV) {
     using Smem = PagedSmem<D, kE4m3>;
     extern __shared__ __align__(1024) unsigned char paged_smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(paged_smem_raw);
-    constexpr int kTile = Smem::kTile, kStages = Smem::kStages, kTileBytes = Smem::kTileBytes, kRowBytes = Smem::kRowBytes;
-    constexpr int kWarpKeys = kTile / 4, kNTiles = kWarpKeys / 8, kKSteps = D / 16, kDTiles = D / 8, kRowF = paged_row_floats(D);
+    constexpr int kTile = Smem::kTile, kStages = Smem::kStages, kRowBytes = Smem::kRowBytes;
+    constexpr int kWarpKeys = kTile / 4, kNTiles = kWarpKeys / 8, kRowF = paged_row_floats(D);
+    constexpr int kMTiles = D / 16;                           // O^T: tiles of 16 d
+    constexpr int kQSlots = kGroups == 1 ? 2 : 1;             // parts whose q is held
+    constexpr int kQSets = kE4m3 && kGroups == 2 ? 2 : 1;     // hi and lo as tiles of their own
+    constexpr int kQSteps = kE4m3 ? D / 32 : D / 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     launch_dependents();
@@ -193,9 +247,11 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
             tc::mbar_init(&sm.full[s], 1);
             tc::mbar_init(&sm.empty[s], 4);
         }
-        tc::mbar_init(&sm.q_full, 1);
-        tc::mbar_init(&sm.q_empty, 4);
-        sm.bad[0] = sm.bad[1] = 0;
+        for (int s = 0; s < 2; ++s) {
+            tc::mbar_init(&sm.q_full[s], 1);
+            tc::mbar_init(&sm.q_empty[s], 4);
+        }
+        for (int s = 0; s < 4; ++s) sm.bad[s] = 0;
         sm.abort_flag = 0;
         tc::fence_barrier_init();
         tc::prefetch_tensormap(&tmK);
@@ -205,7 +261,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     volatile int* abort_flag = &sm.abort_flag;
     wait_for_previous_kernel();
 
-    LineWalk<kTile> w;
+    RunWalk<kTile> w;
     w.line.p = &p;
     w.line.kv_len = a.kv_len;
     w.line.batch = a.batch;
@@ -213,50 +269,54 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     const long long total = w.line.total();
     const int n_runs = run_count(total, gridDim.x);
     if ((int)blockIdx.x >= n_runs) return;                    // (the whole CTA)
-    const long long it0 = run_begin(total, n_runs, blockIdx.x), it1 = run_begin(total, n_runs, blockIdx.x + 1);
-    w.seek(it0);
+    bool more = w.seek(run_begin(total, n_runs, blockIdx.x), run_begin(total, n_runs, blockIdx.x + 1));
     const int page_shift = p.page_shift, page_size = 1 << page_shift;
 
     if (warp == 4) {
         // ------------------------------------------------------------ producer
         const int sub = min(page_size, kTile), n_sub = kTile / sub;        // tokens of a box, boxes of a tile
-        int st = 0, ph = 1, part = 0;
+        int st = 0, ph = 1;
+        // page numbers: this lane's of the 32 columns from `cols` on of sequence `cols_b`, and of the 32 behind them
+        int cols_b = -1, cols = 0, pages = 0, pages_next = 0;
         bool ok = true;
-        for (long long it = it0; it < it1 && ok; ++part) {
-            const int n_here = (int)min((long long)(w.tiles - w.tile), it1 - it), n = a.kv_len[w.b];
+        for (int part = 0; more && ok; ++part, more = w.next()) {
             const int32_t* table = p.table + (size_t)w.b * p.table_width;
-            // page numbers: this lane's of the 32 columns from `cols` on, and of the 32 behind them
-            const int last_col = (n - 1) >> page_shift;
-            int cols = (w.tile * kTile) >> page_shift;
+            const int last_col = (w.n - 1) >> page_shift, col_begin = (w.tile * kTile) >> page_shift;
             auto page_at = [&](int col) -> int { return col <= last_col ? table[col] : 0; };
-            int pages = page_at(cols + lane), pages_next = page_at(cols + 32 + lane);
+            if (cols_b != w.b || col_begin < cols) {
+                cols_b = w.b;
+                cols = col_begin;
+                pages = page_at(cols + lane);
+                pages_next = page_at(cols + 32 + lane);
+            }
             // q of the heads, a row each
-            if (!(ok = tc::mbar_wait_warp(&sm.q_empty, (part & 1) ^ 1, abort_flag))) break;
-            if (lane == 0) tc::mbar_arrive_expect_tx(&sm.q_full, (uint32_t)a.G * D * 2);
+            const int qs = part % kQSlots;
+            if (!(ok = tc::mbar_wait_warp(&sm.q_empty[qs], ((part / kQSlots) & 1) ^ 1, abort_flag))) break;
+            if (lane == 0) tc::mbar_arrive_expect_tx(&sm.q_full[qs], (uint32_t)a.G * D * 2);
             __syncwarp();
-            if (lane < a.G) bulk_load(&sm.q[lane][0], a.q + w.b * a.q_ts + (w.gk * a.G + lane) * a.q_hs, D * 2, &sm.q_full);
-            for (int i = 0; i < n_here; ++i) {
-                const int tile = w.tile + i, pos0 = tile * kTile, col0 = pos0 >> page_shift;
+            if (lane < a.G) bulk_load(&sm.q[qs * 8 + lane][0], a.q + w.b * a.q_ts + (w.gk * a.G + lane) * a.q_hs, D * 2, &sm.q_full[qs]);
+            for (int tile = w.tile; tile < w.end; ++tile) {
+                const int pos0 = tile * kTile, col0 = pos0 >> page_shift;
                 while (col0 >= cols + 32) {
                     cols += 32;
                     pages = pages_next;
                     pages_next = page_at(cols + 32 + lane);
                 }
-                const int boxes = min((n - pos0 + sub - 1) / sub, n_sub);  // those that hold a token
+                const int boxes = min((w.n - pos0 + sub - 1) / sub, n_sub);   // those that hold a token
                 int page = __shfl_sync(0xffffffffu, pages, min(col0 - cols + lane, 31));
                 const int over = __shfl_sync(0xffffffffu, pages_next, max(col0 - cols + lane - 32, 0) & 31);
                 if (col0 - cols + lane >= 32) page = over;
                 const bool there = page >= 0 && page < p.n_pages;
                 if (__any_sync(0xffffffffu, lane < boxes && !there)) {
                     if (lane == 0) {
-                        sm.bad[part & 1] = part + 1;
+                        sm.bad[part & 3] = part + 1;
                         if (a.status != nullptr) atomicExch(a.status, 1);
                     }
                 } else if (a.k_new != nullptr && tile == w.tiles - 1) {    // the new token: the last of this tile
-                    const int pg = __shfl_sync(0xffffffffu, page, boxes - 1), place = (n - 1) & (page_size - 1);
+                    const int pg = __shfl_sync(0xffffffffu, page, boxes - 1), place = (w.n - 1) & (page_size - 1);
                     append_row<D, kE4m3>(p, pg, w.gk, place, 0, a.k_new + w.b * a.k_ts + w.gk * a.k_hs, lane);
                     append_row<D, kE4m3>(p, pg, w.gk, place, 1, a.v_new + w.b * a.v_ts + w.gk * a.v_hs, lane);
-                    asm volatile("fence.proxy.async;\n" ::: "memory");     // it is read by the copies below
+                    asm volatile("fence.proxy.async;\n" ::: "memory");    // it is read by the copies below
                     __syncwarp();
                 }
                 if (!(ok = tc::mbar_wait_warp(&sm.empty[st], ph, abort_flag))) break;
@@ -282,75 +342,82 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                 __syncwarp();
                 if (++st == kStages) { st = 0; ph ^= 1; }
             }
-            it += n_here;
-            if (it < it1) w.next();
         }
         return;
     }
     // ---------------------------------------------------------------- consumers (they keep to their barriers when a wait has expired)
-    const int rA = lane >> 2, rB = rA + 8, t4 = lane & 3;
-    int st = 0, ph = 0, part = 0;
-    for (long long it = it0; it < it1; ++part) {
-        const int n_here = (int)min((long long)(w.tiles - w.tile), it1 - it), n = a.kv_len[w.b];
-        // ---- q fragments: rows = heads (zero beyond the group)
-        uint32_t qf[kKSteps][4];
-        float fA = a.scale_log2, fB = a.scale_log2;           // what a row's products are multiplied by
-        tc::mbar_wait(&sm.q_full, part & 1, abort_flag);
+    const int g8 = lane >> 2, t4 = lane & 3;                  // the lane's row and column pair of a fragment
+    int st = 0, ph = 0;
+    for (int part = 0; more; ++part, more = w.next()) {
+        const int n = w.n, qs = part % kQSlots;
+        // ---- q fragments
+        uint32_t qf[kQSets][kQSteps][4];
+        float f[kGroups];                                     // what the products of head g8 (g8 + 8) are multiplied by
+        tc::mbar_wait(&sm.q_full[qs], (part / kQSlots) & 1, abort_flag);
         {
-            const __nv_bfloat16 *qa = sm.q[rA], *qb = sm.q[rB];
-            const bool hasA = rA < a.G, hasB = rB < a.G;
+            const __nv_bfloat16* qr[2] = {sm.q[qs * 8 + g8], sm.q[(kGroups == 2 ? 8 : 0) + g8]};
+            const bool has[2] = {g8 < a.G, kGroups == 2 && g8 + 8 < a.G};
             if (!kE4m3) {
+                f[0] = f[kGroups - 1] = a.scale_log2;
 #pragma unroll
-                for (int ks = 0; ks < kKSteps; ++ks) {
-                    const int c = ks * 16 + 2 * t4;
-                    qf[ks][0] = hasA ? *reinterpret_cast<const uint32_t*>(qa + c) : 0u;
-                    qf[ks][1] = hasB ? *reinterpret_cast<const uint32_t*>(qb + c) : 0u;
-                    qf[ks][2] = hasA ? *reinterpret_cast<const uint32_t*>(qa + c + 8) : 0u;
-                    qf[ks][3] = hasB ? *reinterpret_cast<const uint32_t*>(qb + c + 8) : 0u;
-                }
-            } else {
-                // Thread t of a quad has the 16-byte chunks t (D = 64) or 2 t, 2 t + 1 (D = 128) of a key's codes: step (chunk j, word i)
-                // takes d = 16 * chunk + 4 i .. + 3 as the k indexes 2t, 2t + 1, 2t + 8, 2t + 9
-                uint32_t top[2] = {0u, 0u};
-#pragma unroll
-                for (int ks = 0; ks < kKSteps; ++ks) {
-                    const int d = 16 * (D == 128 ? 2 * t4 + (ks >> 2) : t4) + 4 * (ks & 3);
-                    const uint2 x = hasA ? *reinterpret_cast<const uint2*>(qa + d) : make_uint2(0u, 0u);
-                    const uint2 y = hasB ? *reinterpret_cast<const uint2*>(qb + d) : make_uint2(0u, 0u);
-                    qf[ks][0] = x.x; qf[ks][2] = x.y; qf[ks][1] = y.x; qf[ks][3] = y.y;
-                    top[0] = __vmaxu2(top[0], __vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu));
-                    top[1] = __vmaxu2(top[1], __vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu));
-                }
-                float mul[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    uint32_t m = max(top[r] & 0xffffu, top[r] >> 16);
-                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                    const int e = max((int)(m >> 7), 30);                  // biased exponent of the largest; 2^14 is 141
-                    mul[r] = __uint_as_float((uint32_t)(127 + 141 - e) << 23);       // e = 255 (no number): 2^-... and stays one
-                    (r ? fB : fA) = a.scale_log2 * __uint_as_float((uint32_t)min(127 + e - 141, 254) << 23);
-                }
-#pragma unroll
-                for (int ks = 0; ks < kKSteps; ++ks)
+                for (int ks = 0; ks < kQSteps; ++ks)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float f = mul[e & 1];
-                        qf[ks][e] = pack_f16x2(__uint_as_float(qf[ks][e] << 16) * f, __uint_as_float(qf[ks][e] & 0xffff0000u) * f);
+                        const int c = ks * 16 + 2 * t4 + (e >> 1) * 8;
+                        qf[0][ks][e] = has[e & 1] ? *reinterpret_cast<const uint32_t*>(qr[e & 1] + c) : 0u;
                     }
+            } else {
+                // Thread t4 of a quad has the 16-byte chunks 2 t4, 2 t4 + 1 (D = 64: t4) of a key's codes: step (chunk, half u) takes
+                // d = 16 * chunk + 8 u + 0 .. 3 and + 4 .. 7 as the k indexes 4 t4 .. and 16 + 4 t4 ..
+#pragma unroll
+                for (int r = 0; r < kGroups; ++r) {
+                    uint2 x[kQSteps][2];
+                    uint32_t top = 0u;
+#pragma unroll
+                    for (int ks = 0; ks < kQSteps; ++ks)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int d = 16 * (D == 128 ? 2 * t4 + (ks >> 1) : t4) + 8 * (ks & 1) + 4 * y;
+                            x[ks][y] = has[r] ? *reinterpret_cast<const uint2*>(qr[r] + d) : make_uint2(0u, 0u);
+                            top = __vmaxu2(top, __vmaxu2(x[ks][y].x & 0x7fff7fffu, x[ks][y].y & 0x7fff7fffu));
+                        }
+                    top = max(top & 0xffffu, top >> 16);
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    const int e = max((int)(top >> 7), 30);                // biased exponent of the largest: it becomes 2^7
+                    const float mul = __uint_as_float((uint32_t)(127 + 134 - e) << 23);
+                    f[r] = e == 255 ? NAN : a.scale_log2 * __uint_as_float((uint32_t)(127 + e - 134) << 23);   // (no number among them: none comes out)
+#pragma unroll
+                    for (int ks = 0; ks < kQSteps; ++ks)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            uint32_t hi, lo;
+                            split_codes(x[ks][y], mul, hi, lo);
+                            if (kGroups == 1) {                            // rows 0 .. 7: hi, rows 8 .. 15: lo
+                                qf[0][ks][2 * y] = hi;
+                                qf[0][ks][2 * y + 1] = lo;
+                            } else {
+                                qf[0][ks][2 * y + r] = hi;
+                                qf[kQSets - 1][ks][2 * y + r] = lo;
+                            }
+                        }
+                }
             }
         }
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&sm.q_empty);
+        if (lane == 0) tc::mbar_arrive(&sm.q_empty[qs]);
 
-        // running maxima and sums of rows A and B; with e4m3 pages mv is the maximum of the weights of the products
-        float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f, mvA = -INFINITY, mvB = -INFINITY;
-        float o[kDTiles][4];
+        // running maximum and sum of head g8 (g8 + 8); with e4m3 pages mv is the maximum of the weights of the products
+        float m[kGroups], l[kGroups], mv[kGroups], o[kGroups][kMTiles][4];
 #pragma unroll
-        for (int i = 0; i < kDTiles; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-
-        for (int i = 0; i < n_here; ++i) {
-            const int n_vis = n - (w.tile + i) * kTile - warp * kWarpKeys;      // keys of this warp's quarter that are there
+        for (int r = 0; r < kGroups; ++r) {
+            m[r] = mv[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kMTiles; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
+        }
+        for (int tile = w.tile; tile < w.end; ++tile) {
+            const int n_vis = n - tile * kTile - warp * kWarpKeys;         // keys of this warp's quarter that are there
             tc::mbar_wait(&sm.full[st], ph, abort_flag);
             if (n_vis > 0) {
                 unsigned char* kst = sm.kv[st][0];
@@ -366,115 +433,122 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");   // TMA writes there again
                     __syncwarp();
                 }
-                float sc[kNTiles][4];
+                float x[kGroups][kNTiles][2];                 // scores of keys 8 nt + 2 t4, + 1, times scale_log2
+                float ve[kNTiles][2];                         // their values' e_j
+                {
+                    float sc[kQSets][kNTiles][4];
 #pragma unroll
-                for (int nt = 0; nt < kNTiles; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
-                if (!kE4m3) {
+                    for (int nt = 0; nt < kNTiles; ++nt)
 #pragma unroll
-                    for (int ks = 0; ks < kKSteps; ++ks) {
-                        const int row = row0 + (lane & 7) + ((lane >> 4) << 3), chunk = ks * 2 + ((lane >> 3) & 1);
-                        uint32_t b0, b1, b2, b3;
-                        ldmatrix_x4(b0, b1, b2, b3, kst + (chunk >> 3) * (kTile * 128) + sw128(row, chunk & 7));
-                        mma_bf16_16816(sc[0], qf[ks], b0, b1);
-                        mma_bf16_16816(sc[1], qf[ks], b2, b3);
-                    }
-                } else {
+                        for (int y = 0; y < kQSets; ++y) sc[y][nt][0] = sc[y][nt][1] = sc[y][nt][2] = sc[y][nt][3] = 0.f;
+                    if (!kE4m3) {
 #pragma unroll
-                    for (int nt = 0; nt < kNTiles; ++nt) {
-                        const int row = row0 + nt * 8 + rA;
+                        for (int ks = 0; ks < kQSteps; ++ks) {
+                            const int row = row0 + (lane & 7) + ((lane >> 4) << 3), chunk = ks * 2 + ((lane >> 3) & 1);
+                            uint32_t b0, b1, b2, b3;
+                            ldmatrix_x4(b0, b1, b2, b3, kst + (chunk >> 3) * (kTile * 128) + sw128(row, chunk & 7));
+                            mma_bf16_16816(sc[0][0], qf[0][ks], b0, b1);
+                            mma_bf16_16816(sc[0][1], qf[0][ks], b2, b3);
+                        }
+                    } else {
 #pragma unroll
                         for (int j = 0; j < D / 64; ++j) {
-                            const uint4 x = D == 128 ? *reinterpret_cast<const uint4*>(kst + row * 128 + (((2 * t4 + j) ^ (row & 7)) << 4))
-                                                     : *reinterpret_cast<const uint4*>(kst + row * 64 + ((t4 ^ ((row >> 1) & 3)) << 4));
-                            const uint32_t c[4] = {x.x, x.y, x.z, x.w};
+                            uint4 c[kNTiles];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) mma_f16_16816(sc[nt], qf[j * 4 + e], codes_to_f16x2(c[e] & 0xffffu), codes_to_f16x2(c[e] >> 16));
+                            for (int nt = 0; nt < kNTiles; ++nt) {
+                                const int row = row0 + nt * 8 + g8;
+                                c[nt] = D == 128 ? *reinterpret_cast<const uint4*>(kst + row * 128 + (((2 * t4 + j) ^ (row & 7)) << 4))
+                                                 : *reinterpret_cast<const uint4*>(kst + row * 64 + ((t4 ^ ((row >> 1) & 3)) << 4));
+                            }
+#pragma unroll
+                            for (int y = 0; y < kQSets; ++y)
+#pragma unroll
+                                for (int nt = 0; nt < kNTiles; ++nt) {
+                                    mma_e4m3_16832(sc[y][nt], qf[y][2 * j], c[nt].x, c[nt].y);
+                                    mma_e4m3_16832(sc[y][nt], qf[y][2 * j + 1], c[nt].z, c[nt].w);
+                                }
                         }
                     }
-                }
-                // ---- x_j, their maxima, and with e4m3 x_j + e_j and theirs
-                float ve[kNTiles][2];                         // e_j of this thread's keys
-                float mxA = -INFINITY, mxB = -INFINITY, mxvA = -INFINITY, mxvB = -INFINITY;
 #pragma unroll
-                for (int nt = 0; nt < kNTiles; ++nt) {
-                    float k0 = 1.f, k1 = 1.f;
-                    if (kE4m3) {
-                        const uint32_t ks2 = *reinterpret_cast<const uint16_t*>(&sm.scale[st][0][row0 + nt * 8 + 2 * t4]);
-                        const uint32_t vs2 = *reinterpret_cast<const uint16_t*>(&sm.scale[st][1][row0 + nt * 8 + 2 * t4]);
-                        k0 = pow2_of_byte(ks2 & 0xffu);
-                        k1 = pow2_of_byte(ks2 >> 8);
-                        ve[nt][0] = (float)(int)(vs2 & 0xffu) - 127.f;
-                        ve[nt][1] = (float)(int)(vs2 >> 8) - 127.f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const bool seen = nt * 8 + 2 * t4 + e < n_vis;
-                        const float kf = e ? k1 : k0;
-                        const float xa = seen ? (kE4m3 ? sc[nt][e] * fA * kf : sc[nt][e] * fA) : -INFINITY;
-                        const float xb = seen ? (kE4m3 ? sc[nt][2 + e] * fB * kf : sc[nt][2 + e] * fB) : -INFINITY;
-                        sc[nt][e] = xa;
-                        sc[nt][2 + e] = xb;
-                        mxA = fmaxf(mxA, xa);
-                        mxB = fmaxf(mxB, xb);
+                    for (int nt = 0; nt < kNTiles; ++nt) {
+                        float kf[2] = {1.f, 1.f};
                         if (kE4m3) {
-                            mxvA = fmaxf(mxvA, xa + ve[nt][e]);
-                            mxvB = fmaxf(mxvB, xb + ve[nt][e]);
+                            const uint32_t ks2 = *reinterpret_cast<const uint16_t*>(&sm.scale[st][0][row0 + nt * 8 + 2 * t4]);
+                            const uint32_t vs2 = *reinterpret_cast<const uint16_t*>(&sm.scale[st][1][row0 + nt * 8 + 2 * t4]);
+                            kf[0] = __uint_as_float((ks2 & 0xffu) << 23);  // (byte 0 as zero: such a key is below 1e-35)
+                            kf[1] = __uint_as_float((ks2 >> 8) << 23);
+                            ve[nt][0] = (float)(int)(vs2 & 0xffu) - 127.f;
+                            ve[nt][1] = (float)(int)(vs2 >> 8) - 127.f;
                         }
+#pragma unroll
+                        for (int r = 0; r < kGroups; ++r)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float v = !kE4m3 ? sc[0][nt][2 * r + e]
+                                                       : (kGroups == 1 ? sc[0][nt][e] + sc[0][nt][2 + e] : sc[0][nt][2 * r + e] + sc[kQSets - 1][nt][2 * r + e]);
+                                x[r][nt][e] = kE4m3 ? v * f[r] * kf[e] : v * f[r];
+                            }
                     }
                 }
+                if (n_vis < kWarpKeys) {
 #pragma unroll
-                for (int x = 1; x < 4; x <<= 1) {
-                    mxA = fmaxf(mxA, __shfl_xor_sync(0xffffffffu, mxA, x));
-                    mxB = fmaxf(mxB, __shfl_xor_sync(0xffffffffu, mxB, x));
-                    if (kE4m3) {
-                        mxvA = fmaxf(mxvA, __shfl_xor_sync(0xffffffffu, mxvA, x));
-                        mxvB = fmaxf(mxvB, __shfl_xor_sync(0xffffffffu, mxvB, x));
+                    for (int r = 0; r < kGroups; ++r)
+#pragma unroll
+                        for (int nt = 0; nt < kNTiles; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (nt * 8 + 2 * t4 + e >= n_vis) x[r][nt][e] = -INFINITY;
+                }
+                uint32_t pf[kGroups][kNTiles];                // P^T: two keys of a head
+#pragma unroll
+                for (int r = 0; r < kGroups; ++r) {
+                    float mx = -INFINITY, mxv = -INFINITY;
+#pragma unroll
+                    for (int nt = 0; nt < kNTiles; ++nt) {
+                        mx = fmax3(mx, x[r][nt][0], x[r][nt][1]);
+                        if (kE4m3) mxv = fmax3(mxv, x[r][nt][0] + ve[nt][0], x[r][nt][1] + ve[nt][1]);
+                    }
+#pragma unroll
+                    for (int y = 1; y < 4; y <<= 1) {
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, y));
+                        if (kE4m3) mxv = fmaxf(mxv, __shfl_xor_sync(0xffffffffu, mxv, y));
+                    }
+                    if (!kE4m3) mxv = mx;
+                    if (__any_sync(0xffffffffu, mx > m[r] || mxv > mv[r])) {
+                        const float nm = fmaxf(m[r], mx), nmv = fmaxf(mv[r], mxv);
+                        l[r] = m[r] == -INFINITY ? 0.f : l[r] * fast_exp2(m[r] - nm);
+                        const float c = mv[r] == -INFINITY ? 0.f : fast_exp2(mv[r] - nmv);
+                        // of heads 2 t4 and 2 t4 + 1, the columns of O^T
+                        const float c0 = __shfl_sync(0xffffffffu, c, 8 * t4), c1 = __shfl_sync(0xffffffffu, c, 8 * t4 + 4);
+#pragma unroll
+                        for (int i = 0; i < kMTiles; ++i) {
+                            o[r][i][0] *= c0; o[r][i][2] *= c0;
+                            o[r][i][1] *= c1; o[r][i][3] *= c1;
+                        }
+                        m[r] = nm;
+                        mv[r] = nmv;
+                    }
+                    // (a maximum of -inf: every score of the head is; 2^(-inf - 0) = 0 then)
+                    const float ref = m[r] == -INFINITY ? 0.f : m[r], refv = (mv[r] == -INFINITY ? 0.f : mv[r]) - kPagedBias;
+#pragma unroll
+                    for (int nt = 0; nt < kNTiles; ++nt) {
+                        const float p0 = fast_exp2(x[r][nt][0] - ref), p1 = fast_exp2(x[r][nt][1] - ref);
+                        l[r] += p0 + p1;
+                        pf[r][nt] = kE4m3 ? pack_f16x2(fast_exp2(x[r][nt][0] + (ve[nt][0] - refv)), fast_exp2(x[r][nt][1] + (ve[nt][1] - refv))) : pack_bf16x2(p0, p1);
                     }
                 }
                 if (!kE4m3) {
-                    mxvA = mxA;
-                    mxvB = mxB;
-                }
-                if (__any_sync(0xffffffffu, mxA > mA || mxB > mB || mxvA > mvA || mxvB > mvB)) {
-                    const float nA = fmaxf(mA, mxA), nB = fmaxf(mB, mxB), nvA = fmaxf(mvA, mxvA), nvB = fmaxf(mvB, mxvB);
-                    lA = mA == -INFINITY ? 0.f : lA * fast_exp2(mA - nA);
-                    lB = mB == -INFINITY ? 0.f : lB * fast_exp2(mB - nB);
-                    const float cA = mvA == -INFINITY ? 0.f : fast_exp2(mvA - nvA), cB = mvB == -INFINITY ? 0.f : fast_exp2(mvB - nvB);
 #pragma unroll
-                    for (int dt = 0; dt < kDTiles; ++dt) {
-                        o[dt][0] *= cA; o[dt][1] *= cA;
-                        o[dt][2] *= cB; o[dt][3] *= cB;
-                    }
-                    mA = nA; mB = nB; mvA = nvA; mvB = nvB;
-                }
-                // (a maximum of -inf: every score of the row is; 2^(-inf - 0) = 0 then)
-                const float refA = mA == -INFINITY ? 0.f : mA, refB = mB == -INFINITY ? 0.f : mB;
-                const float refvA = (mvA == -INFINITY ? 0.f : mvA) - kPagedBias, refvB = (mvB == -INFINITY ? 0.f : mvB) - kPagedBias;
-                uint32_t pf[kNTiles / 2][4];
+                    for (int i = 0; i < kMTiles; ++i) {       // rows d of V^T: (keys 0..7, d lo), (keys 0..7, d hi), (keys 8..15, d lo), (keys 8..15, d hi)
+                        const int row = row0 + (lane & 7) + ((lane >> 4) << 3), chunk = i * 2 + ((lane >> 3) & 1);
+                        uint32_t v[4];
+                        ldmatrix_x4_trans(v[0], v[1], v[2], v[3], vst + (chunk >> 3) * (kTile * 128) + sw128(row, chunk & 7));
 #pragma unroll
-                for (int nt = 0; nt < kNTiles; ++nt) {
-                    const float p0 = fast_exp2(sc[nt][0] - refA), p1 = fast_exp2(sc[nt][1] - refA), p2 = fast_exp2(sc[nt][2] - refB), p3 = fast_exp2(sc[nt][3] - refB);
-                    lA += p0 + p1;
-                    lB += p2 + p3;
-                    if (kE4m3) {
-                        pf[nt / 2][(nt & 1) * 2] = pack_f16x2(fast_exp2(sc[nt][0] + ve[nt][0] - refvA), fast_exp2(sc[nt][1] + ve[nt][1] - refvA));
-                        pf[nt / 2][(nt & 1) * 2 + 1] = pack_f16x2(fast_exp2(sc[nt][2] + ve[nt][0] - refvB), fast_exp2(sc[nt][3] + ve[nt][1] - refvB));
-                    } else {
-                        pf[nt / 2][(nt & 1) * 2] = pack_bf16x2(p0, p1);
-                        pf[nt / 2][(nt & 1) * 2 + 1] = pack_bf16x2(p2, p3);
-                    }
-                }
-                if (!kE4m3) {
-#pragma unroll
-                    for (int dp = 0; dp < kDTiles / 2; ++dp) {
-                        const int row = row0 + (lane & 7) + (((lane >> 3) & 1) << 3), chunk = dp * 2 + (lane >> 4);
-                        uint32_t b0, b1, b2, b3;
-                        ldmatrix_x4_trans(b0, b1, b2, b3, vst + (chunk >> 3) * (kTile * 128) + sw128(row, chunk & 7));
-                        mma_bf16_16816(o[dp * 2], pf[0], b0, b1);
-                        mma_bf16_16816(o[dp * 2 + 1], pf[0], b2, b3);
+                        for (int r = 0; r < kGroups; ++r) mma_bf16_16816(o[r][i], v, pf[r][0], pf[r][1]);
                     }
                 } else {
-                    // Lane group g has the bytes [g * D / 8, (g + 1) * D / 8) of a key's values: column g of d tile i is d = g * D / 8 + i
+                    // Lane group g8 has the bytes [g8 * D / 8, (g8 + 1) * D / 8) of a key's values: rows g8 and g8 + 8 of d tile i are
+                    // d = g8 * D / 8 + 2 i and + 1
 #pragma unroll
                     for (int s = 0; s < kNTiles / 2; ++s) {
                         uint32_t v[4][D / 32];
@@ -482,22 +556,24 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                         for (int y = 0; y < 4; ++y) {
                             const int row = row0 + s * 16 + 2 * t4 + (y & 1) + (y >> 1) * 8;
                             if (D == 128) {
-                                const uint4 x = *reinterpret_cast<const uint4*>(vst + row * 128 + ((rA ^ (row & 7)) << 4));
-                                v[y][0] = x.x; v[y][1] = x.y; v[y][D / 64] = x.z; v[y][D / 32 - 1] = x.w;
+                                const uint4 c = *reinterpret_cast<const uint4*>(vst + row * 128 + ((g8 ^ (row & 7)) << 4));
+                                v[y][0] = c.x; v[y][1] = c.y; v[y][D / 64] = c.z; v[y][D / 32 - 1] = c.w;
                             } else {
-                                const uint2 x = *reinterpret_cast<const uint2*>(vst + row * 64 + (((rA >> 1) ^ ((row >> 1) & 3)) << 4) + (rA & 1) * 8);
-                                v[y][0] = x.x; v[y][1] = x.y;
+                                const uint2 c = *reinterpret_cast<const uint2*>(vst + row * 64 + (((g8 >> 1) ^ ((row >> 1) & 3)) << 4) + (g8 & 1) * 8);
+                                v[y][0] = c.x; v[y][1] = c.y;
                             }
                         }
 #pragma unroll
-                        for (int x = 0; x < D / 32; ++x) {
-                            const uint32_t lo0 = __byte_perm(v[0][x], v[1][x], 0x5140), hi0 = __byte_perm(v[0][x], v[1][x], 0x7362);
-                            const uint32_t lo1 = __byte_perm(v[2][x], v[3][x], 0x5140), hi1 = __byte_perm(v[2][x], v[3][x], 0x7362);
-                            mma_f16_16816(o[4 * x], pf[s], codes_to_f16x2(lo0 & 0xffffu), codes_to_f16x2(lo1 & 0xffffu));
-                            mma_f16_16816(o[4 * x + 1], pf[s], codes_to_f16x2(lo0 >> 16), codes_to_f16x2(lo1 >> 16));
-                            mma_f16_16816(o[4 * x + 2], pf[s], codes_to_f16x2(hi0 & 0xffffu), codes_to_f16x2(hi1 & 0xffffu));
-                            mma_f16_16816(o[4 * x + 3], pf[s], codes_to_f16x2(hi0 >> 16), codes_to_f16x2(hi1 >> 16));
-                        }
+                        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                const uint32_t sel = y ? 0x7362 : 0x5140;
+                                uint32_t vf[4];
+                                codes_to_f16x4(__byte_perm(v[0][c], v[1][c], sel), vf[0], vf[1]);
+                                codes_to_f16x4(__byte_perm(v[2][c], v[3][c], sel), vf[2], vf[3]);
+#pragma unroll
+                                for (int r = 0; r < kGroups; ++r) mma_f16_16816(o[r][2 * c + y], vf, pf[r][2 * s], pf[r][2 * s + 1]);
+                            }
                     }
                 }
             }
@@ -506,74 +582,87 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
             if (++st == kStages) { st = 0; ph ^= 1; }
         }
 
-        // ---- the four warps' states, one after the other into one (always in the same order)
-        lA += __shfl_xor_sync(0xffffffffu, lA, 1);
-        lA += __shfl_xor_sync(0xffffffffu, lA, 2);
-        lB += __shfl_xor_sync(0xffffffffu, lB, 1);
-        lB += __shfl_xor_sync(0xffffffffu, lB, 2);
-        if (t4 == 0) {
-            *reinterpret_cast<float4*>(sm.stat[warp][rA]) = make_float4(mA, lA, mvA, 0.f);
-            *reinterpret_cast<float4*>(sm.stat[warp][rB]) = make_float4(mB, lB, mvB, 0.f);
+        // ---- the warps' states into one, always in the same order: with 8 heads two halves at a time, (0 and 1) + (2 and 3)
+        float c[kGroups];
+#pragma unroll
+        for (int r = 0; r < kGroups; ++r) {
+            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+            if (t4 == 0) *reinterpret_cast<float4*>(sm.stat[warp][r * 8 + g8]) = make_float4(m[r], l[r], mv[r], 0.f);
         }
+        // warps that had a key of the part (the first ones, where it is one tile)
+        const int live = w.end - w.tile > 1 ? 4 : min(4, (n - w.tile * kTile + kWarpKeys - 1) / kWarpKeys);
         consumer_sync();
-        float allvA = -INFINITY, allvB = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            allvA = fmaxf(allvA, sm.stat[x][rA][2]);
-            allvB = fmaxf(allvB, sm.stat[x][rB][2]);
+        for (int r = 0; r < kGroups; ++r) {
+            float all = -INFINITY;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) all = fmaxf(all, sm.stat[y][r * 8 + g8][2]);
+            c[r] = mv[r] == -INFINITY ? 0.f : fast_exp2(mv[r] - all);
         }
-        const float cA = mvA == -INFINITY ? 0.f : fast_exp2(mvA - allvA), cB = mvB == -INFINITY ? 0.f : fast_exp2(mvB - allvB);
+        constexpr int kHalves = kGroups == 1 ? 2 : 1;
 #pragma unroll 1
-        for (int x = 0; x < 4; ++x) {
-            if (warp == x) {
+        for (int y = 0; y < live; y += kHalves) {
+            if (warp >= y && warp < y + kHalves && warp < live) {
 #pragma unroll
-                for (int dt = 0; dt < kDTiles; ++dt) {
-                    float2* da = reinterpret_cast<float2*>(&sm.red[rA][(dt * 8 + 2 * t4) ^ ((rA & 3) << 3)]);
-                    float2* db = reinterpret_cast<float2*>(&sm.red[rB][(dt * 8 + 2 * t4) ^ ((rB & 3) << 3)]);
-                    const float2 wasA = x ? *da : make_float2(0.f, 0.f);
-                    *da = make_float2(wasA.x + o[dt][0] * cA, wasA.y + o[dt][1] * cA);
-                    if (a.G > 8) {
-                        const float2 wasB = x ? *db : make_float2(0.f, 0.f);
-                        *db = make_float2(wasB.x + o[dt][2] * cB, wasB.y + o[dt][3] * cB);
+                for (int r = 0; r < kGroups; ++r) {
+                    const float c0 = __shfl_sync(0xffffffffu, c[r], 8 * t4), c1 = __shfl_sync(0xffffffffu, c[r], 8 * t4 + 4);
+                    float* d0 = sm.red[(kGroups == 1 ? warp & 1 : r) * 8 + 2 * t4];
+                    float* d1 = d0 + (D + 4);
+#pragma unroll
+                    for (int i = 0; i < kMTiles; ++i) {
+                        if (kE4m3) {
+                            const int at = (g8 * (D / 8) + 2 * i) ^ ((g8 << 1) & (D / 8 - 1));
+                            const float2 a0 = y ? *reinterpret_cast<float2*>(d0 + at) : make_float2(0.f, 0.f), a1 = y ? *reinterpret_cast<float2*>(d1 + at) : make_float2(0.f, 0.f);
+                            *reinterpret_cast<float2*>(d0 + at) = make_float2(a0.x + o[r][i][0] * c0, a0.y + o[r][i][2] * c0);
+                            *reinterpret_cast<float2*>(d1 + at) = make_float2(a1.x + o[r][i][1] * c1, a1.y + o[r][i][3] * c1);
+                        } else {
+                            const int at = i * 16 + g8;
+                            d0[at] = (y ? d0[at] : 0.f) + o[r][i][0] * c0;
+                            d1[at] = (y ? d1[at] : 0.f) + o[r][i][1] * c1;
+                            d0[at + 8] = (y ? d0[at + 8] : 0.f) + o[r][i][2] * c0;
+                            d1[at + 8] = (y ? d1[at + 8] : 0.f) + o[r][i][3] * c1;
+                        }
                     }
                 }
             }
             consumer_sync();
         }
-        const bool whole = w.tile == 0 && n_here == w.tiles;
-        const bool bad = *(volatile int*)&sm.bad[part & 1] == part + 1;
+        const bool whole = w.tile == 0 && w.end == w.tiles;
+        const bool bad = *(volatile int*)&sm.bad[part & 3] == part + 1;
         const int slot = w.tile > 0 ? 0 : 1;                  // a part that goes on from an earlier run, one that begins here
         float* dst = a.partial + ((size_t)(blockIdx.x * 2 + slot) * a.G) * kRowF;
         for (int idx = tid; idx < a.G * (D / 2); idx += 128) {
             const int row = idx / (D / 2), d = (idx % (D / 2)) * 2;
-            float m = -INFINITY, mv = -INFINITY, l = 0.f;
+            float am = -INFINITY, amv = -INFINITY, al = 0.f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                m = fmaxf(m, sm.stat[x][row][0]);
-                mv = fmaxf(mv, sm.stat[x][row][2]);
+            for (int y = 0; y < 4; ++y) {
+                am = fmaxf(am, sm.stat[y][row][0]);
+                amv = fmaxf(amv, sm.stat[y][row][2]);
             }
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float mx = sm.stat[x][row][0], lx = sm.stat[x][row][1];
-                if (lx != 0.f) l += lx * fast_exp2(mx == -INFINITY ? 0.f : mx - m);
+            for (int y = 0; y < 4; ++y) {
+                const float my = sm.stat[y][row][0], ly = sm.stat[y][row][1];
+                if (ly != 0.f) al += ly * fast_exp2(my == -INFINITY ? 0.f : my - am);
             }
-            // e4m3: column c of d tile i is d = c * D / 8 + i
-            const int c0 = kE4m3 ? (d % (D / 8)) * 8 + d / (D / 8) : d, c1 = kE4m3 ? ((d + 1) % (D / 8)) * 8 + (d + 1) / (D / 8) : d + 1;
-            const float o0 = sm.red[row][c0 ^ ((row & 3) << 3)], o1 = sm.red[row][c1 ^ ((row & 3) << 3)];
+            const int at = kE4m3 ? d ^ (((d / (D / 8)) << 1) & (D / 8 - 1)) : d;
+            float2 v = *reinterpret_cast<const float2*>(&sm.red[row][at]);
+            if (kGroups == 1 && live > 1) {
+                const float2 u = *reinterpret_cast<const float2*>(&sm.red[8 + row][at]);
+                v = make_float2(v.x + u.x, v.y + u.y);
+            }
             if (whole) {
-                const float f = kE4m3 ? exp2f(mv - m - kPagedBias) : 1.f, inv = 1.f / l;
-                const size_t at = (size_t)w.b * a.Hq + w.gk * a.G + row;
-                *reinterpret_cast<uint32_t*>(a.out + at * D + d) = bad ? 0u : pack_bf16x2(o0 * inv * f, o1 * inv * f);
-                if (d == 0 && a.lse != nullptr) a.lse[at] = bad ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+                const float fo = kE4m3 ? exp2f(amv - am - kPagedBias) : 1.f, inv = 1.f / al;
+                const size_t out_at = (size_t)w.b * a.Hq + w.gk * a.G + row;
+                *reinterpret_cast<uint32_t*>(a.out + out_at * D + d) = bad ? 0u : pack_bf16x2(v.x * inv * fo, v.y * inv * fo);
+                if (d == 0 && a.lse != nullptr) a.lse[out_at] = bad ? -INFINITY : (am + log2f(al)) * 0.6931471805599453f;
             } else {
                 float* r = dst + row * kRowF;
-                *reinterpret_cast<float2*>(r + 4 + d) = make_float2(o0, o1);
-                if (d == 0) *reinterpret_cast<float4*>(r) = make_float4(m, bad ? -1.f : l, kE4m3 ? mv - kPagedBias : m, 0.f);
+                *reinterpret_cast<float2*>(r + 4 + d) = v;
+                if (d == 0) *reinterpret_cast<float4*>(r) = make_float4(am, bad ? -1.f : al, kE4m3 ? amv - kPagedBias : am, 0.f);
             }
         }
         consumer_sync();                                      // the statistics and the sums may be overwritten
-        it += n_here;
-        if (it < it1) w.next();
     }
     if (tid == 0 && sm.abort_flag && a.status != nullptr) atomicExch(a.status, 6);
 }
@@ -592,7 +681,7 @@ __global__ void __launch_bounds__(512) paged_join_kernel(PageGeom p, PagedCall a
     launch_dependents();
     wait_for_previous_kernel();
     if (warp == 0) {
-        TileLine<kTile> line;
+        PageLine<kTile> line;
         line.p = &p;
         line.kv_len = a.kv_len;
         line.batch = a.batch;
@@ -600,7 +689,7 @@ __global__ void __launch_bounds__(512) paged_join_kernel(PageGeom p, PagedCall a
         long long before = 0, total = 0;
         for (int c = 0; c < a.batch; c += 32) {
             line.load(c);
-            long long t = line.tiles, u = c + lane < b ? t : 0;
+            long long t = line.places(line.len), u = c + lane < b ? t : 0;
 #pragma unroll
             for (int x = 16; x > 0; x >>= 1) {
                 t += __shfl_xor_sync(0xffffffffu, t, x);
@@ -610,13 +699,13 @@ __global__ void __launch_bounds__(512) paged_join_kernel(PageGeom p, PagedCall a
             before += u;
         }
         if (lane == 0) {
-            const int n = a.kv_len[b], tiles = line.count(n);
+            const int n = a.kv_len[b], tiles = line.in_range(n) ? (n + kTile - 1) / kTile : 0;
             if (tiles == 0) {
                 range[0] = -2;
                 if (n != 0 && h == 0 && a.status != nullptr) atomicExch(a.status, 1);
             } else {
                 total *= p.Hkv;
-                const long long begin = before * p.Hkv + (long long)gk * tiles;
+                const long long begin = before * p.Hkv + (long long)gk * (tiles + kPartCost) + kPartCost;
                 const int n_runs = run_count(total, n_ctas), c0 = run_of(total, n_runs, begin), c1 = run_of(total, n_runs, begin + tiles - 1);
                 range[0] = c0 == c1 ? -1 : c0;
                 range[1] = c1;

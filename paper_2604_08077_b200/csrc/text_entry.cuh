@@ -252,20 +252,24 @@ adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t* h, const adaspark_
     const long long most = (long long)batch * g.Hkv * (((long long)table_width * page_size + tile - 1) / tile);
     const int n_ctas = (int)(most < kPagedCtas ? most : kPagedCtas);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    auto launch = [&](auto d, auto bytes_held) -> adaspark_status_t {
+    auto launch = [&](auto d, auto bytes_held, auto groups) -> adaspark_status_t {
         constexpr int kD = d.value;
         constexpr bool kE4m3 = bytes_held.value;
+        constexpr auto kernel = paged_decode_kernel<kD, kE4m3, groups.value>;
         constexpr size_t bytes = sizeof(PagedSmem<kD, kE4m3>);
-        if (!text_smem<paged_decode_kernel<kD, kE4m3>>(h, bytes, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
-        launch_kernel(true, paged_decode_kernel<kD, kE4m3>, dim3(n_ctas), dim3(kPagedThreads), bytes, st, g, a, tmK, tmV);
+        if (!text_smem<kernel>(h, bytes, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
+        launch_kernel(true, kernel, dim3(n_ctas), dim3(kPagedThreads), bytes, st, g, a, tmK, tmV);
         if (!launch_ok(h, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
         launch_kernel(true, paged_join_kernel<kD, kE4m3>, dim3(Hq, batch), dim3(512), 0, st, g, a, n_ctas);
         return launch_ok(h, "paged_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
     };
+    auto with_groups = [&](auto d, auto bytes_held) -> adaspark_status_t {
+        return a.G > 8 ? launch(d, bytes_held, std::integral_constant<int, 2>()) : launch(d, bytes_held, std::integral_constant<int, 1>());
+    };
     const std::integral_constant<int, 128> wide;
     const std::integral_constant<int, 64> narrow;
-    if (D == 128) return e4m3 ? launch(wide, std::true_type()) : launch(wide, std::false_type());
-    return e4m3 ? launch(narrow, std::true_type()) : launch(narrow, std::false_type());
+    if (D == 128) return e4m3 ? with_groups(wide, std::true_type()) : with_groups(wide, std::false_type());
+    return e4m3 ? with_groups(narrow, std::true_type()) : with_groups(narrow, std::false_type());
 }
 
 }  // extern "C"
