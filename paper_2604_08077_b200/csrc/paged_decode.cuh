@@ -38,13 +38,13 @@ __host__ __device__ constexpr int paged_tile(bool e4m3) { return e4m3 ? 128 : 64
 __host__ __device__ constexpr int paged_row_floats(int D) { return D + 4; }           // m, l, m', -, o[D]
 __host__ __device__ constexpr size_t paged_partial_bytes(int D, int G) { return (size_t)kPagedCtas * 2 * G * paged_row_floats(D) * sizeof(float); }
 
-// The new token's row of one kv head (keys: which = 0, values: 1) into its place; by the 32 lanes of a warp.
+// The new token's row of one kv head (keys: which = 0, values: 1) into its place; by the 32 lanes of a warp, of which lane % (D / 8) holds x, 8
+// values.
 template <int D, bool kE4m3>
-__device__ __forceinline__ void append_row(const PageGeom& p, int page, int head, int place, int which, const __nv_bfloat16* src, int lane) {
+__device__ __forceinline__ void append_row(const PageGeom& p, int page, int head, int place, int which, const uint4& x, int lane) {
     constexpr int kLanes = D / 8;
     const long long row = ((long long)head << p.page_shift) + place;
     const int part = lane % kLanes;
-    const uint4 x = *reinterpret_cast<const uint4*>(src + part * 8);
     if (kE4m3) {
         bool odd;
         uint32_t top = chunk_top(x, odd);
@@ -241,7 +241,6 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     constexpr int kQSteps = kE4m3 ? D / 32 : D / 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
-    launch_dependents();
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             tc::mbar_init(&sm.full[s], 1);
@@ -260,6 +259,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     __syncthreads();
     volatile int* abort_flag = &sm.abort_flag;
     wait_for_previous_kernel();
+    launch_dependents();                                      // (after the wait: the next kernel reads kv_len before its own)
 
     RunWalk<kTile> w;
     w.line.p = &p;
@@ -289,6 +289,11 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                 pages = page_at(cols + lane);
                 pages_next = page_at(cols + 32 + lane);
             }
+            uint4 new_k = make_uint4(0u, 0u, 0u, 0u), new_v = new_k;
+            if (a.k_new != nullptr && w.end == w.tiles) {     // (asked for here, beside the page numbers)
+                new_k = *reinterpret_cast<const uint4*>(a.k_new + w.b * a.k_ts + w.gk * a.k_hs + lane % (D / 8) * 8);
+                new_v = *reinterpret_cast<const uint4*>(a.v_new + w.b * a.v_ts + w.gk * a.v_hs + lane % (D / 8) * 8);
+            }
             // q of the heads, a row each
             const int qs = part % kQSlots;
             if (!(ok = tc::mbar_wait_warp(&sm.q_empty[qs], ((part / kQSlots) & 1) ^ 1, abort_flag))) break;
@@ -314,8 +319,8 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                     }
                 } else if (a.k_new != nullptr && tile == w.tiles - 1) {    // the new token: the last of this tile
                     const int pg = __shfl_sync(0xffffffffu, page, boxes - 1), place = (w.n - 1) & (page_size - 1);
-                    append_row<D, kE4m3>(p, pg, w.gk, place, 0, a.k_new + w.b * a.k_ts + w.gk * a.k_hs, lane);
-                    append_row<D, kE4m3>(p, pg, w.gk, place, 1, a.v_new + w.b * a.v_ts + w.gk * a.v_hs, lane);
+                    append_row<D, kE4m3>(p, pg, w.gk, place, 0, new_k, lane);
+                    append_row<D, kE4m3>(p, pg, w.gk, place, 1, new_v, lane);
                     asm volatile("fence.proxy.async;\n" ::: "memory");    // it is read by the copies below
                     __syncwarp();
                 }
@@ -667,106 +672,124 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     if (tid == 0 && sm.abort_flag && a.status != nullptr) atomicExch(a.status, 6);
 }
 
-// grid (Hq, batch), 512 threads: the parts of one row in the order of the runs, 512 / D groups of threads a share each.  Rows of sequences
-// that are not there (or whose length is out of range: status 1) become zeros.  n_ctas: of the kernel before.
+// grid (Hq, batch): the parts of one row in the order of the runs.  Rows of sequences that are not there (or whose length is out of range:
+// status 1) become zeros.  n_ctas: of the kernel before, which lets this one in when kv_len is there: what comes before the wait runs
+// beside it (256 threads, so that a CTA finds room beside two of that kernel's).  A thread takes 4 values of every kJoinShares-th part;
+// statistics and values of the first parts are loaded together, one round trip to the L2.
+constexpr int kJoinThreads = 256;
+
 template <int D, bool kE4m3>
-__global__ void __launch_bounds__(512) paged_join_kernel(PageGeom p, PagedCall a, int n_ctas) {
-    constexpr int kTile = paged_tile(kE4m3), kGroups = 512 / D, kRowF = paged_row_floats(D);
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PageGeom p, PagedCall a, int n_ctas) {
+    constexpr int kTile = paged_tile(kE4m3), kLanes = D / 4, kShares = kJoinThreads / kLanes, kRowF = paged_row_floats(D), kAhead = 8;
     __shared__ float weight[kPagedCtas];
-    __shared__ float red[kGroups][D];
-    __shared__ float all[4];                                  // m, l, m', bad
-    __shared__ int range[2];                                  // first and last run; first < 0: nothing to join, -2: zeros
+    __shared__ float4 red[kShares][kLanes];
+    __shared__ float tops[8][2], sums[8];
+    __shared__ int bads;
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int gk = h / a.G, row = h - gk * a.G;
-    launch_dependents();
-    wait_for_previous_kernel();
-    if (warp == 0) {
-        PageLine<kTile> line;
-        line.p = &p;
-        line.kv_len = a.kv_len;
-        line.batch = a.batch;
-        line.lane = lane;
-        long long before = 0, total = 0;
-        for (int c = 0; c < a.batch; c += 32) {
-            line.load(c);
-            long long t = line.places(line.len), u = c + lane < b ? t : 0;
-#pragma unroll
-            for (int x = 16; x > 0; x >>= 1) {
-                t += __shfl_xor_sync(0xffffffffu, t, x);
-                u += __shfl_xor_sync(0xffffffffu, u, x);
-            }
-            total += t;
-            before += u;
-        }
-        if (lane == 0) {
-            const int n = a.kv_len[b], tiles = line.in_range(n) ? (n + kTile - 1) / kTile : 0;
-            if (tiles == 0) {
-                range[0] = -2;
-                if (n != 0 && h == 0 && a.status != nullptr) atomicExch(a.status, 1);
-            } else {
-                total *= p.Hkv;
-                const long long begin = before * p.Hkv + (long long)gk * (tiles + kPartCost) + kPartCost;
-                const int n_runs = run_count(total, n_ctas), c0 = run_of(total, n_runs, begin), c1 = run_of(total, n_runs, begin + tiles - 1);
-                range[0] = c0 == c1 ? -1 : c0;
-                range[1] = c1;
-            }
-        }
-    }
-    __syncthreads();
-    const int c0 = range[0], c1 = range[1];
-    const size_t at = (size_t)b * a.Hq + h;
-    if (c0 == -1) return;
-    if (c0 == -2) {
-        if (tid < D / 2) *reinterpret_cast<uint32_t*>(a.out + at * D + 2 * tid) = 0u;
-        if (tid == 0 && a.lse != nullptr) a.lse[at] = -INFINITY;
-        return;
-    }
-    const int n = c1 - c0 + 1;
-    // part i lies with run c0 + i: the first in its slot 1, the others in slot 0
-    auto part = [&](int i) -> const float* { return a.partial + ((size_t)((c0 + i) * 2 + (i == 0 ? 1 : 0)) * a.G + row) * kRowF; };
-    if (warp == 0) {
-        float m = -INFINITY, mv = -INFINITY, l = 0.f;
-        bool bad = false;
-        for (int i = lane; i < n; i += 32) {
-            const float4 s = *reinterpret_cast<const float4*>(part(i));
-            m = fmaxf(m, s.x);
-            mv = fmaxf(mv, s.z);
-            bad = bad || s.y == -1.f;
-        }
+    PageLine<kTile> line;
+    line.p = &p;
+    line.kv_len = a.kv_len;
+    line.batch = a.batch;
+    line.lane = lane;
+    long long before = 0, total = 0;
+    int n_tok = 0;
+    for (int c = 0; c < a.batch; c += 32) {
+        line.load(c);
+        long long t = line.places(line.len), u = c + lane < b ? t : 0;
 #pragma unroll
         for (int x = 16; x > 0; x >>= 1) {
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-            mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
+            t += __shfl_xor_sync(0xffffffffu, t, x);
+            u += __shfl_xor_sync(0xffffffffu, u, x);
         }
-        for (int i = lane; i < n; i += 32) {
-            const float4 s = *reinterpret_cast<const float4*>(part(i));
-            if (s.y != 0.f) l += s.y * fast_exp2(s.x == -INFINITY ? 0.f : s.x - m);
-            weight[i] = s.z == -INFINITY ? 0.f : fast_exp2(s.z - mv);
-        }
+        total += t;
+        before += u;
+        if (b >= c && b < c + 32) n_tok = __shfl_sync(0xffffffffu, line.len, b - c);
+    }
+    int c0 = 0, n = 0;                                        // first run, runs
+    if (n_tok > 0) {
+        const int tiles = (n_tok + kTile - 1) / kTile;
+        total *= p.Hkv;
+        const long long begin = before * p.Hkv + (long long)gk * (tiles + kPartCost) + kPartCost;
+        const int n_runs = run_count(total, n_ctas);
+        c0 = run_of(total, n_runs, begin);
+        n = run_of(total, n_runs, begin + tiles - 1) - c0 + 1;
+    }
+    if (tid == 0) bads = 0;
+    __syncthreads();
+    launch_dependents();
+    wait_for_previous_kernel();
+    const size_t at = (size_t)b * a.Hq + h;
+    if (n_tok == 0) {
+        if (tid < D / 2) *reinterpret_cast<uint32_t*>(a.out + at * D + 2 * tid) = 0u;
+        if (tid == 0 && a.lse != nullptr) a.lse[at] = -INFINITY;
+        if (tid == 0 && h == 0 && a.status != nullptr && a.kv_len[b] != 0) atomicExch(a.status, 1);
+        return;
+    }
+    if (n == 1) return;                                       // finished where it was computed
+    // part i lies with run c0 + i: the first in its slot 1, the others in slot 0
+    const float* base = a.partial + ((size_t)(c0 * 2) * a.G + row) * kRowF;
+    const size_t step = (size_t)2 * a.G * kRowF, first = (size_t)a.G * kRowF;
+    auto part = [&](int i) -> const float* { return base + i * step + (i == 0 ? first : 0); };
+    const int d4 = tid % kLanes, share = tid / kLanes;
+    float4 st = make_float4(-INFINITY, 0.f, -INFINITY, 0.f), st2 = st;    // of parts tid and tid + 256
+    if (tid < n) st = *reinterpret_cast<const float4*>(part(tid));
+    if (tid + kJoinThreads < n) st2 = *reinterpret_cast<const float4*>(part(tid + kJoinThreads));
+    float4 v[kAhead];
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-        bad = __any_sync(0xffffffffu, bad);
-        if (lane == 0) {
-            all[0] = m;
-            all[1] = l;
-            all[2] = mv;
-            all[3] = bad ? 1.f : 0.f;
-        }
+    for (int i = 0; i < kAhead; ++i) {
+        const int x = share + i * kShares;
+        v[i] = x < n ? *reinterpret_cast<const float4*>(part(x) + 4 + 4 * d4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    float m = fmaxf(st.x, st2.x), mv = fmaxf(st.z, st2.z);
+    if (st.y == -1.f || st2.y == -1.f) bads = 1;
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+        mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
+    }
+    if (lane == 0) {
+        tops[warp][0] = m;
+        tops[warp][1] = mv;
     }
     __syncthreads();
-    const int d = tid & (D - 1), grp = tid / D;
-    float acc = 0.f;
-#pragma unroll 8
-    for (int i = grp; i < n; i += kGroups) acc = fmaf(part(i)[4 + d], weight[i], acc);
-    red[grp][d] = acc;
-    __syncthreads();
-    if (grp == 0) {
 #pragma unroll
-        for (int i = 1; i < kGroups; ++i) acc += red[i][d];
-        const float f = kE4m3 ? exp2f(all[2] - all[0]) : 1.f;
-        const bool bad = all[3] != 0.f;
-        a.out[at * D + d] = __float2bfloat16(bad ? 0.f : acc / all[1] * f);
-        if (d == 0 && a.lse != nullptr) a.lse[at] = bad ? -INFINITY : (all[0] + log2f(all[1])) * 0.6931471805599453f;
+    for (int x = 0; x < 8; ++x) {
+        m = fmaxf(m, tops[x][0]);
+        mv = fmaxf(mv, tops[x][1]);
+    }
+    float l = 0.f;
+    if (st.y != 0.f) l += st.y * fast_exp2(st.x == -INFINITY ? 0.f : st.x - m);
+    if (st2.y != 0.f) l += st2.y * fast_exp2(st2.x == -INFINITY ? 0.f : st2.x - m);
+    if (tid < n) weight[tid] = st.z == -INFINITY ? 0.f : fast_exp2(st.z - mv);
+    if (tid + kJoinThreads < n) weight[tid + kJoinThreads] = st2.z == -INFINITY ? 0.f : fast_exp2(st2.z - mv);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+    if (lane == 0) sums[warp] = l;
+    __syncthreads();
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float4& y, float f) {
+        acc.x = fmaf(y.x, f, acc.x);
+        acc.y = fmaf(y.y, f, acc.y);
+        acc.z = fmaf(y.z, f, acc.z);
+        acc.w = fmaf(y.w, f, acc.w);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (share + i * kShares < n) add(v[i], weight[share + i * kShares]);
+#pragma unroll 8
+    for (int x = share + kAhead * kShares; x < n; x += kShares) add(*reinterpret_cast<const float4*>(part(x) + 4 + 4 * d4), weight[x]);
+    red[share][d4] = acc;
+    __syncthreads();
+    if (tid < kLanes) {
+        for (int x = 1; x < kShares; ++x) add(red[x][d4], 1.f);
+        l = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) l += sums[x];
+        const float f = (kE4m3 ? exp2f(mv - m) : 1.f) / l;
+        const bool bad = bads != 0;
+        *reinterpret_cast<uint2*>(a.out + at * D + 4 * d4) = bad ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+        if (tid == 0 && a.lse != nullptr) a.lse[at] = bad ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
     }
 }
 
