@@ -31,7 +31,8 @@ namespace adaspark {
 constexpr int kPagedThreads = 160;
 constexpr int kPagedCtas = 296;              // two per SM of a B200
 constexpr int kPagedRing = 96 * 1024;        // bytes of a CTA's ring
-constexpr int kPartCost = 1;                 // what a part costs beside its tiles, in tiles
+constexpr int kPartCost = 2;                 // what a part costs beside its tiles, in tiles
+constexpr int kPagedFewSequences = 16;       // up to so many (sequence, kv head)s: at least 18 runs each, a CTA joins a row
 constexpr float kPagedBias = 14.f;           // f16 weights are at most 2^14: 2^-28 of the largest one is still a normal number
 
 __host__ __device__ constexpr int paged_tile(bool e4m3) { return e4m3 ? 128 : 64; }   // keys of a tile
@@ -137,6 +138,24 @@ struct RunWalk {
             before += all;
         }
         return false;
+    }
+    // to the first place of (sequence b, kv head gk); false: it has none
+    __device__ __forceinline__ bool seek_sequence(int seq, int head, long long total) {
+        stop = total;
+        place = 0;
+        for (int c = 0; c <= seq; c += 32) {
+            line.load(c);
+            long long x = c + line.lane < seq ? line.places(line.len) : 0;
+#pragma unroll
+            for (int s = 16; s > 0; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
+            place += x * line.p->Hkv;
+        }
+        n = __shfl_sync(0xffffffffu, line.len, seq & 31);
+        b = seq;
+        gk = head;
+        tiles = (n + kTile - 1) / kTile;
+        place += (long long)head * line.places(n);
+        return begin(0);
     }
     // the part that begins with tile t; false: the run ends in front of it
     __device__ __forceinline__ bool begin(int t) {
@@ -268,8 +287,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     w.line.lane = lane;
     const long long total = w.line.total();
     const int n_runs = run_count(total, gridDim.x);
-    if ((int)blockIdx.x >= n_runs) return;                    // (the whole CTA)
-    bool more = w.seek(run_begin(total, n_runs, blockIdx.x), run_begin(total, n_runs, blockIdx.x + 1));
+    bool more = (int)blockIdx.x < n_runs && w.seek(run_begin(total, n_runs, blockIdx.x), run_begin(total, n_runs, blockIdx.x + 1));
     const int page_shift = p.page_shift, page_size = 1 << page_shift;
 
     if (warp == 4) {
@@ -669,127 +687,175 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
         }
         consumer_sync();                                      // the statistics and the sums may be overwritten
     }
+    // rows of sequences that are not there, or whose length is out of range
+    for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+        const int n = a.kv_len[b];
+        if (n > 0 && w.line.in_range(n)) continue;
+        for (int i = tid; i < a.Hq * (D / 8); i += 128) *reinterpret_cast<uint4*>(a.out + (size_t)b * a.Hq * D + i * 8) = make_uint4(0u, 0u, 0u, 0u);
+        if (a.lse != nullptr)
+            for (int i = tid; i < a.Hq; i += 128) a.lse[(size_t)b * a.Hq + i] = -INFINITY;
+        if (tid == 0 && n != 0 && a.status != nullptr) atomicExch(a.status, 1);
+    }
     if (tid == 0 && sm.abort_flag && a.status != nullptr) atomicExch(a.status, 6);
 }
 
-// grid (Hq, batch): the parts of one row in the order of the runs.  Rows of sequences that are not there (or whose length is out of range:
-// status 1) become zeros.  n_ctas: of the kernel before, which lets this one in when kv_len is there: what comes before the wait runs
-// beside it (256 threads, so that a CTA finds room beside two of that kernel's).  A thread takes 4 values of every kJoinShares-th part;
-// statistics and values of the first parts are loaded together, one round trip to the L2.
+// Joins what is cut.  Many (sequence, kv head)s: grid (runs - 1), CTA i joins the one that is cut by the end of run i and has its first tile in
+// that run; there are as many as cuts at most, however large the batch (a CTA for every row of 256 sequences: 55 us instead of 21 for the
+// step).  Few, of many parts each: grid (batch * Hkv, G), a CTA a row.  The kernel before lets this one in when kv_len is
+// there: what comes before the wait runs beside it.  Up to 16 parts, a warp joins a row by itself; more are shared out over the CTA's warps.
+// Statistics and values of the first parts are loaded together, one round trip to the L2.
 constexpr int kJoinThreads = 256;
+constexpr int kJoinBlocks = 4, kJoinWarpAhead = 8;
 
-template <int D, bool kE4m3>
-__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PageGeom p, PagedCall a, int n_ctas) {
-    constexpr int kTile = paged_tile(kE4m3), kLanes = D / 4, kShares = kJoinThreads / kLanes, kRowF = paged_row_floats(D), kAhead = 8;
+template <int D, bool kE4m3, bool kFew>
+__global__ void __launch_bounds__(kJoinThreads, kFew ? 2 : kJoinBlocks) paged_join_kernel(PageGeom p, PagedCall a, int n_ctas) {
+    constexpr int kTile = paged_tile(kE4m3), kLanes = D / 4, kShares = kJoinThreads / kLanes, kRowF = paged_row_floats(D), kAhead = kFew ? 8 : 4;
     __shared__ float weight[kPagedCtas];
-    __shared__ float4 red[kShares][kLanes];
+    __shared__ float4 red[kShares / 2][kLanes];
     __shared__ float tops[8][2], sums[8];
     __shared__ int bads;
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int gk = h / a.G, row = h - gk * a.G;
-    PageLine<kTile> line;
-    line.p = &p;
-    line.kv_len = a.kv_len;
-    line.batch = a.batch;
-    line.lane = lane;
-    long long before = 0, total = 0;
-    int n_tok = 0;
-    for (int c = 0; c < a.batch; c += 32) {
-        line.load(c);
-        long long t = line.places(line.len), u = c + lane < b ? t : 0;
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) {
-            t += __shfl_xor_sync(0xffffffffu, t, x);
-            u += __shfl_xor_sync(0xffffffffu, u, x);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    RunWalk<kTile> w;
+    w.line.p = &p;
+    w.line.kv_len = a.kv_len;
+    w.line.batch = a.batch;
+    w.line.lane = lane;
+    const long long total = w.line.total();
+    const int n_runs = run_count(total, n_ctas);
+    int run = blockIdx.x, n = 0;                              // first of the n runs that hold its tiles; n < 2: not this CTA's
+    if (kFew) {
+        const int b = blockIdx.x / p.Hkv, gk = blockIdx.x - b * p.Hkv;
+        if (w.seek_sequence(b, gk, total)) {
+            run = run_of(total, n_runs, w.place + kPartCost);
+            n = run_of(total, n_runs, w.place + kPartCost + w.tiles - 1) - run + 1;
         }
-        total += t;
-        before += u;
-        if (b >= c && b < c + 32) n_tok = __shfl_sync(0xffffffffu, line.len, b - c);
+    } else if (run + 1 < n_runs) {
+        const long long cut = run_begin(total, n_runs, run + 1);
+        w.seek(cut, total);
+        const long long first = w.place + kPartCost;
+        if (first < cut && run_of(total, n_runs, first) == run) n = run_of(total, n_runs, first + w.tiles - 1) - run + 1;
     }
-    int c0 = 0, n = 0;                                        // first run, runs
-    if (n_tok > 0) {
-        const int tiles = (n_tok + kTile - 1) / kTile;
-        total *= p.Hkv;
-        const long long begin = before * p.Hkv + (long long)gk * (tiles + kPartCost) + kPartCost;
-        const int n_runs = run_count(total, n_ctas);
-        c0 = run_of(total, n_runs, begin);
-        n = run_of(total, n_runs, begin + tiles - 1) - c0 + 1;
-    }
-    if (tid == 0) bads = 0;
-    __syncthreads();
     launch_dependents();
     wait_for_previous_kernel();
-    const size_t at = (size_t)b * a.Hq + h;
-    if (n_tok == 0) {
-        if (tid < D / 2) *reinterpret_cast<uint32_t*>(a.out + at * D + 2 * tid) = 0u;
-        if (tid == 0 && a.lse != nullptr) a.lse[at] = -INFINITY;
-        if (tid == 0 && h == 0 && a.status != nullptr && a.kv_len[b] != 0) atomicExch(a.status, 1);
-        return;
-    }
-    if (n == 1) return;                                       // finished where it was computed
-    // part i lies with run c0 + i: the first in its slot 1, the others in slot 0
-    const float* base = a.partial + ((size_t)(c0 * 2) * a.G + row) * kRowF;
-    const size_t step = (size_t)2 * a.G * kRowF, first = (size_t)a.G * kRowF;
-    auto part = [&](int i) -> const float* { return base + i * step + (i == 0 ? first : 0); };
-    const int d4 = tid % kLanes, share = tid / kLanes;
-    float4 st = make_float4(-INFINITY, 0.f, -INFINITY, 0.f), st2 = st;    // of parts tid and tid + 256
-    if (tid < n) st = *reinterpret_cast<const float4*>(part(tid));
-    if (tid + kJoinThreads < n) st2 = *reinterpret_cast<const float4*>(part(tid + kJoinThreads));
-    float4 v[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-        const int x = share + i * kShares;
-        v[i] = x < n ? *reinterpret_cast<const float4*>(part(x) + 4 + 4 * d4) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    float m = fmaxf(st.x, st2.x), mv = fmaxf(st.z, st2.z);
-    if (st.y == -1.f || st2.y == -1.f) bads = 1;
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) {
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-        mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
-    }
-    if (lane == 0) {
-        tops[warp][0] = m;
-        tops[warp][1] = mv;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-        m = fmaxf(m, tops[x][0]);
-        mv = fmaxf(mv, tops[x][1]);
-    }
-    float l = 0.f;
-    if (st.y != 0.f) l += st.y * fast_exp2(st.x == -INFINITY ? 0.f : st.x - m);
-    if (st2.y != 0.f) l += st2.y * fast_exp2(st2.x == -INFINITY ? 0.f : st2.x - m);
-    if (tid < n) weight[tid] = st.z == -INFINITY ? 0.f : fast_exp2(st.z - mv);
-    if (tid + kJoinThreads < n) weight[tid + kJoinThreads] = st2.z == -INFINITY ? 0.f : fast_exp2(st2.z - mv);
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-    if (lane == 0) sums[warp] = l;
-    __syncthreads();
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](const float4& y, float f) {
+    if (n < 2) return;                                        // (finished where it was computed)
+    // part i lies with run + i: the first in its slot 1, the others in slot 0
+    const size_t step = (size_t)2 * a.G * kRowF;
+    const float* parts = a.partial + (size_t)run * step;
+    auto part = [&](int i, int row) -> const float* { return parts + i * step + ((i == 0 ? a.G : 0) + row) * kRowF; };
+    auto add = [](float4& acc, const float4& y, float f) {
         acc.x = fmaf(y.x, f, acc.x);
         acc.y = fmaf(y.y, f, acc.y);
         acc.z = fmaf(y.z, f, acc.z);
         acc.w = fmaf(y.w, f, acc.w);
     };
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        if (share + i * kShares < n) add(v[i], weight[share + i * kShares]);
-#pragma unroll 8
-    for (int x = share + kAhead * kShares; x < n; x += kShares) add(*reinterpret_cast<const float4*>(part(x) + 4 + 4 * d4), weight[x]);
-    red[share][d4] = acc;
-    __syncthreads();
-    if (tid < kLanes) {
-        for (int x = 1; x < kShares; ++x) add(red[x][d4], 1.f);
-        l = 0.f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) l += sums[x];
+    auto finish = [&](int row, int d4, const float4& acc, float m, float mv, float l, bool bad) {
+        const size_t at = (size_t)w.b * a.Hq + w.gk * a.G + row;
         const float f = (kE4m3 ? exp2f(mv - m) : 1.f) / l;
-        const bool bad = bads != 0;
         *reinterpret_cast<uint2*>(a.out + at * D + 4 * d4) = bad ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
-        if (tid == 0 && a.lse != nullptr) a.lse[at] = bad ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        if (d4 == 0 && a.lse != nullptr) a.lse[at] = bad ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    };
+    if (n <= 16) {
+        constexpr int kPer = 32 / kLanes;                     // parts that a warp takes at a time
+        const int d4 = lane % kLanes, sub = lane / kLanes;
+        for (int row = blockIdx.y + warp * gridDim.y; row < a.G; row += 8 * gridDim.y) {
+            float4 st = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+            if (lane < n) st = *reinterpret_cast<const float4*>(part(lane, row));
+            float4 v[kJoinWarpAhead];
+#pragma unroll
+            for (int i = 0; i < kJoinWarpAhead; ++i) {
+                const int x = sub + i * kPer;
+                v[i] = x < n ? *reinterpret_cast<const float4*>(part(x, row) + 4 + 4 * d4) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            float m = st.x, mv = st.z;
+#pragma unroll
+            for (int x = 8; x > 0; x >>= 1) {
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
+            }
+            float l = st.y != 0.f && lane < 16 ? st.y * fast_exp2(st.x == -INFINITY ? 0.f : st.x - m) : 0.f;
+            const float wt = st.z == -INFINITY ? 0.f : fast_exp2(st.z - mv);
+            const bool bad = __any_sync(0xffffffffu, st.y == -1.f);
+#pragma unroll
+            for (int x = 8; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < 16 / kPer; ++i) {
+                const int x = sub + i * kPer;
+                const float f = __shfl_sync(0xffffffffu, wt, x & 15);
+                if (x < n) add(acc, i < kJoinWarpAhead ? v[i < kJoinWarpAhead ? i : 0] : *reinterpret_cast<const float4*>(part(x, row) + 4 + 4 * d4), f);
+            }
+            if (kPer == 2) {
+                const float4 y = make_float4(__shfl_xor_sync(0xffffffffu, acc.x, 16), __shfl_xor_sync(0xffffffffu, acc.y, 16), __shfl_xor_sync(0xffffffffu, acc.z, 16),
+                                             __shfl_xor_sync(0xffffffffu, acc.w, 16));
+                add(acc, y, 1.f);
+            }
+            // (lanes 16 .. 31 hold no statistics of theirs: the first lane's)
+            m = __shfl_sync(0xffffffffu, m, 0);
+            mv = __shfl_sync(0xffffffffu, mv, 0);
+            l = __shfl_sync(0xffffffffu, l, 0);
+            if (lane < kLanes) finish(row, d4, acc, m, mv, l, bad);
+        }
+        return;
+    }
+    const int d4 = tid % kLanes, share = tid / kLanes;
+    for (int row = blockIdx.y; row < a.G; row += gridDim.y) {
+        __syncthreads();
+        if (tid == 0) bads = 0;
+        float4 st = make_float4(-INFINITY, 0.f, -INFINITY, 0.f), st2 = st;    // of parts tid and tid + 256
+        if (tid < n) st = *reinterpret_cast<const float4*>(part(tid, row));
+        if (tid + kJoinThreads < n) st2 = *reinterpret_cast<const float4*>(part(tid + kJoinThreads, row));
+        float4 v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int x = share + i * kShares;
+            v[i] = x < n ? *reinterpret_cast<const float4*>(part(x, row) + 4 + 4 * d4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float m = fmaxf(st.x, st2.x), mv = fmaxf(st.z, st2.z);
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) {
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+            mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
+        }
+        if (lane == 0) {
+            tops[warp][0] = m;
+            tops[warp][1] = mv;
+        }
+        __syncthreads();
+        if (st.y == -1.f || st2.y == -1.f) bads = 1;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            m = fmaxf(m, tops[x][0]);
+            mv = fmaxf(mv, tops[x][1]);
+        }
+        float l = 0.f;
+        if (st.y != 0.f) l += st.y * fast_exp2(st.x == -INFINITY ? 0.f : st.x - m);
+        if (st2.y != 0.f) l += st2.y * fast_exp2(st2.x == -INFINITY ? 0.f : st2.x - m);
+        if (tid < n) weight[tid] = st.z == -INFINITY ? 0.f : fast_exp2(st.z - mv);
+        if (tid + kJoinThreads < n) weight[tid + kJoinThreads] = st2.z == -INFINITY ? 0.f : fast_exp2(st2.z - mv);
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+        if (lane == 0) sums[warp] = l;
+        __syncthreads();
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (share + i * kShares < n) add(acc, v[i], weight[share + i * kShares]);
+#pragma unroll 4
+        for (int x = share + kAhead * kShares; x < n; x += kShares) add(acc, *reinterpret_cast<const float4*>(part(x, row) + 4 + 4 * d4), weight[x]);
+        if (share >= kShares / 2) red[share - kShares / 2][d4] = acc;
+        __syncthreads();
+        if (share < kShares / 2) {
+            add(acc, red[share][d4], 1.f);
+            red[share][d4] = acc;
+        }
+        __syncthreads();
+        if (tid < kLanes) {
+            for (int x = 1; x < kShares / 2; ++x) add(acc, red[x][d4], 1.f);
+            l = 0.f;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) l += sums[x];
+            finish(row, d4, acc, m, mv, l, bads != 0);
+        }
     }
 }
 

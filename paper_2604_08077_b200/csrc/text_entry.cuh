@@ -260,7 +260,11 @@ adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t* h, const adaspark_
         if (!text_smem<kernel>(h, bytes, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
         launch_kernel(true, kernel, dim3(n_ctas), dim3(kPagedThreads), bytes, st, g, a, tmK, tmV);
         if (!launch_ok(h, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
-        launch_kernel(true, paged_join_kernel<kD, kE4m3>, dim3(Hq, batch), dim3(kJoinThreads), 0, st, g, a, n_ctas);
+        if (n_ctas == 1) return ADASPARK_OK;                   // nothing is cut
+        if ((long long)batch * g.Hkv <= kPagedFewSequences)
+            launch_kernel(true, paged_join_kernel<kD, kE4m3, true>, dim3(batch * g.Hkv, a.G), dim3(kJoinThreads), 0, st, g, a, n_ctas);
+        else
+            launch_kernel(true, paged_join_kernel<kD, kE4m3, false>, dim3(n_ctas - 1), dim3(kJoinThreads), 0, st, g, a, n_ctas);
         return launch_ok(h, "paged_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
     };
     auto with_groups = [&](auto d, auto bytes_held) -> adaspark_status_t {
