@@ -37,53 +37,53 @@ __device__ __forceinline__ long long page_of(const PageGeom& p, int seq, int pos
 // 2^(s - 127), s in 0 .. 254
 __device__ __forceinline__ float pow2_of_byte(uint32_t s) { return __uint_as_float(s == 0 ? 0x00400000u : s << 23); }
 
-// The byte of the power of two for the largest magnitude `top` (bf16 bits without the sign, finite) of a row.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
-    const int s = (int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);      // 448 = 1.75 * 2^8, 0x60: the .75
-    return (uint32_t)max(s, 0);
-}
+// The byte of the power of two for the largest magnitude `top` (bf16 bits without the sign, finite) of a row: 448 = 1.75 * 2^8, and 0x1f
+// carries into the exponent from the first mantissa above .75 on.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) { return (uint32_t)max((int)((top + 0x1fu) >> 7) - 8, 0); }
 
-// 8 bf16 -> the largest finite magnitude, as bf16 bits; `odd` is set where one is infinite or no number.
-__device__ __forceinline__ uint32_t chunk_top(const uint4& x, bool& odd) {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t m = 0;
-    odd = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t a = w[i] & 0x7fff7fffu;
-        m = __vmaxu2(m, a);
-    }
-    uint32_t top = max(m & 0xffffu, m >> 16);
-    if (top >= 0x7f80u) {                                                     // rare
-        odd = true;
-        top = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t a = (w[i] >> (16 * e)) & 0x7fffu;
-                if (a < 0x7f80u) top = max(top, a);
-            }
-    }
-    return top;
+// 8 bf16 -> the larger of each pair's halves' magnitudes, as two bf16 without sign
+__device__ __forceinline__ uint32_t chunk_tops(const uint4& x) {
+    return __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
 }
-// 8 bf16 times 2^(127 - s) -> 8 codes.  What is infinite or no number becomes e4m3's NaN: it has no infinity, and a saturated 448
-// would pass for a value.
-__device__ __forceinline__ uint2 chunk_codes(const uint4& x, uint32_t s, bool odd) {
+// The same over the finite ones alone (infinite or no number: exponent bits all ones).
+__device__ __forceinline__ uint32_t chunk_finite_tops(const uint4& x) {
+    const uint32_t w[4] = {x.x & 0x7fff7fffu, x.y & 0x7fff7fffu, x.z & 0x7fff7fffu, x.w & 0x7fff7fffu};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & __vcmpltu2(w[i], 0x7f807f80u));
+    return m;
+}
+// Largest magnitudes of two rows (their D / 8 lanes hold a and b), in the halves of the result; every lane of the warp takes part.
+template <int kLanes>
+__device__ __forceinline__ uint32_t row_tops(uint32_t a, uint32_t b) {
+    uint32_t t = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+#pragma unroll
+    for (int s = 1; s < kLanes; s <<= 1) t = __vmaxu2(t, __shfl_xor_sync(0xffffffffu, t, s));
+    return t;
+}
+__device__ __forceinline__ bool any_odd(uint32_t tops) { return (tops & 0xffffu) >= 0x7f80u || (tops >> 16) >= 0x7f80u; }
+// 8 bf16 times 2^(127 - s) -> 8 codes
+__device__ __forceinline__ uint2 chunk_codes(const uint4& x, uint32_t s) {
     const float inv = __uint_as_float((254u - s) << 23);
+    const unsigned long long inv2 = pack_f32x2(inv, inv);
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     uint32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float lo = __uint_as_float(w[i] << 16) * inv, hi = __uint_as_float(w[i] & 0xffff0000u) * inv;
-        if (odd) {
-            if ((w[i] & 0x7f80u) == 0x7f80u) lo = NAN;
-            if ((w[i] & 0x7f800000u) == 0x7f800000u) hi = NAN;
-        }
+        float lo, hi;
+        unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), inv2), lo, hi);
         uint16_t two;
         asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(two) : "f"(hi), "f"(lo));
         c[i] = two;
     }
     return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+}
+// What is infinite becomes NaN: e4m3 has no infinity, and a saturated 448 would pass for a value.
+__device__ __forceinline__ uint4 infinities_to_nan(const uint4& x) {
+    uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] |= __vcmpgeu2(w[i] & 0x7fff7fffu, 0x7f807f80u) & 0x007f007fu;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // two codes (low 16 bits) -> f16 pair: exact
 __device__ __forceinline__ uint32_t codes_to_f16x2(uint32_t two) {
@@ -117,138 +117,144 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int at)
     return lo;
 }
 
-constexpr int kCacheTokens = 8;      // tokens of a CTA
 constexpr int kCacheThreads = 256;
 
-// Page and place of the CTA's tokens, by its first threads: page in [0, n_pages) or -1 (not ours), place in the page.
-__device__ __forceinline__ void find_tokens(const PageGeom& p, const int32_t* cu, const int32_t* kv_len, int batch, int n, int t0,
-                                            int (&page)[kCacheTokens], int (&place)[kCacheTokens], int32_t* status) {
-    if (threadIdx.x < kCacheTokens) {
-        const int at = t0 + threadIdx.x;
-        int pg = -1, pl = 0;
+// Places of the CTA's kTokens tokens from t0 on, by its first threads: offsets (elements, scales) of a token's first kv head in the pages;
+// first < 0: -1 a row of no sequence, -2 one of a sequence that has no place for it.
+template <int kTokens, int D>
+__device__ __forceinline__ void find_tokens(const PageGeom& p, const int32_t* cu, const int32_t* kv_len, int batch, int n, int t0, long long (&place)[kTokens],
+                                            long long (&scale_place)[kTokens], int32_t* status) {
+    for (int i = threadIdx.x; i < kTokens; i += kCacheThreads) {
+        const int at = t0 + i;
+        long long x = -1, y = 0;
         const int seq = at < n ? sequence_of(cu, batch, at) : -1;
         if (seq >= 0) {
-            const int pos = kv_len[seq] - (cu[seq + 1] - at);
-            pg = (int)page_of(p, seq, pos);
-            pl = pos & ((1 << p.page_shift) - 1);
-            if (pg < 0) {
-                pg = -2;                                                      // a row of a sequence that has no place for it
+            const int pos = kv_len[seq] - (cu[seq + 1] - at), in = pos & ((1 << p.page_shift) - 1);
+            const long long page = page_of(p, seq, pos);
+            if (page < 0) {
+                x = -2;
                 if (status != nullptr) atomicExch(status, 1);
+            } else {
+                x = page * p.page_stride + (long long)in * D;
+                y = page * p.scale_stride + in;
             }
         }
-        page[threadIdx.x] = pg;
-        place[threadIdx.x] = pl;
+        place[i] = x;
+        scale_place[i] = y;
     }
 }
 
-// k, v [n][Hkv][D] (row and head strides in elements) -> pages.  Bound by HBM: every value read once and written once.  A thread takes
-// 16 bytes (8 values) at a time, D / 8 neighbouring threads a row, whose largest magnitude they find by shuffles; the loads of a
-// thread are under way before its CTA has looked up where they go.
-template <int D, bool kE4m3>
+// Both kernels: a CTA has kTokens tokens, a thread one 16-byte piece (8 values) of a row of one head of K or V and every
+// kCacheThreads / columns-th token: what belongs to the column is worked out once, a token costs an offset from shared memory.  Bound by HBM, every
+// value read once and written once.  (With the pieces of 8 tokens dealt to the threads one by one, index arithmetic took the issue slots: 131072 tokens, 4
+// heads of 128, 8 bits: 107 us written and 88 read.)  grid (tokens / kTokens, columns / 256).
+
+// k, v [n][Hkv][D] (row and head strides in elements) -> pages.  D / 8 neighbouring threads find a row's largest magnitude by shuffles; the
+// first loads of a thread are under way before its CTA has looked up where they go.
+template <int D, bool kE4m3, int kTokens>
 __global__ void __launch_bounds__(kCacheThreads) paged_write_kernel(
     PageGeom p, const __nv_bfloat16* k, long long k_ts, long long k_hs, const __nv_bfloat16* v, long long v_ts, long long v_hs,
-    const int32_t* cu, const int32_t* kv_len, int batch, int n, FastDiv div_rows, FastDiv div_heads, int32_t* status) {
-    constexpr int kLanes = D / 8, kBatch = 4;
-    __shared__ int page[kCacheTokens], place[kCacheTokens];
-    const int t0 = blockIdx.x * kCacheTokens;
+    const int32_t* cu, const int32_t* kv_len, int batch, int n, int32_t* status) {
+    constexpr int kLanes = D / 8, kAhead = 4;
+    __shared__ long long place[kTokens], scale_place[kTokens];
+    const int t0 = blockIdx.x * kTokens, cols = 2 * p.Hkv * kLanes, col0 = blockIdx.y * kCacheThreads, width = min(cols - col0, kCacheThreads);
+    const int tokens = kCacheThreads / width, mine = (int)threadIdx.x / width;             // of a pass, of this thread
+    const int col = col0 + (int)threadIdx.x - mine * width, row = col / kLanes, part = col % kLanes;
+    const bool is_v = row >= p.Hkv;
+    const int head = is_v ? row - p.Hkv : row;
+    const long long ts = is_v ? v_ts : k_ts;
+    const __nv_bfloat16* src = (is_v ? v + head * v_hs : k + head * k_hs) + part * 8 + t0 * ts;
+    uint8_t* dst = (is_v ? p.v : p.k) + (((long long)head << p.page_shift) * D + part * 8) * (kE4m3 ? 1 : 2);
+    uint8_t* scales = (is_v ? p.vs : p.ks) + ((long long)head << p.page_shift);
+    const int count = mine < tokens ? min(kTokens, n - t0) : 0;
     launch_dependents();
     wait_for_previous_kernel();
-    const int n_chunks = kCacheTokens * 2 * p.Hkv * kLanes;                   // (a multiple of a warp)
     bool looked = false;
-    for (int c0 = threadIdx.x; c0 < n_chunks; c0 += kBatch * kCacheThreads) {
-        uint4 x[kBatch];
-        int tok[kBatch], head[kBatch], is_v[kBatch];
+    for (int pass = 0; pass < kTokens; pass += kAhead * tokens) {   // (as often for every thread: the shuffles and the barrier need all of them)
+        const int t = pass + mine;
+        uint4 x[kAhead];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int c = c0 + i * kCacheThreads, row = c / kLanes, d = (c % kLanes) * 8;
-            int r, w, h;
-            div_rows.divmod(row, r, w);                                       // [token][k, v][head]
-            div_heads.divmod(w, w, h);
-            tok[i] = r;
-            head[i] = h;
-            is_v[i] = w;
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (c < n_chunks && t0 + r < n) {
-                const __nv_bfloat16* src = w ? v + (long long)(t0 + r) * v_ts + h * v_hs : k + (long long)(t0 + r) * k_ts + h * k_hs;
-                x[i] = *reinterpret_cast<const uint4*>(src + d);
-            }
-        }
+        for (int i = 0; i < kAhead; ++i) x[i] = t + i * tokens < count ? *reinterpret_cast<const uint4*>(src + (t + i * tokens) * ts) : make_uint4(0u, 0u, 0u, 0u);
         if (!looked) {
-            find_tokens(p, cu, kv_len, batch, n, t0, page, place, status);
+            find_tokens<kTokens, D>(p, cu, kv_len, batch, n, t0, place, scale_place, status);
             __syncthreads();
             looked = true;
         }
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int c = c0 + i * kCacheThreads, part = c % kLanes;
-            if (c - (int)(threadIdx.x & 31) >= n_chunks) break;               // (the same for the whole warp)
-            const int pg = page[tok[i]];
-            const long long row = ((long long)head[i] << p.page_shift) + place[tok[i]];
+        for (int i = 0; i < kAhead; i += 2) {                 // two rows at a time
+            uint32_t tops = 0u;
             if (kE4m3) {
-                bool odd;
-                uint32_t top = chunk_top(x[i], odd);
-#pragma unroll
-                for (int s = 1; s < kLanes; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-                const uint32_t s = scale_byte(top);
-                if (pg >= 0) {
-                    uint8_t* dst = (is_v[i] ? p.v : p.k) + (long long)pg * p.page_stride + row * D + part * 8;
-                    *reinterpret_cast<uint2*>(dst) = chunk_codes(x[i], s, odd);
-                    if (part == 0) (is_v[i] ? p.vs : p.ks)[(long long)pg * p.scale_stride + row] = (uint8_t)s;
+                tops = row_tops<kLanes>(chunk_tops(x[i]), chunk_tops(x[i + 1]));
+                if (__any_sync(0xffffffffu, any_odd(tops))) { // rare
+                    tops = row_tops<kLanes>(chunk_finite_tops(x[i]), chunk_finite_tops(x[i + 1]));
+                    x[i] = infinities_to_nan(x[i]);
+                    x[i + 1] = infinities_to_nan(x[i + 1]);
                 }
-            } else if (pg >= 0) {
-                uint8_t* dst = (is_v[i] ? p.v : p.k) + ((long long)pg * p.page_stride + row * D + part * 8) * 2;
-                *reinterpret_cast<uint4*>(dst) = x[i];
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int tt = t + (i + y) * tokens;
+                const long long at = tt < count ? place[tt] : -1;
+                if (at < 0) continue;
+                if (kE4m3) {
+                    const uint32_t s = scale_byte(y ? tops >> 16 : tops & 0xffffu);
+                    *reinterpret_cast<uint2*>(dst + at) = chunk_codes(x[i + y], s);
+                    if (part == 0) scales[scale_place[tt]] = (uint8_t)s;
+                } else {
+                    *reinterpret_cast<uint4*>(dst + at * 2) = x[i + y];
+                }
             }
         }
     }
 }
 
-// pages -> k_out, v_out [n][Hkv][D] bf16 (row and head strides in elements).  Rows of no sequence are left as they are; rows of a sequence that have no place in
-// its pages read as zeros.
-template <int D, bool kE4m3>
+// pages -> k_out, v_out [n][Hkv][D] bf16 (row and head strides in elements).  Rows of no sequence are left as they are; rows of a sequence that
+// have no place in its pages read as zeros.
+template <int D, bool kE4m3, int kTokens>
 __global__ void __launch_bounds__(kCacheThreads) paged_read_kernel(
     PageGeom p, __nv_bfloat16* k_out, long long k_ts, long long k_hs, __nv_bfloat16* v_out, long long v_ts, long long v_hs, const int32_t* cu,
-    const int32_t* kv_len, int batch, int n, FastDiv div_rows, FastDiv div_heads, int32_t* status) {
-    constexpr int kLanes = D / 8, kBatch = 4;
-    __shared__ int page[kCacheTokens], place[kCacheTokens];
-    const int t0 = blockIdx.x * kCacheTokens;
+    const int32_t* kv_len, int batch, int n, int32_t* status) {
+    constexpr int kLanes = D / 8, kAhead = kE4m3 ? 8 : 4;
+    __shared__ long long place[kTokens], scale_place[kTokens];
+    const int t0 = blockIdx.x * kTokens, cols = 2 * p.Hkv * kLanes, col0 = blockIdx.y * kCacheThreads, width = min(cols - col0, kCacheThreads);
+    const int tokens = kCacheThreads / width, mine = (int)threadIdx.x / width;
+    const int col = col0 + (int)threadIdx.x - mine * width, row = col / kLanes, part = col % kLanes;
+    const bool is_v = row >= p.Hkv;
+    const int head = is_v ? row - p.Hkv : row;
+    const long long ts = is_v ? v_ts : k_ts;
+    __nv_bfloat16* dst = (is_v ? v_out + head * v_hs : k_out + head * k_hs) + part * 8 + t0 * ts;
+    const uint8_t* src = (is_v ? p.v : p.k) + (((long long)head << p.page_shift) * D + part * 8) * (kE4m3 ? 1 : 2);
+    const uint8_t* scales = (is_v ? p.vs : p.ks) + ((long long)head << p.page_shift);
+    const int count = mine < tokens ? min(kTokens, n - t0) : 0;
     launch_dependents();
     wait_for_previous_kernel();
-    const int n_chunks = kCacheTokens * 2 * p.Hkv * kLanes;
-    find_tokens(p, cu, kv_len, batch, n, t0, page, place, status);
+    find_tokens<kTokens, D>(p, cu, kv_len, batch, n, t0, place, scale_place, status);
     __syncthreads();
-    for (int c0 = threadIdx.x; c0 < n_chunks; c0 += kBatch * kCacheThreads) {
-        uint4 x[kBatch];
-        uint32_t s[kBatch];
-        __nv_bfloat16* dst[kBatch];
+    for (int t = mine; t < count; t += kAhead * tokens) {
+        uint4 x[kAhead];
+        uint32_t s[kAhead];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int c = c0 + i * kCacheThreads, row = c / kLanes, part = c % kLanes;
-            int r, w, h;
-            div_rows.divmod(row, r, w);
-            div_heads.divmod(w, w, h);
+        for (int i = 0; i < kAhead; ++i) {
+            const int tt = t + i * tokens;
+            const long long at = tt < count ? place[tt] : -1;
             x[i] = make_uint4(0u, 0u, 0u, 0u);
-            s[i] = 0;
-            dst[i] = nullptr;
-            if (c < n_chunks && page[r] != -1) {
-                const int pg = page[r];
-                dst[i] = (w ? v_out + (long long)(t0 + r) * v_ts + h * v_hs : k_out + (long long)(t0 + r) * k_ts + h * k_hs) + part * 8;
-                if (pg >= 0) {
-                    const long long at = ((long long)h << p.page_shift) + place[r];
-                    if (kE4m3) {
-                        const uint2 cc = *reinterpret_cast<const uint2*>((w ? p.v : p.k) + (long long)pg * p.page_stride + at * D + part * 8);
-                        x[i].x = cc.x;
-                        x[i].y = cc.y;
-                        s[i] = (w ? p.vs : p.ks)[(long long)pg * p.scale_stride + at];
-                    } else {
-                        x[i] = *reinterpret_cast<const uint4*>((w ? p.v : p.k) + ((long long)pg * p.page_stride + at * D + part * 8) * 2);
-                    }
+            s[i] = 0u;
+            if (at >= 0) {
+                if (kE4m3) {
+                    const uint2 c = *reinterpret_cast<const uint2*>(src + at);
+                    x[i].x = c.x;
+                    x[i].y = c.y;
+                    s[i] = scales[scale_place[tt]];
+                } else {
+                    x[i] = *reinterpret_cast<const uint4*>(src + at * 2);
                 }
             }
         }
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-            if (dst[i] != nullptr) *reinterpret_cast<uint4*>(dst[i]) = kE4m3 ? chunk_values(make_uint2(x[i].x, x[i].y), s[i]) : x[i];
+        for (int i = 0; i < kAhead; ++i) {
+            const int tt = t + i * tokens;
+            if (tt < count && place[tt] != -1) *reinterpret_cast<uint4*>(dst + tt * ts) = kE4m3 ? chunk_values(make_uint2(x[i].x, x[i].y), s[i]) : x[i];
+        }
     }
 }
 

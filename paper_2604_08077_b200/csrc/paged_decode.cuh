@@ -39,23 +39,30 @@ __host__ __device__ constexpr int paged_tile(bool e4m3) { return e4m3 ? 128 : 64
 __host__ __device__ constexpr int paged_row_floats(int D) { return D + 4; }           // m, l, m', -, o[D]
 __host__ __device__ constexpr size_t paged_partial_bytes(int D, int G) { return (size_t)kPagedCtas * 2 * G * paged_row_floats(D) * sizeof(float); }
 
-// The new token's row of one kv head (keys: which = 0, values: 1) into its place; by the 32 lanes of a warp, of which lane % (D / 8) holds x, 8
-// values.
+// The new token's rows of one kv head into their place; by the 32 lanes of a warp, of which lane % (D / 8) holds k and v, 8 values each.
 template <int D, bool kE4m3>
-__device__ __forceinline__ void append_row(const PageGeom& p, int page, int head, int place, int which, const uint4& x, int lane) {
+__device__ __forceinline__ void append_rows(const PageGeom& p, int page, int head, int place, uint4 k, uint4 v, int lane) {
     constexpr int kLanes = D / 8;
-    const long long row = ((long long)head << p.page_shift) + place;
-    const int part = lane % kLanes;
+    const long long row = ((long long)head << p.page_shift) + place, at = (long long)page * p.page_stride + row * D + lane % kLanes * 8;
     if (kE4m3) {
-        bool odd;
-        uint32_t top = chunk_top(x, odd);
-#pragma unroll
-        for (int s = 1; s < kLanes; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-        const uint32_t s = scale_byte(top);
-        if (lane < kLanes) *reinterpret_cast<uint2*>((which ? p.v : p.k) + (long long)page * p.page_stride + row * D + part * 8) = chunk_codes(x, s, odd);
-        if (lane == 0) (which ? p.vs : p.ks)[(long long)page * p.scale_stride + row] = (uint8_t)s;
+        uint32_t tops = row_tops<kLanes>(chunk_tops(k), chunk_tops(v));
+        if (__any_sync(0xffffffffu, any_odd(tops))) {
+            tops = row_tops<kLanes>(chunk_finite_tops(k), chunk_finite_tops(v));
+            k = infinities_to_nan(k);
+            v = infinities_to_nan(v);
+        }
+        const uint32_t sk = scale_byte(tops & 0xffffu), sv = scale_byte(tops >> 16);
+        if (lane < kLanes) {
+            *reinterpret_cast<uint2*>(p.k + at) = chunk_codes(k, sk);
+            *reinterpret_cast<uint2*>(p.v + at) = chunk_codes(v, sv);
+        }
+        if (lane == 0) {
+            p.ks[(long long)page * p.scale_stride + row] = (uint8_t)sk;
+            p.vs[(long long)page * p.scale_stride + row] = (uint8_t)sv;
+        }
     } else if (lane < kLanes) {
-        *reinterpret_cast<uint4*>((which ? p.v : p.k) + ((long long)page * p.page_stride + row * D + part * 8) * 2) = x;
+        *reinterpret_cast<uint4*>(p.k + at * 2) = k;
+        *reinterpret_cast<uint4*>(p.v + at * 2) = v;
     }
 }
 
@@ -337,8 +344,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                     }
                 } else if (a.k_new != nullptr && tile == w.tiles - 1) {    // the new token: the last of this tile
                     const int pg = __shfl_sync(0xffffffffu, page, boxes - 1), place = (w.n - 1) & (page_size - 1);
-                    append_row<D, kE4m3>(p, pg, w.gk, place, 0, new_k, lane);
-                    append_row<D, kE4m3>(p, pg, w.gk, place, 1, new_v, lane);
+                    append_rows<D, kE4m3>(p, pg, w.gk, place, new_k, new_v, lane);
                     asm volatile("fence.proxy.async;\n" ::: "memory");    // it is read by the copies below
                     __syncwarp();
                 }

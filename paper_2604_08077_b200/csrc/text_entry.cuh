@@ -10,6 +10,8 @@
 
 namespace {
 
+constexpr int kCacheManyTokens = 16384;
+
 // The handle's device for the length of a call; the caller's is current again afterwards.
 struct DeviceScope {
     int before = -1;
@@ -117,21 +119,25 @@ adaspark_status_t paged_rows_impl(adaspark_attn* h, const char* who, const adasp
     if (!c->cu || !c->kv_len) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL cu or kv_len", who);
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));
-    FastDiv rows, heads;
-    rows.init(2 * g.Hkv);
-    heads.init(g.Hkv);
+    const bool e4m3 = c->pages.format == ADASPARK_PAGES_E4M3;
+    const int D = h->cfg.head_dim, columns = (2 * g.Hkv * (D / 8) + kCacheThreads - 1) / kCacheThreads;
+    // 32 tokens a CTA where that leaves every SM several, 8 where there are few
+    const bool many = c->n >= kCacheManyTokens;
     auto launch = [&](auto kernel) {
-        launch_kernel(true, kernel, dim3((unsigned)((c->n + kCacheTokens - 1) / kCacheTokens)), dim3(kCacheThreads), 0, (cudaStream_t)cuda_stream, g, rk.p, rk.ts, rk.hs, rv.p, rv.ts,
-                      rv.hs, c->cu, c->kv_len, c->batch, c->n, rows, heads, c->status);
+        const int tokens = many ? 32 : 8;
+        launch_kernel(true, kernel, dim3((unsigned)((c->n + tokens - 1) / tokens), columns), dim3(kCacheThreads), 0, (cudaStream_t)cuda_stream, g, rk.p, rk.ts, rk.hs, rv.p,
+                      rv.ts, rv.hs, c->cu, c->kv_len, c->batch, c->n, c->status);
     };
-    const bool e4m3 = c->pages.format == ADASPARK_PAGES_E4M3, wide = h->cfg.head_dim == 128;
-    if (write) {
-        if (wide) e4m3 ? launch(paged_write_kernel<128, true>) : launch(paged_write_kernel<128, false>);
-        else e4m3 ? launch(paged_write_kernel<64, true>) : launch(paged_write_kernel<64, false>);
-    } else {
-        if (wide) e4m3 ? launch(paged_read_kernel<128, true>) : launch(paged_read_kernel<128, false>);
-        else e4m3 ? launch(paged_read_kernel<64, true>) : launch(paged_read_kernel<64, false>);
-    }
+    auto with = [&](auto d, auto bytes_held) {
+        constexpr int kD = d.value;
+        constexpr bool kE4m3 = bytes_held.value;
+        if (write) many ? launch(paged_write_kernel<kD, kE4m3, 32>) : launch(paged_write_kernel<kD, kE4m3, 8>);
+        else many ? launch(paged_read_kernel<kD, kE4m3, 32>) : launch(paged_read_kernel<kD, kE4m3, 8>);
+    };
+    const std::integral_constant<int, 128> wide;
+    const std::integral_constant<int, 64> narrow;
+    if (D == 128) e4m3 ? with(wide, std::true_type()) : with(wide, std::false_type());
+    else e4m3 ? with(narrow, std::true_type()) : with(narrow, std::false_type());
     return launch_ok(h, write ? "paged_write_kernel" : "paged_read_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
 }
 
