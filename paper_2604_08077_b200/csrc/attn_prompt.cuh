@@ -2,7 +2,11 @@
 //
 //   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = 2^(scale_log2 q_i.k_j - m_i),  j <= n_k - n_q + i
 //
-// One pass over the keys with a running reference m_i and sum, scores and weights in tensor memory alone.  Work is dealt out in
+// One pass over the keys with a reference m_i and running sum, scores and weights in tensor memory alone.  The reference is the largest of the
+// row's first 128 scores and moves only when a later score is 2^40 above it: weights, sums and outputs are floating-point numbers, whose
+// relative precision does not depend on it, and 2^40 is far from where they end.  So a step needs no maximum before its exponentials
+// (one over every 32 scores, in registers, says whether the reference has to move), and the three softmax warpgroups do not wait for
+// each other's.  References are whole numbers: moving one multiplies by powers of two and rounds nothing.  Work is dealt out in
 // tiles of 256 rows, a CTA pair (cta_group::2) each: the rows are (token, head of the group) pairs, 128 / G tokens per CTA, so that
 // K and V are read once for all heads of a group, a sequence of a few tokens fills rows that it would leave empty head by head, and
 // the diagonal wastes little (256 rows of a group of 7 are 36 tokens: 2 % of the scores of 8192 tokens lie above it, 256 tokens of one head: 4.7 %).
@@ -31,19 +35,19 @@
 
 namespace adaspark {
 
-constexpr int kPromptGroups = 3;                              // softmax warpgroups
-constexpr int kPromptThreads = (kPromptGroups + 1) * 128;
-constexpr int kPromptSoftmaxRegs = 144, kPromptHelperRegs = 80;
-static_assert(kPromptGroups * 128 * kPromptSoftmaxRegs + 128 * kPromptHelperRegs <= kPromptThreads * 128, "setmaxnreg must stay inside the CTA's launch allocation");
-constexpr int kPromptBufs = 3;                                // score tiles in TMEM, one per warpgroup
+constexpr int kPromptTeams = 2;                               // softmax teams, of two warpgroups each
+constexpr int kPromptThreads = (2 * kPromptTeams + 1) * 128;
+constexpr int kPromptBufs = 3;                                // score tiles in TMEM
 constexpr int kPromptRefSlots = 4;
+constexpr float kPromptGrow = 40.f;                           // a reference moves when a score is more than 2^40 above it
 constexpr int kPromptOddSlots = 8;                            // more than tiles whose V can be under way at once (a step each)
-__host__ __device__ constexpr int prompt_stages(int D) { return D == 64 ? 6 : 3; }
-static_assert(prompt_stages(64) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
+__host__ __device__ constexpr int prompt_k_stages(int D) { return D == 64 ? 6 : 3; }   // steps whose K, V are under way
+__host__ __device__ constexpr int prompt_v_stages(int D) { return D == 64 ? 6 : 3; }
+static_assert(prompt_v_stages(64) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
 
 // 2^x on the FMA pipe (every 8th exponential of steps without a mask; MUFU gives 16 a cycle and is the busier pipe): 2^f on
 // [-0.5, 0.5] by a minimax polynomial of degree 4 (relative error 2.6e-6), n through a multiplication, so that what is no number stays
-// one.  x is clamped at -125: a weight that would vanish is 2^-125 beside a largest one of at least 2^-8.
+// one.  x is clamped at -125: a weight that would vanish is 2^-125 beside a largest one of at least 1/2.
 __device__ __forceinline__ float poly_exp2(float x) {
     float xc;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(xc) : "f"(x), "f"(-125.f));
@@ -96,12 +100,14 @@ struct PromptSeq {
 template <int D>
 struct PromptSmem {
     __nv_bfloat16 q[2][D / 64][128][64];                      // [tile & 1][d panel][row][64 d]
-    __nv_bfloat16 kv[2 * prompt_stages(D)][64 * D];           // K: [d panel][this CTA's 64 keys][64 d]; V: [128 keys][this CTA's half of d]
+    __nv_bfloat16 k[prompt_k_stages(D)][64 * D];              // [d panel][this CTA's 64 keys][64 d]
+    __nv_bfloat16 v[prompt_v_stages(D)][64 * D];              // [128 keys][this CTA's half of d]
     unsigned char out[128][2 * D + 16];
-    float ref[kPromptRefSlots][128];
-    float part_l[2][kPromptGroups][128], part_m[2][kPromptGroups][128];
-    uint64_t q_full[2], q_peer[2], q_empty[2], k_full[prompt_stages(D)], k_empty[prompt_stages(D)], v_full[prompt_stages(D)], v_empty[prompt_stages(D)];
-    uint64_t v_raw, s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], o_full, o_free;
+    float ref[kPromptRefSlots][128], first_ref[2][128];      // reference of a row after a step, after the first 128 keys of a tile
+    float part_l[2][2][128], part_m[2][2][128];             // sums and reference of the team that does not finish a tile, by half
+    float other_l[kPromptTeams][2][128], other_ref[kPromptTeams][2][128];   // between the halves of a row
+    uint64_t q_full[2], q_peer[2], q_empty[2], k_full[prompt_k_stages(D)], k_empty[prompt_k_stages(D)], v_full[prompt_v_stages(D)], v_empty[prompt_v_stages(D)];
+    uint64_t v_raw, s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], first_done[2][4], o_full, o_free;
     uint64_t plan_full[2], plan_empty[2], part_full[2], part_free[2], out_free;
     PromptTile tile[2];
     int odd_tile[kPromptOddSlots];                            // number + 1 of a tile with masked values that are no numbers
@@ -115,12 +121,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     __nv_bfloat16* out, float* lse, int32_t* status) {
     extern __shared__ unsigned char prompt_smem_raw[];
     PromptSmem<D>& sm = *reinterpret_cast<PromptSmem<D>*>((reinterpret_cast<uintptr_t>(prompt_smem_raw) + 1023) & ~(uintptr_t)1023);
-    constexpr int kPanels = D / 64, kQKSteps = D / 16, kStages = prompt_stages(D);
+    constexpr int kPanels = D / 64, kQKSteps = D / 16, kKStages = prompt_k_stages(D), kVStages = prompt_v_stages(D);
     constexpr uint32_t kIdescS = tc::make_idesc_bf16(256, 128);
     constexpr uint32_t kIdescO = tc::make_idesc_bf16(256, D) | (1u << 16);   // B = V: rows along N
     constexpr uint32_t kTileBytes = 64 * D * 2;               // a CTA's share of the K or V of a step
     constexpr int kVRow = D;                                  // bytes of a key in a CTA's share of V (half of d)
-    constexpr int kKWarp = kPromptGroups * 4, kMmaWarp = kKWarp + 1, kVWarp = kKWarp + 2, kPlanWarp = kKWarp + 3;
+    constexpr int kKWarp = kPromptTeams * 8, kMmaWarp = kKWarp + 1, kVWarp = kKWarp + 2, kPlanWarp = kKWarp + 3;
     constexpr uint32_t kOCol = kPromptBufs * 128;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -134,27 +140,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             tc::mbar_init(&sm.q_peer[i], 1);
             tc::mbar_init(&sm.q_empty[i], 1);
             tc::mbar_init(&sm.plan_full[i], 1);
-            tc::mbar_init(&sm.plan_empty[i], 3 + kPromptGroups * 4);
-            tc::mbar_init(&sm.part_full[i], (kPromptGroups - 1) * 4);
-            tc::mbar_init(&sm.part_free[i], 4);
+            tc::mbar_init(&sm.plan_empty[i], 3 + kPromptTeams * 8);
+            tc::mbar_init(&sm.part_full[i], 8);
+            tc::mbar_init(&sm.part_free[i], 8);
         }
-        for (int i = 0; i < kStages; ++i) {
+        for (int i = 0; i < kKStages; ++i) {
             tc::mbar_init(&sm.k_full[i], 1);
             tc::mbar_init(&sm.k_empty[i], 1);
+        }
+        for (int i = 0; i < kVStages; ++i) {
             tc::mbar_init(&sm.v_full[i], 2);                  // the V warps of both CTAs
             tc::mbar_init(&sm.v_empty[i], 1);
         }
         for (int i = 0; i < kPromptBufs; ++i) {
             tc::mbar_init(&sm.s_full[i], 1);
-            tc::mbar_init(&sm.p_full[i], 8);
+            tc::mbar_init(&sm.p_full[i], 16);
         }
         for (int i = 0; i < kPromptRefSlots; ++i)
             for (int w = 0; w < 4; ++w) tc::mbar_init(&sm.ref_done[i][w], 1);
+        for (int i = 0; i < 2; ++i)
+            for (int w = 0; w < 4; ++w) tc::mbar_init(&sm.first_done[i][w], 1);
         for (int i = 0; i < kPromptOddSlots; ++i) sm.odd_tile[i] = 0;
         tc::mbar_init(&sm.v_raw, 1);
         tc::mbar_init(&sm.o_full, 1);
-        tc::mbar_init(&sm.o_free, 8);
-        tc::mbar_init(&sm.out_free, 4);
+        tc::mbar_init(&sm.o_free, 16);
+        tc::mbar_init(&sm.out_free, 8);
         sm.abort_flag = 0;
         tc::fence_barrier_init();
         tc::prefetch_tensormap(&tmQ);
@@ -171,7 +181,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     const uint32_t tbase = sm.tmem_base;
     volatile int* abort_flag = &sm.abort_flag;
 
-    if (warp >= kKWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kPromptHelperRegs));
     if (warp == kPlanWarp) {
         // ------------------------------------------------------------ planner
         const int W = 2 * g.T;
@@ -269,8 +278,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     if (!(ok = tc::mbar_wait(&sm.k_empty[st], ph, abort_flag))) break;
                     if (rank == 0) tc::mbar_arrive_expect_tx(&sm.k_full[st], 2 * kTileBytes);
                     for (int p = 0; p < kPanels; ++p)
-                        tc::tma_load_3d_pair(&sm.kv[st][p * 64 * 64], &tmK, p * 64, gk, row0 + j * 128, bar0 + st * 8);
-                    if (++st == kStages) { st = 0; ph ^= 1; }
+                        tc::tma_load_3d_pair(&sm.k[st][p * 64 * 64], &tmK, p * 64, gk, row0 + j * 128, bar0 + st * 8);
+                    if (++st == kKStages) { st = 0; ph ^= 1; }
                 }
                 tc::mbar_arrive(&sm.plan_empty[slot]);
             }
@@ -287,7 +296,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             if (n_steps == 0) break;
             for (int j = 0; j < n_steps; ++j) {
                 if (!(ok = tc::mbar_wait_warp(&sm.v_empty[st], ph, abort_flag))) break;
-                unsigned char* tile = reinterpret_cast<unsigned char*>(&sm.kv[kStages + st][0]);
+                unsigned char* tile = reinterpret_cast<unsigned char*>(&sm.v[st][0]);
                 if (j < first_masked) {
                     if (tc::elect_one()) {
                         if (rank == 0) tc::mbar_arrive_expect_tx(&sm.v_full[st], 2 * kTileBytes);
@@ -330,7 +339,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     }
                     __syncwarp();
                 }
-                if (++st == kStages) { st = 0; ph ^= 1; }
+                if (++st == kVStages) { st = 0; ph ^= 1; }
             }
             if (!ok) break;
             __syncwarp();
@@ -351,12 +360,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         // ------------------------------------------------------------ MMA issuer
         constexpr uint32_t kKStep = 32 >> 4;                                        // 16 elements of a 128-byte row
         constexpr uint32_t kQPanelStep = (128 * 128) >> 4, kKPanelStep = (64 * 128) >> 4, kVStep = (16 * kVRow) >> 4;
-        constexpr uint32_t kQSlotStep = (uint32_t)sizeof(sm.q[0]) >> 4, kStageStep = (uint32_t)sizeof(sm.kv[0]) >> 4;
+        constexpr uint32_t kQSlotStep = (uint32_t)sizeof(sm.q[0]) >> 4, kStageStep = (uint32_t)sizeof(sm.k[0]) >> 4;
         // V: rows of a key's 64 (D = 64: 32) values with the 128- (64-) byte swizzle, groups of 8 keys kVRow * 8 bytes apart
         constexpr uint32_t kVDescHi = (uint32_t)((8 * kVRow) >> 4) | (1u << 14) | ((D == 128 ? 2u : 4u) << 29);
         const uint32_t q_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.q[0][0][0][0])), 0);
-        const uint32_t k_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.kv[0][0])), 0);
-        const uint32_t v_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.kv[kStages][0])), 0);
+        const uint32_t k_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.k[0][0])), 0);
+        const uint32_t v_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.v[0][0])), 0);
         const uint32_t tb = __shfl_sync(0xffffffffu, tbase, 0);
         if (tc::elect_one()) {
             bool ok = true, ended = false;
@@ -388,7 +397,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 tc::umma_commit_pair(&sm.k_empty[kst]);
                 if (--s_left == 0) tc::umma_commit_pair(&sm.q_empty[ks & 1]);
                 if (++sbuf == kPromptBufs) sbuf = 0;
-                if (++kst == kStages) { kst = 0; kph ^= 1; }
+                if (++kst == kKStages) { kst = 0; kph ^= 1; }
                 ++ahead;
                 return true;
             };
@@ -406,10 +415,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     const uint32_t vb = v_lo0 + vst * kStageStep, src = tb + buf * 128;
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
-                        tc::umma_ts_pair(tb + kOCol, src + x * 8, tc::smem_desc_from_halves(vb + x * kVStep, kVDescHi), kIdescO, x > 0 || j > 0);
+                        tc::umma_ts_pair(tb + kOCol, src + (x >> 2) * 64 + (x & 3) * 8, tc::smem_desc_from_halves(vb + x * kVStep, kVDescHi), kIdescO, x > 0 || j > 0);
                     tc::umma_commit_pair(&sm.v_empty[vst]);
                     if (j == steps - 1) tc::umma_commit_pair(&sm.o_full);
-                    if (++vst == kStages) { vst = 0; vph ^= 1; }
+                    if (++vst == kVStages) { vst = 0; vph ^= 1; }
                     if (++buf == kPromptBufs) { buf = 0; buf_ph ^= 1; }
                     --ahead;
                 }
@@ -417,20 +426,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         }
     } else if (warp < kKWarp) {
         // ------------------------------------------------------------ softmax warps
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kPromptSoftmaxRegs));
-        const int wg = warp >> 2, quad = warp & 3;
+        // Warpgroups 2 t and 2 t + 1 are team t, which takes every second step; a thread has half the keys of a row (TMEM lane).
+        const int wg = warp >> 2, team = wg >> 1, half = wg & 1, quad = warp & 3;
         const int row = quad * 32 + lane;
         const uint32_t lane_addr = tbase + ((uint32_t)(quad * 32) << 16);
-        const uint32_t s_addr = lane_addr + wg * 128;
-        const uint32_t p_bar = cluster_address(&sm.p_full[wg], 0), o_free_bar = cluster_address(&sm.o_free, 0);
+        const uint32_t p_bar0 = cluster_address(&sm.p_full[0], 0), o_free_bar = cluster_address(&sm.o_free, 0);
         const float scale_log2 = g.scale_log2;
         const unsigned long long scale2 = pack_f32x2(scale_log2, scale_log2);
+        const int pair_bar = 1 + team * 4 + quad;              // the two warps that share 32 rows
+        auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;\n" ::"r"(pair_bar) : "memory"); };
+        auto pair_any = [&](bool x) -> bool {
+            int r;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 64, p;\n\tselp.s32 %0, 1, 0, q;\n\t}\n" : "=r"(r) : "r"((int)x), "r"(pair_bar) : "memory");
+            return r != 0;
+        };
         int tok, head;                                        // of the row
         g.div_g.divmod(row, tok, head);
         bool ok = true;
         int g0 = 0;                                           // steps of the tiles before this one
-        uint32_t s_ph = 0;
-        bool out_pending = false;                             // the rows of an epilogue leave shared memory while this warpgroup goes on
+        bool out_pending = false;                             // the rows of an epilogue leave shared memory while this team goes on
         auto release_out = [&]() {
             if (out_pending) {
                 asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
@@ -439,185 +453,193 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 out_pending = false;
             }
         };
+        // A wait that has expired does not end the loops below at once, for the two warps of a row meet in barriers: ok says so, and the
+        // loops end with the tile (further waits return quickly).
         for (int k = 0;; ++k) {
             const int slot = k & 1;
-            if (!(ok = tc::mbar_wait(&sm.plan_full[slot], (k >> 1) & 1, abort_flag))) break;
+            if (!tc::mbar_wait(&sm.plan_full[slot], (k >> 1) & 1, abort_flag)) ok = false;
+            if (pair_any(!ok)) break;
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
             const int last = t.last0 + tok;                   // the last key that the row sees
-            const int j0 = (wg + kPromptGroups - g0 % kPromptGroups) % kPromptGroups;
-            const bool last_wg = (g0 + t.n_steps - 1) % kPromptGroups == wg;
-            float m_ref = -INFINITY, l_sum = 0.f;
-            for (int j = j0; j < t.n_steps; j += kPromptGroups) {
-                const int gs = g0 + j, rs = gs & (kPromptRefSlots - 1);
+            const int j0 = (team + g0) & 1;
+            const bool finishes = ((g0 + t.n_steps - 1) & 1) == team;
+            float m_ref = 0.f, l_sum = 0.f;
+            for (int j = j0; j < t.n_steps; j += kPromptTeams) {
+                const int gs = g0 + j, rs = gs & (kPromptRefSlots - 1), buf = gs % kPromptBufs;
+                const uint32_t s_addr = lane_addr + buf * 128 + half * 64;
                 const bool masked = j >= t.first_masked;
-                const int n_vis = masked ? min(max(last + 1 - j * 128, 0), 128) : 128;    // keys of the step that the row sees
-                if (!(ok = tc::mbar_wait(&sm.s_full[wg], s_ph, abort_flag))) break;
-                s_ph ^= 1u;
+                const int n_vis = masked ? last + 1 - j * 128 - half * 64 : 64;    // keys of the half step that the row sees (any number)
+                if (!tc::mbar_wait(&sm.s_full[buf], (gs / kPromptBufs) & 1, abort_flag)) ok = false;
                 tc::tc_fence_after_sync();
-                // ---- the row's largest score; the reference moves through the warpgroups step by step
-                float mx = -INFINITY;
-                {
-                    auto fold = [&](const uint32_t (&s)[32], int c) {
-                        float a0 = -INFINITY, a1 = -INFINITY;
-                        if (masked) {
-                            const int n = n_vis - c * 32;
+                auto hide = [&](uint32_t (&s)[32], int c) {
+                    const int n = n_vis - c * 32;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                a0 = fmaxf(a0, 2 * i < n ? __uint_as_float(s[2 * i]) : -INFINITY);
-                                a1 = fmaxf(a1, 2 * i + 1 < n ? __uint_as_float(s[2 * i + 1]) : -INFINITY);
-                            }
-                        } else {
+                    for (int i = 0; i < 32; ++i)
+                        if (i >= n) s[i] = 0xff800000u;
+                };
+                auto largest = [&](const uint32_t (&s)[32]) -> float {
+                    float a0 = -INFINITY, a1 = -INFINITY;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                a0 = fmax3(a0, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
-                                a1 = fmax3(a1, __uint_as_float(s[16 + 2 * i]), __uint_as_float(s[17 + 2 * i]));
-                            }
-                        }
-                        mx = fmax3(mx, a0, a1);
-                    };
-                    uint32_t s0[32], s1[32];                  // the next chunk is requested before the present one is looked at
-                    tc::tmem_ld_32x32(s_addr, s0);
-                    tc::tmem_wait_ld_for(s0);
-                    tc::tmem_ld_32x32(s_addr + 32, s1);
-                    fold(s0, 0);
-                    tc::tmem_wait_ld_for(s1);
-                    tc::tmem_ld_32x32(s_addr + 64, s0);
-                    fold(s1, 1);
-                    tc::tmem_wait_ld_for(s0);
-                    tc::tmem_ld_32x32(s_addr + 96, s1);
-                    fold(s0, 2);
-                    tc::tmem_wait_ld_for(s1);
-                    fold(s1, 3);
-                }
-                const float mx_x = mx * scale_log2;           // scale > 0
-                float m_prev = -INFINITY;
-                if (gs > 0 && !(ok = tc::mbar_wait(&sm.ref_done[(gs - 1) & (kPromptRefSlots - 1)][quad], ((gs - 1) / kPromptRefSlots) & 1, abort_flag))) break;
-                if (j > 0) m_prev = sm.ref[(gs - 1) & (kPromptRefSlots - 1)][row];
-                // the reference moves only when it grows by more than 2^8 (weights up to 2^8 stay exact enough: fp32 sums, bf16 weights)
-                const bool need = mx_x > m_prev + 8.f;
-                const float m_new = need ? mx_x : m_prev;
-                sm.ref[rs][row] = m_new;
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&sm.ref_done[rs][quad]);
-                const bool rescale = j > 0 && __any_sync(0xffffffffu, need);
-                const float factor = need ? fast_exp2(m_prev - mx_x) : 1.f;   // 0 where nothing was visible before
-                l_sum = m_ref == -INFINITY ? 0.f : l_sum * fast_exp2(m_ref - m_new);
-                m_ref = m_new;
-                // ---- weights, 32 keys at a time over the scores
-                const unsigned long long add2 = pack_f32x2(-m_ref, -m_ref);
-                unsigned long long psA = 0ull, psB = 0ull;
-                {
-                    auto emit = [&](const uint32_t (&s)[32], int c) {
-                        uint32_t pk[16];
-                        if (masked) {
-                            const int n = n_vis - c * 32;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                float x0, x1;
-                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, add2), x0, x1);
-                                const float p0 = fast_exp2(2 * i < n ? x0 : -INFINITY), p1 = fast_exp2(2 * i + 1 < n ? x1 : -INFINITY);
-                                psA = add_f32x2(psA, pack_f32x2(p0, p1));
-                                pk[i] = pack_bf16x2(p0, p1);
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const unsigned long long x01 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), scale2, add2);
-                                const unsigned long long x23 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), scale2, add2);
-                                float x0, x1, x2, x3;
-                                unpack_f32x2(x01, x0, x1);
-                                unpack_f32x2(x23, x2, x3);
-                                const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = (i & 1) ? poly_exp2(x3) : fast_exp2(x3);
-                                psA = add_f32x2(psA, pack_f32x2(p0, p1));
-                                psB = add_f32x2(psB, pack_f32x2(p2, p3));
-                                pk[2 * i] = pack_bf16x2(p0, p1);
-                                pk[2 * i + 1] = pack_bf16x2(p2, p3);
-                            }
-                        }
-                        tc::tmem_st_32x16(s_addr + c * 16, pk);
-                    };
-                    uint32_t s0[32], s1[32];
-                    tc::tmem_ld_32x32(s_addr, s0);
-                    tc::tmem_wait_ld_for(s0);
-                    tc::tmem_ld_32x32(s_addr + 32, s1);
-                    emit(s0, 0);
-                    tc::tmem_wait_ld_for(s1);
-                    tc::tmem_ld_32x32(s_addr + 64, s0);
-                    emit(s1, 1);
-                    tc::tmem_wait_ld_for(s0);
-                    tc::tmem_ld_32x32(s_addr + 96, s1);
-                    emit(s0, 2);
-                    tc::tmem_wait_ld_for(s1);
-                    emit(s1, 3);
-                }
-                if (rescale) {
-                    // O holds the products of all steps up to the last one, and no later one starts before this step's weights are reported
-                    if (!(ok = tc::mbar_wait(&sm.v_empty[(gs - 1) % kStages], ((gs - 1) / kStages) & 1, abort_flag))) break;
-                    tc::tc_fence_after_sync();
-#pragma unroll 1
-                    for (int c = 0; c < D / 32; c += 2) {
-                        uint32_t o0[32], o1[32];
-                        tc::tmem_ld_32x32(lane_addr + kOCol + c * 32, o0);
-                        tc::tmem_wait_ld_for(o0);
-                        tc::tmem_ld_32x32(lane_addr + kOCol + c * 32 + 32, o1);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o0[e] = __float_as_uint(__uint_as_float(o0[e]) * factor);
-                        tc::tmem_st_32x32(lane_addr + kOCol + c * 32, o0);
-                        tc::tmem_wait_ld_for(o1);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o1[e] = __float_as_uint(__uint_as_float(o1[e]) * factor);
-                        tc::tmem_st_32x32(lane_addr + kOCol + c * 32 + 32, o1);
+                    for (int i = 0; i < 8; ++i) {
+                        a0 = fmax3(a0, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+                        a1 = fmax3(a1, __uint_as_float(s[16 + 2 * i]), __uint_as_float(s[17 + 2 * i]));
                     }
+                    return fmaxf(a0, a1);
+                };
+                if (j == 0) {
+                    // ---- the reference of the tile: the largest of the first 128 scores, rounded up
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t s[32];
+                        tc::tmem_ld_32x32(s_addr + c * 32, s);
+                        tc::tmem_wait_ld_for(s);
+                        if (masked) hide(s, c);
+                        top = fmaxf(top, largest(s));
+                    }
+                    sm.other_ref[team][half][row] = top;
+                    pair_sync();
+                    top = fmaxf(top, sm.other_ref[team][half ^ 1][row]) * scale_log2;    // scale > 0
+                    m_ref = top == -INFINITY ? 0.f : ceilf(top);       // (a row that sees nothing: any)
+                    if (half == 0) {
+                        sm.first_ref[k & 1][row] = m_ref;
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(&sm.first_done[k & 1][quad]);
+                    }
+                    pair_sync();                               // (other_ref is written again below)
+                } else if (j == j0) {
+                    if (!tc::mbar_wait(&sm.first_done[k & 1][quad], (k >> 1) & 1, abort_flag)) ok = false;
+                    m_ref = sm.first_ref[k & 1][row];
                 }
-                tc::tmem_wait_st();
-                tc::tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive_cluster(p_bar);
+                // ---- weights, 32 keys at a time over the scores.  The reference stays what it is unless a score is 2^kPromptGrow above it;
+                // then it moves up, and the weights before follow further down (rc: the reference of a chunk).
+                float ref = m_ref, rc0 = ref;
+                unsigned long long add2 = pack_f32x2(-ref, -ref), psA = 0ull, psB = 0ull;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t s[32], pk[16];
+                    tc::tmem_ld_32x32(s_addr + c * 32, s);
+                    tc::tmem_wait_ld_for(s);
+                    if (masked) hide(s, c);
+                    const float over = fmaf(largest(s), scale_log2, -ref);
+                    if (__any_sync(0xffffffffu, over > kPromptGrow)) {
+                        const float up = over > kPromptGrow ? ceilf(over) : 0.f, f = fast_exp2(-up);
+                        ref += up;
+                        add2 = pack_f32x2(-ref, -ref);
+                        psA = mul_f32x2(psA, pack_f32x2(f, f));
+                        psB = mul_f32x2(psB, pack_f32x2(f, f));
+                    }
+                    if (c == 0) rc0 = ref;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const unsigned long long x01 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), scale2, add2);
+                        const unsigned long long x23 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), scale2, add2);
+                        float x0, x1, x2, x3;
+                        unpack_f32x2(x01, x0, x1);
+                        unpack_f32x2(x23, x2, x3);
+                        const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = fast_exp2(x3);
+                        psA = add_f32x2(psA, pack_f32x2(p0, p1));
+                        psB = add_f32x2(psB, pack_f32x2(p2, p3));
+                        pk[2 * i] = pack_bf16x2(p0, p1);
+                        pk[2 * i + 1] = pack_bf16x2(p2, p3);
+                    }
+                    tc::tmem_st_32x16(s_addr + c * 16, pk);
+                }
                 float a0, a1, b0, b1;
                 unpack_f32x2(psA, a0, a1);
                 unpack_f32x2(psB, b0, b1);
-                l_sum += (a0 + a1) + (b0 + b1);
+                float l_step = (a0 + a1) + (b0 + b1);
+                // ---- the steps' references in order: it only grows
+                float m_prev = ref;
+                if (gs > 0 && !tc::mbar_wait(&sm.ref_done[(gs - 1) & (kPromptRefSlots - 1)][quad], ((gs - 1) / kPromptRefSlots) & 1, abort_flag)) ok = false;
+                if (j > 0) m_prev = sm.ref[(gs - 1) & (kPromptRefSlots - 1)][row];
+                float m_new = m_prev;
+                if (pair_any(rc0 != m_prev || ref != m_prev)) {
+                    // rare: the halves' references, or the one before, differ (by powers of two: nothing is rounded)
+                    sm.other_ref[team][half][row] = ref;
+                    pair_sync();
+                    m_new = fmaxf(m_prev, fmaxf(ref, sm.other_ref[team][half ^ 1][row]));
+                    l_step *= fast_exp2(ref - m_new);
+                    l_sum *= fast_exp2(m_ref - m_new);
+                    tc::tmem_wait_st();
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        const float f = fast_exp2((c < 2 ? rc0 : ref) - m_new);
+                        uint32_t w[8];
+                        tc::tmem_ld_32x8(s_addr + c * 8, w);
+                        tc::tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
+                        tc::tmem_st_32x8(s_addr + c * 8, w);
+                    }
+                    if (j > 0 && __any_sync(0xffffffffu, m_new != m_prev)) {
+                        // O holds the products of all steps up to the last one, and no later one starts before this step's weights are
+                        // reported; half its columns each
+                        const float factor = fast_exp2(m_prev - m_new);
+                        if (!tc::mbar_wait(&sm.v_empty[(gs - 1) % kVStages], ((gs - 1) / kVStages) & 1, abort_flag)) ok = false;
+                        tc::tc_fence_after_sync();
+#pragma unroll 1
+                        for (int c = 0; c < D / 64; ++c) {
+                            uint32_t o0[32];
+                            const uint32_t at = lane_addr + kOCol + half * (D / 2) + c * 32;
+                            tc::tmem_ld_32x32(at, o0);
+                            tc::tmem_wait_ld_for(o0);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o0[e] = __float_as_uint(__uint_as_float(o0[e]) * factor);
+                            tc::tmem_st_32x32(at, o0);
+                        }
+                    }
+                    pair_sync();                               // other_ref has been read
+                }
+                if (half == 0) {
+                    sm.ref[rs][row] = m_new;
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&sm.ref_done[rs][quad]);
+                }
+                l_sum += l_step;
+                m_ref = m_new;
+                tc::tmem_wait_st();
+                tc::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive_cluster(p_bar0 + buf * 8);
             }
-            if (!ok) break;
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
-            // ---- the sums of the three warpgroups meet in the one that took the last step; the others go on to the next tile
+            // ---- the teams' sums meet in the one that took the last step; the other goes on to the next tile
             release_out();
             const int ps = k & 1, p_ph = (k >> 1) & 1;
-            if (!last_wg) {
-                if (!(ok = tc::mbar_wait(&sm.part_free[ps], p_ph ^ 1, abort_flag))) break;
-                sm.part_l[ps][wg][row] = l_sum;
-                sm.part_m[ps][wg][row] = m_ref;
+            if (!finishes) {
+                if (!tc::mbar_wait(&sm.part_free[ps], p_ph ^ 1, abort_flag)) ok = false;
+                sm.part_l[ps][half][row] = l_sum;
+                sm.part_m[ps][half][row] = m_ref;
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&sm.part_full[ps]);
             } else {
-                if (!(ok = tc::mbar_wait(&sm.part_full[ps], p_ph, abort_flag))) break;
-                float l_fin = 0.f;                            // the reference only grows: the last step's is the largest
-#pragma unroll
-                for (int r = 0; r < kPromptGroups; ++r) {     // in the order of the steps
-                    int w = g0 % kPromptGroups + r;
-                    w = w >= kPromptGroups ? w - kPromptGroups : w;
-                    const float l = w == wg ? l_sum : sm.part_l[ps][w][row], m = w == wg ? m_ref : sm.part_m[ps][w][row];
-                    if (l != 0.f) l_fin += l * fast_exp2(m - m_ref);
-                }
+                sm.other_l[team][half][row] = l_sum;
+                if (!tc::mbar_wait(&sm.part_full[ps], p_ph, abort_flag)) ok = false;
+                pair_sync();
+                // first halves first: both of a row's threads add in the same order.  The reference only grows: the last step's is the largest
+                float l_fin = sm.other_l[team][0][row] + sm.other_l[team][1][row];
+                const float l_part = sm.part_l[ps][0][row] + sm.part_l[ps][1][row];
+                if (l_part != 0.f) l_fin += l_part * fast_exp2(sm.part_m[ps][0][row] - m_ref);
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&sm.part_free[ps]);
                 const float inv = l_fin != 0.f ? 1.f / l_fin : 0.f;
                 const bool mine = tok < t.n_tok;              // (the tile's last rows may be none, tokens behind the sequence not its own)
                 const long long at = (long long)(t.q0 + tok) * g.Hq + t.gk * g.G + head;
-                if (mine && lse != nullptr) lse[at] = (m_ref + log2f(l_fin)) * 0.6931471805599453f;
-                if (k > 0 && !(ok = tc::mbar_wait(&sm.out_free, (k - 1) & 1, abort_flag))) break;
-                if (!(ok = tc::mbar_wait(&sm.o_full, k & 1, abort_flag))) break;
+                if (mine && half == 0 && lse != nullptr) lse[at] = (m_ref + log2f(l_fin)) * 0.6931471805599453f;
+                if (k > 0 && !tc::mbar_wait(&sm.out_free, (k - 1) & 1, abort_flag)) ok = false;
+                if (!tc::mbar_wait(&sm.o_full, k & 1, abort_flag)) ok = false;
                 tc::tc_fence_after_sync();
                 const bool odd = *(volatile int*)&sm.odd_tile[k % kPromptOddSlots] == k + 1;
-                unsigned char* srow = sm.out[row];
+                unsigned char* srow = sm.out[row] + half * D;     // half the row's bytes
 #pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
+                for (int c = 0; c < D / 64; ++c) {
                     uint32_t o[32];
-                    tc::tmem_ld_32x32(lane_addr + kOCol + c * 32, o);
+                    tc::tmem_ld_32x32(lane_addr + kOCol + half * (D / 2) + c * 32, o);
                     tc::tmem_wait_ld_for(o);
-                    if (c == D / 32 - 1) {
+                    if (c == D / 64 - 1) {
                         tc::tc_fence_before_sync();
                         __syncwarp();
                         if (lane == 0) tc::mbar_arrive_cluster(o_free_bar);
@@ -635,17 +657,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 if (odd && mine) {                            // rare: values that are no numbers and that this row sees
                     __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(srow);
                     for (int key = t.first_masked * 128; key <= last; ++key) {
-                        const __nv_bfloat16* vr = g.v + (long long)(t.k0 + key) * g.v_ts + t.gk * g.v_hs;
-                        for (int d = 0; d < D; ++d) {
+                        const __nv_bfloat16* vr = g.v + (long long)(t.k0 + key) * g.v_ts + t.gk * g.v_hs + half * (D / 2);
+                        for (int d = 0; d < D / 2; ++d) {
                             const float x = __bfloat162float(vr[d]);
                             if (!(fabsf(x) < INFINITY)) o[d] = __float2bfloat16(__bfloat162float(o[d]) + x);
                         }
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-                if (mine) asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(out + at * D), "r"(smem_u32(srow)), "n"(2 * D) : "memory");
+                if (mine) asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(out + at * D + half * (D / 2)), "r"(smem_u32(srow)), "n"(D) : "memory");
                 asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
                 out_pending = true;
+                pair_sync();                                  // other_l has been read
             }
             g0 += t.n_steps;
         }
