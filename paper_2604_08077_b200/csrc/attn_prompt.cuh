@@ -3,24 +3,29 @@
 //   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = 2^(scale_log2 q_i.k_j - m_i),  j <= n_k - n_q + i
 //
 // One pass over the keys with a reference m_i and running sum, scores and weights in tensor memory alone.  The reference is the largest of the
-// row's first 128 scores and moves only when a later score is 2^40 above it: weights, sums and outputs are floating-point numbers, whose
-// relative precision does not depend on it, and 2^40 is far from where they end.  So a step needs no maximum before its exponentials
-// (one over every 32 scores, in registers, says whether the reference has to move), and the three softmax warpgroups do not wait for
-// each other's.  References are whole numbers: moving one multiplies by powers of two and rounds nothing.  Work is dealt out in
-// tiles of 256 rows, a CTA pair (cta_group::2) each: the rows are (token, head of the group) pairs, 128 / G tokens per CTA, so that
-// K and V are read once for all heads of a group, a sequence of a few tokens fills rows that it would leave empty head by head, and
-// the diagonal wastes little (256 rows of a group of 7 are 36 tokens: 2 % of the scores of 8192 tokens lie above it, 256 tokens of one head: 4.7 %).
+// row's first 128 scores, rounded up, and moves only when the weights of 64 keys sum up to more than 2^40: weights, sums and outputs are
+// floating-point numbers, whose relative precision does not depend on it, and 2^40 is far from where they end.  So no step but the first
+// takes a maximum (9 % of the time of a long prompt).  Where a score is 86 and more (in powers of two: 126) above its row's reference, weights of infinity say so, and that
+// half step's scores, which the weights have overwritten, are computed once more by the threads themselves.  References are whole
+// numbers: moving one multiplies by powers of two and rounds nothing.
 //
-// Roles of a CTA (512 threads), coupled by barriers alone, so that set-up, loads and first scores of the next tile overlap the end of
+// Work is dealt out in tiles of 256 rows, a CTA pair (cta_group::2) each: the rows are (token, head of the group) pairs, 128 / G tokens
+// per CTA, so that K and V are read once for all heads of a group, a sequence of a few tokens fills rows that it would leave empty head by
+// head, and the diagonal wastes little (256 rows of a group of 7 are 36 tokens: 2 % of the scores of 8192 tokens lie above it, 256 tokens of
+// one head: 4.7 %).
+//
+// Roles of a CTA (640 threads), coupled by barriers alone, so that set-up, loads and first scores of the next tile overlap the end of
 // the present one:
-//   warps 0-11  softmax, three warpgroups that take the steps of 128 keys in turn (thread = row = TMEM lane)
-//   warp  12    TMA producer of K
-//   warp  13    MMA issuer (CTA 0): S = Q K^T, O += P V (P in TMEM, V with its rows along d); CTA 1: passes on that its Q is there
-//   warp  14    producer of V
-//   warp  15    planner: the next tile and its Q
-// TMEM (512 columns): three score tiles of 128 columns, the weights (bf16 pairs) over the first 64 of each, and O.  The waits are
-// those of the prefill kernel (attn_prefill_tc.cuh): the issuer never waits for a tile that it has not begun while a product of an
-// earlier one is still to be issued.
+//   warps 0-15  softmax, two teams of two warpgroups that take the steps of 128 keys in turn; a row's keys are shared by two threads
+//   warp  16    TMA producer of K
+//   warp  17    MMA issuer (CTA 0): S = Q K^T, O += P V (P in TMEM, V with its rows along d); CTA 1: passes on that its Q is there
+//   warp  18    producer of V
+//   warp  19    planner: the next tile and its Q
+// TMEM (512 columns): three score tiles of 128 columns, each with the weights (bf16 pairs) over the first 32 of either half, and O.  The
+// waits are those of the prefill kernel (attn_prefill_tc.cuh): the issuer never waits for a tile that it has not begun while a product of
+// an earlier one is still to be issued.  What bounds a step is the chain scores -> weights -> product of its score tile: 512 + 512 cycles of
+// tensor core, about 300 between the last of them and the softmax, 2000 to 2200 of softmax, shared with the other team's.  (Three warpgroups with a
+// row each per thread: 2400 of softmax, chains 10 % longer.)
 //
 // Tiles are dealt longest first and back and forth over the pairs of CTAs.  Every planner works the order out for itself from cu_q and
 // cu_k, level by level of the number of steps: no list in memory, no counter, one launch, and nothing to be cleared before it.
@@ -39,22 +44,25 @@ constexpr int kPromptTeams = 2;                               // softmax teams, 
 constexpr int kPromptThreads = (2 * kPromptTeams + 1) * 128;
 constexpr int kPromptBufs = 3;                                // score tiles in TMEM
 constexpr int kPromptRefSlots = 4;
-constexpr float kPromptGrow = 40.f;                           // a reference moves when a score is more than 2^40 above it
+constexpr float kPromptBig = 0x1p40f;                         // a reference moves when a half step's weights sum up to more
 constexpr int kPromptOddSlots = 8;                            // more than tiles whose V can be under way at once (a step each)
 __host__ __device__ constexpr int prompt_k_stages(int D) { return D == 64 ? 6 : 3; }   // steps whose K, V are under way
 __host__ __device__ constexpr int prompt_v_stages(int D) { return D == 64 ? 6 : 3; }
 static_assert(prompt_v_stages(64) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
 
-// 2^x on the FMA pipe (every 8th exponential of steps without a mask; MUFU gives 16 a cycle and is the busier pipe): 2^f on
-// [-0.5, 0.5] by a minimax polynomial of degree 4 (relative error 2.6e-6), n through a multiplication, so that what is no number stays
-// one.  x is clamped at -125: a weight that would vanish is 2^-125 beside a largest one of at least 1/2.
-__device__ __forceinline__ float poly_exp2(float x) {
-    float xc;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(xc) : "f"(x), "f"(-125.f));
-    const float xr = xc + 12582912.f;                         // 1.5 * 2^23: the low mantissa bits hold n = round(x)
-    const float f = xc - (xr - 12582912.f);
-    const float p = fmaf(fmaf(fmaf(fmaf(0.0095701f, f, 0.05591786f), f, 0.24024745f), f, 0.69312181f), f, 0.99999926f);
-    return p * __uint_as_float((__float_as_uint(xr) << 23) + 0x3f800000u);
+// q.k of a row of a Q tile in shared memory ([panel of 64 d][row], 128-byte swizzle) and a key in global memory.
+template <int D>
+__device__ __noinline__ float prompt_dot(const unsigned char* q, int row, const __nv_bfloat16* key) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < D / 8; ++c) {
+        const uint4 a = *reinterpret_cast<const uint4*>(q + (c >> 3) * (128 * 128) + sw128(row, c & 7)), b = *reinterpret_cast<const uint4*>(key + c * 8);
+        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sum = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum));
+    }
+    return sum;
 }
 
 // What one call works on.
@@ -65,8 +73,8 @@ struct PromptGeom {
     int T;                      // tokens of a CTA: 128 / G
     FastDiv div_w, div_g, div_kv;   // by 2 T, G, Hkv
     float scale_log2;
-    const __nv_bfloat16* v;     // for values that are no numbers
-    long long v_ts, v_hs;
+    const __nv_bfloat16 *k, *v; // for scores that leave the range of a step's reference, values that are no numbers
+    long long k_ts, k_hs, v_ts, v_hs;
 };
 
 struct PromptTile {
@@ -512,25 +520,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     if (!tc::mbar_wait(&sm.first_done[k & 1][quad], (k >> 1) & 1, abort_flag)) ok = false;
                     m_ref = sm.first_ref[k & 1][row];
                 }
-                // ---- weights, 32 keys at a time over the scores.  The reference stays what it is unless a score is 2^kPromptGrow above it;
-                // then it moves up, and the weights before follow further down (rc: the reference of a chunk).
-                float ref = m_ref, rc0 = ref;
-                unsigned long long add2 = pack_f32x2(-ref, -ref), psA = 0ull, psB = 0ull;
+                // ---- weights, 32 keys at a time over the scores
+                const float ref = m_ref;
+                const unsigned long long add2 = pack_f32x2(-ref, -ref);
+                unsigned long long psA = 0ull, psB = 0ull;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     uint32_t s[32], pk[16];
                     tc::tmem_ld_32x32(s_addr + c * 32, s);
                     tc::tmem_wait_ld_for(s);
                     if (masked) hide(s, c);
-                    const float over = fmaf(largest(s), scale_log2, -ref);
-                    if (__any_sync(0xffffffffu, over > kPromptGrow)) {
-                        const float up = over > kPromptGrow ? ceilf(over) : 0.f, f = fast_exp2(-up);
-                        ref += up;
-                        add2 = pack_f32x2(-ref, -ref);
-                        psA = mul_f32x2(psA, pack_f32x2(f, f));
-                        psB = mul_f32x2(psB, pack_f32x2(f, f));
-                    }
-                    if (c == 0) rc0 = ref;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const unsigned long long x01 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), scale2, add2);
@@ -555,22 +554,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 if (gs > 0 && !tc::mbar_wait(&sm.ref_done[(gs - 1) & (kPromptRefSlots - 1)][quad], ((gs - 1) / kPromptRefSlots) & 1, abort_flag)) ok = false;
                 if (j > 0) m_prev = sm.ref[(gs - 1) & (kPromptRefSlots - 1)][row];
                 float m_new = m_prev;
-                if (pair_any(rc0 != m_prev || ref != m_prev)) {
-                    // rare: the halves' references, or the one before, differ (by powers of two: nothing is rounded)
-                    sm.other_ref[team][half][row] = ref;
+                const bool over = tok < t.n_tok && !(l_step <= kPromptBig);
+                if (pair_any(over || ref != m_prev)) {
+                    // rare: the reference of one half has to move, or that of the step before has (by powers of two: nothing is rounded)
+                    const bool lost = over && !(l_step < 0x1p126f);   // (a weight near 2^128 is one of infinity in bf16)
+                    const unsigned char* q_tile = reinterpret_cast<const unsigned char*>(&sm.q[slot][0][0][0]);   // (of this tile until plan_empty)
+                    const int key0 = j * 128 + half * 64, n_keys = lost ? min(last + 1 - key0, 64) : 0;
+                    const __nv_bfloat16* keys = g.k + (long long)(t.k0 + key0) * g.k_ts + t.gk * g.k_hs;
+                    float mine = ref;
+                    if (over && !lost) mine += ceilf(log2f(l_step));
+                    for (int i = 0; i < n_keys; ++i) mine = fmaxf(mine, ceilf(prompt_dot<D>(q_tile, row, keys + i * g.k_ts) * scale_log2));
+                    sm.other_ref[team][half][row] = mine;
                     pair_sync();
-                    m_new = fmaxf(m_prev, fmaxf(ref, sm.other_ref[team][half ^ 1][row]));
-                    l_step *= fast_exp2(ref - m_new);
+                    m_new = fmaxf(m_prev, fmaxf(mine, sm.other_ref[team][half ^ 1][row]));
+                    const float f = fast_exp2(ref - m_new);
+                    l_step = lost ? 0.f : l_step * f;
                     l_sum *= fast_exp2(m_ref - m_new);
                     tc::tmem_wait_st();
 #pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
-                        const float f = fast_exp2((c < 2 ? rc0 : ref) - m_new);
                         uint32_t w[8];
                         tc::tmem_ld_32x8(s_addr + c * 8, w);
                         tc::tmem_wait_ld();
+                        if (lost) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
+                            for (int e = 0; e < 8; ++e) {
+                                float p[2];
+#pragma unroll
+                                for (int y = 0; y < 2; ++y) {
+                                    const int i = c * 16 + 2 * e + y;
+                                    p[y] = i < n_keys ? fast_exp2(fmaf(prompt_dot<D>(q_tile, row, keys + i * g.k_ts), scale_log2, -m_new)) : 0.f;
+                                    l_step += p[y];
+                                }
+                                w[e] = pack_bf16x2(p[0], p[1]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
+                        }
+                        __syncwarp();
                         tc::tmem_st_32x8(s_addr + c * 8, w);
                     }
                     if (j > 0 && __any_sync(0xffffffffu, m_new != m_prev)) {

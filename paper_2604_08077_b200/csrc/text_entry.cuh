@@ -183,6 +183,9 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_p
     g.div_g.init(g.G);
     g.div_kv.init(g.Hkv);
     g.scale_log2 = text_scale(h) * 1.4426950408889634f;
+    g.k = rk.p;
+    g.k_ts = rk.ts;
+    g.k_hs = rk.hs;
     g.v = rv.p;
     g.v_ts = rv.ts;
     g.v_hs = rv.hs;
