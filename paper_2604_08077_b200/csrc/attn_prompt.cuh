@@ -83,6 +83,7 @@ struct PromptTile {
     int last0;                  // last key that this CTA's first token sees (-1 and less: none)
     int gk;
     int n_steps, first_masked;  // steps of 128 keys; from this one on rows are masked
+    int part;                   // number of the part of a tile whose keys are cut, -1: a whole tile
 };
 
 // A sequence as a planner sees it; one that leaves the tensors has no tiles.
@@ -103,6 +104,110 @@ struct PromptSeq {
     __device__ __forceinline__ int tiles_up_to(const PromptGeom& g, int x) const {
         return x >= nk ? nt : x <= off ? 0 : min(g.div_w.div(x - off), nt);
     }
+};
+
+// Few tiles over many keys (a turn that continues a long conversation) would leave most pairs of CTAs without work: a tile whose steps are
+// 1.5 times and more what a pair has to do on average (`unit`, no less than kPromptMinUnit) is cut into parts of about that.  Each part
+// leaves its outputs, references and sums, and prompt_join_kernel puts them together.  There are at most 4/3 as many as pairs.
+constexpr int kPromptPairs = 74, kPromptMinUnit = 8;
+constexpr int kPromptParts = 100;
+// Rows of the cut tiles' parts: outputs [part][CTA][128][D], then (reference, sum) [part][CTA][128]
+__host__ __device__ constexpr size_t prompt_partial_bytes(int D) { return (size_t)kPromptParts * 256 * (D + 2) * sizeof(float); }
+// Could a call have tiles to cut?  (If not, there is nothing to join either: 36.1 against 37.9 us for 4301 tokens in 5 prompts, 16 heads of 64.)  More
+// tiles than 4 a pair: no one is long enough to matter.  Whole prompts: the n / W tiles of a prompt of n tokens, W to a tile, average half
+// of its n / 128 steps; that is 1.5 times what a pair has to do only up to n = 99 W / Hkv, and no tile of less than 12 steps is cut.
+inline bool prompt_may_cut(long long most_tiles, int n_k, bool whole, int W, int Hkv) {
+    return most_tiles <= 4 * kPromptPairs && n_k > 128 * 3 * kPromptMinUnit / 2 && (!whole || W > 16 * Hkv);
+}
+
+// The order of the items (tiles, or parts of them): levels from many steps to few, sequences in order, tiles, kv heads, parts.  A warp walks
+// it, with 32 sequences in its lanes.  Parts come first: an item's number is its part's.
+struct PromptWalk {
+    int level, unit;                                          // unit 0: nothing is cut
+    int below;                                                // most steps of a tile of fewer than `level`, among the sequences seen so far
+    int chunk, base;                                          // number of the first item of (level, chunk)
+    int held;                                                 // chunk of `mine`, this lane's sequence
+    PromptSeq mine;
+    // what find() found
+    PromptSeq seq;
+    int tile, gk, part, parts;
+
+    // false: a sequence leaves the tensors
+    __device__ __forceinline__ bool begin(const PromptGeom& g, bool cut, int n_pairs, int lane) {
+        bool fine = true;
+        long long steps = 0;                                  // at least as many as there are
+        level = chunk = base = below = 0;
+        for (held = 0; held * 32 < g.batch; ++held) {
+            mine.nt = 0;
+            if (held * 32 + lane < g.batch) {
+                fine = mine.load(g, held * 32 + lane) && fine;
+                if (mine.nt > 0) {
+                    level = max(level, max(1, (mine.nk + 127) >> 7));
+                    steps += (long long)mine.nt * (max(mine.off, 0) / 128 + 2) + (long long)g.T * mine.nt * (mine.nt + 1) / 128;
+                }
+            }
+        }
+        --held;
+        level = (int)__reduce_max_sync(0xffffffffu, (unsigned)level);
+        unit = 0;
+        if (cut) {
+#pragma unroll
+            for (int x = 16; x > 0; x >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, x);
+            unit = (int)max((steps * g.Hkv + n_pairs - 1) / n_pairs, (long long)kPromptMinUnit);
+        }
+        return fine;
+    }
+    __device__ __forceinline__ int parts_of(int steps) const { return unit > 0 ? max((2 * steps + unit) / (2 * unit), 1) : 1; }
+    // item `number`, which is no smaller than the one before; false: there are not so many (of cut tiles)
+    __device__ __forceinline__ bool find(const PromptGeom& g, int number, int lane, bool cut_only = false) {
+        while (level > 0) {
+            parts = parts_of(level);
+            if (cut_only && parts == 1) return false;
+            if (held != chunk) {                              // (up to 32 sequences: never)
+                held = chunk;
+                mine.nt = 0;
+                if (chunk * 32 + lane < g.batch) mine.load(g, chunk * 32 + lane);
+            }
+            int first = 0, n = 0;
+            if (mine.nt > 0) {
+                first = level == 1 ? 0 : mine.tiles_up_to(g, 128 * (level - 1));
+                n = (mine.tiles_up_to(g, 128 * level) - first) * g.Hkv * parts;
+            }
+            int upto = n;
+#pragma unroll
+            for (int x = 1; x < 32; x <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, upto, x);
+                if (lane >= x) upto += y;
+            }
+            const int total = __shfl_sync(0xffffffffu, upto, 31);
+            if (number < base + total) {
+                const int who = __ffs(__ballot_sync(0xffffffffu, base + upto > number)) - 1;
+                int i = __shfl_sync(0xffffffffu, number - base - (upto - n), who);
+                seq.q0 = __shfl_sync(0xffffffffu, mine.q0, who);
+                seq.k0 = __shfl_sync(0xffffffffu, mine.k0, who);
+                seq.nq = __shfl_sync(0xffffffffu, mine.nq, who);
+                seq.nk = __shfl_sync(0xffffffffu, mine.nk, who);
+                seq.off = __shfl_sync(0xffffffffu, mine.off, who);
+                part = i % parts;
+                i /= parts;
+                g.div_kv.divmod(i, tile, gk);
+                tile += __shfl_sync(0xffffffffu, first, who);
+                return true;
+            }
+            base += total;
+            // the next level is that of the longest tile left: levels without a tile are passed over
+            if (first > 0) below = max(below, max((min(mine.off + 2 * g.T * first, mine.nk) + 127) >> 7, 1));
+            if (++chunk * 32 >= g.batch) {
+                chunk = 0;
+                level = min((int)__reduce_max_sync(0xffffffffu, (unsigned)below), level - 1);   // (down in any case: the walk ends)
+                below = 0;
+            }
+        }
+        return false;
+    }
+    // first token of CTA `rank` of the tile, and how many it has
+    __device__ __forceinline__ int first_token(const PromptGeom& g, int rank) const { return (2 * tile + rank) * g.T; }
+    __device__ __forceinline__ int tokens(const PromptGeom& g, int rank) const { return min(max(seq.nq - first_token(g, rank), 0), g.T); }
 };
 
 template <int D>
@@ -126,7 +231,7 @@ struct PromptSmem {
 template <int D>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) attn_prompt_kernel(
     PromptGeom g, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-    __nv_bfloat16* out, float* lse, int32_t* status) {
+    __nv_bfloat16* out, float* lse, float* partial, int32_t* status) {
     extern __shared__ unsigned char prompt_smem_raw[];
     PromptSmem<D>& sm = *reinterpret_cast<PromptSmem<D>*>((reinterpret_cast<uintptr_t>(prompt_smem_raw) + 1023) & ~(uintptr_t)1023);
     constexpr int kPanels = D / 64, kQKSteps = D / 16, kKStages = prompt_k_stages(D), kVStages = prompt_v_stages(D);
@@ -141,7 +246,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     const int rank = (int)(blockIdx.x & 1u), n_pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
 
     // ---------------------------------------------------------------- set-up
-    launch_dependents();
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&sm.q_full[i], 1);
@@ -181,6 +285,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     }
     __syncwarp();
     wait_for_previous_kernel();
+    launch_dependents();                                      // (after the wait: the next kernel reads cu_q and cu_k before its own)
     // (not before the wait: a CTA of the previous kernel that is still to allocate would wait for this one)
     if (warp == kMmaWarp) tc::tmem_alloc_pair<512>(&sm.tmem_base);
     tc::tc_fence_before_sync();
@@ -191,68 +296,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
 
     if (warp == kPlanWarp) {
         // ------------------------------------------------------------ planner
-        const int W = 2 * g.T;
-        // the most steps of a tile; sequences that leave the tensors are reported
-        int level = 0;
-        for (int b0 = 0; b0 < g.batch; b0 += 32) {
-            PromptSeq s;
-            bool bad = false;
-            if (b0 + lane < g.batch) {
-                bad = !s.load(g, b0 + lane);
-                if (s.nt > 0) level = max(level, max(1, (s.nk + 127) >> 7));
-            }
-            if (bad && blockIdx.x == 0 && status != nullptr) atomicExch(status, 1);
-        }
-        level = (int)__reduce_max_sync(0xffffffffu, (unsigned)level);
-        int chunk = 0, base = 0;                              // number of the first item of (level, chunk)
+        PromptWalk w;
+        if (!w.begin(g, partial != nullptr, n_pairs, lane) && blockIdx.x == 0 && status != nullptr) atomicExch(status, 1);
         for (int k = 0;; ++k) {
             const int slot = k & 1;
-            const int rank_of = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
             if (!tc::mbar_wait(&sm.plan_empty[slot], ((k >> 1) & 1) ^ 1u, abort_flag)) break;
-            // ---- item `rank_of`: levels from many steps to few, sequences in order, tiles, kv heads
-            bool found = false;
+            const int number = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
+            const bool found = w.find(g, number, lane);
             PromptTile t;
-            while (level > 0) {
-                PromptSeq s;
-                int first = 0, n = 0;
-                const int b = chunk * 32 + lane;
-                if (b < g.batch) {
-                    s.load(g, b);
-                    first = level == 1 ? 0 : s.tiles_up_to(g, 128 * (level - 1));
-                    n = (s.tiles_up_to(g, 128 * level) - first) * g.Hkv;
-                }
-                int upto = n;
-#pragma unroll
-                for (int x = 1; x < 32; x <<= 1) {
-                    const int y = __shfl_up_sync(0xffffffffu, upto, x);
-                    if (lane >= x) upto += y;
-                }
-                const int total = __shfl_sync(0xffffffffu, upto, 31);
-                if (rank_of < base + total) {
-                    const int who = __ffs(__ballot_sync(0xffffffffu, base + upto > rank_of)) - 1;
-                    const int mine = rank_of - base - (upto - n);      // the owner's own count
-                    int tt, gk;
-                    g.div_kv.divmod(max(mine, 0), tt, gk);
-                    tt += first;
-                    const int tok = tt * W + rank * g.T, see = s.off + tt * W;   // see: the last key of the pair's first token
-                    t.q0 = s.q0 + tok;
-                    t.n_tok = min(max(s.nq - tok, 0), g.T);
-                    t.k0 = s.k0;
-                    t.last0 = s.off + tok;
-                    t.gk = gk;
-                    t.n_steps = level;
-                    t.first_masked = max(see + 1, 0) >> 7;
-                    if (lane == who) sm.tile[slot] = t;
-                    t.q0 = __shfl_sync(0xffffffffu, t.q0, who);
-                    t.gk = __shfl_sync(0xffffffffu, t.gk, who);
-                    found = true;
-                    break;
-                }
-                base += total;
-                if (++chunk * 32 >= g.batch) {
-                    chunk = 0;
-                    --level;
-                }
+            if (found) {
+                const int tok = w.first_token(g, rank), begin = w.part * w.level / w.parts;
+                t.q0 = w.seq.q0 + tok;
+                t.n_tok = w.tokens(g, rank);
+                t.k0 = w.seq.k0 + begin * 128;                // a part counts its keys from its own first one
+                t.last0 = w.seq.off + tok - begin * 128;
+                t.gk = w.gk;
+                t.n_steps = (w.part + 1) * w.level / w.parts - begin;
+                t.first_masked = max((max(w.seq.off + w.first_token(g, 0) + 1, 0) >> 7) - begin, 0);
+                t.part = w.parts > 1 ? number : -1;
+                if (lane == 0) sm.tile[slot] = t;
             }
             if (!found) {
                 if (lane == 0) {
@@ -650,7 +712,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 const float inv = l_fin != 0.f ? 1.f / l_fin : 0.f;
                 const bool mine = tok < t.n_tok;              // (the tile's last rows may be none, tokens behind the sequence not its own)
                 const long long at = (long long)(t.q0 + tok) * g.Hq + t.gk * g.G + head;
-                if (mine && half == 0 && lse != nullptr) lse[at] = (m_ref + log2f(l_fin)) * 0.6931471805599453f;
+                float* part_o = nullptr;                      // this thread's outputs of a part
+                if (t.part >= 0) {
+                    const size_t part_row = ((size_t)t.part * 2 + rank) * 128 + row;
+                    part_o = partial + part_row * D + half * (D / 2);
+                    if (half == 0) reinterpret_cast<float2*>(partial + (size_t)kPromptParts * 256 * D)[part_row] = make_float2(m_ref, l_fin);
+                } else if (mine && half == 0 && lse != nullptr) lse[at] = (m_ref + log2f(l_fin)) * 0.6931471805599453f;
                 if (k > 0 && !tc::mbar_wait(&sm.out_free, (k - 1) & 1, abort_flag)) ok = false;
                 if (!tc::mbar_wait(&sm.o_full, k & 1, abort_flag)) ok = false;
                 tc::tc_fence_after_sync();
@@ -665,6 +732,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                         tc::tc_fence_before_sync();
                         __syncwarp();
                         if (lane == 0) tc::mbar_arrive_cluster(o_free_bar);
+                    }
+                    if (part_o != nullptr) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(part_o + c * 32 + e * 4) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        continue;
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -682,12 +754,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                         const __nv_bfloat16* vr = g.v + (long long)(t.k0 + key) * g.v_ts + t.gk * g.v_hs + half * (D / 2);
                         for (int d = 0; d < D / 2; ++d) {
                             const float x = __bfloat162float(vr[d]);
-                            if (!(fabsf(x) < INFINITY)) o[d] = __float2bfloat16(__bfloat162float(o[d]) + x);
+                            if (fabsf(x) < INFINITY) continue;
+                            if (part_o != nullptr) part_o[d] += x;
+                            else o[d] = __float2bfloat16(__bfloat162float(o[d]) + x);
                         }
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-                if (mine) asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(out + at * D + half * (D / 2)), "r"(smem_u32(srow)), "n"(D) : "memory");
+                if (mine && part_o == nullptr) asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(out + at * D + half * (D / 2)), "r"(smem_u32(srow)), "n"(D) : "memory");
                 asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
                 out_pending = true;
                 pair_sync();                                  // other_l has been read
@@ -702,6 +776,63 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     cluster_sync();                                           // nothing of the other CTA reaches this one any more
     if (tid == 0 && sm.abort_flag && status != nullptr) atomicExch(status, 6);   // a bounded wait expired
     if (warp == kMmaWarp) tc::tmem_dealloc_pair<512>(tbase);
+}
+
+// Puts the parts of cut tiles together: grid (kPromptParts, 8), CTA (i, y) 32 of the 256 rows of the tile whose first part is item i.
+constexpr int kPromptJoinThreads = 256;
+
+template <int D>
+__global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptGeom g, int n_pairs, const float* partial, __nv_bfloat16* out, float* lse) {
+    constexpr int kLanes = D / 4, kRows = 32 / kLanes;        // threads of a row, rows of a warp
+    __shared__ PromptWalk found;
+    __shared__ int mine;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (warp == 0) {
+        PromptWalk w;
+        w.begin(g, true, n_pairs, lane);
+        const bool x = w.find(g, blockIdx.x, lane, true) && w.part == 0;
+        if (lane == 0) {
+            found = w;
+            mine = x;
+        }
+    }
+    __syncthreads();
+    launch_dependents();
+    wait_for_previous_kernel();
+    if (!mine) return;
+    const PromptWalk& w = found;
+    const float2* stats = reinterpret_cast<const float2*>(partial + (size_t)kPromptParts * 256 * D);
+    const int d4 = lane % kLanes;
+    for (int r = warp * kRows + lane / kLanes; r < 32; r += kRows * (kPromptJoinThreads / 32)) {
+        const int row = blockIdx.y * 32 + r, rank = row >> 7;
+        int tok, head;
+        g.div_g.divmod(row & 127, tok, head);
+        if (tok >= w.tokens(g, rank)) continue;
+        float m = -INFINITY;
+        for (int p = 0; p < w.parts; ++p) {
+            const float2 s = stats[(size_t)(blockIdx.x + p) * 256 + row];
+            if (s.y != 0.f) m = fmaxf(m, s.x);                // (0: the row sees none of the part's keys)
+        }
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float l = 0.f;
+#pragma unroll 4
+        for (int p = 0; p < w.parts; ++p) {
+            const size_t at = (size_t)(blockIdx.x + p) * 256 + row;
+            const float2 s = stats[at];
+            const float4 o = *reinterpret_cast<const float4*>(partial + at * D + 4 * d4);
+            if (s.y == 0.f) continue;
+            const float f = fast_exp2(s.x - m);
+            l = fmaf(s.y, f, l);
+            acc.x = fmaf(o.x, f, acc.x);
+            acc.y = fmaf(o.y, f, acc.y);
+            acc.z = fmaf(o.z, f, acc.z);
+            acc.w = fmaf(o.w, f, acc.w);
+        }
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+        const long long at = (long long)(w.seq.q0 + w.first_token(g, rank) + tok) * g.Hq + w.gk * g.G + head;
+        *reinterpret_cast<uint2*>(out + at * D + 4 * d4) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (d4 == 0 && lse != nullptr) lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    }
 }
 
 }  // namespace adaspark

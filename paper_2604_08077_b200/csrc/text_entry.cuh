@@ -146,7 +146,9 @@ adaspark_status_t paged_rows_impl(adaspark_attn* h, const char* who, const adasp
 extern "C" {
 
 int64_t adaspark_attn_text_workspace_bytes(const adaspark_attn_t* h) {
-    return h ? (int64_t)align_up(paged_partial_bytes(h->cfg.head_dim, h->cfg.n_q_heads / h->cfg.n_kv_heads)) : 0;
+    if (!h) return 0;
+    const size_t decode = paged_partial_bytes(h->cfg.head_dim, h->cfg.n_q_heads / h->cfg.n_kv_heads), prompt = prompt_partial_bytes(h->cfg.head_dim);
+    return (int64_t)align_up(decode > prompt ? decode : prompt);
 }
 
 adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_prompt_t* c, void* cuda_stream) {
@@ -196,13 +198,20 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_p
         return fail(h, ADASPARK_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
     // a pair of CTAs per tile, at most as many as there are SMs: 2 T tokens a tile, at most one tile of each sequence not full
     const long long most = ((long long)n_q / (2 * g.T) + batch) * g.Hkv;
-    const int pairs = (int)(most < h->sm_count / 2 ? most : h->sm_count / 2);
+    int pairs = h->sm_count / 2 < kPromptPairs ? h->sm_count / 2 : kPromptPairs;
+    const bool cut = prompt_may_cut(most, n_k, c->cu_q == c->cu_k, 2 * g.T, g.Hkv);
+    float* partial = cut ? (float*)c->workspace : nullptr;
+    if (!cut && most < pairs) pairs = (int)most;
     auto launch = [&](auto d) -> adaspark_status_t {
         constexpr auto kernel = attn_prompt_kernel<d.value>;
         const size_t bytes = sizeof(PromptSmem<d.value>) + 1024;
         if (!text_smem<kernel>(h, bytes, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
-        launch_kernel(true, kernel, dim3(2 * pairs), dim3(kPromptThreads), bytes, (cudaStream_t)cuda_stream, g, tmQ, tmK, tmV, (__nv_bfloat16*)c->out, c->lse, c->status);
-        return launch_ok(h, "attn_prompt_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+        cudaStream_t st = (cudaStream_t)cuda_stream;
+        launch_kernel(true, kernel, dim3(2 * pairs), dim3(kPromptThreads), bytes, st, g, tmQ, tmK, tmV, (__nv_bfloat16*)c->out, c->lse, partial, c->status);
+        if (!launch_ok(h, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
+        if (!cut) return ADASPARK_OK;
+        launch_kernel(true, prompt_join_kernel<d.value>, dim3(kPromptParts, 8), dim3(kPromptJoinThreads), 0, st, g, pairs, (const float*)partial, (__nv_bfloat16*)c->out, c->lse);
+        return launch_ok(h, "prompt_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
     };
     return D == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>());
 }

@@ -45,6 +45,26 @@ def test_prompts_that_continue_or_see_too_little(Hq, Hkv, D, new, total):
     check(Hq, Hkv, D, draw(4, sum(new), Hq, D), draw(5, sum(total), Hkv, D), draw(6, sum(total), Hkv, D), tu.cumulative(new), tu.cumulative(total))
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 4, 64), (28, 4, 128), (16, 1, 128), (5, 1, 64)])
+@pytest.mark.parametrize("new,total", [([1], [5000]), ([40], [9000]), ([130, 1, 3, 0], [4100, 7000, 3, 900]), ([256, 17], [8192, 4113]), ([2, 2, 2, 2], [2500, 30, 2501, 1])])
+def test_few_rows_over_many_keys(Hq, Hkv, D, new, total):
+    """Tiles whose keys are cut over the chip, beside some that are not."""
+    check(Hq, Hkv, D, draw(70, sum(new), Hq, D), draw(71, sum(total), Hkv, D), draw(72, sum(total), Hkv, D), tu.cumulative(new), tu.cumulative(total))
+
+
+def test_cut_keys_sharp_and_with_values_that_are_no_numbers():
+    new, total, Hq, Hkv, D = [50], [6000], 14, 2, 128
+    q, k, v = draw(73, 50, Hq, D, 8.0), draw(74, 6000, Hkv, D), draw(75, 6000, Hkv, D)
+    cu_q, cu_k = tu.cumulative(new), tu.cumulative(total)
+    clean, _ = check(Hq, Hkv, D, q, k, v, cu_q, cu_k)
+    v[6000 - 20, 0, 5] = math.inf                            # row 29 is the last one that does not see it
+    out, _ = tu.engine(Hq, Hkv, D).prompt(q, k, v, cu_q, cu_k)
+    assert torch.equal(out[:30], clean[:30]) and torch.equal(out[:, 7:], clean[:, 7:])
+    assert not torch.isfinite(out[30:, :7, 5]).any()
+    others = [i for i in range(D) if i != 5]
+    assert torch.equal(out[..., others], clean[..., others])
+
+
 def test_no_keys_at_all():
     k = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
     out, lse = check(4, 2, 64, draw(7, 6, 4, 64), k, k, tu.cumulative([2, 4]), tu.cumulative([0, 0]))
