@@ -778,8 +778,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     if (warp == kMmaWarp) tc::tmem_dealloc_pair<512>(tbase);
 }
 
-// Puts the parts of cut tiles together: grid (kPromptParts, 8), CTA (i, y) 32 of the 256 rows of the tile whose first part is item i.
-constexpr int kPromptJoinThreads = 256;
+// Puts the parts of cut tiles together: grid (kPromptParts, 256 / kPromptJoinRows), CTA (i, y) kPromptJoinRows rows of the tile whose first
+// part is item i.
+constexpr int kPromptJoinThreads = 256, kPromptJoinRows = 16;
 
 template <int D>
 __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptGeom g, int n_pairs, const float* partial, __nv_bfloat16* out, float* lse) {
@@ -803,30 +804,41 @@ __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptG
     const PromptWalk& w = found;
     const float2* stats = reinterpret_cast<const float2*>(partial + (size_t)kPromptParts * 256 * D);
     const int d4 = lane % kLanes;
-    for (int r = warp * kRows + lane / kLanes; r < 32; r += kRows * (kPromptJoinThreads / 32)) {
-        const int row = blockIdx.y * 32 + r, rank = row >> 7;
+    for (int r = warp * kRows + lane / kLanes; r < kPromptJoinRows; r += kRows * (kPromptJoinThreads / 32)) {
+        const int row = blockIdx.y * kPromptJoinRows + r, rank = row >> 7;
         int tok, head;
         g.div_g.divmod(row & 127, tok, head);
         if (tok >= w.tokens(g, rank)) continue;
-        float m = -INFINITY;
-        for (int p = 0; p < w.parts; ++p) {
-            const float2 s = stats[(size_t)(blockIdx.x + p) * 256 + row];
-            if (s.y != 0.f) m = fmaxf(m, s.x);                // (0: the row sees none of the part's keys)
-        }
+        // statistics and outputs of four parts are asked for together; more are joined to what these gave
+        float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float l = 0.f;
-#pragma unroll 4
-        for (int p = 0; p < w.parts; ++p) {
-            const size_t at = (size_t)(blockIdx.x + p) * 256 + row;
-            const float2 s = stats[at];
-            const float4 o = *reinterpret_cast<const float4*>(partial + at * D + 4 * d4);
-            if (s.y == 0.f) continue;
-            const float f = fast_exp2(s.x - m);
-            l = fmaf(s.y, f, l);
-            acc.x = fmaf(o.x, f, acc.x);
-            acc.y = fmaf(o.y, f, acc.y);
-            acc.z = fmaf(o.z, f, acc.z);
-            acc.w = fmaf(o.w, f, acc.w);
+        for (int p0 = 0; p0 < w.parts; p0 += 4) {
+            float2 s[4];
+            float4 o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const size_t at = (size_t)(blockIdx.x + min(p0 + i, w.parts - 1)) * 256 + row;
+                s[i] = stats[at];
+                o[i] = *reinterpret_cast<const float4*>(partial + at * D + 4 * d4);
+            }
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (p0 + i < w.parts && s[i].y != 0.f) top = fmaxf(top, s[i].x);      // (0: the row sees none of the part's keys)
+            const float c = l != 0.f ? fast_exp2(m - top) : 0.f;
+            l *= c;
+            acc.x *= c; acc.y *= c; acc.z *= c; acc.w *= c;
+            m = top;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (p0 + i >= w.parts || s[i].y == 0.f) continue;
+                const float f = fast_exp2(s[i].x - m);
+                l = fmaf(s[i].y, f, l);
+                acc.x = fmaf(o[i].x, f, acc.x);
+                acc.y = fmaf(o[i].y, f, acc.y);
+                acc.z = fmaf(o[i].z, f, acc.z);
+                acc.w = fmaf(o[i].w, f, acc.w);
+            }
         }
         const float inv = l != 0.f ? 1.f / l : 0.f;
         const long long at = (long long)(w.seq.q0 + w.first_token(g, rank) + tok) * g.Hq + w.gk * g.G + head;

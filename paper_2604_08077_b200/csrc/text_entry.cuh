@@ -199,7 +199,7 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_p
     // a pair of CTAs per tile, at most as many as there are SMs: 2 T tokens a tile, at most one tile of each sequence not full
     const long long most = ((long long)n_q / (2 * g.T) + batch) * g.Hkv;
     int pairs = h->sm_count / 2 < kPromptPairs ? h->sm_count / 2 : kPromptPairs;
-    const bool cut = prompt_may_cut(most, n_k, c->cu_q == c->cu_k, 2 * g.T, g.Hkv);
+    const bool cut = prompt_may_cut(most, n_k, c->cu_q == c->cu_k || n_q == n_k, 2 * g.T, g.Hkv);
     float* partial = cut ? (float*)c->workspace : nullptr;
     if (!cut && most < pairs) pairs = (int)most;
     auto launch = [&](auto d) -> adaspark_status_t {
@@ -210,7 +210,7 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_p
         launch_kernel(true, kernel, dim3(2 * pairs), dim3(kPromptThreads), bytes, st, g, tmQ, tmK, tmV, (__nv_bfloat16*)c->out, c->lse, partial, c->status);
         if (!launch_ok(h, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
         if (!cut) return ADASPARK_OK;
-        launch_kernel(true, prompt_join_kernel<d.value>, dim3(kPromptParts, 8), dim3(kPromptJoinThreads), 0, st, g, pairs, (const float*)partial, (__nv_bfloat16*)c->out, c->lse);
+        launch_kernel(true, prompt_join_kernel<d.value>, dim3(kPromptParts, 256 / kPromptJoinRows), dim3(kPromptJoinThreads), 0, st, g, pairs, (const float*)partial, (__nv_bfloat16*)c->out, c->lse);
         return launch_ok(h, "prompt_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
     };
     return D == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>());
