@@ -17,10 +17,10 @@
 // Roles of a CTA (640 threads), coupled by barriers alone, so that set-up, loads and first scores of the next tile overlap the end of
 // the present one:
 //   warps 0-15  softmax, two teams of two warpgroups that take the steps of 128 keys in turn; a row's keys are shared by two threads
-//   warp  16    TMA producer of K
+//   warp  16    TMA producer of K; masked steps: looks for values that are no numbers (below)
 //   warp  17    MMA issuer (CTA 0): S = Q K^T, O += P V (P in TMEM, V with its rows along d); CTA 1: passes on that its Q is there
-//   warp  18    producer of V
-//   warp  19    planner: the next tile and its Q
+//   warp  18    TMA producer of V
+//   warp  19    planner: the next tiles and their Q
 // TMEM (512 columns): three score tiles of 128 columns, each with the weights (bf16 pairs) over the first 32 of either half, and O.  The
 // waits are those of the prefill kernel (attn_prefill_tc.cuh): the issuer never waits for a tile that it has not begun while a product of
 // an earlier one is still to be issued.  What bounds a step is the chain scores -> weights -> product of its score tile: 512 + 512 cycles of
@@ -42,6 +42,7 @@ namespace adaspark {
 
 constexpr int kPromptTeams = 2;                               // softmax teams, of two warpgroups each
 constexpr int kPromptThreads = (2 * kPromptTeams + 1) * 128;
+constexpr int kPromptPlans = 4;                               // tiles planned at once
 constexpr int kPromptBufs = 3;                                // score tiles in TMEM
 constexpr int kPromptRefSlots = 4;
 constexpr float kPromptBig = 0x1p40f;                         // a reference moves when a half step's weights sum up to more
@@ -50,13 +51,13 @@ __host__ __device__ constexpr int prompt_k_stages(int D) { return D == 64 ? 6 : 
 __host__ __device__ constexpr int prompt_v_stages(int D) { return D == 64 ? 6 : 3; }
 static_assert(prompt_v_stages(64) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
 
-// q.k of a row of a Q tile in shared memory ([panel of 64 d][row], 128-byte swizzle) and a key in global memory.
+// q.k of two rows in global memory
 template <int D>
-__device__ __noinline__ float prompt_dot(const unsigned char* q, int row, const __nv_bfloat16* key) {
+__device__ __noinline__ float prompt_dot(const __nv_bfloat16* q, const __nv_bfloat16* key) {
     float sum = 0.f;
 #pragma unroll 1
-    for (int c = 0; c < D / 8; ++c) {
-        const uint4 a = *reinterpret_cast<const uint4*>(q + (c >> 3) * (128 * 128) + sw128(row, c & 7)), b = *reinterpret_cast<const uint4*>(key + c * 8);
+    for (int c = 0; c < D; c += 8) {
+        const uint4 a = *reinterpret_cast<const uint4*>(q + c), b = *reinterpret_cast<const uint4*>(key + c);
         const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -73,8 +74,8 @@ struct PromptGeom {
     int T;                      // tokens of a CTA: 128 / G
     FastDiv div_w, div_g, div_kv;   // by 2 T, G, Hkv
     float scale_log2;
-    const __nv_bfloat16 *k, *v; // for scores that leave the range of a step's reference, values that are no numbers
-    long long k_ts, k_hs, v_ts, v_hs;
+    const __nv_bfloat16 *q, *k, *v; // for scores that leave the range of a step's reference, values that are no numbers
+    long long q_ts, q_hs, k_ts, k_hs, v_ts, v_hs;
 };
 
 struct PromptTile {
@@ -220,9 +221,9 @@ struct PromptSmem {
     float part_l[2][2][128], part_m[2][2][128];             // sums and reference of the team that does not finish a tile, by half
     float other_l[kPromptTeams][2][128], other_ref[kPromptTeams][2][128];   // between the halves of a row
     uint64_t q_full[2], q_peer[2], q_empty[2], k_full[prompt_k_stages(D)], k_empty[prompt_k_stages(D)], v_full[prompt_v_stages(D)], v_empty[prompt_v_stages(D)];
-    uint64_t v_raw, s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], first_done[2][4], o_full, o_free;
-    uint64_t plan_full[2], plan_empty[2], part_full[2], part_free[2], out_free;
-    PromptTile tile[2];
+    uint64_t v_raw[prompt_v_stages(D)], s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], first_done[2][4], o_full, o_free;
+    uint64_t plan_full[kPromptPlans], plan_empty[kPromptPlans], part_full[2], part_free[2], out_free;
+    PromptTile tile[kPromptPlans];
     int odd_tile[kPromptOddSlots];                            // number + 1 of a tile with masked values that are no numbers
     uint32_t tmem_base;
     int abort_flag;
@@ -251,17 +252,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             tc::mbar_init(&sm.q_full[i], 1);
             tc::mbar_init(&sm.q_peer[i], 1);
             tc::mbar_init(&sm.q_empty[i], 1);
-            tc::mbar_init(&sm.plan_full[i], 1);
-            tc::mbar_init(&sm.plan_empty[i], 3 + kPromptTeams * 8);
             tc::mbar_init(&sm.part_full[i], 8);
             tc::mbar_init(&sm.part_free[i], 8);
+        }
+        for (int i = 0; i < kPromptPlans; ++i) {
+            tc::mbar_init(&sm.plan_full[i], 1);
+            tc::mbar_init(&sm.plan_empty[i], 4 + kPromptTeams * 8);
         }
         for (int i = 0; i < kKStages; ++i) {
             tc::mbar_init(&sm.k_full[i], 1);
             tc::mbar_init(&sm.k_empty[i], 1);
         }
         for (int i = 0; i < kVStages; ++i) {
-            tc::mbar_init(&sm.v_full[i], 2);                  // the V warps of both CTAs
+            tc::mbar_init(&sm.v_full[i], 2);                  // of both CTAs
+            tc::mbar_init(&sm.v_raw[i], 1);
             tc::mbar_init(&sm.v_empty[i], 1);
         }
         for (int i = 0; i < kPromptBufs; ++i) {
@@ -273,7 +277,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         for (int i = 0; i < 2; ++i)
             for (int w = 0; w < 4; ++w) tc::mbar_init(&sm.first_done[i][w], 1);
         for (int i = 0; i < kPromptOddSlots; ++i) sm.odd_tile[i] = 0;
-        tc::mbar_init(&sm.v_raw, 1);
         tc::mbar_init(&sm.o_full, 1);
         tc::mbar_init(&sm.o_free, 16);
         tc::mbar_init(&sm.out_free, 8);
@@ -299,8 +302,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         PromptWalk w;
         if (!w.begin(g, partial != nullptr, n_pairs, lane) && blockIdx.x == 0 && status != nullptr) atomicExch(status, 1);
         for (int k = 0;; ++k) {
-            const int slot = k & 1;
-            if (!tc::mbar_wait(&sm.plan_empty[slot], ((k >> 1) & 1) ^ 1u, abort_flag)) break;
+            const int slot = k % kPromptPlans, qs = k & 1;
+            if (!tc::mbar_wait(&sm.plan_empty[slot], ((k / kPromptPlans) & 1) ^ 1u, abort_flag)) break;
             const int number = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
             const bool found = w.find(g, number, lane);
             PromptTile t;
@@ -323,65 +326,68 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 }
                 break;
             }
-            if (!tc::mbar_wait(&sm.q_empty[slot], ((k >> 1) & 1) ^ 1, abort_flag)) break;
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm.plan_full[slot]);
+            if (!tc::mbar_wait(&sm.q_empty[qs], ((k >> 1) & 1) ^ 1, abort_flag)) break;
             __syncwarp();
             if (lane == 0) {
                 // rows (token, head of the group); tokens behind the tensor read zeros, those of the next sequence are not stored
-                tc::mbar_arrive_expect_tx(&sm.q_full[slot], (uint32_t)(g.T * g.G) * D * 2);
-                for (int p = 0; p < kPanels; ++p) tc::tma_load_3d(&sm.q[slot][p][0][0], &tmQ, p * 64, t.gk * g.G, t.q0, &sm.q_full[slot]);
-                tc::mbar_arrive(&sm.plan_full[slot]);
+                tc::mbar_arrive_expect_tx(&sm.q_full[qs], (uint32_t)(g.T * g.G) * D * 2);
+                for (int p = 0; p < kPanels; ++p) tc::tma_load_3d(&sm.q[qs][p][0][0], &tmQ, p * 64, t.gk * g.G, t.q0, &sm.q_full[qs]);
             }
             __syncwarp();
         }
     } else if (warp == kKWarp) {
-        // ------------------------------------------------------------ K: CTA r fetches the keys r * 64 .. of a step
-        if (tc::elect_one()) {
-            const uint32_t bar0 = cluster_address(sm.k_full, 0);
-            int st = 0, ph = 1;
-            bool ok = true;
-            for (int k = 0; ok; ++k) {
-                const int slot = k & 1;
-                if (!(ok = tc::mbar_wait(&sm.plan_full[slot], (k >> 1) & 1, abort_flag))) break;
-                const int n_steps = sm.tile[slot].n_steps, row0 = sm.tile[slot].k0 + rank * 64, gk = sm.tile[slot].gk;
-                if (n_steps == 0) break;
-                for (int j = 0; j < n_steps; ++j) {
-                    if (!(ok = tc::mbar_wait(&sm.k_empty[st], ph, abort_flag))) break;
-                    if (rank == 0) tc::mbar_arrive_expect_tx(&sm.k_full[st], 2 * kTileBytes);
-                    for (int p = 0; p < kPanels; ++p)
-                        tc::tma_load_3d_pair(&sm.k[st][p * 64 * 64], &tmK, p * 64, gk, row0 + j * 128, bar0 + st * 8);
-                    if (++st == kKStages) { st = 0; ph ^= 1; }
+        // ------------------------------------------------------------ K: CTA r fetches the keys r * 64 .. of a step.  And masked steps:
+        // values that are no numbers.  Whichever is ready, so that neither waits for the other.
+        const uint32_t bar0 = cluster_address(sm.k_full, 0), v_bar0 = cluster_address(sm.v_full, 0);
+        const uint32_t odd0 = cluster_address(sm.odd_tile, 0), odd1 = cluster_address(sm.odd_tile, 1);
+        auto ready = [&](uint64_t* bar, uint32_t phase) -> bool { return __all_sync(0xffffffffu, tc::mbar_test(bar, phase)); };
+        struct { int k = 0, j = 0, n = 0, st = 0; bool done = false; } kp, look;      // tile, step, steps of the tile (0: not begun), stage
+        int k_ph = 1, row0 = 0, gk = 0, first_masked = 0;
+        uint32_t raw_phases = 0, idle = 0;                    // (of v_raw, a bit each)
+        uint64_t since = 0;
+        while (!kp.done || !look.done) {
+            bool moved = false;
+            if (!kp.done) {
+                const int slot = kp.k % kPromptPlans;
+                if (kp.n == 0 && ready(&sm.plan_full[slot], (kp.k / kPromptPlans) & 1)) {
+                    kp.n = sm.tile[slot].n_steps;
+                    row0 = sm.tile[slot].k0 + rank * 64;
+                    gk = sm.tile[slot].gk;
+                    kp.done = kp.n == 0;
+                    moved = true;
                 }
-                tc::mbar_arrive(&sm.plan_empty[slot]);
+                if (kp.n > 0 && ready(&sm.k_empty[kp.st], k_ph)) {
+                    if (tc::elect_one()) {
+                        if (rank == 0) tc::mbar_arrive_expect_tx(&sm.k_full[kp.st], 2 * kTileBytes);
+                        for (int p = 0; p < kPanels; ++p)
+                            tc::tma_load_3d_pair(&sm.k[kp.st][p * 64 * 64], &tmK, p * 64, gk, row0 + kp.j * 128, bar0 + kp.st * 8);
+                    }
+                    __syncwarp();
+                    if (++kp.st == kKStages) { kp.st = 0; k_ph ^= 1; }
+                    if (++kp.j == kp.n) {
+                        if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
+                        kp.j = kp.n = 0;
+                        ++kp.k;
+                    }
+                    moved = true;
+                }
             }
-        }
-    } else if (warp == kVWarp) {
-        // ------------------------------------------------------------ V: CTA r fetches half r of d of a step's 128 keys
-        const uint32_t bar0 = cluster_address(sm.v_full, 0), odd0 = cluster_address(sm.odd_tile, 0), odd1 = cluster_address(sm.odd_tile, 1);
-        int st = 0, ph = 1, raw_ph = 0;
-        bool ok = true;
-        for (int k = 0; ok; ++k) {
-            const int slot = k & 1;
-            if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k >> 1) & 1, abort_flag))) break;
-            const int n_steps = sm.tile[slot].n_steps, k0 = sm.tile[slot].k0, gk = sm.tile[slot].gk, first_masked = sm.tile[slot].first_masked;
-            if (n_steps == 0) break;
-            for (int j = 0; j < n_steps; ++j) {
-                if (!(ok = tc::mbar_wait_warp(&sm.v_empty[st], ph, abort_flag))) break;
-                unsigned char* tile = reinterpret_cast<unsigned char*>(&sm.v[st][0]);
-                if (j < first_masked) {
-                    if (tc::elect_one()) {
-                        if (rank == 0) tc::mbar_arrive_expect_tx(&sm.v_full[st], 2 * kTileBytes);
-                        else tc::mbar_arrive_cluster(bar0 + st * 8);
-                        tc::tma_load_3d_pair(tile, &tmV, rank * (D / 2), gk, k0 + j * 128, bar0 + st * 8);
-                    }
-                } else {
-                    if (tc::elect_one()) {
-                        tc::mbar_arrive_expect_tx(&sm.v_raw, kTileBytes);
-                        tc::tma_load_3d(tile, &tmV, rank * (D / 2), gk, k0 + j * 128, &sm.v_raw);
-                    }
-                    if (!(ok = tc::mbar_wait_warp(&sm.v_raw, raw_ph, abort_flag))) break;
-                    raw_ph ^= 1;
+            if (!look.done) {
+                const int slot = look.k % kPromptPlans;
+                if (look.n == 0 && ready(&sm.plan_full[slot], (look.k / kPromptPlans) & 1)) {
+                    look.n = sm.tile[slot].n_steps;
+                    first_masked = sm.tile[slot].first_masked;
+                    look.done = look.n == 0;
+                    look.j = min(first_masked, look.n);
+                    look.st = (look.st + look.j) % kVStages;
+                    moved = true;
+                }
+                if (look.n > 0 && look.j < look.n && ready(&sm.v_raw[look.st], (raw_phases >> look.st) & 1)) {
+                    raw_phases ^= 1u << look.st;
                     // exponents of all ones: adding 0x80 to (x & 0x7f80) carries into bit 15
-                    uint4* chunks = reinterpret_cast<uint4*>(tile);
+                    uint4* chunks = reinterpret_cast<uint4*>(&sm.v[look.st][0]);
                     uint32_t any = 0;
 #pragma unroll 8
                     for (int i = lane; i < (int)kTileBytes / 16; i += 32) {
@@ -399,31 +405,71 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                             chunks[i] = make_uint4(x[0], x[1], x[2], x[3]);
                         }
                         if (lane < 2)                         // (keys of other sequences among them: the rows look for themselves)
-                            asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"((lane ? odd1 : odd0) + (k % kPromptOddSlots) * 4), "r"(k + 1) : "memory");
+                            asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"((lane ? odd1 : odd0) + (look.k % kPromptOddSlots) * 4), "r"(look.k + 1) : "memory");
                     }
                     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
                         asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
-                        tc::mbar_arrive_release_cluster(bar0 + st * 8);
+                        tc::mbar_arrive_release_cluster(v_bar0 + look.st * 8);
                     }
                     __syncwarp();
+                    if (++look.st == kVStages) look.st = 0;
+                    ++look.j;
+                    moved = true;
                 }
-                if (++st == kVStages) { st = 0; ph ^= 1; }
+                if (look.n > 0 && look.j == look.n) {
+                    if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
+                    look.n = 0;
+                    ++look.k;
+                    moved = true;
+                }
             }
-            if (!ok) break;
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
+            if (moved) {
+                idle = 0;
+            } else if ((++idle & 0xff) == 0) {                // bounded, as every wait
+                const uint64_t now = tc::global_timer_ns();
+                if (idle == 0x100) since = now;
+                if (now - since > tc::kWaitLimitNs) *abort_flag = 1;
+                if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
+            }
+        }
+    } else if (warp == kVWarp) {
+        // ------------------------------------------------------------ V: CTA r fetches half r of d of a step's 128 keys
+        if (tc::elect_one()) {
+            const uint32_t bar0 = cluster_address(sm.v_full, 0);
+            int st = 0, ph = 1;
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                const int slot = k % kPromptPlans;
+                if (!(ok = tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag))) break;
+                const int n_steps = sm.tile[slot].n_steps, k0 = sm.tile[slot].k0, gk = sm.tile[slot].gk, first_masked = sm.tile[slot].first_masked;
+                if (n_steps == 0) break;
+                for (int j = 0; j < n_steps; ++j) {
+                    if (!(ok = tc::mbar_wait(&sm.v_empty[st], ph, abort_flag))) break;
+                    if (j < first_masked) {
+                        if (rank == 0) tc::mbar_arrive_expect_tx(&sm.v_full[st], 2 * kTileBytes);
+                        else tc::mbar_arrive_cluster(bar0 + st * 8);
+                        tc::tma_load_3d_pair(&sm.v[st][0], &tmV, rank * (D / 2), gk, k0 + j * 128, bar0 + st * 8);
+                    } else {                                  // K's warp looks for what is no number and says that it is there
+                        tc::mbar_arrive_expect_tx(&sm.v_raw[st], kTileBytes);
+                        tc::tma_load_3d(&sm.v[st][0], &tmV, rank * (D / 2), gk, k0 + j * 128, &sm.v_raw[st]);
+                    }
+                    if (++st == kVStages) { st = 0; ph ^= 1; }
+                }
+                tc::mbar_arrive(&sm.plan_empty[slot]);
+            }
         }
     } else if (warp == kMmaWarp && rank == 1) {
         // ------------------------------------------------------------ CTA 1: Q is there, said to the issuing warp of CTA 0
         if (lane == 0) {
             for (int k = 0;; ++k) {
-                if (!tc::mbar_wait(&sm.plan_full[k & 1], (k >> 1) & 1, abort_flag) || sm.tile[k & 1].n_steps == 0) break;
+                const int slot = k % kPromptPlans;
+                if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag) || sm.tile[slot].n_steps == 0) break;
                 if (!tc::mbar_wait(&sm.q_full[k & 1], (k >> 1) & 1, abort_flag)) break;
                 asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
                 tc::mbar_arrive_cluster(cluster_address(&sm.q_peer[k & 1], 0));
-                tc::mbar_arrive(&sm.plan_empty[k & 1]);
+                tc::mbar_arrive(&sm.plan_empty[slot]);
             }
         }
     } else if (warp == kMmaWarp) {
@@ -445,11 +491,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             auto next_scores = [&](bool must) -> bool {
                 if (s_left == 0) {
                     if (ended) return false;
-                    const int kn = ks + 1, slot = kn & 1;
+                    const int kn = ks + 1, slot = kn % kPromptPlans;
                     auto there = [&](uint64_t* bar, uint32_t phase) -> bool { return must ? (ok = tc::mbar_wait(bar, phase, abort_flag)) : tc::mbar_test(bar, phase); };
-                    if (!there(&sm.plan_full[slot], (kn >> 1) & 1)) return false;
+                    if (!there(&sm.plan_full[slot], (kn / kPromptPlans) & 1)) return false;
                     if ((ended = sm.tile[slot].n_steps == 0)) return false;
-                    if (!there(&sm.q_full[slot], (kn >> 1) & 1) || !there(&sm.q_peer[slot], (kn >> 1) & 1)) return false;
+                    if (!there(&sm.q_full[kn & 1], (kn >> 1) & 1) || !there(&sm.q_peer[kn & 1], (kn >> 1) & 1)) return false;
                     ks = kn;
                     n_steps2 = n_steps1;
                     n_steps1 = n_steps0;
@@ -526,8 +572,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         // A wait that has expired does not end the loops below at once, for the two warps of a row meet in barriers: ok says so, and the
         // loops end with the tile (further waits return quickly).
         for (int k = 0;; ++k) {
-            const int slot = k & 1;
-            if (!tc::mbar_wait(&sm.plan_full[slot], (k >> 1) & 1, abort_flag)) ok = false;
+            const int slot = k % kPromptPlans;
+            if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag)) ok = false;
             if (pair_any(!ok)) break;
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
@@ -620,12 +666,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 if (pair_any(over || ref != m_prev)) {
                     // rare: the reference of one half has to move, or that of the step before has (by powers of two: nothing is rounded)
                     const bool lost = over && !(l_step < 0x1p126f);   // (a weight near 2^128 is one of infinity in bf16)
-                    const unsigned char* q_tile = reinterpret_cast<const unsigned char*>(&sm.q[slot][0][0][0]);   // (of this tile until plan_empty)
+                    const __nv_bfloat16* q_row = g.q + (long long)(t.q0 + tok) * g.q_ts + (t.gk * g.G + head) * g.q_hs;
                     const int key0 = j * 128 + half * 64, n_keys = lost ? min(last + 1 - key0, 64) : 0;
                     const __nv_bfloat16* keys = g.k + (long long)(t.k0 + key0) * g.k_ts + t.gk * g.k_hs;
                     float mine = ref;
                     if (over && !lost) mine += ceilf(log2f(l_step));
-                    for (int i = 0; i < n_keys; ++i) mine = fmaxf(mine, ceilf(prompt_dot<D>(q_tile, row, keys + i * g.k_ts) * scale_log2));
+                    for (int i = 0; i < n_keys; ++i) mine = fmaxf(mine, ceilf(prompt_dot<D>(q_row, keys + i * g.k_ts) * scale_log2));
                     sm.other_ref[team][half][row] = mine;
                     pair_sync();
                     m_new = fmaxf(m_prev, fmaxf(mine, sm.other_ref[team][half ^ 1][row]));
@@ -645,7 +691,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
 #pragma unroll
                                 for (int y = 0; y < 2; ++y) {
                                     const int i = c * 16 + 2 * e + y;
-                                    p[y] = i < n_keys ? fast_exp2(fmaf(prompt_dot<D>(q_tile, row, keys + i * g.k_ts), scale_log2, -m_new)) : 0.f;
+                                    p[y] = i < n_keys ? fast_exp2(fmaf(prompt_dot<D>(q_row, keys + i * g.k_ts), scale_log2, -m_new)) : 0.f;
                                     l_step += p[y];
                                 }
                                 w[e] = pack_bf16x2(p[0], p[1]);

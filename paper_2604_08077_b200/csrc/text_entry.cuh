@@ -185,6 +185,9 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_p
     g.div_g.init(g.G);
     g.div_kv.init(g.Hkv);
     g.scale_log2 = text_scale(h) * 1.4426950408889634f;
+    g.q = rq.p;
+    g.q_ts = rq.ts;
+    g.q_hs = rq.hs;
     g.k = rk.p;
     g.k_ts = rk.ts;
     g.k_hs = rk.hs;
