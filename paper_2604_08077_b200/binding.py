@@ -475,6 +475,8 @@ class AdaSAttn:
 
     def _text_buffers(self):
         """(status pointer, workspace pointer, workspace bytes) of the text calls, made once."""
+        if torch.cuda.is_current_stream_capturing():
+            _refuse("the first text call of an object allocates its workspace: make one before a capture begins")
         n = adaspark_attn_text_workspace_bytes(self.handle)
         self._text_ws = torch.empty(n, dtype=torch.uint8, device=self.device)
         self._text_flag = torch.zeros(1, dtype=torch.int32, device=self.device)

@@ -218,7 +218,7 @@ def check_decode(eng, cache, table, lens, q, k_new=None, v_new=None):
 
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("append", [False, True])
-@pytest.mark.parametrize("Hq,Hkv,D,page", [(28, 4, 128, 16), (16, 1, 64, 64), (4, 4, 64, 32), (6, 2, 128, 256), (5, 1, 128, 128), (16, 2, 64, 16)])
+@pytest.mark.parametrize("Hq,Hkv,D,page", [(28, 4, 128, 16), (16, 1, 64, 64), (4, 4, 64, 32), (6, 2, 128, 256), (5, 1, 128, 128), (16, 2, 64, 16), (16, 1, 128, 64), (11, 1, 128, 32)])
 @pytest.mark.parametrize("lens", [[1], [2, 0, 1, 17], [64, 63, 65, 128, 129], [1000, 16, 0, 400]])
 def test_decode(e4m3, append, Hq, Hkv, D, page, lens):
     """Pages hold codes of every kind behind the last token (NaN among them): no row may take anything from there."""
@@ -273,6 +273,52 @@ def test_decode_many_sequences():
     filled(g, cache, table, lens)
     B = len(lens)
     check_decode(tu.engine(Hq, Hkv, D), cache, table, lens, draw(g, B, Hq, D), draw(g, B, Hkv, D), draw(g, B, Hkv, D))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_decode_one_long_sequence_among_many(e4m3):
+    """More than 32 sequences, one of them in more than 16 parts, unused slots in front and behind."""
+    g = torch.Generator().manual_seed(115)
+    Hq, Hkv, D, page = 14, 2, 128, 32
+    lens = [0, 0] + [5] * 20 + [14001] + [70] * 20 + [0]
+    table, n_pages = tu.scattered(g, [-(-n // page) for n in lens])
+    cache = make_cache(g, n_pages, Hkv, page, D, e4m3)
+    filled(g, cache, table, lens)
+    B = len(lens)
+    check_decode(tu.engine(Hq, Hkv, D), cache, table, lens, draw(g, B, Hq, D), draw(g, B, Hkv, D), draw(g, B, Hkv, D))
+
+
+def test_decode_values_that_are_no_numbers():
+    """A key that is no number makes its sequence's rows none; an infinite value reaches its own coordinate; other sequences keep theirs."""
+    g = torch.Generator().manual_seed(116)
+    Hq, Hkv, D, page, lens = 8, 2, 128, 16, [200, 90, 40]
+    table, n_pages = tu.scattered(g, [-(-n // page) for n in lens])
+    cache = make_cache(g, n_pages, Hkv, page, D, False)
+    filled(g, cache, table, lens)
+    eng = tu.engine(Hq, Hkv, D)
+    q, kv_len = draw(g, 3, Hq, D), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    clean, _ = eng.paged_decode(q, None, None, cache, table, kv_len)
+    cache.k_pages[int(table[0, 3]), 0, 2, 7] = math.nan
+    cache.v_pages[int(table[1, 2]), 1, 5, 9] = math.inf
+    out, _ = eng.paged_decode(q, None, None, cache, table, kv_len)
+    assert torch.isnan(out[0, :4]).all() and torch.equal(out[0, 4:], clean[0, 4:])
+    assert (out[1, 4:, 9] == math.inf).all() and torch.equal(out[1, :4], clean[1, :4])
+    others = [i for i in range(D) if i != 9]
+    assert torch.equal(out[1, 4:][:, others], clean[1, 4:][:, others]) and torch.equal(out[2], clean[2])
+
+
+def test_first_call_inside_a_capture_is_refused():
+    eng = tu.engine(4, 2, 64)
+    cache = eng.paged_cache(4, 16)
+    q, table, kv_len = torch.zeros(1, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    g, x = torch.cuda.CUDAGraph(), torch.zeros(1, device="cuda")
+    with torch.cuda.graph(g):
+        x.add_(1)
+        with pytest.raises(binding.AdasparkError):
+            eng.paged_decode(q, None, None, cache, table, kv_len, out=out)
+    eng.paged_decode(q, None, None, cache, table, kv_len, out=out)
+    assert eng.text_status() == 0
 
 
 @pytest.mark.parametrize("e4m3", [False, True])

@@ -52,6 +52,15 @@ def test_few_rows_over_many_keys(Hq, Hkv, D, new, total):
     check(Hq, Hkv, D, draw(70, sum(new), Hq, D), draw(71, sum(total), Hkv, D), draw(72, sum(total), Hkv, D), tu.cumulative(new), tu.cumulative(total))
 
 
+def test_many_sequences_some_over_many_keys():
+    """More than 32 sequences of a few rows, the keys of some of them cut."""
+    g = torch.Generator().manual_seed(76)
+    new = torch.randint(0, 4, (45,), generator=g).tolist()
+    total = [n + (5000 if i % 9 == 0 else 20 * i) for i, n in enumerate(new)]
+    Hq, Hkv, D = 8, 1, 64
+    check(Hq, Hkv, D, draw(77, sum(new), Hq, D), draw(78, sum(total), Hkv, D), draw(79, sum(total), Hkv, D), tu.cumulative(new), tu.cumulative(total))
+
+
 def test_cut_keys_sharp_and_with_values_that_are_no_numbers():
     new, total, Hq, Hkv, D = [50], [6000], 14, 2, 128
     q, k, v = draw(73, 50, Hq, D, 8.0), draw(74, 6000, Hkv, D), draw(75, 6000, Hkv, D)
