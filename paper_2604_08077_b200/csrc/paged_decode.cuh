@@ -15,12 +15,11 @@
 // The scores are S = q K^T with the heads as rows (an 8-row half of the m16 tile where the group has at most 8), the outputs
 // O^T = V^T P^T with the heads as columns: S's accumulators are P^T's operand as they stand, and O takes half the registers and products.
 //
-// 8-bit pages: the scores take K as it is (e4m3 products): q is brought to 2^7 .. by a power of two per row and split into two
-// e4m3 parts, q = hi + lo, exact for every element down to 2^-9 of the row's largest and off by at most 2^-17 of that largest below; with up to 8 heads hi
-// and lo are the two halves of one tile.  A key's power of two multiplies its score.  V goes through the tensor cores as f16, which holds every
-// e4m3 value (8-bit weights would lose a long tail beside one large weight).  A value's power of two e_j joins its
-// weight: the weights of the product are 2^(x_j + e_j - m') with their own maximum m', so that they stay within f16 whatever the
-// rows' sizes, and beside them the sum of 2^(x_j - m) is kept.
+// 8-bit pages go through the tensor cores as f16, which holds every e4m3 value.  q is brought to f16 by a power of two per row (largest
+// magnitude 2^14 ..: what falls below 2^-28 of it loses bits, 2^-39 of it at most); a key's power of two multiplies its score.  A value's
+// power of two e_j joins its weight: the weights of the product are 2^(x_j + e_j - m') with their own maximum m', so that they stay
+// within f16 whatever the rows' sizes, and beside them the sum of 2^(x_j - m) is kept.  (K as e4m3 against q in two e4m3 parts: no faster, the
+// legacy 8-bit products are converted, too, and half as fast with more than 8 heads.)
 #pragma once
 #include "common.cuh"
 #include "paged_cache.cuh"
@@ -31,7 +30,9 @@ namespace adaspark {
 constexpr int kPagedThreads = 160;
 constexpr int kPagedCtas = 296;              // two per SM of a B200
 constexpr int kPagedRing = 96 * 1024;        // bytes of a CTA's ring
-constexpr int kPartCost = 2;                 // what a part costs beside its tiles, in tiles
+// What a part costs beside its tiles, in tiles (24 sequences of up to 8192 tokens, bf16, at 0 / 1 / 2 / 3: 35.9 / 28.7 / 25.2 / 24.2 us, 128 of 20 to
+// 1000 at 2 / 3: 30.4 / 31.4; 64 of 16 to 8192 in 8 bits, tiles of twice the keys, at 1 / 2 / 4: 39.7 / 40.5 / 43.2).
+__host__ __device__ constexpr int paged_part_cost(int tile) { return tile == 64 ? 2 : 1; }
 constexpr int kPagedFewSequences = 16;       // up to so many (sequence, kv head)s: at least 18 runs each, a CTA joins a row
 constexpr float kPagedBias = 14.f;           // f16 weights are at most 2^14: 2^-28 of the largest one is still a normal number
 
@@ -79,7 +80,7 @@ struct PagedCall {
     int32_t* status;
 };
 
-// The line of tiles: sequence by sequence, kv head by kv head, in front of each (sequence, kv head) kPartCost places for what a part costs
+// The line of tiles: sequence by sequence, kv head by kv head, in front of each (sequence, kv head) paged_part_cost places for what a part costs
 // beside its tiles (q, the merge of the warps, the output).  Held by a whole warp, which has the lengths of 32 sequences in its lanes.
 template <int kTile>
 struct PageLine {
@@ -94,7 +95,7 @@ struct PageLine {
         len = in_range(n) ? n : 0;
     }
     // places of one (sequence, kv head) of n tokens
-    static __device__ __forceinline__ int places(int n) { return n > 0 ? (n + kTile - 1) / kTile + kPartCost : 0; }
+    static __device__ __forceinline__ int places(int n) { return n > 0 ? (n + kTile - 1) / kTile + paged_part_cost(kTile) : 0; }
     __device__ __forceinline__ long long total() {
         long long sum = 0;
         for (int c = 0; c < batch; c += 32) {
@@ -137,10 +138,10 @@ struct RunWalk {
                 b = c + who;
                 n = __shfl_sync(0xffffffffu, line.len, who);
                 tiles = (n + kTile - 1) / kTile;
-                const int per = tiles + kPartCost, rest = (int)(x - first);
+                const int per = tiles + paged_part_cost(kTile), rest = (int)(x - first);
                 gk = rest / per;
                 place = first + (long long)gk * per;
-                return begin(max(rest - gk * per - kPartCost, 0));
+                return begin(max(rest - gk * per - paged_part_cost(kTile), 0));
             }
             before += all;
         }
@@ -167,12 +168,12 @@ struct RunWalk {
     // the part that begins with tile t; false: the run ends in front of it
     __device__ __forceinline__ bool begin(int t) {
         tile = t;
-        end = (int)min((long long)tiles, max(stop - place - kPartCost, 0ll));
+        end = (int)min((long long)tiles, max(stop - place - paged_part_cost(kTile), 0ll));
         return end > tile;
     }
     // the next part
     __device__ __forceinline__ bool next() {
-        place += tiles + kPartCost;
+        place += tiles + paged_part_cost(kTile);
         if (place >= stop) return false;
         if (++gk < line.p->Hkv) return begin(0);
         gk = 0;
@@ -217,27 +218,6 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// D = A(16x32, row) * B(32x8, col) + D, e4m3 inputs, fp32 accumulate.
-__device__ __forceinline__ void mma_e4m3_16832(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// 4 bf16 (two words) times f -> 4 codes of the values and 4 of what is left
-__device__ __forceinline__ void split_codes(const uint2& x, float f, uint32_t& hi, uint32_t& lo) {
-    const float v[4] = {__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f, __uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f};
-    hi = lo = 0u;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        uint16_t h2, l2;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(h2) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
-        const uint32_t back = codes_to_f16x2(h2);
-        const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&back));
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(l2) : "f"(v[2 * i + 1] - b.y), "f"(v[2 * i] - b.x));
-        hi |= (uint32_t)h2 << (16 * i);
-        lo |= (uint32_t)l2 << (16 * i);
-    }
-}
 // four codes -> two f16 pairs
 __device__ __forceinline__ void codes_to_f16x4(uint32_t c, uint32_t& a, uint32_t& b) {
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}\n" : "=r"(a), "=r"(b) : "r"(c));
@@ -263,8 +243,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     constexpr int kWarpKeys = kTile / 4, kNTiles = kWarpKeys / 8, kRowF = paged_row_floats(D);
     constexpr int kMTiles = D / 16;                           // O^T: tiles of 16 d
     constexpr int kQSlots = kGroups == 1 ? 2 : 1;             // parts whose q is held
-    constexpr int kQSets = kE4m3 && kGroups == 2 ? 2 : 1;     // hi and lo as tiles of their own
-    constexpr int kQSteps = kE4m3 ? D / 32 : D / 16;
+    constexpr int kQSteps = D / 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     if (tid == 0) {
@@ -379,57 +358,41 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     int st = 0, ph = 0;
     for (int part = 0; more; ++part, more = w.next()) {
         const int n = w.n, qs = part % kQSlots;
-        // ---- q fragments
-        uint32_t qf[kQSets][kQSteps][4];
+        // ---- q fragments: rows = heads
+        uint32_t qf[kQSteps][4];
         float f[kGroups];                                     // what the products of head g8 (g8 + 8) are multiplied by
         tc::mbar_wait(&sm.q_full[qs], (part / kQSlots) & 1, abort_flag);
         {
             const __nv_bfloat16* qr[2] = {sm.q[qs * 8 + g8], sm.q[(kGroups == 2 ? 8 : 0) + g8]};
             const bool has[2] = {g8 < a.G, kGroups == 2 && g8 + 8 < a.G};
-            if (!kE4m3) {
-                f[0] = f[kGroups - 1] = a.scale_log2;
 #pragma unroll
-                for (int ks = 0; ks < kQSteps; ++ks)
+            for (int ks = 0; ks < kQSteps; ++ks)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int c = ks * 16 + 2 * t4 + (e >> 1) * 8;
-                        qf[0][ks][e] = has[e & 1] ? *reinterpret_cast<const uint32_t*>(qr[e & 1] + c) : 0u;
-                    }
-            } else {
-                // Thread t4 of a quad has the 16-byte chunks 2 t4, 2 t4 + 1 (D = 64: t4) of a key's codes: step (chunk, half u) takes
-                // d = 16 * chunk + 8 u + 0 .. 3 and + 4 .. 7 as the k indexes 4 t4 .. and 16 + 4 t4 ..
+                for (int r = 0; r < 2; ++r) {
+                    // e4m3: thread t4 of a quad has the 16-byte chunks 2 t4, 2 t4 + 1 (D = 64: t4) of a key's codes; step (chunk, word w) takes
+                    // d = 16 * chunk + 4 w + 0, 1 and + 2, 3 as the k indexes 2 t4, + 1 and 2 t4 + 8, + 9
+                    const int d = kE4m3 ? 16 * (D == 128 ? 2 * t4 + (ks >> 2) : t4) + 4 * (ks & 3) : ks * 16 + 2 * t4;
+                    qf[ks][r] = has[r] ? *reinterpret_cast<const uint32_t*>(qr[r] + d) : 0u;
+                    qf[ks][2 + r] = has[r] ? *reinterpret_cast<const uint32_t*>(qr[r] + d + (kE4m3 ? 2 : 8)) : 0u;
+                }
 #pragma unroll
-                for (int r = 0; r < kGroups; ++r) {
-                    uint2 x[kQSteps][2];
+            for (int r = 0; r < kGroups; ++r) {
+                f[r] = a.scale_log2;
+                if (kE4m3) {
                     uint32_t top = 0u;
 #pragma unroll
-                    for (int ks = 0; ks < kQSteps; ++ks)
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const int d = 16 * (D == 128 ? 2 * t4 + (ks >> 1) : t4) + 8 * (ks & 1) + 4 * y;
-                            x[ks][y] = has[r] ? *reinterpret_cast<const uint2*>(qr[r] + d) : make_uint2(0u, 0u);
-                            top = __vmaxu2(top, __vmaxu2(x[ks][y].x & 0x7fff7fffu, x[ks][y].y & 0x7fff7fffu));
-                        }
+                    for (int ks = 0; ks < kQSteps; ++ks) top = __vmaxu2(top, __vmaxu2(qf[ks][r] & 0x7fff7fffu, qf[ks][2 + r] & 0x7fff7fffu));
                     top = max(top & 0xffffu, top >> 16);
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const int e = max((int)(top >> 7), 30);                // biased exponent of the largest: it becomes 2^7
-                    const float mul = __uint_as_float((uint32_t)(127 + 134 - e) << 23);
-                    f[r] = e == 255 ? NAN : a.scale_log2 * __uint_as_float((uint32_t)(127 + e - 134) << 23);   // (no number among them: none comes out)
+                    const int e = max((int)(top >> 7), 30);                // biased exponent of the largest: it becomes 2^14
+                    const float mul = __uint_as_float((uint32_t)(127 + 141 - e) << 23);
+                    f[r] *= __uint_as_float((uint32_t)min(127 + e - 141, 254) << 23);     // (e = 255, no number: it stays one)
 #pragma unroll
                     for (int ks = 0; ks < kQSteps; ++ks)
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            uint32_t hi, lo;
-                            split_codes(x[ks][y], mul, hi, lo);
-                            if (kGroups == 1) {                            // rows 0 .. 7: hi, rows 8 .. 15: lo
-                                qf[0][ks][2 * y] = hi;
-                                qf[0][ks][2 * y + 1] = lo;
-                            } else {
-                                qf[0][ks][2 * y + r] = hi;
-                                qf[kQSets - 1][ks][2 * y + r] = lo;
-                            }
-                        }
+                        for (int y = 0; y < 4; y += 2)
+                            qf[ks][y + r] = pack_f16x2(__uint_as_float(qf[ks][y + r] << 16) * mul, __uint_as_float(qf[ks][y + r] & 0xffff0000u) * mul);
                 }
             }
         }
@@ -465,19 +428,17 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                 float x[kGroups][kNTiles][2];                 // scores of keys 8 nt + 2 t4, + 1, times scale_log2
                 float ve[kNTiles][2];                         // their values' e_j
                 {
-                    float sc[kQSets][kNTiles][4];
+                    float sc[kNTiles][4];
 #pragma unroll
-                    for (int nt = 0; nt < kNTiles; ++nt)
-#pragma unroll
-                        for (int y = 0; y < kQSets; ++y) sc[y][nt][0] = sc[y][nt][1] = sc[y][nt][2] = sc[y][nt][3] = 0.f;
+                    for (int nt = 0; nt < kNTiles; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
                     if (!kE4m3) {
 #pragma unroll
                         for (int ks = 0; ks < kQSteps; ++ks) {
                             const int row = row0 + (lane & 7) + ((lane >> 4) << 3), chunk = ks * 2 + ((lane >> 3) & 1);
                             uint32_t b0, b1, b2, b3;
                             ldmatrix_x4(b0, b1, b2, b3, kst + (chunk >> 3) * (kTile * 128) + sw128(row, chunk & 7));
-                            mma_bf16_16816(sc[0][0], qf[0][ks], b0, b1);
-                            mma_bf16_16816(sc[0][1], qf[0][ks], b2, b3);
+                            mma_bf16_16816(sc[0], qf[ks], b0, b1);
+                            mma_bf16_16816(sc[1], qf[ks], b2, b3);
                         }
                     } else {
 #pragma unroll
@@ -490,11 +451,12 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                                                  : *reinterpret_cast<const uint4*>(kst + row * 64 + ((t4 ^ ((row >> 1) & 3)) << 4));
                             }
 #pragma unroll
-                            for (int y = 0; y < kQSets; ++y)
+                            for (int y = 0; y < 4; ++y)
 #pragma unroll
                                 for (int nt = 0; nt < kNTiles; ++nt) {
-                                    mma_e4m3_16832(sc[y][nt], qf[y][2 * j], c[nt].x, c[nt].y);
-                                    mma_e4m3_16832(sc[y][nt], qf[y][2 * j + 1], c[nt].z, c[nt].w);
+                                    uint32_t b0, b1;
+                                    codes_to_f16x4(y == 0 ? c[nt].x : y == 1 ? c[nt].y : y == 2 ? c[nt].z : c[nt].w, b0, b1);
+                                    mma_f16_16816(sc[nt], qf[j * 4 + y], b0, b1);
                                 }
                         }
                     }
@@ -512,11 +474,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
 #pragma unroll
                         for (int r = 0; r < kGroups; ++r)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const float v = !kE4m3 ? sc[0][nt][2 * r + e]
-                                                       : (kGroups == 1 ? sc[0][nt][e] + sc[0][nt][2 + e] : sc[0][nt][2 * r + e] + sc[kQSets - 1][nt][2 * r + e]);
-                                x[r][nt][e] = kE4m3 ? v * f[r] * kf[e] : v * f[r];
-                            }
+                            for (int e = 0; e < 2; ++e) x[r][nt][e] = kE4m3 ? sc[nt][2 * r + e] * f[r] * kf[e] : sc[nt][2 * r + e] * f[r];
                     }
                 }
                 if (n_vis < kWarpKeys) {
@@ -732,13 +690,13 @@ __global__ void __launch_bounds__(kJoinThreads, kFew ? 2 : kJoinBlocks) paged_jo
     if (kFew) {
         const int b = blockIdx.x / p.Hkv, gk = blockIdx.x - b * p.Hkv;
         if (w.seek_sequence(b, gk, total)) {
-            run = run_of(total, n_runs, w.place + kPartCost);
-            n = run_of(total, n_runs, w.place + kPartCost + w.tiles - 1) - run + 1;
+            run = run_of(total, n_runs, w.place + paged_part_cost(kTile));
+            n = run_of(total, n_runs, w.place + paged_part_cost(kTile) + w.tiles - 1) - run + 1;
         }
     } else if (run + 1 < n_runs) {
         const long long cut = run_begin(total, n_runs, run + 1);
         w.seek(cut, total);
-        const long long first = w.place + kPartCost;
+        const long long first = w.place + paged_part_cost(kTile);
         if (first < cut && run_of(total, n_runs, first) == run) n = run_of(total, n_runs, first + w.tiles - 1) - run + 1;
     }
     launch_dependents();
