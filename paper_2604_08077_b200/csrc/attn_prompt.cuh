@@ -3,11 +3,12 @@
 //   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = 2^(scale_log2 q_i.k_j - m_i),  j <= n_k - n_q + i
 //
 // One pass over the keys with a reference m_i and running sum, scores and weights in tensor memory alone.  The reference is the largest of the
-// row's first 128 scores, rounded up, and moves only when the weights of 64 keys sum up to more than 2^40: weights, sums and outputs are
+// row's first 128 scores (itself, so that its weight, 1, is not rounded: with the next whole number the outputs were 1.2 times as far from 64 bits)
+// and moves only when the weights of 64 keys sum up to more than 2^40: weights, sums and outputs are
 // floating-point numbers, whose relative precision does not depend on it, and 2^40 is far from where they end.  So no step but the first
-// takes a maximum (9 % of the time of a long prompt).  Where a score is 86 and more (in powers of two: 126) above its row's reference, weights of infinity say so, and that
-// half step's scores, which the weights have overwritten, are computed once more by the threads themselves.  References are whole
-// numbers: moving one multiplies by powers of two and rounds nothing.
+// takes a maximum (9 % of the time of a long prompt).  Where they sum up to 2^100 and more, infinity included, that half step's scores, which
+// the weights have overwritten, are computed once more by the threads themselves.  Otherwise a reference moves by a
+// whole number: by powers of two, which round nothing.
 //
 // Work is dealt out in tiles of 256 rows, a CTA pair (cta_group::2) each: the rows are (token, head of the group) pairs, 128 / G tokens
 // per CTA, so that K and V are read once for all heads of a group, a sequence of a few tokens fills rows that it would leave empty head by
@@ -604,7 +605,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     return fmaxf(a0, a1);
                 };
                 if (j == 0) {
-                    // ---- the reference of the tile: the largest of the first 128 scores, rounded up
+                    // ---- the reference of the tile: the largest of the first 128 scores
                     float top = -INFINITY;
 #pragma unroll 1
                     for (int c = 0; c < 2; ++c) {
@@ -617,7 +618,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     sm.other_ref[team][half][row] = top;
                     pair_sync();
                     top = fmaxf(top, sm.other_ref[team][half ^ 1][row]) * scale_log2;    // scale > 0
-                    m_ref = top == -INFINITY ? 0.f : ceilf(top);       // (a row that sees nothing: any)
+                    m_ref = top == -INFINITY ? 0.f : top;              // (a row that sees nothing: any)
                     if (half == 0) {
                         sm.first_ref[k & 1][row] = m_ref;
                         __syncwarp();
@@ -664,8 +665,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 float m_new = m_prev;
                 const bool over = tok < t.n_tok && !(l_step <= kPromptBig);
                 if (pair_any(over || ref != m_prev)) {
-                    // rare: the reference of one half has to move, or that of the step before has (by powers of two: nothing is rounded)
-                    const bool lost = over && !(l_step < 0x1p126f);   // (a weight near 2^128 is one of infinity in bf16)
+                    // rare: the reference of one half has to move, or that of the step before has
+                    const bool lost = over && !(l_step < 0x1p100f);   // (weights near 2^128 are infinite, their factors near 2^-126 zero)
                     const __nv_bfloat16* q_row = g.q + (long long)(t.q0 + tok) * g.q_ts + (t.gk * g.G + head) * g.q_hs;
                     const int key0 = j * 128 + half * 64, n_keys = lost ? min(last + 1 - key0, 64) : 0;
                     const __nv_bfloat16* keys = g.k + (long long)(t.k0 + key0) * g.k_ts + t.gk * g.k_hs;

@@ -123,7 +123,7 @@ def test_maximum_grows_along_the_keys():
     check(4, 1, D, q, k, v, tu.cumulative([n]), None)
 
 
-@pytest.mark.parametrize("jump", [30.0, 60.0, 100.0, 400.0, 3000.0])
+@pytest.mark.parametrize("jump", [30.0, 60.0, 99.7, 100.0, 113.0, 125.7, 126.4, 127.9, 128.3, 400.0, 3000.0])
 @pytest.mark.parametrize("D", [64, 128])
 def test_one_key_far_above_the_first_ones(jump, D):
     """Scores that leave the range of the first keys' by 2^jump all at once, for some rows, some of them in one half of a step, one row
@@ -133,7 +133,7 @@ def test_one_key_far_above_the_first_ones(jump, D):
     q[..., 0] = torch.where(torch.arange(n, device="cuda")[:, None] % 3 == 0, 4.0, 0.0).to(torch.bfloat16)
     k[..., 0] = 0
     step = jump / (4.0 * D ** -0.5 * math.log2(math.e))
-    for at, f in ((200, 1.0), (250, 1.2), (513, 2.0)):
+    for at, f in ((200, 1.0), (250, 1.01), (513, 2.0)):
         k[at, :, 0] = f * step
     check(Hq, Hkv, D, q, k, v, tu.cumulative([n]), None)
 
