@@ -387,7 +387,8 @@ int64_t adaspark_attn_text_workspace_bytes(const adaspark_attn_t *handle);
  * keys; its row i sees the keys 0 .. n_k - n_q + i (cu_k = cu_q: a prompt from its first token; n_k > n_q: a prompt that
  * continues tokens whose keys and values are given too, e.g. by adaspark_attn_paged_read; n_k < n_q: the first rows see nothing).
  * A sequence whose rows leave the tensors sets status 1 and is left out; the others are worked on.
- * Keys and values that a row does not see do not reach it, whatever they hold (infinities and NaN included). */
+ * Keys and values that a row does not see do not reach it, whatever they hold (infinities and NaN included).  Values of a magnitude above
+ * 2^70 may overflow where a row's weights grow along its keys. */
 typedef struct {
     adaspark_attn_rows_t q, k, v; /* in: n_q rows of Hq heads, n_k rows of Hkv heads                   */
     const int32_t *cu_q, *cu_k;
