@@ -500,11 +500,11 @@ class AdaSAttn:
         shape, strides = t.shape, t.stride()
         if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[1] != heads or shape[2] != self._head_dim:
             _refuse(f"{what}: {t.dtype} {tuple(shape)} is not bfloat16 [rows, {heads}, {self._head_dim}]")
-        if strides[2] != 1:
-            _refuse(f"{what}: the values of a row have to lie side by side")
+        n = shape[0]
+        if strides[2] != 1 or (n > 1 and strides[0] < shape[2]) or (heads > 1 and strides[1] < shape[2]):    # (0 would say dense)
+            _refuse(f"{what}: the values of a row have to lie side by side, and rows apart (strides {tuple(strides)})")
         if t.get_device() != self._index:
             _refuse(f"{what} is on {t.device}, not on {self.device}")
-        n = shape[0]
         # (the stride of an axis of one entry says nothing)
         return (t.data_ptr(), strides[0] if n > 1 else 0, strides[1] if heads > 1 else 0), n
 

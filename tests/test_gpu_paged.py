@@ -307,6 +307,26 @@ def test_decode_values_that_are_no_numbers():
     assert torch.equal(out[1, 4:][:, others], clean[1, 4:][:, others]) and torch.equal(out[2], clean[2])
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_what_the_workspace_held_does_not_matter(e4m3):
+    g = torch.Generator().manual_seed(117)
+    Hq, Hkv, D, page, lens = 14, 2, 64, 64, [3000, 0, 100, 2000]
+    table, n_pages = tu.scattered(g, [-(-n // page) for n in lens])
+    cache = make_cache(g, n_pages, Hkv, page, D, e4m3)
+    filled(g, cache, table, lens)
+    eng, q = tu.engine(Hq, Hkv, D), draw(g, 4, Hq, D)
+    out, lse = check_decode(eng, cache, table, lens, q)
+    eng._text_ws.fill_(255)
+    again, lse2 = check_decode(eng, cache, table, lens, q)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_only_unused_slots():
+    g = torch.Generator().manual_seed(118)
+    cache = make_cache(g, 3, 2, 16, 64, False)
+    check_decode(tu.engine(4, 2, 64), cache, torch.zeros(3, 2, dtype=torch.int32, device="cuda"), [0, 0, 0], draw(g, 3, 4, 64), draw(g, 3, 2, 64), draw(g, 3, 2, 64))
+
+
 def test_first_call_inside_a_capture_is_refused():
     eng = tu.engine(4, 2, 64)
     cache = eng.paged_cache(4, 16)

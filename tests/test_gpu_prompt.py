@@ -175,6 +175,21 @@ def test_large_head_count_and_long_rows():
     check(64, 8, 64, draw(35, 2000, 64, 64), draw(36, 2000, 8, 64), draw(37, 2000, 8, 64), tu.cumulative(lens), None)
 
 
+def test_nothing_but_empty_sequences():
+    q, k, v = draw(80, 5, 4, 64), draw(81, 5, 2, 64), draw(82, 5, 2, 64)
+    check(4, 2, 64, q, k, v, tu.cumulative([0, 0, 0], first=3), None)
+    check(4, 2, 64, q, k, v, tu.cumulative([0]), tu.cumulative([5]))
+
+
+def test_what_the_workspace_held_does_not_matter():
+    q, k, v = draw(83, 20, 14, 128), draw(84, 4000, 2, 128), draw(85, 4000, 2, 128)
+    eng, cu_q, cu_k = tu.engine(14, 2, 128), tu.cumulative([20]), tu.cumulative([4000])
+    out, lse = eng.prompt(q, k, v, cu_q, cu_k, want_lse=True)
+    eng._text_ws.fill_(255)
+    again, lse2 = eng.prompt(q, k, v, cu_q, cu_k, want_lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 def test_bad_sequence_bounds_are_reported_and_not_followed():
     """Sequences that leave the tensors are not worked on; the others are."""
     q, k, v = draw(38, 64, 4, 64), draw(39, 64, 2, 64), draw(40, 64, 2, 64)
@@ -228,6 +243,9 @@ def test_refusals():
     eng = tu.engine(4, 2, 64)
     q, k, v, cu = draw(48, 8, 4, 64), draw(49, 8, 2, 64), draw(50, 8, 2, 64), tu.cumulative([8])
     for bad in [(q.half(), k, v, cu), (q, k[:, :1], v, cu), (q.cpu(), k, v, cu), (q, k, v[:5], cu), (q, k, v, cu.long()), (q.transpose(1, 2), k, v, cu), (q, k, v, cu.cpu())]:
+        with pytest.raises(binding.AdasparkError):
+            eng.prompt(*bad)
+    for bad in [(q[:1].expand(8, 4, 64), k, v, cu), (q, k[:, :1].expand(8, 2, 64), v, cu), (q, k, v, cu.view(1, 2)), (q, k, v, cu[:0])]:
         with pytest.raises(binding.AdasparkError):
             eng.prompt(*bad)
     for kw in [dict(out=torch.empty_like(q)[:4]), dict(out=torch.empty_like(q).float()), dict(lse=torch.empty(8, 4, dtype=torch.float64, device="cuda"))]:
