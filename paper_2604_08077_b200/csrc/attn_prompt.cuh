@@ -579,6 +579,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
             const int last = t.last0 + tok;                   // the last key that the row sees
+            const bool valid = tok < t.n_tok;                 // (the tile's last rows may be none, tokens behind the sequence not its own)
             const int j0 = (team + g0) & 1;
             const bool finishes = ((g0 + t.n_steps - 1) & 1) == team;
             float m_ref = 0.f, l_sum = 0.f;
@@ -595,6 +596,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     for (int i = 0; i < 32; ++i)
                         if (i >= n) s[i] = 0xff800000u;
                 };
+                // what the warp's rows see of a chunk of 32 keys: nothing, all of it, or each its own (hide).  Most chunks of masked steps are of
+                // the first two kinds
+                auto sees_none = [&](int c) -> bool { return masked && __all_sync(0xffffffffu, !valid || n_vis - c * 32 <= 0); };
+                auto sees_all = [&](int c) -> bool { return !masked || __all_sync(0xffffffffu, !valid || n_vis - c * 32 >= 32); };
                 auto largest = [&](const uint32_t (&s)[32]) -> float {
                     float a0 = -INFINITY, a1 = -INFINITY;
 #pragma unroll
@@ -609,10 +614,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     float top = -INFINITY;
 #pragma unroll 1
                     for (int c = 0; c < 2; ++c) {
+                        if (sees_none(c)) break;
                         uint32_t s[32];
                         tc::tmem_ld_32x32(s_addr + c * 32, s);
                         tc::tmem_wait_ld_for(s);
-                        if (masked) hide(s, c);
+                        if (!sees_all(c)) hide(s, c);
                         top = fmaxf(top, largest(s));
                     }
                     sm.other_ref[team][half][row] = top;
@@ -636,9 +642,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     uint32_t s[32], pk[16];
+                    if (sees_none(c)) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) pk[i] = 0u;
+                        tc::tmem_st_32x16(s_addr + c * 16, pk);
+                        continue;
+                    }
                     tc::tmem_ld_32x32(s_addr + c * 32, s);
                     tc::tmem_wait_ld_for(s);
-                    if (masked) hide(s, c);
+                    if (!sees_all(c)) hide(s, c);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const unsigned long long x01 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), scale2, add2);
@@ -663,7 +675,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 if (gs > 0 && !tc::mbar_wait(&sm.ref_done[(gs - 1) & (kPromptRefSlots - 1)][quad], ((gs - 1) / kPromptRefSlots) & 1, abort_flag)) ok = false;
                 if (j > 0) m_prev = sm.ref[(gs - 1) & (kPromptRefSlots - 1)][row];
                 float m_new = m_prev;
-                const bool over = tok < t.n_tok && !(l_step <= kPromptBig);
+                const bool over = valid && !(l_step <= kPromptBig);
                 if (pair_any(over || ref != m_prev)) {
                     // rare: the reference of one half has to move, or that of the step before has
                     const bool lost = over && !(l_step < 0x1p100f);   // (weights near 2^128 are infinite, their factors near 2^-126 zero)
@@ -757,7 +769,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&sm.part_free[ps]);
                 const float inv = l_fin != 0.f ? 1.f / l_fin : 0.f;
-                const bool mine = tok < t.n_tok;              // (the tile's last rows may be none, tokens behind the sequence not its own)
+                const bool mine = valid;
                 const long long at = (long long)(t.q0 + tok) * g.Hq + t.gk * g.G + head;
                 float* part_o = nullptr;                      // this thread's outputs of a part
                 if (t.part >= 0) {
