@@ -675,7 +675,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 if (gs > 0 && !tc::mbar_wait(&sm.ref_done[(gs - 1) & (kPromptRefSlots - 1)][quad], ((gs - 1) / kPromptRefSlots) & 1, abort_flag)) ok = false;
                 if (j > 0) m_prev = sm.ref[(gs - 1) & (kPromptRefSlots - 1)][row];
                 float m_new = m_prev;
-                const bool over = valid && !(l_step <= kPromptBig);
+                const bool over = valid && l_step > kPromptBig;   // (no number: some score is none, and so will the row be)
                 if (pair_any(over || ref != m_prev)) {
                     // rare: the reference of one half has to move, or that of the step before has
                     const bool lost = over && !(l_step < 0x1p100f);   // (weights near 2^128 are infinite, their factors near 2^-126 zero)
