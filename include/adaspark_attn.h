@@ -408,7 +408,9 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t *handle, const adaspark_a
  * _write puts the rows k, v into their places.  A row without a place (before token 0, behind the table, page number outside
  * [0, n_pages)) is not written and sets status 1.  Two rows with the same place in one call: either may win.
  * _read gets the last cu[b+1] - cu[b] tokens of every sequence back into the rows k, v.  Exact: every value that a page holds
- * is a bf16 number.  A row without a place becomes zeros and sets status 1. */
+ * is a bf16 number.  A row without a place becomes zeros and sets status 1.
+ * A sequence whose rows leave the tensors (cu[b] < 0, cu[b+1] < cu[b] or > n) sets status 1, and its rows have no place; the others are
+ * worked on.  Where cu decreases, a row that the bounds give to several sequences goes to one of those that are in order, or to none. */
 typedef struct {
     adaspark_attn_pages_t pages;
     adaspark_attn_rows_t k, v;    /* n rows of Hkv heads                                               */

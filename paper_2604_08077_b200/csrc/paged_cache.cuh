@@ -105,7 +105,7 @@ __device__ __forceinline__ uint4 chunk_values(const uint2& c, uint32_t s) {
 }
 
 // The sequence that row `at` of the packed tensors belongs to: the last one with cu[seq] <= at, or -1 (rows in front of
-// the first sequence or behind the last one).
+// the first sequence or behind the last one).  If cu decreases somewhere, some sequence with cu[seq] <= at < cu[seq + 1], or -1.
 __device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int at) {
     if (at < cu[0] || at >= cu[batch]) return -1;
     int lo = 0, hi = batch;                                                   // cu[lo] <= at < cu[hi]
@@ -117,10 +117,13 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int at)
     return lo;
 }
 
+// Are these the first row and the one behind the last of a sequence in tensors of n rows?
+__device__ __forceinline__ bool bounds_fit(int begin, int end, int n) { return 0 <= begin && begin <= end && end <= n; }
+
 constexpr int kCacheThreads = 256;
 
 // Places of the CTA's kTokens tokens from t0 on, by its first threads: offsets (elements, scales) of a token's first kv head in the pages;
-// first < 0: -1 a row of no sequence, -2 one of a sequence that has no place for it.
+// first < 0: -1 a row of no sequence, -2 one of a sequence that has no place for it, or whose bounds are none.
 template <int kTokens, int D>
 __device__ __forceinline__ void find_tokens(const PageGeom& p, const int32_t* cu, const int32_t* kv_len, int batch, int n, int t0, long long (&place)[kTokens],
                                             long long (&scale_place)[kTokens], int32_t* status) {
@@ -129,8 +132,9 @@ __device__ __forceinline__ void find_tokens(const PageGeom& p, const int32_t* cu
         long long x = -1, y = 0;
         const int seq = at < n ? sequence_of(cu, batch, at) : -1;
         if (seq >= 0) {
-            const int pos = kv_len[seq] - (cu[seq + 1] - at), in = pos & ((1 << p.page_shift) - 1);
-            const long long page = page_of(p, seq, pos);
+            const int len = kv_len[seq], end = cu[seq + 1];
+            const int pos = len > 0 ? len - (end - at) : -1, in = pos & ((1 << p.page_shift) - 1);
+            const long long page = bounds_fit(cu[seq], end, n) ? page_of(p, seq, pos) : -1;
             if (page < 0) {
                 x = -2;
                 if (status != nullptr) atomicExch(status, 1);
@@ -144,6 +148,15 @@ __device__ __forceinline__ void find_tokens(const PageGeom& p, const int32_t* cu
     }
 }
 
+// A sequence with bad bounds may have no row in the tensors (all of it behind them): the CTAs share the batch out among them and look at every
+// sequence's.  (Behind the copies: in front of them it took registers that left room for a CTA less, 157 instead of 146 us for 131072 tokens
+// written and read in 8 bits; hence the bound of 4 CTAs on both kernels, too.)
+__device__ __forceinline__ void report_bounds(const int32_t* cu, int batch, int n, int32_t* status) {
+    if (status == nullptr || blockIdx.y != 0) return;
+    for (long long b = blockIdx.x * (long long)kCacheThreads + threadIdx.x; b < batch; b += gridDim.x * (long long)kCacheThreads)
+        if (!bounds_fit(cu[b], cu[b + 1], n)) atomicExch(status, 1);
+}
+
 // Both kernels: a CTA has kTokens tokens, a thread one 16-byte piece (8 values) of a row of one head of K or V and every
 // kCacheThreads / columns-th token: what belongs to the column is worked out once, a token costs an offset from shared memory.  Bound by HBM, every
 // value read once and written once.  (With the pieces of 8 tokens dealt to the threads one by one, index arithmetic took the issue slots: 131072 tokens, 4
@@ -152,7 +165,7 @@ __device__ __forceinline__ void find_tokens(const PageGeom& p, const int32_t* cu
 // k, v [n][Hkv][D] (row and head strides in elements) -> pages.  D / 8 neighbouring threads find a row's largest magnitude by shuffles; the
 // first loads of a thread are under way before its CTA has looked up where they go.
 template <int D, bool kE4m3, int kTokens>
-__global__ void __launch_bounds__(kCacheThreads) paged_write_kernel(
+__global__ void __launch_bounds__(kCacheThreads, 4) paged_write_kernel(
     PageGeom p, const __nv_bfloat16* k, long long k_ts, long long k_hs, const __nv_bfloat16* v, long long v_ts, long long v_hs,
     const int32_t* cu, const int32_t* kv_len, int batch, int n, int32_t* status) {
     constexpr int kLanes = D / 8, kAhead = 4;
@@ -206,12 +219,13 @@ __global__ void __launch_bounds__(kCacheThreads) paged_write_kernel(
             }
         }
     }
+    report_bounds(cu, batch, n, status);
 }
 
 // pages -> k_out, v_out [n][Hkv][D] bf16 (row and head strides in elements).  Rows of no sequence are left as they are; rows of a sequence that
 // have no place in its pages read as zeros.
 template <int D, bool kE4m3, int kTokens>
-__global__ void __launch_bounds__(kCacheThreads) paged_read_kernel(
+__global__ void __launch_bounds__(kCacheThreads, 4) paged_read_kernel(
     PageGeom p, __nv_bfloat16* k_out, long long k_ts, long long k_hs, __nv_bfloat16* v_out, long long v_ts, long long v_hs, const int32_t* cu,
     const int32_t* kv_len, int batch, int n, int32_t* status) {
     constexpr int kLanes = D / 8, kAhead = kE4m3 ? 8 : 4;
@@ -256,6 +270,7 @@ __global__ void __launch_bounds__(kCacheThreads) paged_read_kernel(
             if (tt < count && place[tt] != -1) *reinterpret_cast<uint4*>(dst + tt * ts) = kE4m3 ? chunk_values(make_uint2(x[i].x, x[i].y), s[i]) : x[i];
         }
     }
+    report_bounds(cu, batch, n, status);
 }
 
 }  // namespace adaspark
