@@ -474,22 +474,34 @@ class AdaSAttn:
         return PagedCache(*pages, *scales)
 
     def _text_buffers(self):
-        """(status pointer, workspace pointer, workspace bytes) of the text calls, made once."""
-        if torch.cuda.is_current_stream_capturing():
+        """(status pointer, workspace pointer, workspace bytes) of the text calls, made once.  Waits for the stream that they are made on, so
+        that a call on any stream comes behind the clearing of the status and whatever used this memory before."""
+        if self._capturing():
             _refuse("the first text call of an object allocates its workspace: make one before a capture begins")
         n = adaspark_attn_text_workspace_bytes(self.handle)
         self._text_ws = torch.empty(n, dtype=torch.uint8, device=self.device)
         self._text_flag = torch.zeros(1, dtype=torch.int32, device=self.device)
+        torch.cuda.current_stream(self.device).synchronize()
         self._text = (self._text_flag.data_ptr(), self._text_ws.data_ptr(), n)
         return self._text
 
+    def _capturing(self) -> bool:
+        """Is the current stream of this object's device in capture?"""
+        with torch.cuda.device(self.device):
+            return torch.cuda.is_current_stream_capturing()
+
     def text_status(self) -> int:
-        """What the text calls of this object found wrong on the device since the last look: 0 = nothing (waits for the device)."""
+        """What the text calls of this object found wrong on the device since the last look: 0 = nothing.  Waits for the device, whatever
+        streams the calls are on (so not inside a capture), and for the clearing of what it returns."""
         if self._text is None:
             return 0
+        if self._capturing():
+            _refuse("text_status waits for the device: not inside a capture")
+        torch.cuda.synchronize(self.device)
         got = int(self._text_flag.item())
         if got:
             self._text_flag.zero_()
+            torch.cuda.current_stream(self.device).synchronize()
         return got
 
     def _stream(self, stream):
