@@ -473,21 +473,22 @@ class AdaSAttn:
         scales = [torch.zeros(shape[:3], dtype=torch.uint8, device=dev) for _ in range(2)] if e4m3 else [None, None]
         return PagedCache(*pages, *scales)
 
-    def _text_buffers(self):
+    def _text_buffers(self, stream):
         """(status pointer, workspace pointer, workspace bytes) of the text calls, made once.  Waits for the stream that they are made on, so
         that a call on any stream comes behind the clearing of the status and whatever used this memory before."""
-        if self._capturing():
+        if self._capturing() or (stream is not None and self._capturing(stream)):
             _refuse("the first text call of an object allocates its workspace: make one before a capture begins")
         n = adaspark_attn_text_workspace_bytes(self.handle)
         self._text_ws = torch.empty(n, dtype=torch.uint8, device=self.device)
         self._text_flag = torch.zeros(1, dtype=torch.int32, device=self.device)
         torch.cuda.current_stream(self.device).synchronize()
+        self._text_streams = {_raw_stream(self._index)}
         self._text = (self._text_flag.data_ptr(), self._text_ws.data_ptr(), n)
         return self._text
 
-    def _capturing(self) -> bool:
-        """Is the current stream of this object's device in capture?"""
-        with torch.cuda.device(self.device):
+    def _capturing(self, stream=None) -> bool:
+        """Is a stream (None: the current one of this object's device) in capture?"""
+        with torch.cuda.device(self.device), torch.cuda.stream(stream):
             return torch.cuda.is_current_stream_capturing()
 
     def text_status(self) -> int:
@@ -505,7 +506,24 @@ class AdaSAttn:
         return got
 
     def _stream(self, stream):
-        return (_raw_stream(self._index) if stream is None else stream.cuda_stream) or None
+        """The stream of a text call for the C entry.  The first time that one is seen, torch's allocator is told that it uses the workspace and
+        the status, which are not handed on before it has come to the end of its calls then."""
+        raw = _raw_stream(self._index) if stream is None else stream.cuda_stream
+        if raw not in self._text_streams:
+            for t in (self._text_ws, self._text_flag):
+                t.record_stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+            self._text_streams.add(raw)
+        return raw or None
+
+    def _empty(self, shape, dtype, stream):
+        """An output of a call on `stream`: memory of that stream, whose earlier uses it comes behind, and not handed on before the current stream
+        has come to the end of what it does with it, either."""
+        if stream is None or stream.cuda_stream == _raw_stream(self._index):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream(self.device))
+        return t
 
     def _rows(self, t, heads: int, what: str):
         """(pointer, token stride, head stride) of a bf16 tensor [rows, heads, head_dim] on this device, and its rows."""
@@ -546,7 +564,7 @@ class AdaSAttn:
         """Causal attention of packed prompts: q [n_q, Hq, D], k and v [n_k, Hkv, D] bf16, cu_q (and cu_k, if the keys of a sequence
         are more than its queries) int32 [batch + 1].  Returns (out, lse); lse is None unless given or wanted.  The text calls of one
         object share a workspace: calls that may overlap on the GPU (other streams, graphs replayed side by side) need an object each."""
-        status, ws, ws_bytes = self._text or self._text_buffers()
+        status, ws, ws_bytes = self._text or self._text_buffers(stream)
         Hq, D = self._n_q_heads, self._head_dim
         (qr, n_q), (kr, n_k), (vr, n_v) = self._rows(q, Hq, "q"), self._rows(k, self._n_kv_heads, "k"), self._rows(v, self._n_kv_heads, "v")
         if n_v != n_k:
@@ -556,9 +574,9 @@ class AdaSAttn:
         if n_cu == 0:
             _refuse("cu_q: batch + 1 entries are needed")
         if out is None:
-            out = torch.empty(n_q, Hq, D, dtype=torch.bfloat16, device=self.device)
+            out = self._empty((n_q, Hq, D), torch.bfloat16, stream)
         if lse is None and want_lse:
-            lse = torch.empty(n_q, Hq, dtype=torch.float32, device=self.device)
+            lse = self._empty((n_q, Hq), torch.float32, stream)
         adaspark_attn_prompt(self.handle, qr, kr, vr, cq, cq if cu_k is None else self._ints(cu_k, n_cu, "cu_k"), n_cu - 1, n_q, n_k,
                              self._dense(out, (n_q, Hq, D), torch.bfloat16, "out"),
                              None if lse is None else self._dense(lse, (n_q, Hq), torch.float32, "lse"), ws, ws_bytes, status,
@@ -576,7 +594,7 @@ class AdaSAttn:
         return k_out, v_out
 
     def _paged_rows(self, call, cache, k, v, cu, block_table, kv_len, stream):
-        status = (self._text or self._text_buffers())[0]
+        status = (self._text or self._text_buffers(stream))[0]
         (kr, n), (vr, n_v) = self._rows(k, self._n_kv_heads, "k"), self._rows(v, self._n_kv_heads, "v")
         if n_v != n:
             _refuse(f"v has {n_v} rows, k {n}")
@@ -587,7 +605,7 @@ class AdaSAttn:
                      stream=None):
         """One new token per sequence against its pages.  q [batch, Hq, D]; k_new, v_new [batch, Hkv, D] are stored as token
         kv_len[b] - 1 first (None: they are there).  kv_len 0: a slot without a sequence.  Returns (out, lse)."""
-        status, ws, ws_bytes = self._text or self._text_buffers()
+        status, ws, ws_bytes = self._text or self._text_buffers(stream)
         Hq, D = self._n_q_heads, self._head_dim
         batch, table, width, lens = self._tables(block_table, kv_len)
         qr, n = self._rows(q, Hq, "q")
@@ -600,9 +618,9 @@ class AdaSAttn:
         if n != batch or n_k != batch or n_v != batch:
             _refuse(f"q, k_new and v_new hold a row for each of the {batch} entries of kv_len")
         if out is None:
-            out = torch.empty(batch, Hq, D, dtype=torch.bfloat16, device=self.device)
+            out = self._empty((batch, Hq, D), torch.bfloat16, stream)
         if lse is None and want_lse:
-            lse = torch.empty(batch, Hq, dtype=torch.float32, device=self.device)
+            lse = self._empty((batch, Hq), torch.float32, stream)
         adaspark_attn_paged_decode(self.handle, qr, kr, vr, self._cache(cache), table, width, lens, batch,
                                    self._dense(out, (batch, Hq, D), torch.bfloat16, "out"),
                                    None if lse is None else self._dense(lse, (batch, Hq), torch.float32, "lse"), ws, ws_bytes, status,
