@@ -387,6 +387,21 @@ class AdaSAttn:
         self._text = None
         self._index, self._n_q_heads, self._n_kv_heads, self._head_dim = device, n_q_heads, n_kv_heads, head_dim
 
+    def _capturing(self, stream=None) -> bool:
+        """Is a stream (None: the current one of this object's device) in capture?"""
+        with torch.cuda.device(self.device), torch.cuda.stream(stream):
+            return torch.cuda.is_current_stream_capturing()
+
+    def _empty(self, shape, dtype, stream):
+        """An output of a call on `stream`: memory of that stream, whose earlier uses it comes behind, and not handed on before the current stream
+        has come to the end of what it does with it, either."""
+        if stream is None or stream.cuda_stream == _raw_stream(self._index):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream(self.device))
+        return t
+
     def set_gather(self, pairs_per_block: float, budget_bytes: int = 24 << 30):
         """Threshold and workspace budget of the query-gather path (budget: before partition())."""
         adaspark_attn_set_gather(self.handle, pairs_per_block, budget_bytes)
@@ -403,20 +418,33 @@ class AdaSAttn:
         self.cube_keys = torch.empty(batch, c.n_kv_heads, lay.n_cubes, c.head_dim,
                                      dtype=torch.float32, device=dev)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+        if not self._capturing():
+            torch.cuda.current_stream(dev).synchronize()             # what used this memory before; calls may be on any stream
+        self._streams = {_raw_stream(self._index)}
         return self
+
+    def _use(self, stream):
+        """A video call on `stream` (None: torch's current one).  The first time that one is seen, torch's allocator is told that it uses the
+        caches and the workspace, which are not handed on before it has come to the end of its calls then."""
+        raw = _raw_stream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+        if raw not in self._streams:
+            for t in (self.k_cube, self.v_cube, self.cube_keys, self.workspace):
+                t.record_stream(torch.cuda.current_stream() if stream is None else stream)
+            self._streams.add(raw)
 
     def forward(self, q, k, v, n_text, *, out=None, want_selection=False, stream=None, n_prefix=0):
         """q may be None: builds only the caches.  Returns (out, sel_bitmap, sel_count).
         n_prefix > 0: the first n_prefix tokens of the tensors are text that precedes the video."""
         lay = self.layout
+        self._use(stream)
         bitmap = count = None
         if q is not None:
             if out is None:
-                out = torch.empty_like(q)
+                out = self._empty(q.shape, q.dtype, stream)
             if want_selection:
                 B, S, Hq, _ = q.shape
-                bitmap = torch.empty(B, Hq, S, lay.bitmap_words, dtype=torch.int32, device=q.device)
-                count = torch.empty(B, Hq, S, dtype=torch.int32, device=q.device)
+                bitmap = self._empty((B, Hq, S, lay.bitmap_words), torch.int32, stream)
+                count = self._empty((B, Hq, S), torch.int32, stream)
         if n_prefix:
             adaspark_attn_forward_prefix(self.handle, q, k, v, n_prefix, n_text, out, self.k_cube, self.v_cube,
                                          self.cube_keys, bitmap, count, self.workspace, self.ws_bytes, stream)
@@ -428,6 +456,7 @@ class AdaSAttn:
     def forward_host(self, q_host, k_host, v_host, n_text, out_host, staging, stream=None):
         """Prefill with host tensors; `staging` = (q, k, v, out) device tensors of the same shapes."""
         qd, kd, vd, od = staging
+        self._use(stream)
         adaspark_attn_forward_host(self.handle, q_host, k_host, v_host, n_text, out_host, qd, kd, vd, od,
                                    self.k_cube, self.v_cube, self.cube_keys, self.workspace, self.ws_bytes, stream)
         return out_host
@@ -436,14 +465,15 @@ class AdaSAttn:
                       stream=None):
         """One chunk of a chunked prefill (n_text < 0: more video follows).  q may be None."""
         lay = self.layout
+        self._use(stream)
         bitmap = count = None
         if q is not None:
             if out is None:
-                out = torch.empty_like(q)
+                out = self._empty(q.shape, q.dtype, stream)
             if want_selection:
                 B, S, Hq, _ = q.shape
-                bitmap = torch.empty(B, Hq, S, lay.bitmap_words, dtype=torch.int32, device=q.device)
-                count = torch.empty(B, Hq, S, dtype=torch.int32, device=q.device)
+                bitmap = self._empty((B, Hq, S, lay.bitmap_words), torch.int32, stream)
+                count = self._empty((B, Hq, S), torch.int32, stream)
         adaspark_attn_forward_chunk(self.handle, q, k, v, frame_begin, frame_count, n_text, out, self.k_cube,
                                     self.v_cube, self.cube_keys, bitmap, count, self.workspace, self.ws_bytes,
                                     stream)
@@ -451,12 +481,13 @@ class AdaSAttn:
 
     def decode(self, q_new, k_new, v_new, text_len, *, out=None, want_selection=False, stream=None):
         lay = self.layout
+        self._use(stream)
         if out is None:
-            out = torch.empty_like(q_new)
+            out = self._empty(q_new.shape, q_new.dtype, stream)
         bitmap = None
         if want_selection:
             B, _, Hq, _ = q_new.shape
-            bitmap = torch.empty(B, Hq, lay.bitmap_words, dtype=torch.int32, device=q_new.device)
+            bitmap = self._empty((B, Hq, lay.bitmap_words), torch.int32, stream)
         adaspark_attn_decode(self.handle, q_new, k_new, v_new, self.k_cube, self.v_cube,
                              self.cube_keys, text_len, out, bitmap, self.workspace, self.ws_bytes,
                              stream)
@@ -486,11 +517,6 @@ class AdaSAttn:
         self._text = (self._text_flag.data_ptr(), self._text_ws.data_ptr(), n)
         return self._text
 
-    def _capturing(self, stream=None) -> bool:
-        """Is a stream (None: the current one of this object's device) in capture?"""
-        with torch.cuda.device(self.device), torch.cuda.stream(stream):
-            return torch.cuda.is_current_stream_capturing()
-
     def text_status(self) -> int:
         """What the text calls of this object found wrong on the device since the last look: 0 = nothing.  Waits for the device, whatever
         streams the calls are on (so not inside a capture), and for the clearing of what it returns."""
@@ -514,16 +540,6 @@ class AdaSAttn:
                 t.record_stream(torch.cuda.current_stream(self.device) if stream is None else stream)
             self._text_streams.add(raw)
         return raw or None
-
-    def _empty(self, shape, dtype, stream):
-        """An output of a call on `stream`: memory of that stream, whose earlier uses it comes behind, and not handed on before the current stream
-        has come to the end of what it does with it, either."""
-        if stream is None or stream.cuda_stream == _raw_stream(self._index):
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(stream):
-            t = torch.empty(shape, dtype=dtype, device=self.device)
-        t.record_stream(torch.cuda.current_stream(self.device))
-        return t
 
     def _rows(self, t, heads: int, what: str):
         """(pointer, token stride, head stride) of a bf16 tensor [rows, heads, head_dim] on this device, and its rows."""
@@ -628,7 +644,8 @@ class AdaSAttn:
         return out, lse
 
     def header(self) -> WorkspaceHeader:
-        """Copy of the workspace header of the last call (synchronises the device)."""
+        """Copy of the workspace header of the last call (waits for the device, whatever stream that call is on)."""
+        torch.cuda.synchronize(self.device)
         raw = self.workspace[:ctypes.sizeof(WorkspaceHeader)].cpu().numpy().tobytes()
         return WorkspaceHeader.from_buffer_copy(raw)
 
