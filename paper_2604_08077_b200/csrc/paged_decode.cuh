@@ -37,6 +37,9 @@ constexpr int kPagedFewSequences = 16;       // up to so many (sequence, kv head
 constexpr float kPagedBias = 14.f;           // f16 weights are at most 2^14: 2^-28 of the largest one is still a normal number
 
 __host__ __device__ constexpr int paged_tile(bool e4m3) { return e4m3 ? 128 : 64; }   // keys of a tile
+// Tiles of n tokens, and pieces of `size` that the first tile of n > 0 tokens holds keys in; a table may have room for 2^31 - 1 tokens.
+__host__ __device__ constexpr int paged_tiles(int n, int tile) { return n > 0 ? (n - 1) / tile + 1 : 0; }
+__host__ __device__ constexpr int paged_pieces(int n, int tile, int size) { return ((n < tile ? n : tile) + size - 1) / size; }
 __host__ __device__ constexpr int paged_row_floats(int D) { return D + 4; }           // m, l, m', -, o[D]
 __host__ __device__ constexpr size_t paged_partial_bytes(int D, int G) { return (size_t)kPagedCtas * 2 * G * paged_row_floats(D) * sizeof(float); }
 
@@ -95,7 +98,7 @@ struct PageLine {
         len = in_range(n) ? n : 0;
     }
     // places of one (sequence, kv head) of n tokens
-    static __device__ __forceinline__ int places(int n) { return n > 0 ? (n + kTile - 1) / kTile + paged_part_cost(kTile) : 0; }
+    static __device__ __forceinline__ int places(int n) { return n > 0 ? paged_tiles(n, kTile) + paged_part_cost(kTile) : 0; }
     __device__ __forceinline__ long long total() {
         long long sum = 0;
         for (int c = 0; c < batch; c += 32) {
@@ -137,7 +140,7 @@ struct RunWalk {
                 const long long first = before + __shfl_sync(0xffffffffu, upto - mine, who);
                 b = c + who;
                 n = __shfl_sync(0xffffffffu, line.len, who);
-                tiles = (n + kTile - 1) / kTile;
+                tiles = paged_tiles(n, kTile);
                 const int per = tiles + paged_part_cost(kTile), rest = (int)(x - first);
                 gk = rest / per;
                 place = first + (long long)gk * per;
@@ -161,7 +164,7 @@ struct RunWalk {
         n = __shfl_sync(0xffffffffu, line.len, seq & 31);
         b = seq;
         gk = head;
-        tiles = (n + kTile - 1) / kTile;
+        tiles = paged_tiles(n, kTile);
         place += (long long)head * line.places(n);
         return begin(0);
     }
@@ -184,7 +187,7 @@ struct RunWalk {
                 const int who = __ffs(there) - 1;
                 b = line.chunk + who;
                 n = __shfl_sync(0xffffffffu, line.len, who);
-                tiles = (n + kTile - 1) / kTile;
+                tiles = paged_tiles(n, kTile);
                 return begin(0);
             }
             if (line.chunk + 32 >= line.batch) return false;
@@ -278,7 +281,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
 
     if (warp == 4) {
         // ------------------------------------------------------------ producer
-        const int sub = min(page_size, kTile), n_sub = kTile / sub;        // tokens of a box, boxes of a tile
+        const int sub = min(page_size, kTile);               // tokens of a box
         int st = 0, ph = 1;
         // page numbers: this lane's of the 32 columns from `cols` on of sequence `cols_b`, and of the 32 behind them
         int cols_b = -1, cols = 0, pages = 0, pages_next = 0;
@@ -311,7 +314,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                     pages = pages_next;
                     pages_next = page_at(cols + 32 + lane);
                 }
-                const int boxes = min((w.n - pos0 + sub - 1) / sub, n_sub);   // those that hold a token
+                const int boxes = paged_pieces(w.n - pos0, kTile, sub);   // those that hold a token
                 int page = __shfl_sync(0xffffffffu, pages, min(col0 - cols + lane, 31));
                 const int over = __shfl_sync(0xffffffffu, pages_next, max(col0 - cols + lane - 32, 0) & 31);
                 if (col0 - cols + lane >= 32) page = over;
@@ -578,7 +581,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
             if (t4 == 0) *reinterpret_cast<float4*>(sm.stat[warp][r * 8 + g8]) = make_float4(m[r], l[r], mv[r], 0.f);
         }
         // warps that had a key of the part (the first ones, where it is one tile)
-        const int live = w.end - w.tile > 1 ? 4 : min(4, (n - w.tile * kTile + kWarpKeys - 1) / kWarpKeys);
+        const int live = w.end - w.tile > 1 ? 4 : paged_pieces(n - w.tile * kTile, kTile, kWarpKeys);
         consumer_sync();
 #pragma unroll
         for (int r = 0; r < kGroups; ++r) {
