@@ -392,9 +392,10 @@ int64_t adaspark_attn_text_workspace_bytes(const adaspark_attn_t *handle);
 typedef struct {
     adaspark_attn_rows_t q, k, v; /* in: n_q rows of Hq heads, n_k rows of Hkv heads                   */
     const int32_t *cu_q, *cu_k;
-    void *out;                    /* bf16 [n_q][Hq][head_dim]; zeros for a row that sees nothing       */
+    void *out;                    /* bf16 [n_q][Hq][head_dim]; zeros for a row that sees nothing, or
+                                     nothing but scores of -infinity                                   */
     float *lse;                   /* nullable: fp32 [n_q][Hq], natural logarithm of the sum of the exponentials of the row's
-                                     scaled scores; -infinity for a row that sees nothing              */
+                                     scaled scores; -infinity for such a row                           */
     void *workspace;
     int64_t workspace_bytes;
     int32_t *status;
@@ -424,7 +425,7 @@ adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t *handle, const adaspa
 /* One new token per sequence: the row q of sequence b attends the tokens 0 .. kv_len[b] - 1 of its pages.
  * kv_len 0 marks a slot of the batch without a sequence (nothing is appended).  Where kv_len is negative or more than the table
  * holds, or a page number among the tokens is outside [0, n_pages), status is set to 1 and nothing is appended into a place that is
- * not there; the row becomes zeros (lse: -infinity), as it does with kv_len 0.
+ * not there; the row becomes zeros (lse: -infinity), as it does with kv_len 0, and where every score is -infinity.
  * Two sequences may share pages that neither of them appends to. */
 typedef struct {
     adaspark_attn_pages_t pages;

@@ -642,7 +642,8 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                 v = make_float2(v.x + u.x, v.y + u.y);
             }
             if (whole) {
-                const float fo = kE4m3 ? exp2f(amv - am - kPagedBias) : 1.f, inv = 1.f / al;
+                // (every score -inf: the maxima are, sum and outputs are zeros, or none where a value is none)
+                const float fo = kE4m3 && am != -INFINITY ? exp2f(amv - am - kPagedBias) : 1.f, inv = al != 0.f ? 1.f / al : 0.f;
                 const size_t out_at = (size_t)w.b * a.Hq + w.gk * a.G + row;
                 *reinterpret_cast<uint32_t*>(a.out + out_at * D + d) = bad ? 0u : pack_bf16x2(v.x * inv * fo, v.y * inv * fo);
                 if (d == 0 && a.lse != nullptr) a.lse[out_at] = bad ? -INFINITY : (am + log2f(al)) * 0.6931471805599453f;
@@ -717,7 +718,7 @@ __global__ void __launch_bounds__(kJoinThreads, kFew ? 2 : kJoinBlocks) paged_jo
     };
     auto finish = [&](int row, int d4, const float4& acc, float m, float mv, float l, bool bad) {
         const size_t at = (size_t)w.b * a.Hq + w.gk * a.G + row;
-        const float f = (kE4m3 ? exp2f(mv - m) : 1.f) / l;
+        const float f = (kE4m3 && m != -INFINITY ? exp2f(mv - m) : 1.f) * (l != 0.f ? 1.f / l : 0.f);   // (every score -inf: as in a whole part)
         *reinterpret_cast<uint2*>(a.out + at * D + 4 * d4) = bad ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
         if (d4 == 0 && a.lse != nullptr) a.lse[at] = bad ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
     };

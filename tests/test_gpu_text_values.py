@@ -1,0 +1,47 @@
+"""GPU tests of the text operators at the ends of what keys, queries and scores can hold, against plain forms in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import text_util as tu
+from paper_2604_08077_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+def draw(g, *shape, size=1.0):
+    return (torch.randn(*shape, generator=g) * size).to(torch.bfloat16).cuda()
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def zero_cache(n_pages, Hkv, page, D, e4m3):
+    dtype = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+    pages = [torch.zeros(n_pages, Hkv, page, D, dtype=dtype, device="cuda") for _ in range(2)]
+    return binding.PagedCache(*pages, *([torch.zeros(n_pages, Hkv, page, dtype=torch.uint8, device="cuda") for _ in range(2)] if e4m3 else []))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("Hq,Hkv", [(4, 2), (11, 1)])
+@pytest.mark.parametrize("n", [5, 300, 6000])
+def test_decode_rows_whose_scores_are_all_minus_infinity(e4m3, Hq, Hkv, n):
+    """They give zeros, as rows without a key do; the other sequence of the call keeps its own."""
+    g = torch.Generator().manual_seed(220)
+    D, page = 128, 64
+    per = -(-n // page)
+    cache, eng = zero_cache(2 * per, Hkv, page, D, e4m3), tu.engine(Hq, Hkv, D)
+    table, kv_len = torch.arange(2 * per, dtype=torch.int32, device="cuda").view(2, per), ints(n, n)
+    k, v, q = draw(g, 2 * n, Hkv, D), draw(g, 2 * n, Hkv, D), draw(g, 2, Hq, D)
+    k[n:] = 0
+    k[n:, :, 0], q[1, :, 0] = (-2.0 ** 100, 2.0 ** 120) if e4m3 else (-math.inf, 1.0)     # (8 bits hold no infinity: a product beyond the range)
+    eng.paged_write(cache, k, v, tu.cumulative([n, n]), table, kv_len)
+    out, lse = eng.paged_decode(q, None, None, cache, table, kv_len, want_lse=True)
+    assert eng.text_status() == 0
+    assert (lse[1] == -math.inf).all() and (out[1] == 0).all()
+    kk, vv = tu.sequence_values(cache, table, 0, n)
+    want, wl, tol, ltol = tu.attend(q[:1], kk, vv, torch.tensor([n - 1], device="cuda"), D ** -0.5)
+    tu.assert_close(out[:1], want, tol, "out")
+    tu.assert_lse(lse[:1], wl, ltol)
