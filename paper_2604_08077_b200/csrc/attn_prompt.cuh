@@ -6,7 +6,8 @@
 // row's first 128 scores (itself, so that its weight, 1, is not rounded: with the next whole number the outputs were 1.2 times as far from 64 bits)
 // and moves only when the weights of 64 keys sum up to more than 2^40: weights, sums and outputs are
 // floating-point numbers, whose relative precision does not depend on it, and 2^40 is far from where they end.  So no step but the first
-// takes a maximum (9 % of the time of a long prompt).  Where they sum up to 2^100 and more, infinity included, that half step's scores, which
+// takes a maximum (9 % of the time of a long prompt).  (A row whose first scores are all -inf has the lowest float as its reference, so that
+// the first step with any other score moves it.)  Where they sum up to 2^100 and more, infinity included, that half step's scores, which
 // the weights have overwritten, are computed once more by the threads themselves.  Otherwise a reference moves by a
 // whole number: by powers of two, which round nothing.
 //
@@ -47,6 +48,7 @@ constexpr int kPromptPlans = 4;                               // tiles planned a
 constexpr int kPromptBufs = 3;                                // score tiles in TMEM
 constexpr int kPromptRefSlots = 4;
 constexpr float kPromptBig = 0x1p40f;                         // a reference moves when a half step's weights sum up to more
+constexpr float kPromptLowest = -3.402823466e38f;             // a reference below any score
 constexpr int kPromptOddSlots = 8;                            // more than tiles whose V can be under way at once (a step each)
 __host__ __device__ constexpr int prompt_k_stages(int D) { return D == 64 ? 6 : 3; }   // steps whose K, V are under way
 __host__ __device__ constexpr int prompt_v_stages(int D) { return D == 64 ? 6 : 3; }
@@ -624,7 +626,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     sm.other_ref[team][half][row] = top;
                     pair_sync();
                     top = fmaxf(top, sm.other_ref[team][half ^ 1][row]) * scale_log2;    // scale > 0
-                    m_ref = top == -INFINITY ? 0.f : top;              // (a row that sees nothing: any)
+                    // (-inf: so far the row sees nothing, or scores of -inf alone; the lowest reference there is, above which any score is
+                    // far, and the first step that has one moves it.  An overflow of the product with the scale ends there, too)
+                    m_ref = fmaxf(top, kPromptLowest);
                     if (half == 0) {
                         sm.first_ref[k & 1][row] = m_ref;
                         __syncwarp();

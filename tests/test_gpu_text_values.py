@@ -45,3 +45,25 @@ def test_decode_rows_whose_scores_are_all_minus_infinity(e4m3, Hq, Hkv, n):
     want, wl, tol, ltol = tu.attend(q[:1], kk, vv, torch.tensor([n - 1], device="cuda"), D ** -0.5)
     tu.assert_close(out[:1], want, tol, "out")
     tu.assert_lse(lse[:1], wl, ltol)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,total", [(700, 700), (40, 9000)])
+@pytest.mark.parametrize("level", [-3000.0, -30000.0, 0.0, 3000.0])
+def test_prompt_whose_first_scores_are_all_minus_infinity(D, new, total, level):
+    """The first 128 keys of every row (and some others) score minus infinity, those behind them far from zero: rows that see only the
+    former give zeros, the others what the rest of their keys gives."""
+    Hq, Hkv, g = 6, 2, torch.Generator().manual_seed(221)
+    q, k, v = draw(g, new, Hq, D), draw(g, total, Hkv, D), draw(g, total, Hkv, D)
+    k[:, :, :2], q[:, :, :2] = 0.0, 1.0
+    k[128:, :, 1] = level
+    hidden = torch.zeros(total, dtype=torch.bool, device="cuda")
+    hidden[:128] = True
+    hidden[200:270] = True
+    k[hidden, :, 0] = -math.inf
+    out, lse = tu.engine(Hq, Hkv, D).prompt(q, k, v, tu.cumulative([new]), tu.cumulative([total]), want_lse=True)
+    last = torch.arange(new, device="cuda") + total - new
+    seen = (~hidden).cumsum(0)[last] - 1                             # the last of the keys that are left
+    want, wl, tol, ltol = tu.attend(q, k[~hidden], v[~hidden], seen, D ** -0.5)
+    tu.assert_close(out, want, tol, "out")
+    tu.assert_lse(lse, wl, ltol)
