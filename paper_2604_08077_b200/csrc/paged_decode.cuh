@@ -399,6 +399,8 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                 }
             }
         }
+        // a factor above 1 (queries above 2^16) comes behind the keys' powers of two, which may be as far at the other end of the range
+        const bool large = kE4m3 && __any_sync(0xffffffffu, f[0] > 1.f || f[kGroups - 1] > 1.f);
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&sm.q_empty[qs]);
 
@@ -469,15 +471,24 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                         if (kE4m3) {
                             const uint32_t ks2 = *reinterpret_cast<const uint16_t*>(&sm.scale[st][0][row0 + nt * 8 + 2 * t4]);
                             const uint32_t vs2 = *reinterpret_cast<const uint16_t*>(&sm.scale[st][1][row0 + nt * 8 + 2 * t4]);
-                            kf[0] = __uint_as_float((ks2 & 0xffu) << 23);  // (byte 0 as zero: such a key is below 1e-35)
-                            kf[1] = __uint_as_float((ks2 >> 8) << 23);
+                            kf[0] = __uint_as_float(max((ks2 & 0xffu) << 23, 0x00400000u));   // (byte 0: 2^-127, a subnormal number)
+                            kf[1] = __uint_as_float(max((ks2 >> 8) << 23, 0x00400000u));
                             ve[nt][0] = (float)(int)(vs2 & 0xffu) - 127.f;
                             ve[nt][1] = (float)(int)(vs2 >> 8) - 127.f;
                         }
 #pragma unroll
                         for (int r = 0; r < kGroups; ++r)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) x[r][nt][e] = kE4m3 ? sc[nt][2 * r + e] * f[r] * kf[e] : sc[nt][2 * r + e] * f[r];
+                            for (int e = 0; e < 2; ++e) x[r][nt][e] = kE4m3 ? sc[nt][2 * r + e] * fminf(f[r], 1.f) * kf[e] : sc[nt][2 * r + e] * f[r];
+                    }
+                    if (kE4m3 && large) {
+#pragma unroll
+                        for (int r = 0; r < kGroups; ++r)
+#pragma unroll
+                            for (int nt = 0; nt < kNTiles; ++nt) {
+                                x[r][nt][0] *= fmaxf(f[r], 1.f);
+                                x[r][nt][1] *= fmaxf(f[r], 1.f);
+                            }
                     }
                 }
                 if (n_vis < kWarpKeys) {

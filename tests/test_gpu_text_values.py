@@ -67,3 +67,43 @@ def test_prompt_whose_first_scores_are_all_minus_infinity(D, new, total, level):
     want, wl, tol, ltol = tu.attend(q, k[~hidden], v[~hidden], seen, D ** -0.5)
     tu.assert_close(out, want, tol, "out")
     tu.assert_lse(lse, wl, ltol)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq", [7, 16])
+@pytest.mark.parametrize("byte", [0, 1, 6, 20])
+def test_decode_of_the_smallest_keys(D, Hq, byte):
+    """Keys at the small end of what 8-bit pages hold (s = 0 is a power of two as any other), against queries as far at the large one:
+    ordinary scores."""
+    g = torch.Generator().manual_seed(222)
+    page, n = 16, 200
+    per = -(-n // page)
+    cache = zero_cache(per, 1, page, D, True)
+    cache.k_pages.copy_((torch.randn(per, 1, page, D, generator=g) * 32).cuda().to(torch.float8_e4m3fn))
+    cache.v_pages.copy_((torch.randn(per, 1, page, D, generator=g) * 100).cuda().to(torch.float8_e4m3fn))
+    cache.k_scale.fill_(byte)
+    cache.v_scale.fill_(120)
+    table = torch.arange(per, dtype=torch.int32, device="cuda").view(1, per)
+    q = (torch.randn(1, Hq, D, generator=g).clamp(-3, 3) * 2.0 ** (122 - byte)).to(torch.bfloat16).cuda()
+    out, lse = tu.engine(Hq, 1, D).paged_decode(q, None, None, cache, table, ints(n), want_lse=True)
+    kk, vv = tu.sequence_values(cache, table, 0, n)
+    want, wl, tol, ltol = tu.attend(q, kk, vv, torch.tensor([n - 1], device="cuda"), D ** -0.5)
+    assert (wl - math.log(n)).abs().max() > 0.1                      # (the scores are not all zero)
+    tu.assert_close(out, want, tol, "out")
+    tu.assert_lse(lse, wl, ltol)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_of_zero_keys_and_queries_beside_the_largest(D):
+    """A score of zero is one whatever the powers of two around it."""
+    cache, table, n = zero_cache(1, 1, 16, D, True), torch.zeros(1, 1, dtype=torch.int32, device="cuda"), 9
+    cache.k_pages[:, :, :, 0] = 256.0
+    cache.v_pages.fill_(1.0)
+    cache.k_scale.fill_(247)
+    cache.v_scale.fill_(127)
+    q = torch.zeros(1, 3, D, dtype=torch.bfloat16, device="cuda")
+    q[0, 1:, 1] = 2.0 ** 127                                         # head 0: zeros; the others: at right angles to the keys
+    q[0, 2, 2] = 2.0 ** -100
+    out, lse = tu.engine(3, 1, D).paged_decode(q, None, None, cache, table, ints(n), want_lse=True)
+    assert (out == 1).all()
+    assert (lse - math.log(n)).abs().max() <= 2.0 ** -20
