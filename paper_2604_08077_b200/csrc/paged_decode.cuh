@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                     if (!kE4m3) mxv = mx;
                     if (__any_sync(0xffffffffu, mx > m[r] || mxv > mv[r])) {
                         const float nm = fmaxf(m[r], mx), nmv = fmaxf(mv[r], mxv);
-                        l[r] = m[r] == -INFINITY ? 0.f : l[r] * fast_exp2(m[r] - nm);
+                        if (m[r] != -INFINITY) l[r] *= fast_exp2(m[r] - nm);   // (else it is zero, or no number and stays that)
                         const float c = mv[r] == -INFINITY ? 0.f : fast_exp2(mv[r] - nmv);
                         // of heads 2 t4 and 2 t4 + 1, the columns of O^T
                         const float c0 = __shfl_sync(0xffffffffu, c, 8 * t4), c1 = __shfl_sync(0xffffffffu, c, 8 * t4 + 4);

@@ -107,3 +107,23 @@ def test_decode_of_zero_keys_and_queries_beside_the_largest(D):
     out, lse = tu.engine(3, 1, D).paged_decode(q, None, None, cache, table, ints(n), want_lse=True)
     assert (out == 1).all()
     assert (lse - math.log(n)).abs().max() <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("n", [40, 300, 6000])
+def test_decode_keys_that_are_no_numbers_show_in_the_logarithm(e4m3, n):
+    """A whole first stretch of keys that are no numbers, ordinary ones behind them: neither the outputs nor the sum is a number."""
+    g = torch.Generator().manual_seed(223)
+    Hq, Hkv, D, page = 8, 2, 128, 16
+    per = -(-n // page)
+    cache, eng = zero_cache(per, Hkv, page, D, e4m3), tu.engine(Hq, Hkv, D)
+    table, kv_len = torch.arange(per, dtype=torch.int32, device="cuda").view(1, per), ints(n)
+    k, v, q = draw(g, n, Hkv, D), draw(g, n, Hkv, D), draw(g, 1, Hq, D)
+    k[:32, 0, 5] = math.nan                                          # (all that a warp has of the first tile)
+    eng.paged_write(cache, k, v, tu.cumulative([n]), table, kv_len)
+    out, lse = eng.paged_decode(q, None, None, cache, table, kv_len, want_lse=True)
+    assert torch.isnan(out[0, :4]).all() and torch.isnan(lse[0, :4]).all()
+    kk, vv = tu.sequence_values(cache, table, 0, n)
+    want, wl, tol, ltol = tu.attend(q[:, 4:], kk[:, 1:], vv[:, 1:], torch.tensor([n - 1], device="cuda"), D ** -0.5)
+    tu.assert_close(out[:, 4:], want, tol, "out")
+    tu.assert_lse(lse[:, 4:], wl, ltol)
