@@ -425,7 +425,8 @@ adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t *handle, const adaspa
 /* One new token per sequence: the row q of sequence b attends the tokens 0 .. kv_len[b] - 1 of its pages.
  * kv_len 0 marks a slot of the batch without a sequence (nothing is appended).  Where kv_len is negative or more than the table
  * holds, or a page number among the tokens is outside [0, n_pages), status is set to 1 and nothing is appended into a place that is
- * not there; the row becomes zeros (lse: -infinity), as it does with kv_len 0, and where every score is -infinity.
+ * not there (the new token is written if its own is, whatever the other pages); the row becomes zeros (lse: -infinity), as it does
+ * with kv_len 0, and where every score is -infinity.
  * Two sequences may share pages that neither of them appends to. */
 typedef struct {
     adaspark_attn_pages_t pages;

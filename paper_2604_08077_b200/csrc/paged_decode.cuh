@@ -324,11 +324,14 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                         sm.bad[part & 3] = part + 1;
                         if (a.status != nullptr) atomicExch(a.status, 1);
                     }
-                } else if (a.k_new != nullptr && tile == w.tiles - 1) {    // the new token: the last of this tile
+                }
+                if (a.k_new != nullptr && tile == w.tiles - 1) {           // the new token: the last of this tile
                     const int pg = __shfl_sync(0xffffffffu, page, boxes - 1), place = (w.n - 1) & (page_size - 1);
-                    append_rows<D, kE4m3>(p, pg, w.gk, place, new_k, new_v, lane);
-                    asm volatile("fence.proxy.async;\n" ::: "memory");    // it is read by the copies below
-                    __syncwarp();
+                    if (pg >= 0 && pg < p.n_pages) {                       // (whatever the other pages are)
+                        append_rows<D, kE4m3>(p, pg, w.gk, place, new_k, new_v, lane);
+                        asm volatile("fence.proxy.async;\n" ::: "memory");    // it is read by the copies below
+                        __syncwarp();
+                    }
                 }
                 if (!(ok = tc::mbar_wait_warp(&sm.empty[st], ph, abort_flag))) break;
                 if (lane == 0) tc::mbar_arrive_expect_tx(&sm.full[st], (uint32_t)(boxes * sub * 2 * (kRowBytes + (kE4m3 ? 1 : 0))));

@@ -127,3 +127,25 @@ def test_decode_keys_that_are_no_numbers_show_in_the_logarithm(e4m3, n):
     want, wl, tol, ltol = tu.attend(q[:, 4:], kk[:, 1:], vv[:, 1:], torch.tensor([n - 1], device="cuda"), D ** -0.5)
     tu.assert_close(out[:, 4:], want, tol, "out")
     tu.assert_lse(lse[:, 4:], wl, ltol)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_decode_appends_where_only_an_earlier_page_is_missing(e4m3):
+    """The new token is written wherever its own place is there, whether the page that is not there lies in the same tile or in another."""
+    g = torch.Generator().manual_seed(224)
+    Hq, Hkv, D, page = 4, 2, 64, 16
+    cache, eng = zero_cache(64, Hkv, page, D, e4m3), tu.engine(Hq, Hkv, D)
+    table = torch.arange(60, dtype=torch.int32, device="cuda").view(3, 20)
+    lens = [40, 300, 40]
+    table[0, 0], table[1, 0], table[2, 2] = -1, 64, 64               # the tile of the new token | another tile | the new token's own page
+    k, v, q = draw(g, 3, Hkv, D), draw(g, 3, Hkv, D), draw(g, 3, Hq, D)
+    before = [x.clone() for x in tu.page_values(cache)]
+    out, lse = eng.paged_decode(q, k, v, cache, table, ints(*lens), want_lse=True)
+    assert eng.text_status() == 1
+    assert (out == 0).all() and (lse == -math.inf).all()
+    for was, now, x in zip(before, tu.page_values(cache), (k, v)):
+        for b in (0, 1):
+            pg, pl = int(table[b, (lens[b] - 1) // page]), (lens[b] - 1) % page
+            assert torch.equal(now[pg, :, pl], tu.quantise(x[b])[0] if e4m3 else x[b].double())
+            was[pg, :, pl] = now[pg, :, pl]
+        assert torch.equal(was, now)
