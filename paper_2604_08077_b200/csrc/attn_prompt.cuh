@@ -8,8 +8,9 @@
 // floating-point numbers, whose relative precision does not depend on it, and 2^40 is far from where they end.  So no step but the first
 // takes a maximum (9 % of the time of a long prompt).  (A row whose first scores are all -inf has the lowest float as its reference, so that
 // the first step with any other score moves it.)  Where they sum up to 2^100 and more, infinity included, that half step's scores, which
-// the weights have overwritten, are computed once more by the threads themselves.  Otherwise a reference moves by a
-// whole number: by powers of two, which round nothing.
+// the weights have overwritten, are computed once more by the threads themselves.  A reference moves by a
+// whole number: the weights that stand are multiplied by a power of two, which rounds nothing (a second rounding took outputs of two keys
+// near 2^100 past the bound of one).
 //
 // Work is dealt out in tiles of 256 rows, a CTA pair (cta_group::2) each: the rows are (token, head of the group) pairs, 128 / G tokens
 // per CTA, so that K and V are read once for all heads of a group, a sequence of a few tokens fills rows that it would leave empty head by
@@ -688,7 +689,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     const __nv_bfloat16* keys = g.k + (long long)(t.k0 + key0) * g.k_ts + t.gk * g.k_hs;
                     float mine = ref;
                     if (over && !lost) mine += ceilf(log2f(l_step));
-                    for (int i = 0; i < n_keys; ++i) mine = fmaxf(mine, ceilf(prompt_dot<D>(q_row, keys + i * g.k_ts) * scale_log2));
+                    for (int i = 0; i < n_keys; ++i) mine = fmaxf(mine, prompt_dot<D>(q_row, keys + i * g.k_ts) * scale_log2);
+                    // up by a whole number, as above; so far (or from the lowest reference) that what stood before is zero: to the score itself
+                    if (lost && mine - ref < 512.f) mine = ref + ceilf(mine - ref);
                     sm.other_ref[team][half][row] = mine;
                     pair_sync();
                     m_new = fmaxf(m_prev, fmaxf(mine, sm.other_ref[team][half ^ 1][row]));

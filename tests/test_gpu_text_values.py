@@ -149,3 +149,35 @@ def test_decode_appends_where_only_an_earlier_page_is_missing(e4m3):
             assert torch.equal(now[pg, :, pl], tu.quantise(x[b])[0] if e4m3 else x[b].double())
             was[pg, :, pl] = now[pg, :, pl]
         assert torch.equal(was, now)
+
+
+# (first, k0, k1) of a head, each a pair of bf16 numbers whose sum is the score: the largest of the first 128 keys, and one key in
+# each half of the second 128, just below and above 2^100 times its weight.  Chosen so that a second rounding of the one's weight shows.
+BOTH_HALVES = [
+    (7.65625, -0.003936767578125, 77.0, -0.05859375, 77.0, -0.003814697265625), (18.0, 0.04150390625, 87.5, -0.1533203125, 87.5, -0.12890625),
+    (2.125, -0.0023956298828125, 71.5, -0.08837890625, 71.5, -0.056640625), (8.375, -0.02587890625, 77.5, 0.150390625, 77.5, 0.1669921875),
+    (18.75, 0.0274658203125, 88.0, 0.0625, 88.0, 0.09375), (26.375, 0.0302734375, 95.5, 0.1982421875, 95.5, 0.2333984375),
+    (33.25, 0.07666015625, 102.5, 0.095703125, 102.5, 0.1572265625), (36.75, 0.001983642578125, 106.0, 0.056884765625, 106.0, 0.09375),
+    (34.75, -0.06494140625, 104.0, -0.0257568359375, 104.0, 0.04345703125), (7.6875, -0.006927490234375, 77.0, -0.054931640625, 77.0, 0.01129150390625),
+    (36.75, 0.0966796875, 106.0, 0.10302734375, 106.0, 0.166015625), (18.75, 0.0311279296875, 88.0, 0.06591796875, 88.0, 0.1015625),
+    (22.25, -0.01348876953125, 91.5, 0.0010223388671875, 91.5, 0.095703125), (39.5, 0.0830078125, 109.0, -0.1279296875, 109.0, -0.09716796875),
+    (18.75, 0.0150146484375, 88.0, 0.0703125, 88.0, 0.08642578125), (28.5, -0.00494384765625, 98.0, -0.2001953125, 98.0, -0.1728515625)]
+
+
+def test_prompt_weights_are_rounded_once_when_both_halves_move_the_reference():
+    """Scores of two exact products each, so that only these errors are left: 2^-22 of the score (its scale, its reference), 2^-17 for
+    the exponential, both twice (numerator and sum), 2^-8 of a weight where it is rounded for the product with V, 2^-8 of the output."""
+    H, D, n = len(BOTH_HALVES), 64, 256
+    pairs = torch.tensor(BOTH_HALVES, dtype=torch.float64, device="cuda")
+    q, k, v = (torch.zeros(r, H, D, dtype=torch.bfloat16, device="cuda") for r in (1, n, n))
+    q[..., :2] = 1.0
+    for at, (x, value) in {60: (0, 0.0), 150: (2, 1.0), 230: (4, -1.0)}.items():
+        k[at, :, :2] = pairs[:, x:x + 2].to(torch.bfloat16)
+        v[at] = value
+    assert torch.equal(k[230, :, :2].double(), pairs[:, 4:])
+    out, _ = tu.engine(H, H, D, softmax_scale=1.0).prompt(q, k, v, tu.cumulative([1]), tu.cumulative([n]))
+    logits = k[..., :2].double().sum(-1)
+    w = torch.softmax(logits, 0)
+    want = (w[150] - w[230])[:, None]
+    tol = 2.0 ** -8 * want.abs() + 2.0 ** -8 + 2 * (2.0 ** -22 * logits[230, :, None] + 2.0 ** -17)
+    tu.assert_close(out[0], want.expand(H, D), tol.expand(H, D), "out")
