@@ -407,7 +407,9 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t *handle, const adaspark_a
 /* Keys and values of packed rows and their places in the pages: row cu[b] + i of sequence b is token
  * kv_len[b] - (cu[b+1] - cu[b]) + i.
  * _write puts the rows k, v into their places.  A row without a place (before token 0, behind the table, page number outside
- * [0, n_pages)) is not written and sets status 1.  Two rows with the same place in one call: either may win.
+ * [0, n_pages)) is not written and sets status 1.  The rows of one call need places of their own (a page that two sequences
+ * write to, or that a table lists twice among the tokens written, has others): two rows with the same place may leave a mixture of
+ * both there, codes of one with the power of two of the other among them, and nothing reports it.  Other places are not affected.
  * _read gets the last cu[b+1] - cu[b] tokens of every sequence back into the rows k, v.  Exact: every value that a page holds
  * is a bf16 number.  A row without a place becomes zeros and sets status 1.
  * A sequence whose rows leave the tensors (cu[b] < 0, cu[b+1] < cu[b] or > n) sets status 1, and its rows have no place; the others are

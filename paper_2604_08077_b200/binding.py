@@ -601,7 +601,7 @@ class AdaSAttn:
 
     def paged_write(self, cache: PagedCache, k, v, cu, block_table, kv_len, *, stream=None):
         """Packed keys and values into the pages: the rows cu[b] .. cu[b + 1] - 1 become the last tokens of sequence b, which
-        then holds kv_len[b].  block_table int32 [batch, width]."""
+        then holds kv_len[b].  block_table int32 [batch, width].  No two rows of a call may have the same place: it would hold a mixture."""
         self._paged_rows(adaspark_attn_paged_write, cache, k, v, cu, block_table, kv_len, stream)
 
     def paged_read(self, cache: PagedCache, cu, block_table, kv_len, k_out, v_out, *, stream=None):

@@ -79,3 +79,24 @@ def test_many_sequences_one_of_them_out_of_range():
         assert eng.text_status() == 1, at
     eng.paged_write(cache, k, v, torch.tensor([1] * B + [2], dtype=torch.int32, device="cuda"), table, lens)
     assert eng.text_status() == 0
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_rows_with_the_same_place_leave_the_others_alone(e4m3):
+    """Such a place holds a mixture; every other one what belongs there, and nothing else is written."""
+    cache, k, v, _ = make(e4m3)
+    eng = tu.engine(2 * HKV, HKV, D)
+    table = torch.tensor([[3], [3], [5], [3], [7]], dtype=torch.int32, device="cuda")       # three sequences write to page 3
+    cu, kv_len = tu.cumulative([1, 2, 10, 4, 16]), torch.tensor([4, 4, 10, 4, 16], dtype=torch.int32, device="cuda")
+    before = raw(cache)
+    eng.paged_write(cache, k, v, cu, table, kv_len)
+    assert eng.text_status() == 0
+    held = [(i, int(table[b, 0]), int(kv_len[b]) - (int(cu[b + 1]) - i)) for b in (2, 4) for i in range(int(cu[b]), int(cu[b + 1]))]
+    held += [(13, 3, 0), (14, 3, 1)]                                     # (the fourth sequence's first two rows have places of their own)
+    row, page, place = (torch.tensor([h[x] for h in held], dtype=torch.long, device="cuda") for x in range(3))
+    for x, values in zip((k, v), tu.page_values(cache)):
+        assert torch.equal(values[page, :, place], tu.quantise(x[row])[0] if e4m3 else x[row].double())
+    for was, now in zip(before, raw(cache)):
+        now[page, :, place] = was[page, :, place]
+        now[3, :, 2:4] = was[3, :, 2:4]
+        assert torch.equal(was, now)
