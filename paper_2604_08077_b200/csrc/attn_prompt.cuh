@@ -838,6 +838,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     }
     // ---------------------------------------------------------------- teardown
     __syncwarp();
+    tc::settle_after_abort(abort_flag);
+    __syncwarp();
     tc::tc_fence_before_sync();
     cluster_sync();                                           // nothing of the other CTA reaches this one any more
     if (tid == 0 && sm.abort_flag && status != nullptr) atomicExch(status, 6);   // a bounded wait expired

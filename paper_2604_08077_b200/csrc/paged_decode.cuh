@@ -679,6 +679,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
         if (tid == 0 && n != 0 && a.status != nullptr) atomicExch(a.status, 1);
     }
     if (tid == 0 && sm.abort_flag && a.status != nullptr) atomicExch(a.status, 6);
+    tc::settle_after_abort(abort_flag);                       // (the producer has stopped, or finds the flag at its next wait)
 }
 
 // Joins what is cut.  Many (sequence, kv head)s: grid (runs - 1), CTA i joins the one that is cut by the end of run i and has its first tile in

@@ -79,6 +79,15 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
     return true;
 }
 
+// In front of a CTA's end, after a wait has expired: copies and products that were under way when the waiting stopped land in its shared
+// and tensor memory, which must not be given up before.  They take microseconds; nothing new is started any more.
+constexpr uint64_t kSettleNs = 1000000ull;
+__device__ __forceinline__ void settle_after_abort(volatile int* abort_flag) {
+    if (*abort_flag == 0) return;
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < kSettleNs) {}
+}
+
 // ------------------------------------------------------------------------------- TMA (tiled, 2-D)
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap* tm) {
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
