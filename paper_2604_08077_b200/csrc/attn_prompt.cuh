@@ -50,6 +50,9 @@ constexpr int kPromptBufs = 3;                                // score tiles in 
 constexpr int kPromptRefSlots = 4;
 constexpr float kPromptBig = 0x1p40f;                         // a reference moves when a half step's weights sum up to more
 constexpr float kPromptLowest = -3.402823466e38f;             // a reference below any score
+// A planner that walks past levels of a long prompt looks at every sequence for each: 16 ns a sequence and level, 150 levels and more from one of
+// a pair's tiles to its next (where a level has one tile).  Waits for its plans last so much longer.
+constexpr uint64_t kPromptPlanNs = 10000;                     // a sequence
 constexpr int kPromptOddSlots = 8;                            // more than tiles whose V can be under way at once (a step each)
 __host__ __device__ constexpr int prompt_k_stages(int D) { return D == 64 ? 6 : 3; }   // steps whose K, V are under way
 __host__ __device__ constexpr int prompt_v_stages(int D) { return D == 64 ? 6 : 3; }
@@ -300,6 +303,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     tc::tc_fence_after_sync();
     const uint32_t tbase = sm.tmem_base;
     volatile int* abort_flag = &sm.abort_flag;
+    const uint64_t plan_limit = tc::kWaitLimitNs + (uint64_t)g.batch * kPromptPlanNs;
 
     if (warp == kPlanWarp) {
         // ------------------------------------------------------------ planner
@@ -434,7 +438,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             } else if ((++idle & 0xff) == 0) {                // bounded, as every wait
                 const uint64_t now = tc::global_timer_ns();
                 if (idle == 0x100) since = now;
-                if (now - since > tc::kWaitLimitNs) *abort_flag = 1;
+                if (now - since > plan_limit) *abort_flag = 1;
                 if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
             }
         }
@@ -446,7 +450,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             bool ok = true;
             for (int k = 0; ok; ++k) {
                 const int slot = k % kPromptPlans;
-                if (!(ok = tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag))) break;
+                if (!(ok = tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
                 const int n_steps = sm.tile[slot].n_steps, k0 = sm.tile[slot].k0, gk = sm.tile[slot].gk, first_masked = sm.tile[slot].first_masked;
                 if (n_steps == 0) break;
                 for (int j = 0; j < n_steps; ++j) {
@@ -469,7 +473,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         if (lane == 0) {
             for (int k = 0;; ++k) {
                 const int slot = k % kPromptPlans;
-                if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag) || sm.tile[slot].n_steps == 0) break;
+                if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit) || sm.tile[slot].n_steps == 0) break;
                 if (!tc::mbar_wait(&sm.q_full[k & 1], (k >> 1) & 1, abort_flag)) break;
                 asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
                 tc::mbar_arrive_cluster(cluster_address(&sm.q_peer[k & 1], 0));
@@ -496,7 +500,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 if (s_left == 0) {
                     if (ended) return false;
                     const int kn = ks + 1, slot = kn % kPromptPlans;
-                    auto there = [&](uint64_t* bar, uint32_t phase) -> bool { return must ? (ok = tc::mbar_wait(bar, phase, abort_flag)) : tc::mbar_test(bar, phase); };
+                    auto there = [&](uint64_t* bar, uint32_t phase) -> bool { return must ? (ok = tc::mbar_wait(bar, phase, abort_flag, plan_limit)) : tc::mbar_test(bar, phase); };
                     if (!there(&sm.plan_full[slot], (kn / kPromptPlans) & 1)) return false;
                     if ((ended = sm.tile[slot].n_steps == 0)) return false;
                     if (!there(&sm.q_full[kn & 1], (kn >> 1) & 1) || !there(&sm.q_peer[kn & 1], (kn >> 1) & 1)) return false;
@@ -577,7 +581,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         // loops end with the tile (further waits return quickly).
         for (int k = 0;; ++k) {
             const int slot = k % kPromptPlans;
-            if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag)) ok = false;
+            if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit)) ok = false;
             if (pair_any(!ok)) break;
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
