@@ -346,7 +346,8 @@ adaspark_status_t adaspark_attn_set_gather(adaspark_attn_t *handle, float pairs_
  *     least head_dim; 0: dense), so that slices of a fused projection or head-major tensors are read where they are; 16-byte
  *     aligned.  Outputs are dense.
  *   - Packed sequences: cu is device int32 [batch + 1], not decreasing; sequence b is the rows cu[b] .. cu[b+1] - 1 and may be
- *     empty.  Rows of the tensors that belong to no sequence (in front of cu[0], behind cu[batch]) are neither read nor written.
+ *     empty.  Rows of the tensors that belong to no sequence (in front of cu[0], behind cu[batch]) are not written, and what they
+ *     hold does not matter.
  *   - kv_len is device int32 [batch]: tokens of each sequence INCLUDING those of this call.  block_table is device int32
  *     [batch][table_width]: the page of tokens [c * page_size, (c + 1) * page_size) in column c; columns behind the last
  *     token are not read.
@@ -429,7 +430,8 @@ adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t *handle, const adaspa
  * holds, or a page number among the tokens is outside [0, n_pages), status is set to 1 and nothing is appended into a place that is
  * not there (the new token is written if its own is, whatever the other pages); the row becomes zeros (lse: -infinity), as it does
  * with kv_len 0, and where every score is -infinity.
- * Two sequences may share pages that neither of them appends to. */
+ * Two sequences may share pages that neither of them appends to.
+ * With 8-bit pages a row of q is held to 2^-28 of its largest magnitude: what is smaller there loses bits. */
 typedef struct {
     adaspark_attn_pages_t pages;
     adaspark_attn_rows_t q;            /* batch rows of Hq heads                                       */

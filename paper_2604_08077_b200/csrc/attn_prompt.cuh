@@ -26,9 +26,10 @@
 //   warp  19    planner: the next tiles and their Q
 // TMEM (512 columns): three score tiles of 128 columns, each with the weights (bf16 pairs) over the first 32 of either half, and O.  The
 // waits are those of the prefill kernel (attn_prefill_tc.cuh): the issuer never waits for a tile that it has not begun while a product of
-// an earlier one is still to be issued.  What bounds a step is the chain scores -> weights -> product of its score tile: 512 + 512 cycles of
-// tensor core, about 300 between the last of them and the softmax, 2000 to 2200 of softmax, shared with the other team's.  (Three warpgroups with a
-// row each per thread: 2400 of softmax, chains 10 % longer.)
+// an earlier one is still to be issued.  A step takes 0.9 to 1.0 us (head_dim 64: 0.73) and a tile about 2 us beside its steps, fitted over calls of
+// 9 to 33 tiles a pair with 1.4 to 18 steps each: 512 + 512 cycles of a step's 1800 at full clock are products (head_dim 64: half as many of
+// 1400), the others the softmax's share of the chain scores -> weights -> product, which three score tiles and two teams work on at a time.
+// (Three warpgroups with a row each per thread: 10 % longer.)
 //
 // Tiles are dealt longest first and back and forth over the pairs of CTAs.  Every planner works the order out for itself from cu_q and
 // cu_k, level by level of the number of steps: no list in memory, no counter, one launch, and nothing to be cleared before it.

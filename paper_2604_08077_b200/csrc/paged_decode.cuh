@@ -18,7 +18,8 @@
 // 8-bit pages go through the tensor cores as f16, which holds every e4m3 value.  q is brought to f16 by a power of two per row (largest
 // magnitude 2^14 ..: what falls below 2^-28 of it loses bits, 2^-39 of it at most); a key's power of two multiplies its score.  A value's
 // power of two e_j joins its weight: the weights of the product are 2^(x_j + e_j - m') with their own maximum m', so that they stay
-// within f16 whatever the rows' sizes, and beside them the sum of 2^(x_j - m) is kept.  (K as e4m3 against q in two e4m3 parts: no faster, the
+// within f16 whatever the rows' sizes, and beside them the sum of 2^(x_j - m) is kept.  A score is multiplied by the powers of two of q and key
+// one after the other, the one below 1 first where q is large: they may lie at opposite ends of the range.  (K as e4m3 against q in two e4m3 parts: no faster, the
 // legacy 8-bit products are converted, too, and half as fast with more than 8 heads.)
 #pragma once
 #include "common.cuh"
@@ -33,7 +34,7 @@ constexpr int kPagedRing = 96 * 1024;        // bytes of a CTA's ring
 // What a part costs beside its tiles, in tiles (24 sequences of up to 8192 tokens, bf16, at 0 / 1 / 2 / 3: 35.9 / 28.7 / 25.2 / 24.2 us, 128 of 20 to
 // 1000 at 2 / 3: 30.4 / 31.4; 64 of 16 to 8192 in 8 bits, tiles of twice the keys, at 1 / 2 / 4: 39.7 / 40.5 / 43.2).
 __host__ __device__ constexpr int paged_part_cost(int tile) { return tile == 64 ? 2 : 1; }
-constexpr int kPagedFewSequences = 16;       // up to so many (sequence, kv head)s: at least 18 runs each, a CTA joins a row
+constexpr int kPagedFewSequences = 16;       // up to so many (sequence, kv head)s, 18 runs each on average where there are tiles enough: a CTA joins a row
 constexpr float kPagedBias = 14.f;           // f16 weights are at most 2^14: 2^-28 of the largest one is still a normal number
 
 __host__ __device__ constexpr int paged_tile(bool e4m3) { return e4m3 ? 128 : 64; }   // keys of a tile
