@@ -447,6 +447,81 @@ typedef struct {
 } adaspark_attn_paged_decode_t;
 adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t *handle, const adaspark_attn_paged_decode_t *call, void *cuda_stream);
 
+/* The same with a window: the new token, at position p = kv_len[b] - 1, sees the tokens j <= p with j > p - window or j < sinks.
+ * Pages that hold nothing that it sees are not read, and their numbers may be any (they may have been given back). */
+typedef struct {
+    adaspark_attn_paged_decode_t step;
+    int32_t window, sinks;             /* window >= 1, sinks >= 0                                      */
+} adaspark_attn_paged_decode_window_t;
+adaspark_status_t adaspark_attn_paged_decode_window(adaspark_attn_t *handle, const adaspark_attn_paged_decode_window_t *call, void *cuda_stream);
+
+/* Several new tokens per sequence, whose keys and values are in its pages already (adaspark_attn_paged_append, _paged_write): row
+ * cu[b] + i of sequence b is token p = kv_len[b] - (cu[b+1] - cu[b]) + i and sees the tokens j <= p; with window > 0 those of them with j >
+ * p - window or j < sinks.  Rows, masks, precision and what a row that sees nothing yields are those of adaspark_attn_prompt (what
+ * 8-bit pages hold are bf16 numbers: the result is that of adaspark_attn_prompt over what adaspark_attn_paged_read gives).
+ * Pages that hold nothing that a row of the sequence sees are not read, and their numbers may be any; a page number outside [0, n_pages) among the
+ * others sets status 1, and what such a page would hold counts as zeros.  A sequence whose rows leave the tensors sets
+ * status 1 and is left out; one whose kv_len is negative or more than the table holds sets status 1, and its rows become rows that see
+ * nothing, as do rows in front of token 0 (kv_len[b] < cu[b+1] - cu[b], status 1). */
+typedef struct {
+    adaspark_attn_pages_t pages;
+    adaspark_attn_rows_t q;            /* n rows of Hq heads                                           */
+    const int32_t *cu, *kv_len, *block_table;
+    void *out;                         /* bf16 [n][Hq][head_dim]                                       */
+    float *lse;                        /* nullable: fp32 [n][Hq], as adaspark_attn_prompt              */
+    void *workspace;
+    int64_t workspace_bytes;
+    int32_t *status;
+    int32_t batch, n, table_width;
+    int32_t window, sinks;             /* window 0: none (sinks says nothing then)                     */
+    int32_t reserved;
+} adaspark_attn_paged_prompt_t;
+adaspark_status_t adaspark_attn_paged_prompt(adaspark_attn_t *handle, const adaspark_attn_paged_prompt_t *call, void *cuda_stream);
+
+/* A rotation by positions.  Pair i of a head, values (a, b), becomes (a cos t - b sin t, b cos t + a sin t) with t = radians[i] times the
+ * token's position on axis[i]; pairs are the values (i, i + pairs) of a head, or (2 i, 2 i + 1) if adjacent; values behind the first 2 *
+ * pairs are not rotated.  pairs is a multiple of 8, up to head_dim / 2 (of the handle that it is used with; 64 at most).
+ * _rotary_init fills the struct on the host (axis NULL: all on axis 0); angles are kept as 64-bit fractions of a whole turn, so
+ * that a position of 31 bits, of either sign, loses nothing that 32-bit outputs show.  ERR_INVALID_ARG: a frequency that is no finite number, an axis outside
+ * [0, axes), a number of pairs that is none. */
+typedef struct {
+    uint64_t turns[64];                /* of pair i per position: fraction of a turn, times 2^64       */
+    uint8_t axis[64];
+    int32_t pairs, axes, adjacent, reserved;
+} adaspark_attn_rotary_t;
+adaspark_status_t adaspark_attn_rotary_init(adaspark_attn_rotary_t *rotary, const double *radians, const int32_t *axis, int32_t pairs,
+                                            int32_t axes, int32_t adjacent);
+
+/* Queries and keys between the projection and the attention: every head is divided by the root of its mean square plus eps and multiplied by
+ * the norm's weights (where they are given), then rotated (where a rotation is given).  In 32 bits, rounded once.
+ * An output may be the very rows of its input; otherwise it must not overlap them. */
+typedef struct {
+    adaspark_attn_rows_t q, k;         /* n rows of Hq, Hkv heads; data NULL: none                     */
+    adaspark_attn_rows_t q_out, k_out;
+    const int32_t *positions;          /* device [axes][n], any sign; NULL if nothing is rotated       */
+    const adaspark_attn_rotary_t *rotary;   /* host, nullable                                          */
+    const void *q_norm, *k_norm;       /* device bf16 [head_dim], 16-byte aligned, nullable            */
+    float eps;                         /* >= 0                                                         */
+    int32_t n;
+} adaspark_attn_rotate_t;
+adaspark_status_t adaspark_attn_rotate(adaspark_attn_t *handle, const adaspark_attn_rotate_t *call, void *cuda_stream);
+
+/* adaspark_attn_rotate on the way into a cache: rotated queries to q_out, rotated keys and the values into their pages (8-bit pages: the keys'
+ * codes are rounded from 32 bits, once).  Rows and places as adaspark_attn_paged_write.  Rows of no sequence are not written; a row
+ * without a place sets status 1, is not stored, and its queries become zeros.  positions NULL: a token's place in its sequence, on all axes. */
+typedef struct {
+    adaspark_attn_pages_t pages;
+    adaspark_attn_rows_t q, k, v;      /* n rows; q.data NULL: no queries                              */
+    adaspark_attn_rows_t q_out;
+    const int32_t *cu, *kv_len, *block_table, *positions;
+    const adaspark_attn_rotary_t *rotary;
+    const void *q_norm, *k_norm;
+    int32_t *status;
+    float eps;
+    int32_t batch, n, table_width;
+} adaspark_attn_paged_append_t;
+adaspark_status_t adaspark_attn_paged_append(adaspark_attn_t *handle, const adaspark_attn_paged_append_t *call, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

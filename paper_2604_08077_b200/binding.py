@@ -43,6 +43,16 @@ _PAGES = struct.Struct("4Q2q4i")          # adaspark_attn_pages_t
 _PROMPT = struct.Struct("QqqQqqQqq5QqQ4i")  # adaspark_attn_prompt_t
 _PAGED_ROWS = struct.Struct("QqqQqq4Q4i")   # adaspark_attn_paged_rows_t behind its pages
 _PAGED_DECODE = struct.Struct("QqqQqqQqq5QqQ2i")   # adaspark_attn_paged_decode_t behind its pages
+_WINDOW = struct.Struct("2i")               # adaspark_attn_paged_decode_window_t behind its step
+_PAGED_PROMPT = struct.Struct("Qqq6QqQ6i")  # adaspark_attn_paged_prompt_t behind its pages
+_ROTATE = struct.Struct("QqqQqqQqqQqq4Qfi")  # adaspark_attn_rotate_t
+_PAGED_APPEND = struct.Struct("QqqQqqQqqQqq8Qf3i")   # adaspark_attn_paged_append_t behind its pages
+
+
+class RotaryStruct(ctypes.Structure):
+    """adaspark_attn_rotary_t."""
+    _fields_ = [("turns", ctypes.c_uint64 * 64), ("axis", ctypes.c_uint8 * 64), ("pairs", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("adjacent", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class AdasparkError(RuntimeError):
@@ -59,7 +69,8 @@ EXPORTS = ["adaspark_attn_create", "adaspark_attn_partition", "adaspark_attn_get
            "adaspark_attn_set_prefill_kernel", "adaspark_attn_set_gather", "adaspark_attn_enable_stage_timing",
            "adaspark_attn_get_stage_times", "adaspark_attn_get_attention_kernel_ms", "adaspark_attn_decode_static",
            "adaspark_attn_text_workspace_bytes", "adaspark_attn_prompt", "adaspark_attn_paged_write",
-           "adaspark_attn_paged_read", "adaspark_attn_paged_decode",
+           "adaspark_attn_paged_read", "adaspark_attn_paged_decode", "adaspark_attn_paged_decode_window",
+           "adaspark_attn_paged_prompt", "adaspark_attn_rotary_init", "adaspark_attn_rotate", "adaspark_attn_paged_append",
            "adaspark_attn_debug_umma_selftest", "adaspark_attn_debug_imma_selftest",
            "adaspark_attn_debug_fastdiv", "adaspark_attn_debug_wait_timeout"]
 
@@ -100,7 +111,8 @@ def load() -> ctypes.CDLL:
     lib.adaspark_attn_get_attention_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
     lib.adaspark_attn_text_workspace_bytes.argtypes = [vp]
     lib.adaspark_attn_text_workspace_bytes.restype = ctypes.c_int64
-    for name in ("prompt", "paged_write", "paged_read", "paged_decode"):
+    lib.adaspark_attn_rotary_init.argtypes = [ctypes.POINTER(RotaryStruct), ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32), i32, i32, i32]
+    for name in ("prompt", "paged_write", "paged_read", "paged_decode", "paged_decode_window", "paged_prompt", "rotate", "paged_append"):
         getattr(lib, "adaspark_attn_" + name).argtypes = [vp, ctypes.c_char_p, vp]
     for name in EXPORTS:
         if name not in ("adaspark_attn_last_error", "adaspark_attn_last_launch_count", "adaspark_attn_text_workspace_bytes"):
@@ -314,6 +326,48 @@ def adaspark_attn_paged_decode(handle: int, q, k_new, v_new, pages: bytes, block
         _check(handle, st)
 
 
+def adaspark_attn_paged_decode_window(handle: int, q, k_new, v_new, pages: bytes, block_table, table_width: int, kv_len, batch: int, out, lse,
+                                      workspace, workspace_bytes: int, status, window: int, sinks: int, stream: Optional[int]):
+    st = (_lib or load()).adaspark_attn_paged_decode_window(handle, pages + _PAGED_DECODE.pack(
+        *q, *k_new, *v_new, kv_len or 0, block_table or 0, out or 0, lse or 0, workspace or 0, workspace_bytes, status or 0, batch, table_width) +
+        _WINDOW.pack(window, sinks), stream)
+    if st != OK:
+        _check(handle, st)
+
+
+def adaspark_attn_paged_prompt(handle: int, q, pages: bytes, cu, batch: int, n: int, block_table, table_width: int, kv_len, window: int, sinks: int,
+                               out, lse, workspace, workspace_bytes: int, status, stream: Optional[int]):
+    st = (_lib or load()).adaspark_attn_paged_prompt(handle, pages + _PAGED_PROMPT.pack(
+        *q, cu or 0, kv_len or 0, block_table or 0, out or 0, lse or 0, workspace or 0, workspace_bytes, status or 0, batch, n, table_width, window, sinks, 0), stream)
+    if st != OK:
+        _check(handle, st)
+
+
+def adaspark_attn_rotary_init(radians, axis, axes: int, adjacent: bool) -> RotaryStruct:
+    """The rotation of pairs that turn by radians[i] per position on axis[i] (None: axis 0)."""
+    got, n = RotaryStruct(), len(radians)
+    st = load().adaspark_attn_rotary_init(ctypes.byref(got), (ctypes.c_double * max(n, 1))(*radians),
+                                          (ctypes.c_int32 * max(n, 1))(*axis) if axis is not None else None, n, axes, int(adjacent))
+    if st != OK:
+        raise AdasparkError(st, f"adaspark_attn_rotary_init: {n} pairs on {axes} axes: not a multiple of 8 up to 64, a frequency that is no number, or an axis that is none")
+    return got
+
+
+def adaspark_attn_rotate(handle: int, q, k, q_out, k_out, positions, rotary: Optional[int], q_norm, k_norm, eps: float, n: int, stream: Optional[int]):
+    """rotary: address of a RotaryStruct, or None."""
+    st = (_lib or load()).adaspark_attn_rotate(handle, _ROTATE.pack(*q, *k, *q_out, *k_out, positions or 0, rotary or 0, q_norm or 0, k_norm or 0, eps, n), stream)
+    if st != OK:
+        _check(handle, st)
+
+
+def adaspark_attn_paged_append(handle: int, q, k, v, q_out, pages: bytes, cu, batch: int, n: int, block_table, table_width: int, kv_len, positions,
+                               rotary: Optional[int], q_norm, k_norm, eps: float, status, stream: Optional[int]):
+    st = (_lib or load()).adaspark_attn_paged_append(handle, pages + _PAGED_APPEND.pack(
+        *q, *k, *v, *q_out, cu or 0, kv_len or 0, block_table or 0, positions or 0, rotary or 0, q_norm or 0, k_norm or 0, status or 0, eps, batch, n, table_width), stream)
+    if st != OK:
+        _check(handle, st)
+
+
 class WorkspaceHeader(ctypes.Structure):
     _fields_ = [("status", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("executed_kv_blocks", ctypes.c_uint64), ("decode_kv_blocks", ctypes.c_uint64),
@@ -373,6 +427,36 @@ class PagedCache:
         self.pages = pages_struct(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if fmt else None,
                                   v_scale.data_ptr() if fmt else None, self.page_stride, stride_of(k_scale, v_scale) if fmt else 0,
                                   self.n_pages, self.page_size, fmt)
+
+class Rotary:
+    """A rotation of a head's pairs by the positions of its token (see adaspark_attn_rotary_t).  sections: how many pairs follow each axis of
+    the positions, one axis behind the other (default: all head_dim / 2 on one), pair i turning by theta^(-i / pairs) per position; frequencies and
+    axis give every pair's own radians per position, and axis, instead (scaled or interleaved rotations).  adjacent: pairs are neighbours (2 i, 2 i + 1),
+    else (i, i + pairs)."""
+
+    def __init__(self, head_dim: int, *, sections=None, theta: float = 1e4, frequencies=None, axis=None, adjacent: bool = False):
+        if frequencies is None:
+            if axis is not None:
+                _refuse("Rotary: axis comes with frequencies")
+            sections = [head_dim // 2] if sections is None else [int(n) for n in sections]
+            if not sections or min(sections) < 0 or not float(theta) > 0:
+                _refuse(f"Rotary: sections {sections}, theta {theta}")
+            n = sum(sections)
+            frequencies, axis = [float(theta) ** (-i / n) for i in range(n)], [a for a, m in enumerate(sections) for _ in range(m)]
+            axes = len(sections)
+        else:
+            if sections is not None:
+                _refuse("Rotary: sections or frequencies, not both")
+            frequencies = [float(f) for f in frequencies]
+            axis = None if axis is None else [int(a) for a in axis]
+            if axis is not None and len(axis) != len(frequencies):
+                _refuse(f"Rotary: {len(axis)} axes for {len(frequencies)} frequencies")
+            axes = 1 + max(axis, default=0) if axis else 1
+        if 2 * len(frequencies) > head_dim:
+            _refuse(f"Rotary: {len(frequencies)} pairs in a head of {head_dim}")
+        self.struct = adaspark_attn_rotary_init(frequencies, axis, axes, adjacent)
+        self.address, self.axes, self.pairs, self.head_dim = ctypes.addressof(self.struct), axes, len(frequencies), head_dim
+
 
 class AdaSAttn:
     """Owns a handle plus the torch-allocated caches and workspace for one partition."""
@@ -576,6 +660,91 @@ class AdaSAttn:
             _refuse(f"cache of {cache.n_kv_heads} heads of {cache.head_dim} on {cache.device}: not this handle's")
         return cache.pages
 
+    def _turn(self, rotary, positions, n: int, q_norm, k_norm):
+        """(positions, rotary, weights of the norms) of n tokens as pointers."""
+        where = turned = None
+        if rotary is not None:
+            if rotary.head_dim != self._head_dim:
+                _refuse(f"rotary is one of heads of {rotary.head_dim}")
+            turned = rotary.address
+        if positions is not None:
+            if positions.dtype is not torch.int32 or positions.numel() != n * (rotary.axes if rotary is not None else 1) or positions.shape[-1:] != (n,) or \
+                    positions.dim() > 2 or not positions.is_contiguous() or positions.get_device() != self._index:
+                _refuse(f"positions: {positions.dtype} {tuple(positions.shape)} on {positions.device} is not dense int32 [axes, {n}] on {self.device}")
+            where = positions.data_ptr()
+        D = self._head_dim
+        return where, turned, *(None if w is None else self._dense(w, (D,), torch.bfloat16, what) for w, what in ((q_norm, "q_norm"), (k_norm, "k_norm")))
+
+    def rotate(self, q, k, positions=None, rotary: Optional[Rotary] = None, *, q_norm=None, k_norm=None, eps: float = 1e-6, q_out=None, k_out=None, stream=None):
+        """Queries [n, Hq, D] and keys [n, Hkv, D] (either may be None), each head with its norm (q_norm, k_norm: bf16 [D]) and turned by its
+        positions, int32 [n] or [axes, n].  Outputs may be the inputs themselves.  Returns (q_out, k_out)."""
+        got, rows, n = [], [], None
+        for x, out, heads, what in ((q, q_out, self._n_q_heads, "q"), (k, k_out, self._n_kv_heads, "k")):
+            if x is None:
+                if out is not None:
+                    _refuse(f"{what}_out without {what}")
+                got.append(None)
+                rows.append((_NO_ROWS, _NO_ROWS))
+                continue
+            r, m = self._rows(x, heads, what)
+            if n is not None and m != n:
+                _refuse(f"q has {n} rows, k {m}")
+            n = m
+            if out is None:
+                out = self._empty((n, heads, self._head_dim), torch.bfloat16, stream)
+            o, m = self._rows(out, heads, what + "_out")
+            if m != n:
+                _refuse(f"{what}_out has {m} rows, {what} {n}")
+            got.append(out)
+            rows.append((r, o))
+        if n is None:
+            _refuse("rotate: neither q nor k")
+        if rotary is not None and rotary.pairs and positions is None:
+            _refuse("rotate: a rotation needs positions")
+        (qr, qo), (kr, ko) = rows
+        adaspark_attn_rotate(self.handle, qr, kr, qo, ko, *self._turn(rotary, positions, n, q_norm, k_norm), eps, n, _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        return tuple(got)
+
+    def paged_append(self, cache: PagedCache, q, k, v, cu, block_table, kv_len, rotary: Optional[Rotary] = None, *, positions=None, q_norm=None, k_norm=None,
+                     eps: float = 1e-6, q_out=None, stream=None):
+        """rotate() on the way into the pages: packed rows as paged_write() takes them, keys with their norm and turned, values as they are; q (may
+        be None) comes back.  positions None: places in the sequence.  Returns q_out."""
+        status = (self._text or self._text_buffers(stream))[0]
+        (kr, n), (vr, n_v) = self._rows(k, self._n_kv_heads, "k"), self._rows(v, self._n_kv_heads, "v")
+        qr = qo = _NO_ROWS
+        n_q = n_o = n
+        if q is not None:
+            qr, n_q = self._rows(q, self._n_q_heads, "q")
+            if q_out is None:
+                q_out = self._empty((n_q, self._n_q_heads, self._head_dim), torch.bfloat16, stream)
+            qo, n_o = self._rows(q_out, self._n_q_heads, "q_out")
+        elif q_out is not None:
+            _refuse("q_out without q")
+        if n_v != n or n_q != n or n_o != n:
+            _refuse(f"q, k, v and q_out have {n_q}, {n}, {n_v} and {n_o} rows")
+        batch, table, width, lens = self._tables(block_table, kv_len)
+        adaspark_attn_paged_append(self.handle, qr, kr, vr, qo, self._cache(cache), self._ints(cu, batch + 1, "cu"), batch, n, table, width, lens,
+                                   *self._turn(rotary, positions, n, q_norm, k_norm), eps, status, self._stream(stream))
+        return q_out
+
+    def paged_prompt(self, q, cache: PagedCache, cu, block_table, kv_len, *, window: int = 0, sinks: int = 0, out=None, lse=None, want_lse=False, stream=None):
+        """Several new tokens per sequence, in the pages already (paged_append, paged_write): the rows cu[b] .. cu[b + 1] - 1 of q [n, Hq, D] are
+        the last tokens of sequence b, which holds kv_len[b].  A token sees those up to itself; with a window, the last `window` of them and the
+        first `sinks` ones of the sequence.  Returns (out, lse)."""
+        status, ws, ws_bytes = self._text or self._text_buffers(stream)
+        Hq, D = self._n_q_heads, self._head_dim
+        batch, table, width, lens = self._tables(block_table, kv_len)
+        qr, n = self._rows(q, Hq, "q")
+        if out is None:
+            out = self._empty((n, Hq, D), torch.bfloat16, stream)
+        if lse is None and want_lse:
+            lse = self._empty((n, Hq), torch.float32, stream)
+        adaspark_attn_paged_prompt(self.handle, qr, self._cache(cache), self._ints(cu, batch + 1, "cu"), batch, n, table, width, lens, window, sinks,
+                                   self._dense(out, (n, Hq, D), torch.bfloat16, "out"),
+                                   None if lse is None else self._dense(lse, (n, Hq), torch.float32, "lse"), ws, ws_bytes, status,
+                                   self._stream(stream))
+        return out, lse
+
     def prompt(self, q, k, v, cu_q, cu_k=None, *, out=None, lse=None, want_lse=False, stream=None):
         """Causal attention of packed prompts: q [n_q, Hq, D], k and v [n_k, Hkv, D] bf16, cu_q (and cu_k, if the keys of a sequence
         are more than its queries) int32 [batch + 1].  Returns (out, lse); lse is None unless given or wanted.  The text calls of one
@@ -617,10 +786,11 @@ class AdaSAttn:
         batch, table, width, lens = self._tables(block_table, kv_len)
         call(self.handle, self._cache(cache), kr, vr, self._ints(cu, batch + 1, "cu"), batch, n, table, width, lens, status, self._stream(stream))
 
-    def paged_decode(self, q, k_new, v_new, cache: PagedCache, block_table, kv_len, *, out=None, lse=None, want_lse=False,
-                     stream=None):
+    def paged_decode(self, q, k_new, v_new, cache: PagedCache, block_table, kv_len, *, window: int = 0, sinks: int = 0, out=None, lse=None,
+                     want_lse=False, stream=None):
         """One new token per sequence against its pages.  q [batch, Hq, D]; k_new, v_new [batch, Hkv, D] are stored as token
-        kv_len[b] - 1 first (None: they are there).  kv_len 0: a slot without a sequence.  Returns (out, lse)."""
+        kv_len[b] - 1 first (None: they are there).  kv_len 0: a slot without a sequence.  window > 0: against the last `window` tokens
+        (itself among them) and the first `sinks` ones.  Returns (out, lse)."""
         status, ws, ws_bytes = self._text or self._text_buffers(stream)
         Hq, D = self._n_q_heads, self._head_dim
         batch, table, width, lens = self._tables(block_table, kv_len)
@@ -637,10 +807,14 @@ class AdaSAttn:
             out = self._empty((batch, Hq, D), torch.bfloat16, stream)
         if lse is None and want_lse:
             lse = self._empty((batch, Hq), torch.float32, stream)
-        adaspark_attn_paged_decode(self.handle, qr, kr, vr, self._cache(cache), table, width, lens, batch,
-                                   self._dense(out, (batch, Hq, D), torch.bfloat16, "out"),
-                                   None if lse is None else self._dense(lse, (batch, Hq), torch.float32, "lse"), ws, ws_bytes, status,
-                                   self._stream(stream))
+        call = (self.handle, qr, kr, vr, self._cache(cache), table, width, lens, batch, self._dense(out, (batch, Hq, D), torch.bfloat16, "out"),
+                None if lse is None else self._dense(lse, (batch, Hq), torch.float32, "lse"), ws, ws_bytes, status)
+        if window == 0:
+            if sinks < 0:
+                _refuse(f"sinks {sinks}")
+            adaspark_attn_paged_decode(*call, self._stream(stream))
+        else:
+            adaspark_attn_paged_decode_window(*call, window, sinks, self._stream(stream))
         return out, lse
 
     def header(self) -> WorkspaceHeader:

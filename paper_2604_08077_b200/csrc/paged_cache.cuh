@@ -122,29 +122,40 @@ __device__ __forceinline__ bool bounds_fit(int begin, int end, int n) { return 0
 
 constexpr int kCacheThreads = 256;
 
-// Places of the CTA's kTokens tokens from t0 on, by its first threads: offsets (elements, scales) of a token's first kv head in the pages;
+// Where row `at` of the packed tensors belongs: offsets (elements, scales) of the token's first kv head in the pages, its place in its sequence;
 // first < 0: -1 a row of no sequence, -2 one of a sequence that has no place for it, or whose bounds are none.
+struct TokenPlace {
+    long long first, scale;
+    int pos;
+};
+template <int D>
+__device__ __forceinline__ TokenPlace place_of(const PageGeom& p, const int32_t* cu, const int32_t* kv_len, int batch, int n, int at, int32_t* status) {
+    TokenPlace x = {-1, 0, 0};
+    const int seq = at < n ? sequence_of(cu, batch, at) : -1;
+    if (seq >= 0) {
+        const int len = kv_len[seq], end = cu[seq + 1];
+        x.pos = len > 0 ? len - (end - at) : -1;
+        const int in = x.pos & ((1 << p.page_shift) - 1);
+        const long long page = bounds_fit(cu[seq], end, n) ? page_of(p, seq, x.pos) : -1;
+        if (page < 0) {
+            x.first = -2;
+            if (status != nullptr) atomicExch(status, 1);
+        } else {
+            x.first = page * p.page_stride + (long long)in * D;
+            x.scale = page * p.scale_stride + in;
+        }
+    }
+    return x;
+}
+
+// Places of the CTA's kTokens tokens from t0 on, by its first threads.
 template <int kTokens, int D>
 __device__ __forceinline__ void find_tokens(const PageGeom& p, const int32_t* cu, const int32_t* kv_len, int batch, int n, int t0, long long (&place)[kTokens],
                                             long long (&scale_place)[kTokens], int32_t* status) {
     for (int i = threadIdx.x; i < kTokens; i += kCacheThreads) {
-        const int at = t0 + i;
-        long long x = -1, y = 0;
-        const int seq = at < n ? sequence_of(cu, batch, at) : -1;
-        if (seq >= 0) {
-            const int len = kv_len[seq], end = cu[seq + 1];
-            const int pos = len > 0 ? len - (end - at) : -1, in = pos & ((1 << p.page_shift) - 1);
-            const long long page = bounds_fit(cu[seq], end, n) ? page_of(p, seq, pos) : -1;
-            if (page < 0) {
-                x = -2;
-                if (status != nullptr) atomicExch(status, 1);
-            } else {
-                x = page * p.page_stride + (long long)in * D;
-                y = page * p.scale_stride + in;
-            }
-        }
-        place[i] = x;
-        scale_place[i] = y;
+        const TokenPlace x = place_of<D>(p, cu, kv_len, batch, n, t0 + i, status);
+        place[i] = x.first;
+        scale_place[i] = x.scale;
     }
 }
 

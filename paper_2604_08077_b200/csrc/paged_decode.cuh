@@ -21,6 +21,10 @@
 // within f16 whatever the rows' sizes, and beside them the sum of 2^(x_j - m) is kept.  A score is multiplied by the powers of two of q and key
 // one after the other, the one below 1 first where q is large: they may lie at opposite ends of the range.  (K as e4m3 against q in two e4m3 parts: no faster, the
 // legacy 8-bit products are converted, too, and half as fast with more than 8 heads.)
+//
+// With a window (kWin) of the last `window` tokens and the `sinks` first ones, a sequence's line holds the tiles of the first ones and those from the
+// window's first on, as if they were neighbours; tiles at the two borders are masked as the last one is.  Pages that hold nothing that is
+// seen are not read, and their numbers may be any.
 #pragma once
 #include "common.cuh"
 #include "paged_cache.cuh"
@@ -82,13 +86,15 @@ struct PagedCall {
     float* lse;
     float* partial;                          // [cta][2][G][paged_row_floats]
     int32_t* status;
+    int window, sinks;                       // kWin
 };
 
 // The line of tiles: sequence by sequence, kv head by kv head, in front of each (sequence, kv head) paged_part_cost places for what a part costs
 // beside its tiles (q, the merge of the warps, the output).  Held by a whole warp, which has the lengths of 32 sequences in its lanes.
-template <int kTile>
+template <int kTile, bool kWin>
 struct PageLine {
     const PageGeom* p;
+    const PagedCall* a;
     const int32_t* kv_len;
     int batch, lane;
     int chunk, len;                          // first sequence of the lanes' 32, tokens of this lane's sequence (0: none, or out of range)
@@ -98,8 +104,15 @@ struct PageLine {
         const int n = c + lane < batch ? kv_len[c + lane] : 0;
         len = in_range(n) ? n : 0;
     }
+    // tiles of n tokens that hold something that is seen
+    __device__ __forceinline__ int tiles_of(int n) const {
+        const int all = paged_tiles(n, kTile);
+        return kWin ? all - max(max(n - a->window, 0) / kTile - paged_tiles(a->sinks, kTile), 0) : all;
+    }
+    // where tile t of those lies in the sequence
+    __device__ __forceinline__ int tile_at(int n, int tiles, int t) const { return kWin && t >= paged_tiles(a->sinks, kTile) ? t + paged_tiles(n, kTile) - tiles : t; }
     // places of one (sequence, kv head) of n tokens
-    static __device__ __forceinline__ int places(int n) { return n > 0 ? paged_tiles(n, kTile) + paged_part_cost(kTile) : 0; }
+    __device__ __forceinline__ int places(int n) const { return n > 0 ? tiles_of(n) + paged_part_cost(kTile) : 0; }
     __device__ __forceinline__ long long total() {
         long long sum = 0;
         for (int c = 0; c < batch; c += 32) {
@@ -117,9 +130,9 @@ __device__ __forceinline__ long long run_begin(long long total, int n_runs, int 
 __device__ __forceinline__ int run_of(long long total, int n_runs, long long x) { return (int)(((x + 1) * n_runs - 1) / total); }
 
 // A walk along a run, part by part: the tiles [tile, end) of (sequence b, kv head gk), which has n tokens in `tiles` tiles.
-template <int kTile>
+template <int kTile, bool kWin>
 struct RunWalk {
-    PageLine<kTile> line;
+    PageLine<kTile, kWin> line;
     long long place, stop;                   // first place of the (sequence, kv head); first place behind the run
     int b, gk, n, tiles, tile, end;
     // to place x < total; false: no tile there (only the places in front of one)
@@ -141,7 +154,7 @@ struct RunWalk {
                 const long long first = before + __shfl_sync(0xffffffffu, upto - mine, who);
                 b = c + who;
                 n = __shfl_sync(0xffffffffu, line.len, who);
-                tiles = paged_tiles(n, kTile);
+                tiles = line.tiles_of(n);
                 const int per = tiles + paged_part_cost(kTile), rest = (int)(x - first);
                 gk = rest / per;
                 place = first + (long long)gk * per;
@@ -165,7 +178,7 @@ struct RunWalk {
         n = __shfl_sync(0xffffffffu, line.len, seq & 31);
         b = seq;
         gk = head;
-        tiles = paged_tiles(n, kTile);
+        tiles = line.tiles_of(n);
         place += (long long)head * line.places(n);
         return begin(0);
     }
@@ -188,7 +201,7 @@ struct RunWalk {
                 const int who = __ffs(there) - 1;
                 b = line.chunk + who;
                 n = __shfl_sync(0xffffffffu, line.len, who);
-                tiles = paged_tiles(n, kTile);
+                tiles = line.tiles_of(n);
                 return begin(0);
             }
             if (line.chunk + 32 >= line.batch) return false;
@@ -238,7 +251,7 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint3
 __device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 128;\n" ::: "memory"); }
 
 // kGroups: groups of 8 heads, (G + 7) / 8.
-template <int D, bool kE4m3, int kGroups>
+template <int D, bool kE4m3, int kGroups, bool kWin>
 __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom p, PagedCall a, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV) {
     using Smem = PagedSmem<D, kE4m3>;
     extern __shared__ __align__(1024) unsigned char paged_smem_raw[];
@@ -270,8 +283,9 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
     wait_for_previous_kernel();
     launch_dependents();                                      // (after the wait: the next kernel reads kv_len before its own)
 
-    RunWalk<kTile> w;
+    RunWalk<kTile, kWin> w;
     w.line.p = &p;
+    w.line.a = &a;
     w.line.kv_len = a.kv_len;
     w.line.batch = a.batch;
     w.line.lane = lane;
@@ -289,7 +303,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
         bool ok = true;
         for (int part = 0; more && ok; ++part, more = w.next()) {
             const int32_t* table = p.table + (size_t)w.b * p.table_width;
-            const int last_col = (w.n - 1) >> page_shift, col_begin = (w.tile * kTile) >> page_shift;
+            const int last_col = (w.n - 1) >> page_shift, col_begin = (w.line.tile_at(w.n, w.tiles, w.tile) * kTile) >> page_shift;
             auto page_at = [&](int col) -> int { return col <= last_col ? table[col] : 0; };
             if (cols_b != w.b || col_begin < cols) {
                 cols_b = w.b;
@@ -309,7 +323,12 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
             __syncwarp();
             if (lane < a.G) bulk_load(&sm.q[qs * 8 + lane][0], a.q + w.b * a.q_ts + (w.gk * a.G + lane) * a.q_hs, D * 2, &sm.q_full[qs]);
             for (int tile = w.tile; tile < w.end; ++tile) {
-                const int pos0 = tile * kTile, col0 = pos0 >> page_shift;
+                const int pos0 = w.line.tile_at(w.n, w.tiles, tile) * kTile, col0 = pos0 >> page_shift;
+                if (kWin && col0 >= cols + 64) {              // over what lies between the first tokens and the window
+                    cols = col0;
+                    pages = page_at(cols + lane);
+                    pages_next = page_at(cols + 32 + lane);
+                }
                 while (col0 >= cols + 32) {
                     cols += 32;
                     pages = pages_next;
@@ -319,8 +338,12 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                 int page = __shfl_sync(0xffffffffu, pages, min(col0 - cols + lane, 31));
                 const int over = __shfl_sync(0xffffffffu, pages_next, max(col0 - cols + lane - 32, 0) & 31);
                 if (col0 - cols + lane >= 32) page = over;
-                const bool there = page >= 0 && page < p.n_pages;
-                if (__any_sync(0xffffffffu, lane < boxes && !there)) {
+                bool there = page >= 0 && page < p.n_pages;
+                // a box of tokens that are not seen is not read: zeros
+                const int box0 = pos0 + lane * sub;
+                const bool seen = !kWin || box0 < a.sinks || box0 + sub > w.n - a.window;
+                if (kWin && !seen) there = false;
+                if (__any_sync(0xffffffffu, lane < boxes && seen && !there)) {
                     if (lane == 0) {
                         sm.bad[part & 3] = part + 1;
                         if (a.status != nullptr) atomicExch(a.status, 1);
@@ -418,9 +441,13 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
             for (int i = 0; i < kMTiles; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
         }
         for (int tile = w.tile; tile < w.end; ++tile) {
-            const int n_vis = n - tile * kTile - warp * kWarpKeys;         // keys of this warp's quarter that are there
+            const int key0 = w.line.tile_at(n, w.tiles, tile) * kTile + warp * kWarpKeys;
+            const int n_vis = n - key0;                                    // keys of this warp's quarter that are there
+            // of these, [hide0, hide1) lie between the first ones and the window
+            const int hide0 = kWin ? max(a.sinks - key0, 0) : 0, hide1 = kWin ? min(n - a.window - key0, kWarpKeys) : 0;
+            const bool hides = kWin && hide0 < hide1;
             tc::mbar_wait(&sm.full[st], ph, abort_flag);
-            if (n_vis > 0) {
+            if (n_vis > 0 && !(kWin && hide0 == 0 && hide1 == kWarpKeys)) {
                 unsigned char* kst = sm.kv[st][0];
                 unsigned char* vst = sm.kv[st][1];
                 const int row0 = warp * kWarpKeys;
@@ -432,6 +459,16 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                         *reinterpret_cast<uint4*>(dst) = make_uint4(0u, 0u, 0u, 0u);
                     }
                     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");   // TMA writes there again
+                    __syncwarp();
+                }
+                if (hides) {                                  // what is hidden may be anything, too
+                    constexpr int kChunks = kRowBytes / 16;
+                    for (int c = lane; c < (hide1 - hide0) * kChunks; c += 32) {
+                        const int r = row0 + hide0 + c / kChunks, x = c % kChunks;
+                        unsigned char* dst = kE4m3 ? vst + r * kRowBytes + x * 16 : vst + (x >> 3) * (kTile * 128) + r * 128 + (x & 7) * 16;
+                        *reinterpret_cast<uint4*>(dst) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                     __syncwarp();
                 }
                 float x[kGroups][kNTiles][2];                 // scores of keys 8 nt + 2 t4, + 1, times scale_log2
@@ -503,6 +540,15 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
 #pragma unroll
                             for (int e = 0; e < 2; ++e)
                                 if (nt * 8 + 2 * t4 + e >= n_vis) x[r][nt][e] = -INFINITY;
+                }
+                if (hides) {
+#pragma unroll
+                    for (int r = 0; r < kGroups; ++r)
+#pragma unroll
+                        for (int nt = 0; nt < kNTiles; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (nt * 8 + 2 * t4 + e >= hide0 && nt * 8 + 2 * t4 + e < hide1) x[r][nt][e] = -INFINITY;
                 }
                 uint32_t pf[kGroups][kNTiles];                // P^T: two keys of a head
 #pragma unroll
@@ -596,7 +642,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
             if (t4 == 0) *reinterpret_cast<float4*>(sm.stat[warp][r * 8 + g8]) = make_float4(m[r], l[r], mv[r], 0.f);
         }
         // warps that had a key of the part (the first ones, where it is one tile)
-        const int live = w.end - w.tile > 1 ? 4 : paged_pieces(n - w.tile * kTile, kTile, kWarpKeys);
+        const int live = w.end - w.tile > 1 ? 4 : paged_pieces(n - w.line.tile_at(n, w.tiles, w.tile) * kTile, kTile, kWarpKeys);
         consumer_sync();
 #pragma unroll
         for (int r = 0; r < kGroups; ++r) {
@@ -691,7 +737,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
 constexpr int kJoinThreads = 256;
 constexpr int kJoinBlocks = 4, kJoinWarpAhead = 8;
 
-template <int D, bool kE4m3, bool kFew>
+template <int D, bool kE4m3, bool kFew, bool kWin>
 __global__ void __launch_bounds__(kJoinThreads, kFew ? 2 : kJoinBlocks) paged_join_kernel(PageGeom p, PagedCall a, int n_ctas) {
     constexpr int kTile = paged_tile(kE4m3), kLanes = D / 4, kShares = kJoinThreads / kLanes, kRowF = paged_row_floats(D), kAhead = kFew ? 8 : 4;
     __shared__ float weight[kPagedCtas];
@@ -699,8 +745,9 @@ __global__ void __launch_bounds__(kJoinThreads, kFew ? 2 : kJoinBlocks) paged_jo
     __shared__ float tops[8][2], sums[8];
     __shared__ int bads;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    RunWalk<kTile> w;
+    RunWalk<kTile, kWin> w;
     w.line.p = &p;
+    w.line.a = &a;
     w.line.kv_len = a.kv_len;
     w.line.batch = a.batch;
     w.line.lane = lane;

@@ -4,13 +4,16 @@
 #include <atomic>
 #include <type_traits>
 
+#include "attn_paged.cuh"
 #include "attn_prompt.cuh"
 #include "paged_cache.cuh"
 #include "paged_decode.cuh"
+#include "rotary.cuh"
 
 namespace {
 
 constexpr int kCacheManyTokens = 16384;
+constexpr int kRotateFew = 1024;             // tokens
 
 // The handle's device for the length of a call; the caller's is current again afterwards.
 struct DeviceScope {
@@ -141,6 +144,130 @@ adaspark_status_t paged_rows_impl(adaspark_attn* h, const char* who, const adasp
     return launch_ok(h, write ? "paged_write_kernel" : "paged_read_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
 }
 
+// window 0: none
+adaspark_status_t paged_decode_impl(adaspark_attn* h, const char* who, const adaspark_attn_paged_decode_t* c, int window, int sinks, void* cuda_stream) {
+    if (!h) return ADASPARK_ERR_INVALID_ARG;
+    if (!c || c->batch < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call or negative batch", who);
+    const int batch = c->batch, table_width = c->table_width;
+    h->launches = 0;
+    if (batch == 0) return ADASPARK_OK;
+    const adaspark_attn_pages_t* pages = &c->pages;
+    PageGeom g;
+    Rows rq, rk = {nullptr, 0, 0}, rv = {nullptr, 0, 0};
+    if ((c->k_new.data == nullptr) != (c->v_new.data == nullptr)) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: k_new and v_new must both be given or both be NULL", who);
+    ADASPARK_TRY(check_pages(h, who, pages, c->block_table, table_width, g));
+    ADASPARK_TRY(check_rows(h, who, "q", c->q, h->cfg.n_q_heads, rq));
+    if (c->k_new.data) {
+        ADASPARK_TRY(check_rows(h, who, "k_new", c->k_new, h->cfg.n_kv_heads, rk));
+        ADASPARK_TRY(check_rows(h, who, "v_new", c->v_new, h->cfg.n_kv_heads, rv));
+    }
+    if (!c->kv_len || !c->out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL kv_len or out", who);
+    if ((uintptr_t)c->out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: out is not 16-byte aligned", who);
+    ADASPARK_TRY(check_workspace(h, who, c->workspace, c->workspace_bytes));
+    DeviceScope scope;
+    ADASPARK_TRY(scope.enter(h, who));
+    const int D = h->cfg.head_dim, Hq = h->cfg.n_q_heads;
+    const bool e4m3 = pages->format == ADASPARK_PAGES_E4M3;
+    const int tile = paged_tile(e4m3), page_size = pages->page_size;
+    PagedCall a;
+    a.kv_len = c->kv_len;
+    a.batch = batch;
+    a.Hq = Hq;
+    a.G = Hq / g.Hkv;
+    a.q = rq.p; a.q_ts = rq.ts; a.q_hs = rq.hs;
+    a.k_new = rk.p; a.k_ts = rk.ts; a.k_hs = rk.hs;
+    a.v_new = rv.p; a.v_ts = rv.ts; a.v_hs = rv.hs;
+    a.scale_log2 = text_scale(h) * 1.4426950408889634f;
+    a.out = (__nv_bfloat16*)c->out;
+    a.lse = c->lse;
+    a.partial = (float*)c->workspace;
+    a.status = c->status;
+    a.window = window;
+    a.sinks = sinks;
+    CUtensorMap tmK, tmV;
+    if (!encode_pages(&tmK, g.k, e4m3, g.n_pages, g.Hkv, page_size, D, g.page_stride, page_size < tile ? page_size : tile) ||
+        !encode_pages(&tmV, g.v, e4m3, g.n_pages, g.Hkv, page_size, D, g.page_stride, page_size < tile ? page_size : tile))
+        return fail(h, ADASPARK_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
+    // two CTAs per SM, or as many as the tables have tiles (a window: those that it and the first tokens may lie in)
+    long long row_tiles = ((long long)table_width * page_size + tile - 1) / tile;
+    if (window > 0) row_tiles = std::min(row_tiles, (long long)window / tile + (long long)sinks / tile + 4);
+    const long long most = (long long)batch * g.Hkv * row_tiles;
+    const int n_ctas = (int)(most < kPagedCtas ? most : kPagedCtas);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    auto launch = [&](auto d, auto bytes_held, auto groups, auto windowed) -> adaspark_status_t {
+        constexpr int kD = d.value;
+        constexpr bool kE4m3 = bytes_held.value, kWin = windowed.value;
+        constexpr auto kernel = paged_decode_kernel<kD, kE4m3, groups.value, kWin>;
+        constexpr size_t bytes = sizeof(PagedSmem<kD, kE4m3>);
+        if (!text_smem<kernel>(h, bytes, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
+        launch_kernel(true, kernel, dim3(n_ctas), dim3(kPagedThreads), bytes, st, g, a, tmK, tmV);
+        if (!launch_ok(h, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
+        if (n_ctas == 1) return ADASPARK_OK;                   // nothing is cut
+        if ((long long)batch * g.Hkv <= kPagedFewSequences)
+            launch_kernel(true, paged_join_kernel<kD, kE4m3, true, kWin>, dim3(batch * g.Hkv, a.G), dim3(kJoinThreads), 0, st, g, a, n_ctas);
+        else
+            launch_kernel(true, paged_join_kernel<kD, kE4m3, false, kWin>, dim3(n_ctas - 1), dim3(kJoinThreads), 0, st, g, a, n_ctas);
+        return launch_ok(h, "paged_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+    };
+    auto with_window = [&](auto d, auto bytes_held, auto groups) -> adaspark_status_t {
+        return window > 0 ? launch(d, bytes_held, groups, std::true_type()) : launch(d, bytes_held, groups, std::false_type());
+    };
+    auto with_groups = [&](auto d, auto bytes_held) -> adaspark_status_t {
+        return a.G > 8 ? with_window(d, bytes_held, std::integral_constant<int, 2>()) : with_window(d, bytes_held, std::integral_constant<int, 1>());
+    };
+    const std::integral_constant<int, 128> wide;
+    const std::integral_constant<int, 64> narrow;
+    if (D == 128) return e4m3 ? with_groups(wide, std::true_type()) : with_groups(wide, std::false_type());
+    return e4m3 ? with_groups(narrow, std::true_type()) : with_groups(narrow, std::false_type());
+}
+
+// What rotate and paged_append share: q (and its out), k, the rotation and the norms.  Rows whose data is NULL are none.
+adaspark_status_t check_turned(adaspark_attn* h, const char* who, int n, const adaspark_attn_rows_t& q, const adaspark_attn_rows_t& q_out, const adaspark_attn_rows_t& k,
+                               const adaspark_attn_rotary_t* rotary, const void* q_norm, const void* k_norm, float eps, RotateCall& a) {
+    const int D = h->cfg.head_dim;
+    Rows r;
+    if (q.data) {
+        ADASPARK_TRY(check_rows(h, who, "q", q, h->cfg.n_q_heads, r));
+        a.q = {r.p, r.ts, r.hs};
+        ADASPARK_TRY(check_rows(h, who, "q_out", q_out, h->cfg.n_q_heads, r));
+        a.q_out = {r.p, r.ts, r.hs};
+        a.Hq = h->cfg.n_q_heads;
+    }
+    if (k.data) {
+        ADASPARK_TRY(check_rows(h, who, "k", k, h->cfg.n_kv_heads, r));
+        a.k = {r.p, r.ts, r.hs};
+        a.Hkv = h->cfg.n_kv_heads;
+    }
+    if ((uintptr_t)q_norm % 16 || (uintptr_t)k_norm % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: weights of the norms are not 16-byte aligned", who);
+    if (!(eps >= 0.f) || std::isinf(eps)) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: eps %g", who, eps);
+    if (rotary) {
+        if (rotary->pairs < 0 || rotary->pairs % 8 || rotary->pairs > D / 2 || rotary->axes < 1)
+            return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: %d pairs of a head of %d, %d axes", who, rotary->pairs, D, rotary->axes);
+        for (int i = 0; i < rotary->pairs; ++i)
+            if (rotary->axis[i] >= rotary->axes) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: pair %d follows axis %d of %d", who, i, rotary->axis[i], rotary->axes);
+        a.pairs = rotary->pairs;
+        a.adjacent = rotary->adjacent;
+        std::memcpy(a.turns, rotary->turns, sizeof(a.turns));
+        std::memcpy(a.axis, rotary->axis, sizeof(a.axis));
+    }
+    a.q_norm = (const __nv_bfloat16*)q_norm;
+    a.k_norm = (const __nv_bfloat16*)k_norm;
+    a.eps = eps;
+    a.n = n;
+    return ADASPARK_OK;
+}
+
+template <int kPages>
+adaspark_status_t launch_rotate(adaspark_attn* h, const RotateCall& a, const PageGeom& p, void* cuda_stream) {
+    const bool many = a.n > kRotateFew;
+    auto launch = [&](auto kernel, int tokens) {
+        launch_kernel(true, kernel, dim3((unsigned)((a.n + tokens - 1) / tokens)), dim3(kRotateThreads), 0, (cudaStream_t)cuda_stream, a, p);
+    };
+    if (h->cfg.head_dim == 128) many ? launch(rotate_kernel<128, kPages, 4>, 4) : launch(rotate_kernel<128, kPages, 1>, 1);
+    else many ? launch(rotate_kernel<64, kPages, 8>, 8) : launch(rotate_kernel<64, kPages, 2>, 2);
+    return launch_ok(h, "rotate_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" {
@@ -228,73 +355,120 @@ adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t* h, const adaspark_at
 }
 
 adaspark_status_t adaspark_attn_paged_decode(adaspark_attn_t* h, const adaspark_attn_paged_decode_t* c, void* cuda_stream) {
+    return paged_decode_impl(h, "paged_decode", c, 0, 0, cuda_stream);
+}
+
+adaspark_status_t adaspark_attn_paged_decode_window(adaspark_attn_t* h, const adaspark_attn_paged_decode_window_t* c, void* cuda_stream) {
     if (!h) return ADASPARK_ERR_INVALID_ARG;
-    const char* who = "paged_decode";
-    if (!c || c->batch < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call or negative batch", who);
-    const int batch = c->batch, table_width = c->table_width;
+    const char* who = "paged_decode_window";
+    if (!c || c->window < 1 || c->sinks < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call, window below 1 or sinks below 0", who);
+    return paged_decode_impl(h, who, &c->step, c->window, c->sinks, cuda_stream);
+}
+
+adaspark_status_t adaspark_attn_paged_prompt(adaspark_attn_t* h, const adaspark_attn_paged_prompt_t* c, void* cuda_stream) {
+    if (!h) return ADASPARK_ERR_INVALID_ARG;
+    const char* who = "paged_prompt";
+    if (!c || c->batch < 0 || c->n < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call or negative size", who);
+    if (c->window < 0 || c->sinks < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: window %d, sinks %d", who, c->window, c->sinks);
     h->launches = 0;
-    if (batch == 0) return ADASPARK_OK;
-    const adaspark_attn_pages_t* pages = &c->pages;
-    PageGeom g;
-    Rows rq, rk = {nullptr, 0, 0}, rv = {nullptr, 0, 0};
-    if ((c->k_new.data == nullptr) != (c->v_new.data == nullptr)) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: k_new and v_new must both be given or both be NULL", who);
-    ADASPARK_TRY(check_pages(h, who, pages, c->block_table, table_width, g));
+    if (c->batch == 0 || c->n == 0) return ADASPARK_OK;
+    PageGeom p;
+    Rows rq;
+    ADASPARK_TRY(check_pages(h, who, &c->pages, c->block_table, c->table_width, p));
     ADASPARK_TRY(check_rows(h, who, "q", c->q, h->cfg.n_q_heads, rq));
-    if (c->k_new.data) {
-        ADASPARK_TRY(check_rows(h, who, "k_new", c->k_new, h->cfg.n_kv_heads, rk));
-        ADASPARK_TRY(check_rows(h, who, "v_new", c->v_new, h->cfg.n_kv_heads, rv));
-    }
-    if (!c->kv_len || !c->out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL kv_len or out", who);
+    if (!c->cu || !c->kv_len || !c->out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL pointer", who);
     if ((uintptr_t)c->out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: out is not 16-byte aligned", who);
     ADASPARK_TRY(check_workspace(h, who, c->workspace, c->workspace_bytes));
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));
-    const int D = h->cfg.head_dim, Hq = h->cfg.n_q_heads;
-    const bool e4m3 = pages->format == ADASPARK_PAGES_E4M3;
-    const int tile = paged_tile(e4m3), page_size = pages->page_size;
-    PagedCall a;
+    ChunkCall a;
+    a.cu = c->cu;
     a.kv_len = c->kv_len;
-    a.batch = batch;
-    a.Hq = Hq;
-    a.G = Hq / g.Hkv;
-    a.q = rq.p; a.q_ts = rq.ts; a.q_hs = rq.hs;
-    a.k_new = rk.p; a.k_ts = rk.ts; a.k_hs = rk.hs;
-    a.v_new = rv.p; a.v_ts = rv.ts; a.v_hs = rv.hs;
+    a.batch = c->batch;
+    a.n = c->n;
+    a.Hq = h->cfg.n_q_heads;
+    a.G = a.Hq / p.Hkv;
+    a.q = rq.p;
+    a.q_ts = rq.ts;
+    a.q_hs = rq.hs;
     a.scale_log2 = text_scale(h) * 1.4426950408889634f;
+    a.window = c->window;
+    a.sinks = c->sinks;
     a.out = (__nv_bfloat16*)c->out;
     a.lse = c->lse;
-    a.partial = (float*)c->workspace;
     a.status = c->status;
-    CUtensorMap tmK, tmV;
-    if (!encode_pages(&tmK, g.k, e4m3, g.n_pages, g.Hkv, page_size, D, g.page_stride, page_size < tile ? page_size : tile) ||
-        !encode_pages(&tmV, g.v, e4m3, g.n_pages, g.Hkv, page_size, D, g.page_stride, page_size < tile ? page_size : tile))
-        return fail(h, ADASPARK_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
-    // two CTAs per SM, or as many as the tables have tiles
-    const long long most = (long long)batch * g.Hkv * (((long long)table_width * page_size + tile - 1) / tile);
-    const int n_ctas = (int)(most < kPagedCtas ? most : kPagedCtas);
+    const dim3 grid((unsigned)(((long long)a.n * a.Hq + kChunkWarps - 1) / kChunkWarps));
+    const bool e4m3 = c->pages.format == ADASPARK_PAGES_E4M3;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    auto launch = [&](auto d, auto bytes_held, auto groups) -> adaspark_status_t {
-        constexpr int kD = d.value;
-        constexpr bool kE4m3 = bytes_held.value;
-        constexpr auto kernel = paged_decode_kernel<kD, kE4m3, groups.value>;
-        constexpr size_t bytes = sizeof(PagedSmem<kD, kE4m3>);
-        if (!text_smem<kernel>(h, bytes, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
-        launch_kernel(true, kernel, dim3(n_ctas), dim3(kPagedThreads), bytes, st, g, a, tmK, tmV);
-        if (!launch_ok(h, "paged_decode_kernel")) return ADASPARK_ERR_CUDA;
-        if (n_ctas == 1) return ADASPARK_OK;                   // nothing is cut
-        if ((long long)batch * g.Hkv <= kPagedFewSequences)
-            launch_kernel(true, paged_join_kernel<kD, kE4m3, true>, dim3(batch * g.Hkv, a.G), dim3(kJoinThreads), 0, st, g, a, n_ctas);
-        else
-            launch_kernel(true, paged_join_kernel<kD, kE4m3, false>, dim3(n_ctas - 1), dim3(kJoinThreads), 0, st, g, a, n_ctas);
-        return launch_ok(h, "paged_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
-    };
-    auto with_groups = [&](auto d, auto bytes_held) -> adaspark_status_t {
-        return a.G > 8 ? launch(d, bytes_held, std::integral_constant<int, 2>()) : launch(d, bytes_held, std::integral_constant<int, 1>());
-    };
-    const std::integral_constant<int, 128> wide;
-    const std::integral_constant<int, 64> narrow;
-    if (D == 128) return e4m3 ? with_groups(wide, std::true_type()) : with_groups(wide, std::false_type());
-    return e4m3 ? with_groups(narrow, std::true_type()) : with_groups(narrow, std::false_type());
+    if (h->cfg.head_dim == 128) launch_kernel(true, e4m3 ? attn_paged_kernel<128, true> : attn_paged_kernel<128, false>, grid, dim3(kChunkWarps * 32), 0, st, p, a);
+    else launch_kernel(true, e4m3 ? attn_paged_kernel<64, true> : attn_paged_kernel<64, false>, grid, dim3(kChunkWarps * 32), 0, st, p, a);
+    return launch_ok(h, "attn_paged_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+}
+
+adaspark_status_t adaspark_attn_rotary_init(adaspark_attn_rotary_t* r, const double* radians, const int32_t* axis, int32_t pairs, int32_t axes, int32_t adjacent) {
+    if (!r || pairs < 0 || pairs > kRotaryPairs || pairs % 8 || axes < 1 || axes > 255 || (pairs && !radians)) return ADASPARK_ERR_INVALID_ARG;
+    adaspark_attn_rotary_t got;
+    std::memset(&got, 0, sizeof(got));
+    for (int i = 0; i < pairs; ++i) {
+        if (!std::isfinite(radians[i]) || (axis && (axis[i] < 0 || axis[i] >= axes))) return ADASPARK_ERR_INVALID_ARG;
+        const long double turns = (long double)radians[i] / 6.283185307179586476925286766559L, part = turns - std::floor(turns);
+        got.turns[i] = part < 1.L ? (uint64_t)(part * 18446744073709551616.L) : 0;
+        got.axis[i] = axis ? (uint8_t)axis[i] : 0;
+    }
+    got.pairs = pairs;
+    got.axes = axes;
+    got.adjacent = adjacent != 0;
+    *r = got;
+    return ADASPARK_OK;
+}
+
+adaspark_status_t adaspark_attn_rotate(adaspark_attn_t* h, const adaspark_attn_rotate_t* c, void* cuda_stream) {
+    if (!h) return ADASPARK_ERR_INVALID_ARG;
+    const char* who = "rotate";
+    if (!c || c->n < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call or negative size", who);
+    h->launches = 0;
+    if (c->n == 0 || (!c->q.data && !c->k.data)) return ADASPARK_OK;
+    RotateCall a;
+    std::memset(&a, 0, sizeof(a));
+    ADASPARK_TRY(check_turned(h, who, c->n, c->q, c->q_out, c->k, c->rotary, c->q_norm, c->k_norm, c->eps, a));
+    if (c->k.data) {
+        Rows out;
+        ADASPARK_TRY(check_rows(h, who, "k_out", c->k_out, a.Hkv, out));
+        a.k_out = {out.p, out.ts, out.hs};
+    }
+    if (a.pairs && !c->positions) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL positions", who);
+    a.positions = c->positions;
+    DeviceScope scope;
+    ADASPARK_TRY(scope.enter(h, who));
+    PageGeom none;
+    std::memset(&none, 0, sizeof(none));
+    return launch_rotate<0>(h, a, none, cuda_stream);
+}
+
+adaspark_status_t adaspark_attn_paged_append(adaspark_attn_t* h, const adaspark_attn_paged_append_t* c, void* cuda_stream) {
+    if (!h) return ADASPARK_ERR_INVALID_ARG;
+    const char* who = "paged_append";
+    if (!c || c->batch < 0 || c->n < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL call or negative size", who);
+    h->launches = 0;
+    if (c->batch == 0 || c->n == 0) return ADASPARK_OK;
+    PageGeom p;
+    Rows rv;
+    RotateCall a;
+    std::memset(&a, 0, sizeof(a));
+    ADASPARK_TRY(check_pages(h, who, &c->pages, c->block_table, c->table_width, p));
+    if (!c->k.data) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL k", who);
+    ADASPARK_TRY(check_turned(h, who, c->n, c->q, c->q_out, c->k, c->rotary, c->q_norm, c->k_norm, c->eps, a));
+    ADASPARK_TRY(check_rows(h, who, "v", c->v, a.Hkv, rv));
+    if (!c->cu || !c->kv_len) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL cu or kv_len", who);
+    a.v = {rv.p, rv.ts, rv.hs};
+    a.positions = c->positions;
+    a.cu = c->cu;
+    a.kv_len = c->kv_len;
+    a.batch = c->batch;
+    a.status = c->status;
+    DeviceScope scope;
+    ADASPARK_TRY(scope.enter(h, who));
+    return c->pages.format == ADASPARK_PAGES_E4M3 ? launch_rotate<2>(h, a, p, cuda_stream) : launch_rotate<1>(h, a, p, cuda_stream);
 }
 
 }  // extern "C"
