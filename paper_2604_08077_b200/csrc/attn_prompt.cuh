@@ -40,12 +40,16 @@
 #pragma once
 #include <type_traits>
 
+#include "paged_cache.cuh"
 #include "tc_common.cuh"
 
 namespace adaspark {
 
+// Where keys and values are: packed rows, pages of bf16, pages of e4m3.
+constexpr int kKeysPacked = 0, kKeysPages = 1, kKeysPages8 = 2;
+
 constexpr int kPromptTeams = 2;                               // softmax teams, of two warpgroups each
-constexpr int kPromptThreads = (2 * kPromptTeams + 1) * 128;
+__host__ __device__ constexpr int prompt_threads(int keys) { return (2 * kPromptTeams + (keys == kKeysPages8 ? 2 : 1)) * 128; }
 constexpr int kPromptPlans = 4;                               // tiles planned at once
 constexpr int kPromptBufs = 3;                                // score tiles in TMEM
 constexpr int kPromptRefSlots = 4;
@@ -56,8 +60,16 @@ constexpr float kPromptLowest = -3.402823466e38f;             // a reference bel
 constexpr uint64_t kPromptPlanNs = 10000;                     // a sequence
 constexpr int kPromptOddSlots = 8;                            // more than tiles whose V can be under way at once (a step each)
 __host__ __device__ constexpr int prompt_k_stages(int D) { return D == 64 ? 6 : 3; }   // steps whose K, V are under way
-__host__ __device__ constexpr int prompt_v_stages(int D) { return D == 64 ? 6 : 3; }
-static_assert(prompt_v_stages(64) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
+__host__ __device__ constexpr int prompt_v_stages(int D, int keys) { return D == 64 ? 6 : keys == kKeysPages8 ? 2 : 3; }
+__host__ __device__ constexpr int prompt_raw_stages(int D, int keys) { return keys != kKeysPages8 ? 0 : D == 64 ? 4 : 2; }   // steps whose codes are under way
+static_assert(prompt_v_stages(64, kKeysPacked) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
+
+// What a reference that grows by -d does to what stands: times 2^d, in two factors, for a weight of up to 2^100 may meet a d below -126.
+struct MovedBy {
+    float a, b;
+    __device__ __forceinline__ explicit MovedBy(float d) : a(fast_exp2(fmaxf(d, -120.f))), b(fast_exp2(fminf(d + 120.f, 0.f))) {}
+    __device__ __forceinline__ float of(float x) const { return x * b * a; }
+};
 
 // q.k of two rows in global memory
 template <int D>
@@ -66,6 +78,30 @@ __device__ __noinline__ float prompt_dot(const __nv_bfloat16* q, const __nv_bflo
 #pragma unroll 1
     for (int c = 0; c < D; c += 8) {
         const uint4 a = *reinterpret_cast<const uint4*>(q + c), b = *reinterpret_cast<const uint4*>(key + c);
+        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sum = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum));
+    }
+    return sum;
+}
+
+// Chunk c (8 values) of a key's or value's row in its page, as bf16; zeros where the page is not there.
+template <int D, bool kCodes>
+__device__ __noinline__ uint4 paged_chunk(const PageGeom& p, const uint8_t* pages, const uint8_t* scales, int seq, int head, int key, int c) {
+    const long long page = page_of(p, seq, key);
+    if (page < 0) return make_uint4(0u, 0u, 0u, 0u);
+    const long long row = ((long long)head << p.page_shift) + (key & ((1 << p.page_shift) - 1)), at = page * p.page_stride + row * D + c * 8;
+    if (!kCodes) return *reinterpret_cast<const uint4*>(pages + at * 2);
+    return chunk_values(*reinterpret_cast<const uint2*>(pages + at), min((uint32_t)scales[page * p.scale_stride + row], 254u));
+}
+// q.k of a row in global memory and one in its page
+template <int D, bool kCodes>
+__device__ __noinline__ float paged_dot(const PageGeom& p, int seq, int head, int key, const __nv_bfloat16* q) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < D / 8; ++c) {
+        const uint4 a = *reinterpret_cast<const uint4*>(q + c * 8), b = paged_chunk<D, kCodes>(p, p.k, p.ks, seq, head, key, c);
         const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -84,6 +120,11 @@ struct PromptGeom {
     float scale_log2;
     const __nv_bfloat16 *q, *k, *v; // for scores that leave the range of a step's reference, values that are no numbers
     long long q_ts, q_hs, k_ts, k_hs, v_ts, v_hs;
+    // keys in pages
+    PageGeom pages;
+    const int32_t* kv_len;
+    int window, sinks;          // window 0: none
+    int most_steps;             // a bound on the steps of a tile that a window leaves
 };
 
 struct PromptTile {
@@ -93,21 +134,41 @@ struct PromptTile {
     int gk;
     int n_steps, first_masked;  // steps of 128 keys; from this one on rows are masked
     int part;                   // number of the part of a tile whose keys are cut, -1: a whole tile
+    // keys in pages (last0 counts from the sequence's first token then)
+    int seq;
+    int step0, sink_steps, jump;    // step j holds the keys from 128 * x on, x = step0 + j, and `jump` more behind the first ones' steps
+    int low_first, low_masked;      // steps [low_first, low_masked) are masked, too
+    int lo, hi;                     // some row sees something of [lo, hi) and of the first ones; of nothing else
+    __device__ __forceinline__ int key_of(int j) const { return (step0 + j + (step0 + j >= sink_steps ? jump : 0)) << 7; }
+    __device__ __forceinline__ bool masked(int j) const { return j >= first_masked || (j >= low_first && j < low_masked); }
+    // the first masked step from step j on (n_steps: none)
+    __device__ __forceinline__ int next_masked(int j) const {
+        const int low = max(j, low_first);
+        return min(low < low_masked ? low : max(j, first_masked), n_steps);
+    }
 };
 
-// A sequence as a planner sees it; one that leaves the tensors has no tiles.
+// A sequence as a planner sees it; one that leaves the tensors has no tiles, one whose length is none no keys.
+template <bool kPaged>
 struct PromptSeq {
-    int q0, k0, nq, nk, off, nt;
-    __device__ __forceinline__ bool load(const PromptGeom& g, int b) {
-        const int a0 = g.cu_q[b], a1 = g.cu_q[b + 1], b0 = g.cu_k[b], b1 = g.cu_k[b + 1];
-        const bool valid = 0 <= a0 && a0 <= a1 && a1 <= g.n_q && 0 <= b0 && b0 <= b1 && b1 <= g.n_k;
+    int q0, k0, nq, nk, off, nt, b;
+    __device__ __forceinline__ bool load(const PromptGeom& g, int i) {
+        const int a0 = g.cu_q[i], a1 = g.cu_q[i + 1], b0 = kPaged ? 0 : g.cu_k[i];
+        int b1 = kPaged ? g.kv_len[i] : g.cu_k[i + 1];
+        bool valid = 0 <= a0 && a0 <= a1 && a1 <= g.n_q && (kPaged || (0 <= b0 && b0 <= b1 && b1 <= g.n_k)), fine = valid;
+        if (kPaged) {
+            const bool there = b1 >= 0 && b1 <= (g.pages.table_width << g.pages.page_shift);
+            fine = valid && (a0 == a1 || (there && b1 >= a1 - a0));
+            if (!there) b1 = 0;
+            b = i;
+        }
         q0 = a0;
         k0 = b0;
         nq = valid ? a1 - a0 : 0;
         nk = valid ? b1 - b0 : 0;
         off = nk - nq;
         nt = nq > 0 ? g.div_w.div(nq + 2 * g.T - 1) : 0;
-        return valid;
+        return fine;
     }
     // tiles whose last row sees at most x keys
     __device__ __forceinline__ int tiles_up_to(const PromptGeom& g, int x) const {
@@ -130,15 +191,17 @@ inline bool prompt_may_cut(long long most_tiles, int n_k, bool whole, int W, int
 }
 
 // The order of the items (tiles, or parts of them): levels from many steps to few, sequences in order, tiles, kv heads, parts.  A warp walks
-// it, with 32 sequences in its lanes.  Parts come first: an item's number is its part's.
+// it, with 32 sequences in its lanes.  Parts come first: an item's number is its part's.  (With a window a tile's level is the bound on its
+// steps where it would be more.)
+template <bool kPaged>
 struct PromptWalk {
     int level, unit;                                          // unit 0: nothing is cut
     int below;                                                // most steps of a tile of fewer than `level`, among the sequences seen so far
     int chunk, base;                                          // number of the first item of (level, chunk)
     int held;                                                 // chunk of `mine`, this lane's sequence
-    PromptSeq mine;
+    PromptSeq<kPaged> mine;
     // what find() found
-    PromptSeq seq;
+    PromptSeq<kPaged> seq;
     int tile, gk, part, parts;
 
     // false: a sequence leaves the tensors
@@ -151,8 +214,10 @@ struct PromptWalk {
             if (held * 32 + lane < g.batch) {
                 fine = mine.load(g, held * 32 + lane) && fine;
                 if (mine.nt > 0) {
-                    level = max(level, max(1, (mine.nk + 127) >> 7));
-                    steps += (long long)mine.nt * (max(mine.off, 0) / 128 + 2) + (long long)g.T * mine.nt * (mine.nt + 1) / 128;
+                    const int longest = max(1, (mine.nk + 127) >> 7);
+                    const long long all = (long long)mine.nt * (max(mine.off, 0) / 128 + 2) + (long long)g.T * mine.nt * (mine.nt + 1) / 128;
+                    level = max(level, kPaged ? min(longest, g.most_steps) : longest);
+                    steps += kPaged ? min(all, (long long)mine.nt * g.most_steps) : all;
                 }
             }
         }
@@ -180,7 +245,7 @@ struct PromptWalk {
             int first = 0, n = 0;
             if (mine.nt > 0) {
                 first = level == 1 ? 0 : mine.tiles_up_to(g, 128 * (level - 1));
-                n = (mine.tiles_up_to(g, 128 * level) - first) * g.Hkv * parts;
+                n = ((kPaged && level == g.most_steps ? mine.nt : mine.tiles_up_to(g, 128 * level)) - first) * g.Hkv * parts;
             }
             int upto = n;
 #pragma unroll
@@ -197,6 +262,7 @@ struct PromptWalk {
                 seq.nq = __shfl_sync(0xffffffffu, mine.nq, who);
                 seq.nk = __shfl_sync(0xffffffffu, mine.nk, who);
                 seq.off = __shfl_sync(0xffffffffu, mine.off, who);
+                if (kPaged) seq.b = chunk * 32 + who;
                 part = i % parts;
                 i /= parts;
                 g.div_kv.divmod(i, tile, gk);
@@ -205,7 +271,7 @@ struct PromptWalk {
             }
             base += total;
             // the next level is that of the longest tile left: levels without a tile are passed over
-            if (first > 0) below = max(below, max((min(mine.off + 2 * g.T * first, mine.nk) + 127) >> 7, 1));
+            if (first > 0) below = max(below, max((min(mine.off + 2 * g.T * first, mine.nk) + 127) >> 7, 1));   // (below `level`, whatever bounds that)
             if (++chunk * 32 >= g.batch) {
                 chunk = 0;
                 level = min((int)__reduce_max_sync(0xffffffffu, (unsigned)below), level - 1);   // (down in any case: the walk ends)
@@ -219,31 +285,40 @@ struct PromptWalk {
     __device__ __forceinline__ int tokens(const PromptGeom& g, int rank) const { return min(max(seq.nq - first_token(g, rank), 0), g.T); }
 };
 
-template <int D>
+template <int D, int kKeys>
 struct PromptSmem {
     __nv_bfloat16 q[2][D / 64][128][64];                      // [tile & 1][d panel][row][64 d]
     __nv_bfloat16 k[prompt_k_stages(D)][64 * D];              // [d panel][this CTA's 64 keys][64 d]
-    __nv_bfloat16 v[prompt_v_stages(D)][64 * D];              // [128 keys][this CTA's half of d]
+    __nv_bfloat16 v[prompt_v_stages(D, kKeys)][64 * D];              // [128 keys][this CTA's half of d]
+    unsigned char raw_k[prompt_raw_stages(D, kKeys)][64 * D]; // codes as they lie in the pages: [this CTA's 64 keys][D]
+    unsigned char raw_v[prompt_raw_stages(D, kKeys)][64 * D]; // [128 keys][this CTA's half of d]
     unsigned char out[128][2 * D + 16];
+    uint8_t raw_ks[prompt_raw_stages(D, kKeys)][64], raw_vs[prompt_raw_stages(D, kKeys)][128];   // their powers of two
     float ref[kPromptRefSlots][128], first_ref[2][128];      // reference of a row after a step, after the first 128 keys of a tile
     float part_l[2][2][128], part_m[2][2][128];             // sums and reference of the team that does not finish a tile, by half
     float other_l[kPromptTeams][2][128], other_ref[kPromptTeams][2][128];   // between the halves of a row
-    uint64_t q_full[2], q_peer[2], q_empty[2], k_full[prompt_k_stages(D)], k_empty[prompt_k_stages(D)], v_full[prompt_v_stages(D)], v_empty[prompt_v_stages(D)];
-    uint64_t v_raw[prompt_v_stages(D)], s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], first_done[2][4], o_full, o_free;
+    uint64_t q_full[2], q_peer[2], q_empty[2], k_full[prompt_k_stages(D)], k_empty[prompt_k_stages(D)], v_full[prompt_v_stages(D, kKeys)], v_empty[prompt_v_stages(D, kKeys)];
+    uint64_t v_raw[prompt_v_stages(D, kKeys)], s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], first_done[2][4], o_full, o_free;
     uint64_t plan_full[kPromptPlans], plan_empty[kPromptPlans], part_full[2], part_free[2], out_free;
+    uint64_t rk_full[prompt_raw_stages(D, kKeys)], rk_empty[prompt_raw_stages(D, kKeys)], rv_full[prompt_raw_stages(D, kKeys)], rv_empty[prompt_raw_stages(D, kKeys)];
     PromptTile tile[kPromptPlans];
     int odd_tile[kPromptOddSlots];                            // number + 1 of a tile with masked values that are no numbers
     uint32_t tmem_base;
     int abort_flag;
 };
 
-template <int D>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) attn_prompt_kernel(
-    PromptGeom g, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+static_assert(sizeof(PromptSmem<128, kKeysPages8>) + 1024 <= 232448 && sizeof(PromptSmem<64, kKeysPages8>) + 1024 <= 232448, "what a CTA may have");
+
+template <int D, int kKeys>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys), 1) attn_prompt_kernel(
+    const __grid_constant__ PromptGeom g, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
     __nv_bfloat16* out, float* lse, float* partial, int32_t* status) {
     extern __shared__ unsigned char prompt_smem_raw[];
-    PromptSmem<D>& sm = *reinterpret_cast<PromptSmem<D>*>((reinterpret_cast<uintptr_t>(prompt_smem_raw) + 1023) & ~(uintptr_t)1023);
-    constexpr int kPanels = D / 64, kQKSteps = D / 16, kKStages = prompt_k_stages(D), kVStages = prompt_v_stages(D);
+    using Smem = PromptSmem<D, kKeys>;
+    Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(prompt_smem_raw) + 1023) & ~(uintptr_t)1023);
+    constexpr int kPanels = D / 64, kQKSteps = D / 16, kKStages = prompt_k_stages(D), kVStages = prompt_v_stages(D, kKeys);
+    constexpr bool kPaged = kKeys != kKeysPacked, kCodes = kKeys == kKeysPages8;
+    [[maybe_unused]] constexpr int kRawStages = prompt_raw_stages(D, kKeys);
     constexpr uint32_t kIdescS = tc::make_idesc_bf16(256, 128);
     constexpr uint32_t kIdescO = tc::make_idesc_bf16(256, D) | (1u << 16);   // B = V: rows along N
     constexpr uint32_t kTileBytes = 64 * D * 2;               // a CTA's share of the K or V of a step
@@ -265,16 +340,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         }
         for (int i = 0; i < kPromptPlans; ++i) {
             tc::mbar_init(&sm.plan_full[i], 1);
-            tc::mbar_init(&sm.plan_empty[i], 4 + kPromptTeams * 8);
+            tc::mbar_init(&sm.plan_empty[i], (kCodes ? 7 : 4) + kPromptTeams * 8);
         }
         for (int i = 0; i < kKStages; ++i) {
-            tc::mbar_init(&sm.k_full[i], 1);
+            tc::mbar_init(&sm.k_full[i], kCodes ? 4 : 1);
             tc::mbar_init(&sm.k_empty[i], 1);
         }
         for (int i = 0; i < kVStages; ++i) {
-            tc::mbar_init(&sm.v_full[i], 2);                  // of both CTAs
+            tc::mbar_init(&sm.v_full[i], kCodes ? 4 : 2);     // of both CTAs
             tc::mbar_init(&sm.v_raw[i], 1);
             tc::mbar_init(&sm.v_empty[i], 1);
+        }
+        for (int i = 0; i < kRawStages; ++i) {
+            tc::mbar_init(&sm.rk_full[i], 1);
+            tc::mbar_init(&sm.rk_empty[i], 2);
+            tc::mbar_init(&sm.rv_full[i], 1);
+            tc::mbar_init(&sm.rv_empty[i], 2);
         }
         for (int i = 0; i < kPromptBufs; ++i) {
             tc::mbar_init(&sm.s_full[i], 1);
@@ -305,10 +386,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
     const uint32_t tbase = sm.tmem_base;
     volatile int* abort_flag = &sm.abort_flag;
     const uint64_t plan_limit = tc::kWaitLimitNs + (uint64_t)g.batch * kPromptPlanNs;
+    // The page of the `sub` keys from `key` on, of which `t`'s rows see some or none; n_pages (boxes outside the pages read zeros): it is not
+    // read, or not there.
+    [[maybe_unused]] auto page_for = [&](const PromptTile& t, int key, int sub) -> int {
+        const bool seen = key < t.hi && (key + sub > t.lo || key < g.sinks);
+        if (!seen) return g.pages.n_pages;
+        const int page = g.pages.table[(size_t)t.seq * g.pages.table_width + (key >> g.pages.page_shift)];
+        if (page >= 0 && page < g.pages.n_pages) return page;
+        if (status != nullptr) atomicExch(status, 1);
+        return g.pages.n_pages;
+    };
 
     if (warp == kPlanWarp) {
         // ------------------------------------------------------------ planner
-        PromptWalk w;
+        PromptWalk<kPaged> w;
         if (!w.begin(g, partial != nullptr, n_pairs, lane) && blockIdx.x == 0 && status != nullptr) atomicExch(status, 1);
         for (int k = 0;; ++k) {
             const int slot = k % kPromptPlans, qs = k & 1;
@@ -316,7 +407,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             const int number = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
             const bool found = w.find(g, number, lane);
             PromptTile t;
-            if (found) {
+            if (kPaged && found) {
+                const int tok = w.first_token(g, rank), tok0 = w.first_token(g, 0), m = min(w.seq.nq - tok0, 2 * g.T);
+                const int p0 = w.seq.off + tok0, p1 = p0 + m - 1;          // places of the pair's first and last token
+                t.hi = max(p1 + 1, 0);
+                int n = max((t.hi + 127) >> 7, 1);
+                t.sink_steps = t.jump = t.lo = t.low_first = t.low_masked = 0;
+                if (g.window > 0) {
+                    t.lo = max(p0 + 1 - g.window, 0);
+                    t.sink_steps = min((g.sinks >> 7) + ((g.sinks & 127) != 0), n);
+                    t.jump = max((t.lo >> 7) - t.sink_steps, 0);
+                    n -= t.jump;
+                    const int lo1 = max(p1 + 1 - g.window, 0);             // (the last row's)
+                    if (lo1 > g.sinks) {
+                        t.low_first = g.sinks >> 7;
+                        t.low_masked = max(((lo1 + 127) >> 7) - t.jump, t.sink_steps);
+                    }
+                }
+                const int begin = w.part * n / w.parts;
+                t.seq = w.seq.b;
+                t.q0 = w.seq.q0 + tok;
+                t.n_tok = w.tokens(g, rank);
+                t.k0 = 0;
+                t.last0 = w.seq.off + tok;
+                t.gk = w.gk;
+                t.n_steps = (w.part + 1) * n / w.parts - begin;
+                t.step0 = begin;
+                t.first_masked = max((max(p0 + 1, 0) >> 7) - t.jump - begin, 0);
+                t.low_first -= begin;
+                t.low_masked -= begin;
+                t.part = w.parts > 1 ? number : -1;
+                if (lane == 0) sm.tile[slot] = t;
+            } else if (found) {
                 const int tok = w.first_token(g, rank), begin = w.part * w.level / w.parts;
                 t.q0 = w.seq.q0 + tok;
                 t.n_tok = w.tokens(g, rank);
@@ -346,6 +468,132 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             }
             __syncwarp();
         }
+    } else if (kCodes && warp == kKWarp) {
+        // ------------------------------------------------------------ K's codes and powers of two, as they lie in the pages
+        const int sub = min(1 << g.pages.page_shift, 64), boxes = 64 / sub;
+        int st = 0, ph = 1;
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            const int slot = k % kPromptPlans;
+            if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
+            const PromptTile t = sm.tile[slot];
+            if (t.n_steps == 0) break;
+            for (int j = 0; j < t.n_steps; ++j) {
+                const int key = t.key_of(j) + rank * 64 + lane * sub, in = key & ((1 << g.pages.page_shift) - 1);
+                const int page = lane < boxes ? page_for(t, key, sub) : 0;
+                if (!(ok = tc::mbar_wait_warp(&sm.rk_empty[st], ph, abort_flag))) break;
+                if (lane == 0) tc::mbar_arrive_expect_tx(&sm.rk_full[st], 64 * (D + 1));
+                __syncwarp();
+                if (lane < boxes) {
+                    tc::tma_load_4d(&sm.raw_k[st][lane * sub * D], &tmK, 0, in, t.gk, page, &sm.rk_full[st]);
+                    const long long at = (page < g.pages.n_pages ? page : 0) * g.pages.scale_stride + ((long long)t.gk << g.pages.page_shift) + in;
+                    tc::bulk_load(&sm.raw_ks[st][lane * sub], g.pages.ks + at, sub, &sm.rk_full[st]);
+                }
+                __syncwarp();
+                if (++st == kRawStages) { st = 0; ph ^= 1; }
+            }
+            if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
+        }
+    } else if (kCodes && warp == kVWarp) {
+        // ------------------------------------------------------------ V's: half `rank` of d of a step's 128 keys
+        const int sub = min(1 << g.pages.page_shift, 128), boxes = 128 / sub;
+        int st = 0, ph = 1;
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            const int slot = k % kPromptPlans;
+            if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
+            const PromptTile t = sm.tile[slot];
+            if (t.n_steps == 0) break;
+            for (int j = 0; j < t.n_steps; ++j) {
+                const int key = t.key_of(j) + lane * sub, in = key & ((1 << g.pages.page_shift) - 1);
+                const int page = lane < boxes ? page_for(t, key, sub) : 0;
+                if (!(ok = tc::mbar_wait_warp(&sm.rv_empty[st], ph, abort_flag))) break;
+                if (lane == 0) tc::mbar_arrive_expect_tx(&sm.rv_full[st], 128 * (D / 2 + 1));
+                __syncwarp();
+                if (lane < boxes) {
+                    tc::tma_load_4d(&sm.raw_v[st][lane * sub * (D / 2)], &tmV, rank * (D / 2), in, t.gk, page, &sm.rv_full[st]);
+                    const long long at = (page < g.pages.n_pages ? page : 0) * g.pages.scale_stride + ((long long)t.gk << g.pages.page_shift) + in;
+                    tc::bulk_load(&sm.raw_vs[st][lane * sub], g.pages.vs + at, sub, &sm.rv_full[st]);
+                }
+                __syncwarp();
+                if (++st == kRawStages) { st = 0; ph ^= 1; }
+            }
+            if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
+        }
+    } else if (kCodes && warp >= kPlanWarp + 1) {
+        // ------------------------------------------------------------ codes to bf16, as TMA would have laid that down: two warps K, two V
+        const int mine = warp - (kPlanWarp + 1), part = mine & 1;
+        const bool is_v = mine >= 2;
+        constexpr int kPieces = D / 16;                       // of 16 codes, of a thread
+        const int shift = (D == 128 ? 3 : 2) - (is_v ? 1 : 0);   // log2 of the pieces of a row
+        const uint32_t full0 = cluster_address(is_v ? sm.v_full : sm.k_full, 0);
+        const uint32_t odd0 = cluster_address(sm.odd_tile, 0), odd1 = cluster_address(sm.odd_tile, 1);
+        const int n_stages = is_v ? kVStages : kKStages;
+        int st = 0, ph = 1, raw = 0, raw_ph = 0;
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            const int slot = k % kPromptPlans;
+            if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
+            const PromptTile t = sm.tile[slot];
+            if (t.n_steps == 0) break;
+            for (int j = 0; j < t.n_steps; ++j) {
+                if (!(ok = tc::mbar_wait_warp(is_v ? &sm.rv_full[raw] : &sm.rk_full[raw], raw_ph, abort_flag))) break;
+                if (!(ok = tc::mbar_wait_warp(is_v ? &sm.v_empty[st] : &sm.k_empty[st], ph, abort_flag))) break;
+                const unsigned char* src = is_v ? sm.raw_v[raw] : sm.raw_k[raw];
+                const uint8_t* scales = is_v ? sm.raw_vs[raw] : sm.raw_ks[raw];
+                unsigned char* dst = reinterpret_cast<unsigned char*>(is_v ? sm.v[st] : sm.k[st]);
+                const bool looks = is_v && t.masked(j);       // for values that are no numbers
+                uint32_t any = 0u;
+#pragma unroll 2
+                for (int i = 0; i < kPieces; ++i) {
+                    const int x = part * kPieces * 32 + i * 32 + lane, row = x >> shift, c = x & ((1 << shift) - 1);
+                    const uint4 codes = *reinterpret_cast<const uint4*>(src + x * 16);
+                    const uint32_t s = min((uint32_t)scales[row], 254u);
+                    uint4 lo = chunk_values(make_uint2(codes.x, codes.y), s), hi = chunk_values(make_uint2(codes.z, codes.w), s);
+                    if (looks) {
+                        // exponents of all ones: adding 0x80 to (x & 0x7f80) carries into bit 15
+                        any |= ((lo.x & 0x7f807f80u) + 0x00800080u) | ((lo.y & 0x7f807f80u) + 0x00800080u) | ((lo.z & 0x7f807f80u) + 0x00800080u) |
+                               ((lo.w & 0x7f807f80u) + 0x00800080u) | ((hi.x & 0x7f807f80u) + 0x00800080u) | ((hi.y & 0x7f807f80u) + 0x00800080u) |
+                               ((hi.z & 0x7f807f80u) + 0x00800080u) | ((hi.w & 0x7f807f80u) + 0x00800080u);
+                    }
+                    // 16-byte chunks 2 c and 2 c + 1 of the row; of K's second panel the second first: the panels lie on the same banks
+                    const bool swap = !is_v && D == 128 && c >= 4;
+                    const uint4 first = swap ? hi : lo, second = swap ? lo : hi;
+                    const int o = 2 * c + (swap ? 1 : 0), o2 = o ^ 1;
+                    auto place = [&](int chunk) -> int {
+                        if (is_v && D == 64) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
+                        return (is_v ? 0 : (chunk >> 3) * (64 * 128)) + sw128(row, chunk & 7);
+                    };
+                    *reinterpret_cast<uint4*>(dst + place(o)) = first;
+                    *reinterpret_cast<uint4*>(dst + place(o2)) = second;
+                }
+                if (looks && __any_sync(0xffffffffu, (any & 0x80008000u) != 0u)) {
+                    // rare: zeros instead, and the rows add what they see (this warp's half of the keys, whole rows, as it has written them)
+                    __syncwarp();
+                    uint4* chunks = reinterpret_cast<uint4*>(dst) + part * kPieces * 64;
+                    for (int i = lane; i < kPieces * 64; i += 32) {
+                        uint32_t x[4] = {chunks[i].x, chunks[i].y, chunks[i].z, chunks[i].w};
+                        for (int e = 0; e < 4; ++e) {
+                            if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+                            if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
+                        }
+                        chunks[i] = make_uint4(x[0], x[1], x[2], x[3]);
+                    }
+                    if (lane < 2) asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"((lane ? odd1 : odd0) + (k % kPromptOddSlots) * 4), "r"(k + 1) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
+                    tc::mbar_arrive_release_cluster(full0 + st * 8);
+                    tc::mbar_arrive(is_v ? &sm.rv_empty[raw] : &sm.rk_empty[raw]);
+                }
+                __syncwarp();
+                if (++st == n_stages) { st = 0; ph ^= 1; }
+                if (++raw == kRawStages) { raw = 0; raw_ph ^= 1; }
+            }
+            if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
+        }
     } else if (warp == kKWarp) {
         // ------------------------------------------------------------ K: CTA r fetches the keys r * 64 .. of a step.  And masked steps:
         // values that are no numbers.  Whichever is ready, so that neither waits for the other.
@@ -354,6 +602,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
         auto ready = [&](uint64_t* bar, uint32_t phase) -> bool { return __all_sync(0xffffffffu, tc::mbar_test(bar, phase)); };
         struct { int k = 0, j = 0, n = 0, st = 0; bool done = false; } kp, look;      // tile, step, steps of the tile (0: not begun), stage
         int k_ph = 1, row0 = 0, gk = 0, first_masked = 0;
+        [[maybe_unused]] PromptTile kt, lt;                   // (pages) tiles of either
+        [[maybe_unused]] const int sub = kPaged ? min(1 << g.pages.page_shift, 64) : 64, boxes = 64 / sub;
         uint32_t raw_phases = 0, idle = 0;                    // (of v_raw, a bit each)
         uint64_t since = 0;
         while (!kp.done || !look.done) {
@@ -364,11 +614,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     kp.n = sm.tile[slot].n_steps;
                     row0 = sm.tile[slot].k0 + rank * 64;
                     gk = sm.tile[slot].gk;
+                    if (kPaged) kt = sm.tile[slot];
                     kp.done = kp.n == 0;
                     moved = true;
                 }
                 if (kp.n > 0 && ready(&sm.k_empty[kp.st], k_ph)) {
-                    if (tc::elect_one()) {
+                    if constexpr (kPaged) {
+                        const int box = lane % boxes, panel = lane / boxes, key = kt.key_of(kp.j) + rank * 64 + box * sub;
+                        const int page = panel < kPanels ? page_for(kt, key, sub) : 0;
+                        if (rank == 0 && lane == 0) tc::mbar_arrive_expect_tx(&sm.k_full[kp.st], 2 * kTileBytes);
+                        __syncwarp();
+                        if (panel < kPanels)
+                            tc::tma_load_4d_pair(&sm.k[kp.st][(panel * 64 + box * sub) * 64], &tmK, panel * 64, key & ((1 << g.pages.page_shift) - 1), gk, page, bar0 + kp.st * 8);
+                    } else if (tc::elect_one()) {
                         if (rank == 0) tc::mbar_arrive_expect_tx(&sm.k_full[kp.st], 2 * kTileBytes);
                         for (int p = 0; p < kPanels; ++p)
                             tc::tma_load_3d_pair(&sm.k[kp.st][p * 64 * 64], &tmK, p * 64, gk, row0 + kp.j * 128, bar0 + kp.st * 8);
@@ -388,8 +646,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 if (look.n == 0 && ready(&sm.plan_full[slot], (look.k / kPromptPlans) & 1)) {
                     look.n = sm.tile[slot].n_steps;
                     first_masked = sm.tile[slot].first_masked;
+                    if (kPaged) lt = sm.tile[slot];
                     look.done = look.n == 0;
-                    look.j = min(first_masked, look.n);
+                    look.j = kPaged ? lt.next_masked(0) : min(first_masked, look.n);
                     look.st = (look.st + look.j) % kVStages;
                     moved = true;
                 }
@@ -425,6 +684,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     __syncwarp();
                     if (++look.st == kVStages) look.st = 0;
                     ++look.j;
+                    if (kPaged) {
+                        const int next = lt.next_masked(look.j);
+                        look.st = (look.st + next - look.j) % kVStages;
+                        look.j = next;
+                    }
                     moved = true;
                 }
                 if (look.n > 0 && look.j == look.n) {
@@ -442,6 +706,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                 if (now - since > plan_limit) *abort_flag = 1;
                 if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
             }
+        }
+    } else if (kPaged && warp == kVWarp) {
+        // ------------------------------------------------------------ V from its pages: CTA r fetches half r of d of a step's 128 keys
+        const uint32_t bar0 = cluster_address(sm.v_full, 0);
+        const int sub = min(1 << g.pages.page_shift, 128), boxes = 128 / sub;
+        int st = 0, ph = 1;
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            const int slot = k % kPromptPlans;
+            if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
+            const PromptTile t = sm.tile[slot];
+            if (t.n_steps == 0) break;
+            for (int j = 0; j < t.n_steps; ++j) {
+                const int key = t.key_of(j) + lane * sub, in = key & ((1 << g.pages.page_shift) - 1);
+                const int page = lane < boxes ? page_for(t, key, sub) : 0;
+                if (!(ok = tc::mbar_wait_warp(&sm.v_empty[st], ph, abort_flag))) break;
+                const bool masked = t.masked(j);              // K's warp looks for what is no number and says that it is there
+                if (lane == 0) {
+                    if (masked) tc::mbar_arrive_expect_tx(&sm.v_raw[st], kTileBytes);
+                    else if (rank == 0) tc::mbar_arrive_expect_tx(&sm.v_full[st], 2 * kTileBytes);
+                    else tc::mbar_arrive_cluster(bar0 + st * 8);
+                }
+                __syncwarp();
+                if (lane < boxes) {
+                    if (masked) tc::tma_load_4d(&sm.v[st][lane * sub * (D / 2)], &tmV, rank * (D / 2), in, t.gk, page, &sm.v_raw[st]);
+                    else tc::tma_load_4d_pair(&sm.v[st][lane * sub * (D / 2)], &tmV, rank * (D / 2), in, t.gk, page, bar0 + st * 8);
+                }
+                __syncwarp();
+                if (++st == kVStages) { st = 0; ph ^= 1; }
+            }
+            if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
         }
     } else if (warp == kVWarp) {
         // ------------------------------------------------------------ V: CTA r fetches half r of d of a step's 128 keys
@@ -588,26 +883,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
             if (t.n_steps == 0) break;
             const int last = t.last0 + tok;                   // the last key that the row sees
             const bool valid = tok < t.n_tok;                 // (the tile's last rows may be none, tokens behind the sequence not its own)
+            const int first = kPaged && g.window > 0 ? max(last + 1 - g.window, 0) : 0;   // of those behind the first ones
+            const bool idle = kPaged && !__any_sync(0xffffffffu, valid);   // no row of the warp is one: nothing is computed
             const int j0 = (team + g0) & 1;
             const bool finishes = ((g0 + t.n_steps - 1) & 1) == team;
             float m_ref = 0.f, l_sum = 0.f;
             for (int j = j0; j < t.n_steps; j += kPromptTeams) {
                 const int gs = g0 + j, rs = gs & (kPromptRefSlots - 1), buf = gs % kPromptBufs;
                 const uint32_t s_addr = lane_addr + buf * 128 + half * 64;
-                const bool masked = j >= t.first_masked;
+                const bool masked = kPaged ? t.masked(j) : j >= t.first_masked;
+                const int key0 = kPaged ? t.key_of(j) + half * 64 : j * 128 + half * 64;
+                // (pages) which of the 32 keys from key0 + 32 c on the row sees
+                auto seen_of = [&](int c) -> uint32_t {
+                    const int k = key0 + c * 32;
+                    auto below = [](int n) -> uint32_t { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+                    return below(last + 1 - k) & (~below(first - k) | below(g.sinks - k));
+                };
                 const int n_vis = masked ? last + 1 - j * 128 - half * 64 : 64;    // keys of the half step that the row sees (any number)
                 if (!tc::mbar_wait(&sm.s_full[buf], (gs / kPromptBufs) & 1, abort_flag)) ok = false;
                 tc::tc_fence_after_sync();
                 auto hide = [&](uint32_t (&s)[32], int c) {
                     const int n = n_vis - c * 32;
+                    const uint32_t seen = kPaged ? seen_of(c) : 0u;
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
-                        if (i >= n) s[i] = 0xff800000u;
+                        if (kPaged ? (seen >> i & 1u) == 0u : i >= n) s[i] = 0xff800000u;
                 };
                 // what the warp's rows see of a chunk of 32 keys: nothing, all of it, or each its own (hide).  Most chunks of masked steps are of
                 // the first two kinds
-                auto sees_none = [&](int c) -> bool { return masked && __all_sync(0xffffffffu, !valid || n_vis - c * 32 <= 0); };
-                auto sees_all = [&](int c) -> bool { return !masked || __all_sync(0xffffffffu, !valid || n_vis - c * 32 >= 32); };
+                auto sees_none = [&](int c) -> bool {
+                    if (kPaged) return idle || (masked && __all_sync(0xffffffffu, !valid || seen_of(c) == 0u));
+                    return masked && __all_sync(0xffffffffu, !valid || n_vis - c * 32 <= 0);
+                };
+                auto sees_all = [&](int c) -> bool {
+                    if (kPaged) return !masked || __all_sync(0xffffffffu, !valid || seen_of(c) == ~0u);
+                    return !masked || __all_sync(0xffffffffu, !valid || n_vis - c * 32 >= 32);
+                };
                 auto largest = [&](const uint32_t (&s)[32]) -> float {
                     float a0 = -INFINITY, a1 = -INFINITY;
 #pragma unroll
@@ -617,12 +928,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     }
                     return fmaxf(a0, a1);
                 };
-                if (j == 0) {
-                    // ---- the reference of the tile: the largest of the first 128 scores
+                // ---- the largest of the step's scores, of both halves; none: the lowest reference there is, above which any score is far, and the
+                // first step that has one moves it.  An overflow of the product with the scale ends there, too
+                auto first_reference = [&]() -> float {
                     float top = -INFINITY;
 #pragma unroll 1
                     for (int c = 0; c < 2; ++c) {
-                        if (sees_none(c)) break;
+                        if (sees_none(c)) {
+                            if (kPaged) continue;             // (a window may hide the first keys alone)
+                            break;
+                        }
                         uint32_t s[32];
                         tc::tmem_ld_32x32(s_addr + c * 32, s);
                         tc::tmem_wait_ld_for(s);
@@ -631,10 +946,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     }
                     sm.other_ref[team][half][row] = top;
                     pair_sync();
-                    top = fmaxf(top, sm.other_ref[team][half ^ 1][row]) * scale_log2;    // scale > 0
-                    // (-inf: so far the row sees nothing, or scores of -inf alone; the lowest reference there is, above which any score is
-                    // far, and the first step that has one moves it.  An overflow of the product with the scale ends there, too)
-                    m_ref = fmaxf(top, kPromptLowest);
+                    return fmaxf(fmaxf(top, sm.other_ref[team][half ^ 1][row]) * scale_log2, kPromptLowest);    // scale > 0
+                };
+                if (j == 0) {
+                    // ---- the reference of the tile: the largest of the first 128 scores
+                    m_ref = first_reference();
                     if (half == 0) {
                         sm.first_ref[k & 1][row] = m_ref;
                         __syncwarp();
@@ -645,14 +961,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     if (!tc::mbar_wait(&sm.first_done[k & 1][quad], (k >> 1) & 1, abort_flag)) ok = false;
                     m_ref = sm.first_ref[k & 1][row];
                 }
+                float ref_now = m_ref;
+                if (kPaged && j > 0 && __any_sync(0xffffffffu, valid && m_ref == kPromptLowest)) {
+                    // rows that have seen nothing (a window that begins behind their tile's first step): their reference is this step's.  (Both
+                    // halves of a row hold the same reference)
+                    const float top = first_reference();
+                    if (m_ref == kPromptLowest) ref_now = top;
+                    pair_sync();
+                }
                 // ---- weights, 32 keys at a time over the scores
-                const float ref = m_ref;
+                const float ref = ref_now;
                 const unsigned long long add2 = pack_f32x2(-ref, -ref);
                 unsigned long long psA = 0ull, psB = 0ull;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     uint32_t s[32], pk[16];
                     if (sees_none(c)) {
+                        if (idle) continue;                   // (rows that nobody reads)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) pk[i] = 0u;
                         tc::tmem_st_32x16(s_addr + c * 16, pk);
@@ -690,22 +1015,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                     // rare: the reference of one half has to move, or that of the step before has
                     const bool lost = over && !(l_step < 0x1p100f);   // (weights near 2^128 are infinite, their factors near 2^-126 zero)
                     const __nv_bfloat16* q_row = g.q + (long long)(t.q0 + tok) * g.q_ts + (t.gk * g.G + head) * g.q_hs;
-                    const int key0 = j * 128 + half * 64, n_keys = lost ? min(last + 1 - key0, 64) : 0;
-                    const __nv_bfloat16* keys = g.k + (long long)(t.k0 + key0) * g.k_ts + t.gk * g.k_hs;
+                    const int n_keys = lost ? min(last + 1 - key0, 64) : 0;
+                    const __nv_bfloat16* keys = kPaged ? nullptr : g.k + (long long)(t.k0 + key0) * g.k_ts + t.gk * g.k_hs;
+                    auto score = [&](int i) -> float {        // -inf: the row does not see it
+                        if constexpr (kPaged) return seen_of(i >> 5) >> (i & 31) & 1u ? paged_dot<D, kCodes>(g.pages, t.seq, t.gk, key0 + i, q_row) * scale_log2 : -INFINITY;
+                        else return prompt_dot<D>(q_row, keys + i * g.k_ts) * scale_log2;
+                    };
                     float mine = ref;
                     if (over && !lost) mine += ceilf(log2f(l_step));
-                    for (int i = 0; i < n_keys; ++i) mine = fmaxf(mine, prompt_dot<D>(q_row, keys + i * g.k_ts) * scale_log2);
+                    for (int i = 0; i < n_keys; ++i) mine = fmaxf(mine, score(i));
                     // up by a whole number, as above; so far (or from the lowest reference) that what stood before is zero: to the score itself
                     if (lost && mine - ref < 512.f) mine = ref + ceilf(mine - ref);
                     sm.other_ref[team][half][row] = mine;
                     pair_sync();
                     m_new = fmaxf(m_prev, fmaxf(mine, sm.other_ref[team][half ^ 1][row]));
-                    const float f = fast_exp2(ref - m_new);
-                    l_step = lost ? 0.f : l_step * f;
+                    // (pages: a reference that did not begin with the other team's may lie a fraction apart)
+                    if (kPaged && m_new - ref < 512.f) m_new = ref + ceilf(m_new - ref);
+                    const MovedBy f(ref - m_new);
+                    l_step = lost ? 0.f : f.of(l_step);
                     l_sum *= fast_exp2(m_ref - m_new);
                     tc::tmem_wait_st();
+                    const bool rewrite = !kPaged || __any_sync(0xffffffffu, ref != m_new);   // (pages: a first reference moves nothing)
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < (rewrite ? 4 : 0); ++c) {
                         uint32_t w[8];
                         tc::tmem_ld_32x8(s_addr + c * 8, w);
                         tc::tmem_wait_ld();
@@ -716,22 +1048,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
 #pragma unroll
                                 for (int y = 0; y < 2; ++y) {
                                     const int i = c * 16 + 2 * e + y;
-                                    p[y] = i < n_keys ? fast_exp2(fmaf(prompt_dot<D>(q_row, keys + i * g.k_ts), scale_log2, -m_new)) : 0.f;
+                                    if constexpr (kPaged) p[y] = i < n_keys ? fast_exp2(score(i) - m_new) : 0.f;
+                                    else p[y] = i < n_keys ? fast_exp2(fmaf(prompt_dot<D>(q_row, keys + i * g.k_ts), scale_log2, -m_new)) : 0.f;
                                     l_step += p[y];
                                 }
                                 w[e] = pack_bf16x2(p[0], p[1]);
                             }
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
+                            for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(f.of(__uint_as_float(w[e] << 16)), f.of(__uint_as_float(w[e] & 0xffff0000u)));
                         }
                         __syncwarp();
                         tc::tmem_st_32x8(s_addr + c * 8, w);
                     }
-                    if (j > 0 && __any_sync(0xffffffffu, m_new != m_prev)) {
+                    if (j > 0 && __any_sync(0xffffffffu, m_new != m_prev && (!kPaged || (valid && m_prev != kPromptLowest)))) {   // (from the lowest: O is zero)
                         // O holds the products of all steps up to the last one, and no later one starts before this step's weights are
                         // reported; half its columns each
-                        const float factor = fast_exp2(m_prev - m_new);
+                        const MovedBy factor(m_prev - m_new);
                         if (!tc::mbar_wait(&sm.v_empty[(gs - 1) % kVStages], ((gs - 1) / kVStages) & 1, abort_flag)) ok = false;
                         tc::tc_fence_after_sync();
 #pragma unroll 1
@@ -741,7 +1074,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                             tc::tmem_ld_32x32(at, o0);
                             tc::tmem_wait_ld_for(o0);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o0[e] = __float_as_uint(__uint_as_float(o0[e]) * factor);
+                            for (int e = 0; e < 32; ++e) o0[e] = __float_as_uint(factor.of(__uint_as_float(o0[e])));
                             tc::tmem_st_32x32(at, o0);
                         }
                     }
@@ -805,6 +1138,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                         if (lane == 0) tc::mbar_arrive_cluster(o_free_bar);
                     }
                     if (part_o != nullptr) {
+                        if (kPaged && !mine) continue;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(part_o + c * 32 + e * 4) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                         continue;
@@ -819,7 +1153,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
                         *reinterpret_cast<uint4*>(srow + (c * 4 + e) * 16) = val;
                     }
                 }
-                if (odd && mine) {                            // rare: values that are no numbers and that this row sees
+                if (kPaged && odd && mine) {                  // rare: values that are no numbers and that this row sees
+                    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(srow);
+                    for (int j = t.next_masked(0); j < t.n_steps; j = t.next_masked(j + 1))
+                        for (int key = t.key_of(j), end = min(key + 128, last + 1); key < end; ++key) {
+                            if (key < first && key >= g.sinks) continue;
+                            for (int c = 0; c < D / 16; ++c) {
+                                const uint4 chunk = paged_chunk<D, kCodes>(g.pages, g.pages.v, g.pages.vs, t.seq, t.gk, key, half * (D / 16) + c);
+                                const uint32_t w[4] = {chunk.x, chunk.y, chunk.z, chunk.w};
+                                for (int e = 0; e < 8; ++e) {
+                                    const float x = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+                                    const int d = c * 8 + e;
+                                    if (fabsf(x) < INFINITY) continue;
+                                    if (part_o != nullptr) part_o[d] += x;
+                                    else o[d] = __float2bfloat16(__bfloat162float(o[d]) + x);
+                                }
+                            }
+                        }
+                }
+                if (!kPaged && odd && mine) {
                     __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(srow);
                     for (int key = t.first_masked * 128; key <= last; ++key) {
                         const __nv_bfloat16* vr = g.v + (long long)(t.k0 + key) * g.v_ts + t.gk * g.v_hs + half * (D / 2);
@@ -855,14 +1207,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromptThreads, 1) a
 // part is item i.
 constexpr int kPromptJoinThreads = 256, kPromptJoinRows = 16;
 
-template <int D>
+template <int D, bool kPaged>
 __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptGeom g, int n_pairs, const float* partial, __nv_bfloat16* out, float* lse) {
     constexpr int kLanes = D / 4, kRows = 32 / kLanes;        // threads of a row, rows of a warp
-    __shared__ PromptWalk found;
+    __shared__ PromptWalk<kPaged> found;
     __shared__ int mine;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (warp == 0) {
-        PromptWalk w;
+        PromptWalk<kPaged> w;
         w.begin(g, true, n_pairs, lane);
         const bool x = w.find(g, blockIdx.x, lane, true) && w.part == 0;
         if (lane == 0) {
@@ -874,7 +1226,7 @@ __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptG
     launch_dependents();
     wait_for_previous_kernel();
     if (!mine) return;
-    const PromptWalk& w = found;
+    const PromptWalk<kPaged>& w = found;
     const float2* stats = reinterpret_cast<const float2*>(partial + (size_t)kPromptParts * 256 * D);
     const int d4 = lane % kLanes;
     for (int r = warp * kRows + lane / kLanes; r < kPromptJoinRows; r += kRows * (kPromptJoinThreads / 32)) {
@@ -898,19 +1250,19 @@ __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptG
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (p0 + i < w.parts && s[i].y != 0.f) top = fmaxf(top, s[i].x);      // (0: the row sees none of the part's keys)
-            const float c = l != 0.f ? fast_exp2(m - top) : 0.f;
-            l *= c;
-            acc.x *= c; acc.y *= c; acc.z *= c; acc.w *= c;
+            const MovedBy c(l != 0.f ? m - top : -INFINITY);
+            l = c.of(l);
+            acc = make_float4(c.of(acc.x), c.of(acc.y), c.of(acc.z), c.of(acc.w));
             m = top;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (p0 + i >= w.parts || s[i].y == 0.f) continue;
-                const float f = fast_exp2(s[i].x - m);
-                l = fmaf(s[i].y, f, l);
-                acc.x = fmaf(o[i].x, f, acc.x);
-                acc.y = fmaf(o[i].y, f, acc.y);
-                acc.z = fmaf(o[i].z, f, acc.z);
-                acc.w = fmaf(o[i].w, f, acc.w);
+                const MovedBy f(s[i].x - m);
+                l = fmaf(s[i].y * f.b, f.a, l);
+                acc.x = fmaf(o[i].x * f.b, f.a, acc.x);
+                acc.y = fmaf(o[i].y * f.b, f.a, acc.y);
+                acc.z = fmaf(o[i].z * f.b, f.a, acc.z);
+                acc.w = fmaf(o[i].w * f.b, f.a, acc.w);
             }
         }
         const float inv = l != 0.f ? 1.f / l : 0.f;

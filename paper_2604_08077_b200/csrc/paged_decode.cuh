@@ -243,11 +243,6 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {   // 16-byte aligned, a multiple of 16 bytes
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(smem_u32(smem_dst)), "l"(src), "r"(bytes),
-                 "r"(smem_u32(bar))
-                 : "memory");
-}
 __device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 128;\n" ::: "memory"); }
 
 // kGroups: groups of 8 heads, (G + 7) / 8.
@@ -321,7 +316,7 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
             if (!(ok = tc::mbar_wait_warp(&sm.q_empty[qs], ((part / kQSlots) & 1) ^ 1, abort_flag))) break;
             if (lane == 0) tc::mbar_arrive_expect_tx(&sm.q_full[qs], (uint32_t)a.G * D * 2);
             __syncwarp();
-            if (lane < a.G) bulk_load(&sm.q[qs * 8 + lane][0], a.q + w.b * a.q_ts + (w.gk * a.G + lane) * a.q_hs, D * 2, &sm.q_full[qs]);
+            if (lane < a.G) tc::bulk_load(&sm.q[qs * 8 + lane][0], a.q + w.b * a.q_ts + (w.gk * a.G + lane) * a.q_hs, D * 2, &sm.q_full[qs]);
             for (int tile = w.tile; tile < w.end; ++tile) {
                 const int pos0 = w.line.tile_at(w.n, w.tiles, tile) * kTile, col0 = pos0 >> page_shift;
                 if (kWin && col0 >= cols + 64) {              // over what lies between the first tokens and the window
@@ -367,8 +362,8 @@ __global__ void __launch_bounds__(kPagedThreads, 2) paged_decode_kernel(PageGeom
                         tc::tma_load_4d(&sm.kv[st][0][lane * sub * kRowBytes], &tmK, 0, slot, w.gk, at, &sm.full[st]);
                         tc::tma_load_4d(&sm.kv[st][1][lane * sub * kRowBytes], &tmV, 0, slot, w.gk, at, &sm.full[st]);
                         const long long s_at = (long long)(there ? page : 0) * p.scale_stride + ((long long)w.gk << page_shift) + slot;
-                        bulk_load(&sm.scale[st][0][lane * sub], p.ks + s_at, sub, &sm.full[st]);
-                        bulk_load(&sm.scale[st][1][lane * sub], p.vs + s_at, sub, &sm.full[st]);
+                        tc::bulk_load(&sm.scale[st][0][lane * sub], p.ks + s_at, sub, &sm.full[st]);
+                        tc::bulk_load(&sm.scale[st][1][lane * sub], p.vs + s_at, sub, &sm.full[st]);
                     } else {
 #pragma unroll
                         for (int x = 0; x < D / 64; ++x) {

@@ -120,7 +120,14 @@ __device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* t
         : "memory");
 }
 
-// The same for a 5-D tensor map: coordinates innermost first.  c0 * element size must be a multiple of 16 bytes.
+// Untiled: both addresses 16-byte aligned, a multiple of 16 bytes.
+__device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(smem_u32(smem_dst)), "l"(src), "r"(bytes),
+                 "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// Tiled, for a 5-D tensor map: coordinates innermost first.  c0 * element size must be a multiple of 16 bytes.
 __device__ __forceinline__ void tma_load_5d(void* smem_dst, const CUtensorMap* tm, int c0, int c1, int c2, int c3, int c4, uint64_t* bar) {
     asm volatile(
         "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];\n" ::"r"(
@@ -270,8 +277,8 @@ __device__ __forceinline__ bool elect_one() {
     return pred != 0;
 }
 // mbar_wait by all lanes of a converged warp with a warp-uniform result.
-__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns = kWaitLimitNs) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit_ns));
 }
 // Arrives on `bar` once every tcgen05.mma issued so far by this thread has completed.
 __device__ __forceinline__ void umma_commit(uint64_t* bar) {
@@ -305,6 +312,13 @@ __device__ __forceinline__ void tma_load_3d_pair(void* smem_dst, const CUtensorM
         "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n" ::"r"(
             smem_u32(smem_dst)),
         "l"(reinterpret_cast<uint64_t>(tm)), "r"(cluster_bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_4d_pair(void* smem_dst, const CUtensorMap* tm, int c0, int c1, int c2, int c3, uint32_t cluster_bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n" ::"r"(
+            smem_u32(smem_dst)),
+        "l"(reinterpret_cast<uint64_t>(tm)), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
@@ -418,20 +432,25 @@ inline bool encode_bf16_rows(CUtensorMap* tm, const void* base, uint64_t n, uint
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Pages [n_pages][heads][page][d] of bf16 or bytes (page_stride in elements): boxes of up to 128 bytes of d x box_n slots of one head, with
-// the swizzle of such a row.  Coordinates outside the tensor read zeros.
-inline bool encode_pages(CUtensorMap* tm, const void* base, bool bytes, uint64_t n_pages, uint64_t heads, uint64_t page, uint64_t d,
-                         uint64_t page_stride, uint32_t box_n) {
+// Pages [n_pages][heads][page][d] of bf16 or bytes (page_stride in elements): boxes of box_d values x box_n slots of one head.  Coordinates
+// outside the tensor read zeros.
+inline bool encode_page_boxes(CUtensorMap* tm, const void* base, bool bytes, uint64_t n_pages, uint64_t heads, uint64_t page, uint64_t d,
+                              uint64_t page_stride, uint32_t box_d, uint32_t box_n, CUtensorMapSwizzle swizzle) {
     PFN_encodeTiled enc = get_encode_tiled();
     if (!enc) return false;
     const uint64_t elem_bytes = bytes ? 1 : 2;
     cuuint64_t dims[4] = {d, page, heads, n_pages};
     cuuint64_t strides[3] = {d * elem_bytes, page * d * elem_bytes, page_stride * elem_bytes};
-    cuuint32_t box[4] = {bytes ? (uint32_t)d : 64u, box_n, 1, 1};
+    cuuint32_t box[4] = {box_d, box_n, 1, 1};
     cuuint32_t elem[4] = {1, 1, 1, 1};
     return enc(tm, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, elem,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, bytes && d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+               CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The same with boxes of up to 128 bytes of d and the swizzle of such a row.
+inline bool encode_pages(CUtensorMap* tm, const void* base, bool bytes, uint64_t n_pages, uint64_t heads, uint64_t page, uint64_t d,
+                         uint64_t page_stride, uint32_t box_n) {
+    return encode_page_boxes(tm, base, bytes, n_pages, heads, page, d, page_stride, bytes ? (uint32_t)d : 64u, box_n,
+                             bytes && d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // A 5-D bf16 tensor map with the 128-byte swizzle: dims / box innermost first, strides (bytes) of dims 1..4.

@@ -4,7 +4,6 @@
 #include <atomic>
 #include <type_traits>
 
-#include "attn_paged.cuh"
 #include "attn_prompt.cuh"
 #include "paged_cache.cuh"
 #include "paged_decode.cuh"
@@ -142,6 +141,50 @@ adaspark_status_t paged_rows_impl(adaspark_attn* h, const char* who, const adasp
     if (D == 128) e4m3 ? with(wide, std::true_type()) : with(wide, std::false_type());
     else e4m3 ? with(narrow, std::true_type()) : with(narrow, std::false_type());
     return launch_ok(h, write ? "paged_write_kernel" : "paged_read_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+}
+
+// What prompts of packed keys and of pages share.
+void prompt_geom(const adaspark_attn* h, const int32_t* cu_q, int batch, int n_q, const Rows& rq, PromptGeom& g) {
+    g.cu_q = cu_q;
+    g.batch = batch;
+    g.n_q = n_q;
+    g.Hq = h->cfg.n_q_heads;
+    g.Hkv = h->cfg.n_kv_heads;
+    g.G = g.Hq / g.Hkv;
+    g.T = 128 / g.G;
+    g.div_w.init(2 * g.T);
+    g.div_g.init(g.G);
+    g.div_kv.init(g.Hkv);
+    g.scale_log2 = text_scale(h) * 1.4426950408889634f;
+    g.q = rq.p;
+    g.q_ts = rq.ts;
+    g.q_hs = rq.hs;
+}
+// 2 T tokens a tile, at most one tile of each sequence not full
+long long prompt_most_tiles(const PromptGeom& g) { return ((long long)g.n_q / (2 * g.T) + g.batch) * g.Hkv; }
+
+struct PromptOut {
+    __nv_bfloat16* out;
+    float *lse, *partial;                          // partial null: nothing is cut
+    int32_t* status;
+};
+template <int D, int kKeys>
+adaspark_status_t launch_prompt(adaspark_attn* h, const PromptGeom& g, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PromptOut& o,
+                                void* cuda_stream) {
+    // a pair of CTAs per tile, at most as many as there are SMs
+    const long long most = prompt_most_tiles(g);
+    int pairs = h->sm_count / 2 < kPromptPairs ? h->sm_count / 2 : kPromptPairs;
+    if (!o.partial && most < pairs) pairs = (int)most;
+    constexpr auto kernel = attn_prompt_kernel<D, kKeys>;
+    const size_t bytes = sizeof(PromptSmem<D, kKeys>) + 1024;
+    if (!text_smem<kernel>(h, bytes, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    launch_kernel(true, kernel, dim3(2 * pairs), dim3(prompt_threads(kKeys)), bytes, st, g, tmQ, tmK, tmV, o.out, o.lse, o.partial, o.status);
+    if (!launch_ok(h, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
+    if (!o.partial) return ADASPARK_OK;
+    launch_kernel(true, prompt_join_kernel<D, kKeys != kKeysPacked>, dim3(kPromptParts, 256 / kPromptJoinRows), dim3(kPromptJoinThreads), 0, st, g, pairs,
+                  (const float*)o.partial, o.out, o.lse);
+    return launch_ok(h, "prompt_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
 }
 
 // window 0: none
@@ -299,22 +342,9 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_p
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));
     PromptGeom g;
-    g.cu_q = c->cu_q;
+    prompt_geom(h, c->cu_q, batch, n_q, rq, g);
     g.cu_k = c->cu_k;
-    g.batch = batch;
-    g.n_q = n_q;
     g.n_k = n_k;
-    g.Hq = h->cfg.n_q_heads;
-    g.Hkv = h->cfg.n_kv_heads;
-    g.G = g.Hq / g.Hkv;
-    g.T = 128 / g.G;
-    g.div_w.init(2 * g.T);
-    g.div_g.init(g.G);
-    g.div_kv.init(g.Hkv);
-    g.scale_log2 = text_scale(h) * 1.4426950408889634f;
-    g.q = rq.p;
-    g.q_ts = rq.ts;
-    g.q_hs = rq.hs;
     g.k = rk.p;
     g.k_ts = rk.ts;
     g.k_hs = rk.hs;
@@ -326,24 +356,9 @@ adaspark_status_t adaspark_attn_prompt(adaspark_attn_t* h, const adaspark_attn_p
     if (!encode_bf16_rows(&tmQ, rq.p, n_q, g.Hq, D, rq.ts, rq.hs, 64, g.G, g.T) || !encode_bf16_rows(&tmK, rk.p, n_rows, g.Hkv, D, rk.ts, rk.hs, 64, 1, 64) ||
         !encode_bf16_rows(&tmV, rv.p, n_rows, g.Hkv, D, rv.ts, rv.hs, D / 2, 1, 128))
         return fail(h, ADASPARK_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
-    // a pair of CTAs per tile, at most as many as there are SMs: 2 T tokens a tile, at most one tile of each sequence not full
-    const long long most = ((long long)n_q / (2 * g.T) + batch) * g.Hkv;
-    int pairs = h->sm_count / 2 < kPromptPairs ? h->sm_count / 2 : kPromptPairs;
-    const bool cut = prompt_may_cut(most, n_k, c->cu_q == c->cu_k || n_q == n_k, 2 * g.T, g.Hkv);
-    float* partial = cut ? (float*)c->workspace : nullptr;
-    if (!cut && most < pairs) pairs = (int)most;
-    auto launch = [&](auto d) -> adaspark_status_t {
-        constexpr auto kernel = attn_prompt_kernel<d.value>;
-        const size_t bytes = sizeof(PromptSmem<d.value>) + 1024;
-        if (!text_smem<kernel>(h, bytes, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
-        cudaStream_t st = (cudaStream_t)cuda_stream;
-        launch_kernel(true, kernel, dim3(2 * pairs), dim3(kPromptThreads), bytes, st, g, tmQ, tmK, tmV, (__nv_bfloat16*)c->out, c->lse, partial, c->status);
-        if (!launch_ok(h, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
-        if (!cut) return ADASPARK_OK;
-        launch_kernel(true, prompt_join_kernel<d.value>, dim3(kPromptParts, 256 / kPromptJoinRows), dim3(kPromptJoinThreads), 0, st, g, pairs, (const float*)partial, (__nv_bfloat16*)c->out, c->lse);
-        return launch_ok(h, "prompt_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
-    };
-    return D == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>());
+    const bool cut = prompt_may_cut(prompt_most_tiles(g), n_k, c->cu_q == c->cu_k || n_q == n_k, 2 * g.T, g.Hkv);
+    const PromptOut o = {(__nv_bfloat16*)c->out, c->lse, cut ? (float*)c->workspace : nullptr, c->status};
+    return D == 128 ? launch_prompt<128, kKeysPacked>(h, g, tmQ, tmK, tmV, o, cuda_stream) : launch_prompt<64, kKeysPacked>(h, g, tmQ, tmK, tmV, o, cuda_stream);
 }
 
 adaspark_status_t adaspark_attn_paged_write(adaspark_attn_t* h, const adaspark_attn_paged_rows_t* c, void* cuda_stream) {
@@ -372,7 +387,8 @@ adaspark_status_t adaspark_attn_paged_prompt(adaspark_attn_t* h, const adaspark_
     if (c->window < 0 || c->sinks < 0) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: window %d, sinks %d", who, c->window, c->sinks);
     h->launches = 0;
     if (c->batch == 0 || c->n == 0) return ADASPARK_OK;
-    PageGeom p;
+    PromptGeom g;
+    PageGeom& p = g.pages;
     Rows rq;
     ADASPARK_TRY(check_pages(h, who, &c->pages, c->block_table, c->table_width, p));
     ADASPARK_TRY(check_rows(h, who, "q", c->q, h->cfg.n_q_heads, rq));
@@ -381,28 +397,26 @@ adaspark_status_t adaspark_attn_paged_prompt(adaspark_attn_t* h, const adaspark_
     ADASPARK_TRY(check_workspace(h, who, c->workspace, c->workspace_bytes));
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));
-    ChunkCall a;
-    a.cu = c->cu;
-    a.kv_len = c->kv_len;
-    a.batch = c->batch;
-    a.n = c->n;
-    a.Hq = h->cfg.n_q_heads;
-    a.G = a.Hq / p.Hkv;
-    a.q = rq.p;
-    a.q_ts = rq.ts;
-    a.q_hs = rq.hs;
-    a.scale_log2 = text_scale(h) * 1.4426950408889634f;
-    a.window = c->window;
-    a.sinks = c->sinks;
-    a.out = (__nv_bfloat16*)c->out;
-    a.lse = c->lse;
-    a.status = c->status;
-    const dim3 grid((unsigned)(((long long)a.n * a.Hq + kChunkWarps - 1) / kChunkWarps));
+    prompt_geom(h, c->cu, c->batch, c->n, rq, g);
+    g.kv_len = c->kv_len;
+    g.window = c->window;
+    g.sinks = c->window ? c->sinks : 0;
+    // first ones and window, each rounded outwards by a step at most, and the 2 T tokens of a tile
+    const long long most = c->window ? (long long)c->sinks / 128 + ((long long)c->window + 2 * g.T) / 128 + 3 : 0x7fffffff;
+    g.most_steps = (int)(most < 0x7fffffff ? most : 0x7fffffff);
+    const int D = h->cfg.head_dim, page = c->pages.page_size, k_box = page < 64 ? page : 64, v_box = page < 128 ? page : 128;
     const bool e4m3 = c->pages.format == ADASPARK_PAGES_E4M3;
-    cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (h->cfg.head_dim == 128) launch_kernel(true, e4m3 ? attn_paged_kernel<128, true> : attn_paged_kernel<128, false>, grid, dim3(kChunkWarps * 32), 0, st, p, a);
-    else launch_kernel(true, e4m3 ? attn_paged_kernel<64, true> : attn_paged_kernel<64, false>, grid, dim3(kChunkWarps * 32), 0, st, p, a);
-    return launch_ok(h, "attn_paged_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
+    CUtensorMap tmQ, tmK, tmV;
+    if (!encode_bf16_rows(&tmQ, rq.p, c->n, g.Hq, D, rq.ts, rq.hs, 64, g.G, g.T) ||
+        !encode_page_boxes(&tmK, p.k, e4m3, p.n_pages, g.Hkv, page, D, p.page_stride, e4m3 ? D : 64, k_box, e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode_page_boxes(&tmV, p.v, e4m3, p.n_pages, g.Hkv, page, D, p.page_stride, D / 2, v_box,
+                           e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
+        return fail(h, ADASPARK_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
+    const long long longest = std::min((long long)c->table_width << p.page_shift, 128ll * g.most_steps);
+    const bool cut = prompt_may_cut(prompt_most_tiles(g), (int)std::min(longest, 0x7fffffffll), false, 2 * g.T, g.Hkv);
+    const PromptOut o = {(__nv_bfloat16*)c->out, c->lse, cut ? (float*)c->workspace : nullptr, c->status};
+    if (D == 128) return e4m3 ? launch_prompt<128, kKeysPages8>(h, g, tmQ, tmK, tmV, o, cuda_stream) : launch_prompt<128, kKeysPages>(h, g, tmQ, tmK, tmV, o, cuda_stream);
+    return e4m3 ? launch_prompt<64, kKeysPages8>(h, g, tmQ, tmK, tmV, o, cuda_stream) : launch_prompt<64, kKeysPages>(h, g, tmQ, tmK, tmV, o, cuda_stream);
 }
 
 adaspark_status_t adaspark_attn_rotary_init(adaspark_attn_rotary_t* r, const double* radians, const int32_t* axis, int32_t pairs, int32_t axes, int32_t adjacent) {
