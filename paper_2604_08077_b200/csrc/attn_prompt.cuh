@@ -64,6 +64,41 @@ __host__ __device__ constexpr int prompt_v_stages(int D, int keys) { return D ==
 __host__ __device__ constexpr int prompt_raw_stages(int D, int keys) { return keys != kKeysPages8 ? 0 : D == 64 ? 4 : 2; }   // steps whose codes are under way
 static_assert(prompt_v_stages(64, kKeysPacked) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
 
+// Shared memory by its 32-bit address
+__device__ __forceinline__ uint4 load_shared_16(uint32_t at) {
+    uint4 r;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at) : "memory");
+    return r;
+}
+__device__ __forceinline__ uint2 load_shared_8(uint32_t at) {
+    uint2 r;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];\n" : "=r"(r.x), "=r"(r.y) : "r"(at) : "memory");
+    return r;
+}
+__device__ __forceinline__ uint32_t load_shared_byte(uint32_t at) {
+    uint32_t r;
+    asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(r) : "r"(at) : "memory");
+    return r;
+}
+__device__ __forceinline__ void store_shared_16(uint32_t at, const uint4& v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// Bit 7 of each byte: the code is no number (0x7f, 0xff)
+__device__ __forceinline__ uint32_t odd_codes(uint32_t c) { return (c & 0x7f7f7f7fu) + 0x01010101u; }
+// 8 codes that are numbers times 2^(s - 127), s in 8 .. 134, as bf16: exact.  A code's exponent and mantissa four bits below bf16's are the same number
+// times 2^-120, subnormal ones too; f is 2^(s - 7) twice.  (Codes to f16, to f32, multiplied and rounded: as many instructions, but a chain
+// of conversions.)
+__device__ __forceinline__ uint4 codes_to_bf16x8(uint32_t a, uint32_t b, uint32_t f) {
+    const uint32_t p[4] = {__byte_perm(a, 0u, 0x1404), __byte_perm(a, 0u, 0x3424), __byte_perm(b, 0u, 0x1404), __byte_perm(b, 0u, 0x3424)};
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = ((p[i] >> 4) & 0x07f007f0u) | (p[i] & 0x80008000u);
+        asm("mul.rn.bf16x2 %0, %1, %2;\n" : "=r"(r[i]) : "r"(x), "r"(f));
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
 // What a reference that grows by -d does to what stands: times 2^d, in two factors, for a weight of up to 2^100 may meet a d below -126.
 struct MovedBy {
     float a, b;
@@ -526,6 +561,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
         const bool is_v = mine >= 2;
         constexpr int kPieces = D / 16;                       // of 16 codes, of a thread
         const int shift = (D == 128 ? 3 : 2) - (is_v ? 1 : 0);   // log2 of the pieces of a row
+        const int rows = 32 >> shift, c = lane & ((1 << shift) - 1), row0 = part * kPieces * rows + (lane >> shift);
+        // The thread's pieces are those of column c in the rows row0 + i * rows; their values 16-byte chunks 2 c and 2 c + 1 of the row, of K's
+        // second panel the second one first: the panels lie on the same banks.  Where the chunks of even and of odd pieces go:
+        auto place = [&](int row, int chunk) -> uint32_t {
+            if (is_v && D == 64) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
+            return (is_v ? 0 : (chunk >> 3) * (64 * 128)) + sw128(row, chunk & 7);
+        };
+        const bool swap = !is_v && D == 128 && c >= 4;
+        const int o = 2 * c + (swap ? 1 : 0);
+        const uint32_t even0 = place(row0, o), even1 = place(row0, o ^ 1), odd0p = place(row0 + rows, o), odd1p = place(row0 + rows, o ^ 1);
+        const uint32_t pair_step = 2 * rows * (is_v && D == 64 ? 64 : 128);   // two pieces on
+        const uint32_t raw0 = smem_u32(is_v ? sm.raw_v[0] : sm.raw_k[0]) + (part * kPieces * 32 + lane) * 16, scale0 = smem_u32(is_v ? sm.raw_vs[0] : sm.raw_ks[0]) + row0;
+        const uint32_t raw_first = swap ? 8 : 0, raw_second = swap ? 0 : 8;
+        const uint32_t tile0 = smem_u32(is_v ? sm.v[0] : sm.k[0]);
         const uint32_t full0 = cluster_address(is_v ? sm.v_full : sm.k_full, 0);
         const uint32_t odd0 = cluster_address(sm.odd_tile, 0), odd1 = cluster_address(sm.odd_tile, 1);
         const int n_stages = is_v ? kVStages : kKStages;
@@ -538,39 +587,54 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             if (t.n_steps == 0) break;
             for (int j = 0; j < t.n_steps; ++j) {
                 if (!(ok = tc::mbar_wait_warp(is_v ? &sm.rv_full[raw] : &sm.rk_full[raw], raw_ph, abort_flag))) break;
+                const uint32_t src = raw0 + raw * (64 * D), scales = scale0 + raw * (is_v ? 128 : 64), dst = tile0 + st * (64 * D * 2);
                 if (!(ok = tc::mbar_wait_warp(is_v ? &sm.v_empty[st] : &sm.k_empty[st], ph, abort_flag))) break;
-                const unsigned char* src = is_v ? sm.raw_v[raw] : sm.raw_k[raw];
-                const uint8_t* scales = is_v ? sm.raw_vs[raw] : sm.raw_ks[raw];
-                unsigned char* dst = reinterpret_cast<unsigned char*>(is_v ? sm.v[st] : sm.k[st]);
                 const bool looks = is_v && t.masked(j);       // for values that are no numbers
-                uint32_t any = 0u;
-#pragma unroll 2
-                for (int i = 0; i < kPieces; ++i) {
-                    const int x = part * kPieces * 32 + i * 32 + lane, row = x >> shift, c = x & ((1 << shift) - 1);
-                    const uint4 codes = *reinterpret_cast<const uint4*>(src + x * 16);
-                    const uint32_t s = min((uint32_t)scales[row], 254u);
-                    uint4 lo = chunk_values(make_uint2(codes.x, codes.y), s), hi = chunk_values(make_uint2(codes.z, codes.w), s);
-                    if (looks) {
+                uint32_t odd = 0u, any = 0u;
+#pragma unroll 1
+                for (int i = 0; i < kPieces; i += 2) {
+                    uint2 x[2][2];
+                    uint32_t sc[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        x[y][0] = load_shared_8(src + (i + y) * 512 + raw_first);
+                        x[y][1] = load_shared_8(src + (i + y) * 512 + raw_second);
+                        sc[y] = load_shared_byte(scales + (i + y) * rows);
+                    }
+                    uint4 r[2][2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint32_t f = (sc[y] + 120u) * 0x00800080u;      // 2^(s - 7) twice
+                        odd |= odd_codes(x[y][0].x) | odd_codes(x[y][0].y) | odd_codes(x[y][1].x) | odd_codes(x[y][1].y) | (sc[y] - 8u <= 126u ? 0u : 0x80u);
+                        r[y][0] = codes_to_bf16x8(x[y][0].x, x[y][0].y, f);
+                        r[y][1] = codes_to_bf16x8(x[y][1].x, x[y][1].y, f);
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint32_t at = dst + ((i + y) >> 1) * pair_step;
+                        store_shared_16(at + ((y & 1) ? odd0p : even0), r[y][0]);
+                        store_shared_16(at + ((y & 1) ? odd1p : even1), r[y][1]);
+                    }
+                }
+                if (__any_sync(0xffffffffu, (odd & 0x80808080u) != 0u)) {
+                    // rare: codes that are no numbers, powers of two far out
+#pragma unroll 1
+                    for (int i = 0; i < kPieces; ++i) {
+                        const uint32_t s = min(load_shared_byte(scales + i * rows), 254u);
+                        const uint4 lo = chunk_values(load_shared_8(src + i * 512 + raw_first), s), hi = chunk_values(load_shared_8(src + i * 512 + raw_second), s);
                         // exponents of all ones: adding 0x80 to (x & 0x7f80) carries into bit 15
                         any |= ((lo.x & 0x7f807f80u) + 0x00800080u) | ((lo.y & 0x7f807f80u) + 0x00800080u) | ((lo.z & 0x7f807f80u) + 0x00800080u) |
                                ((lo.w & 0x7f807f80u) + 0x00800080u) | ((hi.x & 0x7f807f80u) + 0x00800080u) | ((hi.y & 0x7f807f80u) + 0x00800080u) |
                                ((hi.z & 0x7f807f80u) + 0x00800080u) | ((hi.w & 0x7f807f80u) + 0x00800080u);
+                        const uint32_t at = dst + (i >> 1) * pair_step;
+                        store_shared_16(at + ((i & 1) ? odd0p : even0), lo);
+                        store_shared_16(at + ((i & 1) ? odd1p : even1), hi);
                     }
-                    // 16-byte chunks 2 c and 2 c + 1 of the row; of K's second panel the second first: the panels lie on the same banks
-                    const bool swap = !is_v && D == 128 && c >= 4;
-                    const uint4 first = swap ? hi : lo, second = swap ? lo : hi;
-                    const int o = 2 * c + (swap ? 1 : 0), o2 = o ^ 1;
-                    auto place = [&](int chunk) -> int {
-                        if (is_v && D == 64) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
-                        return (is_v ? 0 : (chunk >> 3) * (64 * 128)) + sw128(row, chunk & 7);
-                    };
-                    *reinterpret_cast<uint4*>(dst + place(o)) = first;
-                    *reinterpret_cast<uint4*>(dst + place(o2)) = second;
                 }
                 if (looks && __any_sync(0xffffffffu, (any & 0x80008000u) != 0u)) {
-                    // rare: zeros instead, and the rows add what they see (this warp's half of the keys, whole rows, as it has written them)
+                    // zeros instead, and the rows add what they see (this warp's half of the keys, whole rows, as it has written them)
                     __syncwarp();
-                    uint4* chunks = reinterpret_cast<uint4*>(dst) + part * kPieces * 64;
+                    uint4* chunks = reinterpret_cast<uint4*>(sm.v[st]) + part * kPieces * 64;
                     for (int i = lane; i < kPieces * 64; i += 32) {
                         uint32_t x[4] = {chunks[i].x, chunks[i].y, chunks[i].z, chunks[i].w};
                         for (int e = 0; e < 4; ++e) {
@@ -580,12 +644,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                         chunks[i] = make_uint4(x[0], x[1], x[2], x[3]);
                     }
                     if (lane < 2) asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"((lane ? odd1 : odd0) + (k % kPromptOddSlots) * 4), "r"(k + 1) : "memory");
+                    asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
-                    tc::mbar_arrive_release_cluster(full0 + st * 8);
+                    tc::mbar_arrive_cluster(full0 + st * 8);  // (what was written is this SM's own to read)
                     tc::mbar_arrive(is_v ? &sm.rv_empty[raw] : &sm.rk_empty[raw]);
                 }
                 __syncwarp();
