@@ -12,7 +12,7 @@
 namespace {
 
 constexpr int kCacheManyTokens = 16384;
-constexpr int kRotateFew = 1024;             // tokens
+constexpr int kRotateFew = 300, kRotateMany = 2400;   // tokens
 
 // The handle's device for the length of a call; the caller's is current again afterwards.
 struct DeviceScope {
@@ -302,12 +302,15 @@ adaspark_status_t check_turned(adaspark_attn* h, const char* who, int n, const a
 
 template <int kPages>
 adaspark_status_t launch_rotate(adaspark_attn* h, const RotateCall& a, const PageGeom& p, void* cuda_stream) {
-    const bool many = a.n > kRotateFew;
     auto launch = [&](auto kernel, int tokens) {
         launch_kernel(true, kernel, dim3((unsigned)((a.n + tokens - 1) / tokens)), dim3(kRotateThreads), 0, (cudaStream_t)cuda_stream, a, p);
     };
-    if (h->cfg.head_dim == 128) many ? launch(rotate_kernel<128, kPages, 4>, 4) : launch(rotate_kernel<128, kPages, 1>, 1);
-    else many ? launch(rotate_kernel<64, kPages, 8>, 8) : launch(rotate_kernel<64, kPages, 2>, 2);
+    // as many tokens a CTA as leave every SM two
+    const int step = a.n >= kRotateMany ? 2 : a.n >= kRotateFew ? 1 : 0;
+    if (h->cfg.head_dim == 128)
+        step == 2 ? launch(rotate_kernel<128, kPages, 8>, 8) : step == 1 ? launch(rotate_kernel<128, kPages, 4>, 4) : launch(rotate_kernel<128, kPages, 1>, 1);
+    else
+        step == 2 ? launch(rotate_kernel<64, kPages, 16>, 16) : step == 1 ? launch(rotate_kernel<64, kPages, 4>, 4) : launch(rotate_kernel<64, kPages, 1>, 1);
     return launch_ok(h, "rotate_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
 }
 
