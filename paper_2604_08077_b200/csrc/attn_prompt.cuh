@@ -49,6 +49,7 @@ namespace adaspark {
 constexpr int kKeysPacked = 0, kKeysPages = 1, kKeysPages8 = 2;
 
 constexpr int kPromptTeams = 2;                               // softmax teams, of two warpgroups each
+constexpr int kPromptCodeWarps = 4;                           // 8-bit pages: warps that see to codes and queries
 __host__ __device__ constexpr int prompt_threads(int keys) { return (2 * kPromptTeams + (keys == kKeysPages8 ? 2 : 1)) * 128; }
 constexpr int kPromptPlans = 4;                               // tiles planned at once
 constexpr int kPromptBufs = 3;                                // score tiles in TMEM
@@ -59,10 +60,12 @@ constexpr float kPromptLowest = -3.402823466e38f;             // a reference bel
 // a pair's tiles to its next (where a level has one tile).  Waits for its plans last so much longer.
 constexpr uint64_t kPromptPlanNs = 10000;                     // a sequence
 constexpr int kPromptOddSlots = 8;                            // more than tiles whose V can be under way at once (a step each)
-__host__ __device__ constexpr int prompt_k_stages(int D) { return D == 64 ? 6 : 3; }   // steps whose K, V are under way
-__host__ __device__ constexpr int prompt_v_stages(int D, int keys) { return D == 64 ? 6 : keys == kKeysPages8 ? 2 : 3; }
-__host__ __device__ constexpr int prompt_raw_stages(int D, int keys) { return keys != kKeysPages8 ? 0 : D == 64 ? 4 : 2; }   // steps whose codes are under way
-static_assert(prompt_v_stages(64, kKeysPacked) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
+__host__ __device__ constexpr int prompt_k_stages(int D, int keys) { return D == 64 ? 6 : keys == kKeysPages8 ? 4 : 3; }   // steps whose K, V are under way
+__host__ __device__ constexpr int prompt_v_stages(int D) { return D == 64 ? 6 : 3; }
+__host__ __device__ constexpr int prompt_raw_stages(int D, int keys) { return keys != kKeysPages8 ? 0 : D == 64 ? 6 : 3; }   // steps whose codes of V are under way
+constexpr int kPromptFactorSlots = 8;                         // steps whose keys' powers of two are kept
+static_assert(prompt_v_stages(64) + 2 <= kPromptFactorSlots, "a step's are written when the values of the step before have their place");
+static_assert(prompt_v_stages(64) + 1 < kPromptOddSlots, "a slot is not written again before it has been read");
 
 // Shared memory by its 32-bit address
 __device__ __forceinline__ uint4 load_shared_16(uint32_t at) {
@@ -70,10 +73,14 @@ __device__ __forceinline__ uint4 load_shared_16(uint32_t at) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at) : "memory");
     return r;
 }
-__device__ __forceinline__ uint2 load_shared_8(uint32_t at) {
-    uint2 r;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];\n" : "=r"(r.x), "=r"(r.y) : "r"(at) : "memory");
+// (not held to its place among other accesses)
+__device__ __forceinline__ uint4 load_shared_16_free(uint32_t at) {
+    uint4 r;
+    asm("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at));
     return r;
+}
+__device__ __forceinline__ void store_shared_8(uint32_t at, const uint2& v) {
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(at), "r"(v.x), "r"(v.y) : "memory");
 }
 __device__ __forceinline__ uint32_t load_shared_byte(uint32_t at) {
     uint32_t r;
@@ -323,19 +330,20 @@ struct PromptWalk {
 template <int D, int kKeys>
 struct PromptSmem {
     __nv_bfloat16 q[2][D / 64][128][64];                      // [tile & 1][d panel][row][64 d]
-    __nv_bfloat16 k[prompt_k_stages(D)][64 * D];              // [d panel][this CTA's 64 keys][64 d]
-    __nv_bfloat16 v[prompt_v_stages(D, kKeys)][64 * D];              // [128 keys][this CTA's half of d]
-    unsigned char raw_k[prompt_raw_stages(D, kKeys)][64 * D]; // codes as they lie in the pages: [this CTA's 64 keys][D]
-    unsigned char raw_v[prompt_raw_stages(D, kKeys)][64 * D]; // [128 keys][this CTA's half of d]
+    __nv_bfloat16 k[prompt_k_stages(D, kKeys)][64 * D / (kKeys == kKeysPages8 ? 2 : 1)];   // [d panel][this CTA's 64 keys][64 d]; codes: [64 keys][D]
+    __nv_bfloat16 v[prompt_v_stages(D)][64 * D];              // [128 keys][this CTA's half of d]
+    unsigned char raw_v[prompt_raw_stages(D, kKeys)][64 * D]; // V's codes as they lie in the pages: [128 keys][this CTA's half of d]
     unsigned char out[128][2 * D + 16];
-    uint8_t raw_ks[prompt_raw_stages(D, kKeys)][64], raw_vs[prompt_raw_stages(D, kKeys)][128];   // their powers of two
+    uint8_t raw_ks[prompt_raw_stages(D, kKeys)][128], raw_vs[prompt_raw_stages(D, kKeys)][128];   // powers of two of the keys and values
+    float key_factor[kKeys == kKeysPages8 ? kPromptFactorSlots : 0][128], row_factor[kKeys == kKeysPages8 ? kPromptPlans : 0][128];
     float ref[kPromptRefSlots][128], first_ref[2][128];      // reference of a row after a step, after the first 128 keys of a tile
     float part_l[2][2][128], part_m[2][2][128];             // sums and reference of the team that does not finish a tile, by half
     float other_l[kPromptTeams][2][128], other_ref[kPromptTeams][2][128];   // between the halves of a row
-    uint64_t q_full[2], q_peer[2], q_empty[2], k_full[prompt_k_stages(D)], k_empty[prompt_k_stages(D)], v_full[prompt_v_stages(D, kKeys)], v_empty[prompt_v_stages(D, kKeys)];
-    uint64_t v_raw[prompt_v_stages(D, kKeys)], s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], first_done[2][4], o_full, o_free;
+    uint64_t q_full[2], q_peer[2], q_empty[2], k_full[prompt_k_stages(D, kKeys)], k_empty[prompt_k_stages(D, kKeys)], v_full[prompt_v_stages(D)], v_empty[prompt_v_stages(D)];
+    uint64_t v_raw[prompt_v_stages(D)], s_full[kPromptBufs], p_full[kPromptBufs], ref_done[kPromptRefSlots][4], first_done[2][4], o_full, o_free;
     uint64_t plan_full[kPromptPlans], plan_empty[kPromptPlans], part_full[2], part_free[2], out_free;
-    uint64_t rk_full[prompt_raw_stages(D, kKeys)], rk_empty[prompt_raw_stages(D, kKeys)], rv_full[prompt_raw_stages(D, kKeys)], rv_empty[prompt_raw_stages(D, kKeys)];
+    uint64_t rv_full[prompt_raw_stages(D, kKeys)], rv_empty[prompt_raw_stages(D, kKeys)], key_factor_full[kKeys == kKeysPages8 ? kPromptFactorSlots : 0],
+        row_factor_full[kKeys == kKeysPages8 ? kPromptPlans : 0];
     PromptTile tile[kPromptPlans];
     int odd_tile[kPromptOddSlots];                            // number + 1 of a tile with masked values that are no numbers
     uint32_t tmem_base;
@@ -351,12 +359,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
     extern __shared__ unsigned char prompt_smem_raw[];
     using Smem = PromptSmem<D, kKeys>;
     Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(prompt_smem_raw) + 1023) & ~(uintptr_t)1023);
-    constexpr int kPanels = D / 64, kQKSteps = D / 16, kKStages = prompt_k_stages(D), kVStages = prompt_v_stages(D, kKeys);
+    constexpr int kPanels = D / 64, kQKSteps = D / 16, kKStages = prompt_k_stages(D, kKeys), kVStages = prompt_v_stages(D);
     constexpr bool kPaged = kKeys != kKeysPacked, kCodes = kKeys == kKeysPages8;
     [[maybe_unused]] constexpr int kRawStages = prompt_raw_stages(D, kKeys);
     constexpr uint32_t kIdescS = tc::make_idesc_bf16(256, 128);
     constexpr uint32_t kIdescO = tc::make_idesc_bf16(256, D) | (1u << 16);   // B = V: rows along N
     constexpr uint32_t kTileBytes = 64 * D * 2;               // a CTA's share of the K or V of a step
+    constexpr uint32_t kKTileBytes = kKeys == kKeysPages8 ? kTileBytes / 2 : kTileBytes;
     constexpr int kVRow = D;                                  // bytes of a key in a CTA's share of V (half of d)
     constexpr int kKWarp = kPromptTeams * 8, kMmaWarp = kKWarp + 1, kVWarp = kKWarp + 2, kPlanWarp = kKWarp + 3;
     constexpr uint32_t kOCol = kPromptBufs * 128;
@@ -368,30 +377,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&sm.q_full[i], 1);
-            tc::mbar_init(&sm.q_peer[i], 1);
+            tc::mbar_init(&sm.q_peer[i], kCodes ? 2 * kPromptCodeWarps : 1);
             tc::mbar_init(&sm.q_empty[i], 1);
             tc::mbar_init(&sm.part_full[i], 8);
             tc::mbar_init(&sm.part_free[i], 8);
         }
         for (int i = 0; i < kPromptPlans; ++i) {
             tc::mbar_init(&sm.plan_full[i], 1);
-            tc::mbar_init(&sm.plan_empty[i], (kCodes ? 7 : 4) + kPromptTeams * 8);
+            tc::mbar_init(&sm.plan_empty[i], (kCodes ? 3 + kPromptCodeWarps : 4) + kPromptTeams * 8);
         }
         for (int i = 0; i < kKStages; ++i) {
-            tc::mbar_init(&sm.k_full[i], kCodes ? 4 : 1);
+            tc::mbar_init(&sm.k_full[i], 1);
             tc::mbar_init(&sm.k_empty[i], 1);
         }
         for (int i = 0; i < kVStages; ++i) {
-            tc::mbar_init(&sm.v_full[i], kCodes ? 4 : 2);     // of both CTAs
+            tc::mbar_init(&sm.v_full[i], kCodes ? 2 * kPromptCodeWarps : 2);   // of both CTAs
             tc::mbar_init(&sm.v_raw[i], 1);
             tc::mbar_init(&sm.v_empty[i], 1);
         }
         for (int i = 0; i < kRawStages; ++i) {
-            tc::mbar_init(&sm.rk_full[i], 1);
-            tc::mbar_init(&sm.rk_empty[i], 2);
             tc::mbar_init(&sm.rv_full[i], 1);
-            tc::mbar_init(&sm.rv_empty[i], 2);
+            tc::mbar_init(&sm.rv_empty[i], kPromptCodeWarps);
         }
+        for (int i = 0; i < (kCodes ? kPromptFactorSlots : 0); ++i) tc::mbar_init(&sm.key_factor_full[i], kPromptCodeWarps);
+        for (int i = 0; i < (kCodes ? kPromptPlans : 0); ++i) tc::mbar_init(&sm.row_factor_full[i], kPromptCodeWarps);
         for (int i = 0; i < kPromptBufs; ++i) {
             tc::mbar_init(&sm.s_full[i], 1);
             tc::mbar_init(&sm.p_full[i], 16);
@@ -421,17 +430,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
     const uint32_t tbase = sm.tmem_base;
     volatile int* abort_flag = &sm.abort_flag;
     const uint64_t plan_limit = tc::kWaitLimitNs + (uint64_t)g.batch * kPromptPlanNs;
-    // The page of the `sub` keys from `key` on, of which `t`'s rows see some or none; n_pages (boxes outside the pages read zeros): it is not
-    // read, or not there.
-    [[maybe_unused]] auto page_for = [&](const PromptTile& t, int key, int sub) -> int {
-        const bool seen = key < t.hi && (key + sub > t.lo || key < g.sinks);
-        if (!seen) return g.pages.n_pages;
-        const int page = g.pages.table[(size_t)t.seq * g.pages.table_width + (key >> g.pages.page_shift)];
-        if (page >= 0 && page < g.pages.n_pages) return page;
+    // The page of the `sub` keys from `key` on: its number as the table has it, asked for a step ahead; then n_pages (boxes outside the pages read
+    // zeros) where `t`'s rows see none of them, or where it is not there.
+    [[maybe_unused]] auto seen_by = [&](const PromptTile& t, int key, int sub) -> bool { return key < t.hi && (key + sub > t.lo || key < g.sinks); };
+    [[maybe_unused]] auto entry_of = [&](const PromptTile& t, int key, int sub) -> int {
+        return seen_by(t, key, sub) ? g.pages.table[(size_t)t.seq * g.pages.table_width + (key >> g.pages.page_shift)] : 0;
+    };
+    [[maybe_unused]] auto page_for = [&](const PromptTile& t, int key, int sub, int entry) -> int {
+        if (!seen_by(t, key, sub)) return g.pages.n_pages;
+        if (entry >= 0 && entry < g.pages.n_pages) return entry;
         if (status != nullptr) atomicExch(status, 1);
         return g.pages.n_pages;
     };
-
     if (warp == kPlanWarp) {
         // ------------------------------------------------------------ planner
         PromptWalk<kPaged> w;
@@ -504,7 +514,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             __syncwarp();
         }
     } else if (kCodes && warp == kKWarp) {
-        // ------------------------------------------------------------ K's codes and powers of two, as they lie in the pages
+        // ------------------------------------------------------------ K: CTA r fetches the codes of the keys r * 64 .. of a step
+        const uint32_t bar0 = cluster_address(sm.k_full, 0);
         const int sub = min(1 << g.pages.page_shift, 64), boxes = 64 / sub;
         int st = 0, ph = 1;
         bool ok = true;
@@ -513,24 +524,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
+            auto key_at = [&](int j) -> int { return t.key_of(j) + rank * 64 + min(lane, boxes - 1) * sub; };
+            int entry = entry_of(t, key_at(0), sub);
             for (int j = 0; j < t.n_steps; ++j) {
-                const int key = t.key_of(j) + rank * 64 + lane * sub, in = key & ((1 << g.pages.page_shift) - 1);
-                const int page = lane < boxes ? page_for(t, key, sub) : 0;
-                if (!(ok = tc::mbar_wait_warp(&sm.rk_empty[st], ph, abort_flag))) break;
-                if (lane == 0) tc::mbar_arrive_expect_tx(&sm.rk_full[st], 64 * (D + 1));
+                const int key = key_at(j), page = page_for(t, key, sub, entry);
+                if (j + 1 < t.n_steps) entry = entry_of(t, key_at(j + 1), sub);
+                if (!(ok = tc::mbar_wait_warp(&sm.k_empty[st], ph, abort_flag))) break;
+                if (rank == 0 && lane == 0) tc::mbar_arrive_expect_tx(&sm.k_full[st], 2 * kKTileBytes);
                 __syncwarp();
-                if (lane < boxes) {
-                    tc::tma_load_4d(&sm.raw_k[st][lane * sub * D], &tmK, 0, in, t.gk, page, &sm.rk_full[st]);
-                    const long long at = (page < g.pages.n_pages ? page : 0) * g.pages.scale_stride + ((long long)t.gk << g.pages.page_shift) + in;
-                    tc::bulk_load(&sm.raw_ks[st][lane * sub], g.pages.ks + at, sub, &sm.rk_full[st]);
-                }
+                if (lane < boxes) tc::tma_load_4d_pair(reinterpret_cast<unsigned char*>(sm.k[st]) + lane * sub * D, &tmK, 0, key & ((1 << g.pages.page_shift) - 1), t.gk, page, bar0 + st * 8);
                 __syncwarp();
-                if (++st == kRawStages) { st = 0; ph ^= 1; }
+                if (++st == kKStages) { st = 0; ph ^= 1; }
             }
             if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
         }
     } else if (kCodes && warp == kVWarp) {
-        // ------------------------------------------------------------ V's: half `rank` of d of a step's 128 keys
+        // ------------------------------------------------------------ V's codes, half `rank` of d of a step's 128 keys, and the powers of two of keys and values
         const int sub = min(1 << g.pages.page_shift, 128), boxes = 128 / sub;
         int st = 0, ph = 1;
         bool ok = true;
@@ -539,15 +548,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
+            auto key_at = [&](int j) -> int { return t.key_of(j) + min(lane, boxes - 1) * sub; };
+            int entry = entry_of(t, key_at(0), sub);
             for (int j = 0; j < t.n_steps; ++j) {
-                const int key = t.key_of(j) + lane * sub, in = key & ((1 << g.pages.page_shift) - 1);
-                const int page = lane < boxes ? page_for(t, key, sub) : 0;
+                const int key = key_at(j), page = page_for(t, key, sub, entry), in = key & ((1 << g.pages.page_shift) - 1);
+                if (j + 1 < t.n_steps) entry = entry_of(t, key_at(j + 1), sub);
                 if (!(ok = tc::mbar_wait_warp(&sm.rv_empty[st], ph, abort_flag))) break;
-                if (lane == 0) tc::mbar_arrive_expect_tx(&sm.rv_full[st], 128 * (D / 2 + 1));
+                if (lane == 0) tc::mbar_arrive_expect_tx(&sm.rv_full[st], 128 * (D / 2 + 2));
                 __syncwarp();
                 if (lane < boxes) {
                     tc::tma_load_4d(&sm.raw_v[st][lane * sub * (D / 2)], &tmV, rank * (D / 2), in, t.gk, page, &sm.rv_full[st]);
                     const long long at = (page < g.pages.n_pages ? page : 0) * g.pages.scale_stride + ((long long)t.gk << g.pages.page_shift) + in;
+                    tc::bulk_load(&sm.raw_ks[st][lane * sub], g.pages.ks + at, sub, &sm.rv_full[st]);
                     tc::bulk_load(&sm.raw_vs[st][lane * sub], g.pages.vs + at, sub, &sm.rv_full[st]);
                 }
                 __syncwarp();
@@ -556,83 +568,124 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
         }
     } else if (kCodes && warp >= kPlanWarp + 1) {
-        // ------------------------------------------------------------ codes to bf16, as TMA would have laid that down: two warps K, two V
-        const int mine = warp - (kPlanWarp + 1), part = mine & 1;
-        const bool is_v = mine >= 2;
-        constexpr int kPieces = D / 16;                       // of 16 codes, of a thread
-        const int shift = (D == 128 ? 3 : 2) - (is_v ? 1 : 0);   // log2 of the pieces of a row
-        const int rows = 32 >> shift, c = lane & ((1 << shift) - 1), row0 = part * kPieces * rows + (lane >> shift);
-        // The thread's pieces are those of column c in the rows row0 + i * rows; their values 16-byte chunks 2 c and 2 c + 1 of the row, of K's
-        // second panel the second one first: the panels lie on the same banks.  Where the chunks of even and of odd pieces go:
-        auto place = [&](int row, int chunk) -> uint32_t {
-            if (is_v && D == 64) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
-            return (is_v ? 0 : (chunk >> 3) * (64 * 128)) + sw128(row, chunk & 7);
+        // ------------------------------------------------------------ 8-bit pages: q in two parts, the keys' powers of two, V's codes to bf16
+        const int part = warp - (kPlanWarp + 1);
+        // Q of tile k, of which this warp has 32 rows: q * 2^(127 - s) = a + b in e4m3, s as a row of 8-bit pages has it.  A bf16 number's 8 bits are two of
+        // four, so that the sum is q itself down to 2^-10 of the row's largest magnitude; what is smaller is off by 2^-18 of that at most.  In place:
+        // the row's panels become its parts (head_dim 64: the two halves of its one panel).
+        const uint32_t q_peer0 = cluster_address(sm.q_peer, 0);
+        auto split_q = [&](int k) -> bool {
+            const int slot = k % kPromptPlans, qs = k & 1;
+            if (!tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit)) return false;
+            if (sm.tile[slot].n_steps == 0) return true;
+            if (!tc::mbar_wait_warp(&sm.q_full[qs], (k >> 1) & 1, abort_flag)) return false;
+            constexpr int kLanes = D / 8, kRows = 32 / kLanes;   // lanes of a row, rows at a time
+            const uint32_t q0 = smem_u32(&sm.q[qs][0][0][0]);
+            const int c = lane % kLanes;
+#pragma unroll 1
+            for (int r = 0; r < 32; r += kRows) {
+                const int row = part * 32 + r + lane / kLanes;
+                const uint4 x = load_shared_16(q0 + (c >> 3) * (128 * 128) + sw128(row, c & 7));
+                uint32_t top = chunk_tops(x);
+                top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+                for (int b = 1; b < kLanes; b <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, b));
+                const uint32_t s = min(scale_byte(top), 247u);
+                const float inv = __uint_as_float((254u - s) << 23);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                uint32_t a[4], b[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float lo = __uint_as_float(w[i] << 16) * inv, hi = __uint_as_float(w[i] & 0xffff0000u) * inv;
+                    uint16_t two;
+                    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(two) : "f"(hi), "f"(lo));
+                    a[i] = two;
+                    const uint32_t h = codes_to_f16x2(a[i]);
+                    const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(two) : "f"(hi - back.y), "f"(lo - back.x));
+                    b[i] = two;
+                }
+                const uint32_t first = q0 + sw128(row, c >> 1) + (c & 1) * 8, second = D == 128 ? first + 128 * 128 : q0 + sw128(row, 4 + (c >> 1)) + (c & 1) * 8;
+                store_shared_8(first, make_uint2(a[0] | (a[1] << 16), a[2] | (a[3] << 16)));   // (the row has been read by all of its lanes: the shuffles)
+                store_shared_8(second, make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16)));
+                // no number, or an infinity: a row without numbers
+                if (c == 0) sm.row_factor[slot][row] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : g.scale_log2 * pow2_of_byte(s);
+            }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                tc::mbar_arrive(&sm.row_factor_full[slot]);
+                tc::mbar_arrive_cluster(q_peer0 + qs * 8);
+            }
+            __syncwarp();
+            return true;
         };
-        const bool swap = !is_v && D == 128 && c >= 4;
-        const int o = 2 * c + (swap ? 1 : 0);
-        const uint32_t even0 = place(row0, o), even1 = place(row0, o ^ 1), odd0p = place(row0 + rows, o), odd1p = place(row0 + rows, o ^ 1);
-        const uint32_t pair_step = 2 * rows * (is_v && D == 64 ? 64 : 128);   // two pieces on
-        const uint32_t raw0 = smem_u32(is_v ? sm.raw_v[0] : sm.raw_k[0]) + (part * kPieces * 32 + lane) * 16, scale0 = smem_u32(is_v ? sm.raw_vs[0] : sm.raw_ks[0]) + row0;
-        const uint32_t raw_first = swap ? 8 : 0, raw_second = swap ? 0 : 8;
-        const uint32_t tile0 = smem_u32(is_v ? sm.v[0] : sm.k[0]);
-        const uint32_t full0 = cluster_address(is_v ? sm.v_full : sm.k_full, 0);
+        constexpr int kPieces = D / 32;                       // of 16 codes, of a thread
+        constexpr int kShift = D == 128 ? 2 : 1, kRows = 32 >> kShift, kRowBytes = D;   // log2 of the pieces of a row of V
+        // The thread's pieces are those of column c in the rows row0 + i * kRows; their values are the 16-byte chunks 2 c and 2 c + 1 of the row.
+        const int c = lane & ((1 << kShift) - 1), row0 = part * kPieces * kRows + (lane >> kShift);
+        auto place = [&](int chunk) -> uint32_t { return D == 128 ? sw128(row0, chunk) : row0 * 64 + ((chunk ^ ((row0 >> 1) & 3)) << 4); };
+        const uint32_t to0 = smem_u32(sm.v[0]) + place(2 * c), to1 = smem_u32(sm.v[0]) + place(2 * c + 1);
+        const uint32_t raw0 = smem_u32(sm.raw_v[0]) + (part * kPieces * 32 + lane) * 16, scale0 = smem_u32(sm.raw_vs[0]) + row0;
+        const uint32_t full0 = cluster_address(sm.v_full, 0);
         const uint32_t odd0 = cluster_address(sm.odd_tile, 0), odd1 = cluster_address(sm.odd_tile, 1);
-        const int n_stages = is_v ? kVStages : kKStages;
-        int st = 0, ph = 1, raw = 0, raw_ph = 0;
-        bool ok = true;
+        int st = 0, ph = 1, raw = 0, raw_ph = 0, gs = 0;
+        bool ok = split_q(0);
         for (int k = 0; ok; ++k) {
             const int slot = k % kPromptPlans;
             if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
-            for (int j = 0; j < t.n_steps; ++j) {
-                if (!(ok = tc::mbar_wait_warp(is_v ? &sm.rv_full[raw] : &sm.rk_full[raw], raw_ph, abort_flag))) break;
-                const uint32_t src = raw0 + raw * (64 * D), scales = scale0 + raw * (is_v ? 128 : 64), dst = tile0 + st * (64 * D * 2);
-                if (!(ok = tc::mbar_wait_warp(is_v ? &sm.v_empty[st] : &sm.k_empty[st], ph, abort_flag))) break;
-                const bool looks = is_v && t.masked(j);       // for values that are no numbers
+            for (int j = 0; j < t.n_steps; ++j, ++gs) {
+                if (!(ok = tc::mbar_wait_warp(&sm.rv_full[raw], raw_ph, abort_flag))) break;
+                // the keys' powers of two.  (Their slot's last readers, kPromptFactorSlots steps ago, are through: the step before this has found its
+                // place for V, which products with the weights of a step of less than kPromptFactorSlots - 1 before had left)
+                sm.key_factor[gs % kPromptFactorSlots][part * 32 + lane] = pow2_of_byte(min((uint32_t)sm.raw_ks[raw][part * 32 + lane], 254u));
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm.key_factor_full[gs % kPromptFactorSlots]);
+                const uint32_t src = raw0 + raw * (64 * D), scales = scale0 + raw * 128, dst = st * (64 * D * 2);
+                if (!(ok = tc::mbar_wait_warp(&sm.v_empty[st], ph, abort_flag))) break;
                 uint32_t odd = 0u, any = 0u;
 #pragma unroll 1
                 for (int i = 0; i < kPieces; i += 2) {
-                    uint2 x[2][2];
+                    uint4 x[2];
                     uint32_t sc[2];
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        x[y][0] = load_shared_8(src + (i + y) * 512 + raw_first);
-                        x[y][1] = load_shared_8(src + (i + y) * 512 + raw_second);
-                        sc[y] = load_shared_byte(scales + (i + y) * rows);
+                        x[y] = load_shared_16(src + (i + y) * 512);
+                        sc[y] = load_shared_byte(scales + (i + y) * kRows);
                     }
                     uint4 r[2][2];
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const uint32_t f = (sc[y] + 120u) * 0x00800080u;      // 2^(s - 7) twice
-                        odd |= odd_codes(x[y][0].x) | odd_codes(x[y][0].y) | odd_codes(x[y][1].x) | odd_codes(x[y][1].y) | (sc[y] - 8u <= 126u ? 0u : 0x80u);
-                        r[y][0] = codes_to_bf16x8(x[y][0].x, x[y][0].y, f);
-                        r[y][1] = codes_to_bf16x8(x[y][1].x, x[y][1].y, f);
+                        odd |= odd_codes(x[y].x) | odd_codes(x[y].y) | odd_codes(x[y].z) | odd_codes(x[y].w) | (sc[y] - 8u <= 126u ? 0u : 0x80u);
+                        r[y][0] = codes_to_bf16x8(x[y].x, x[y].y, f);
+                        r[y][1] = codes_to_bf16x8(x[y].z, x[y].w, f);
                     }
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const uint32_t at = dst + ((i + y) >> 1) * pair_step;
-                        store_shared_16(at + ((y & 1) ? odd0p : even0), r[y][0]);
-                        store_shared_16(at + ((y & 1) ? odd1p : even1), r[y][1]);
+                        store_shared_16(to0 + dst + (i + y) * (kRows * kRowBytes), r[y][0]);
+                        store_shared_16(to1 + dst + (i + y) * (kRows * kRowBytes), r[y][1]);
                     }
                 }
                 if (__any_sync(0xffffffffu, (odd & 0x80808080u) != 0u)) {
                     // rare: codes that are no numbers, powers of two far out
 #pragma unroll 1
                     for (int i = 0; i < kPieces; ++i) {
-                        const uint32_t s = min(load_shared_byte(scales + i * rows), 254u);
-                        const uint4 lo = chunk_values(load_shared_8(src + i * 512 + raw_first), s), hi = chunk_values(load_shared_8(src + i * 512 + raw_second), s);
+                        const uint32_t s = min(load_shared_byte(scales + i * kRows), 254u);
+                        const uint4 codes = load_shared_16(src + i * 512);
+                        const uint4 lo = chunk_values(make_uint2(codes.x, codes.y), s), hi = chunk_values(make_uint2(codes.z, codes.w), s);
                         // exponents of all ones: adding 0x80 to (x & 0x7f80) carries into bit 15
                         any |= ((lo.x & 0x7f807f80u) + 0x00800080u) | ((lo.y & 0x7f807f80u) + 0x00800080u) | ((lo.z & 0x7f807f80u) + 0x00800080u) |
                                ((lo.w & 0x7f807f80u) + 0x00800080u) | ((hi.x & 0x7f807f80u) + 0x00800080u) | ((hi.y & 0x7f807f80u) + 0x00800080u) |
                                ((hi.z & 0x7f807f80u) + 0x00800080u) | ((hi.w & 0x7f807f80u) + 0x00800080u);
-                        const uint32_t at = dst + (i >> 1) * pair_step;
-                        store_shared_16(at + ((i & 1) ? odd0p : even0), lo);
-                        store_shared_16(at + ((i & 1) ? odd1p : even1), hi);
+                        store_shared_16(to0 + dst + i * (kRows * kRowBytes), lo);
+                        store_shared_16(to1 + dst + i * (kRows * kRowBytes), hi);
                     }
                 }
-                if (looks && __any_sync(0xffffffffu, (any & 0x80008000u) != 0u)) {
-                    // zeros instead, and the rows add what they see (this warp's half of the keys, whole rows, as it has written them)
+                if (t.masked(j) && __any_sync(0xffffffffu, (any & 0x80008000u) != 0u)) {
+                    // zeros instead, and the rows add what they see (this warp's part of the keys, whole rows, as it has written them)
                     __syncwarp();
                     uint4* chunks = reinterpret_cast<uint4*>(sm.v[st]) + part * kPieces * 64;
                     for (int i = lane; i < kPieces * 64; i += 32) {
@@ -650,11 +703,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 __syncwarp();
                 if (lane == 0) {
                     tc::mbar_arrive_cluster(full0 + st * 8);  // (what was written is this SM's own to read)
-                    tc::mbar_arrive(is_v ? &sm.rv_empty[raw] : &sm.rk_empty[raw]);
+                    tc::mbar_arrive(&sm.rv_empty[raw]);
                 }
                 __syncwarp();
-                if (++st == n_stages) { st = 0; ph ^= 1; }
+                if (++st == kVStages) { st = 0; ph ^= 1; }
                 if (++raw == kRawStages) { raw = 0; raw_ph ^= 1; }
+                if (j == 0 && !(ok = split_q(k + 1))) break;  // beside the first steps of this tile
             }
             if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
         }
@@ -667,7 +721,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
         struct { int k = 0, j = 0, n = 0, st = 0; bool done = false; } kp, look;      // tile, step, steps of the tile (0: not begun), stage
         int k_ph = 1, row0 = 0, gk = 0, first_masked = 0;
         [[maybe_unused]] PromptTile kt, lt;                   // (pages) tiles of either
-        [[maybe_unused]] const int sub = kPaged ? min(1 << g.pages.page_shift, 64) : 64, boxes = 64 / sub;
+        [[maybe_unused]] const int sub = kPaged ? min(1 << g.pages.page_shift, 64) : 64, boxes = 64 / sub, box = lane % boxes, panel = lane / boxes;
+        [[maybe_unused]] int entry = 0;
         uint32_t raw_phases = 0, idle = 0;                    // (of v_raw, a bit each)
         uint64_t since = 0;
         while (!kp.done || !look.done) {
@@ -678,14 +733,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                     kp.n = sm.tile[slot].n_steps;
                     row0 = sm.tile[slot].k0 + rank * 64;
                     gk = sm.tile[slot].gk;
-                    if (kPaged) kt = sm.tile[slot];
+                    if (kPaged) {
+                        kt = sm.tile[slot];
+                        if (kp.n > 0) entry = entry_of(kt, kt.key_of(0) + rank * 64 + box * sub, sub);
+                    }
                     kp.done = kp.n == 0;
                     moved = true;
                 }
                 if (kp.n > 0 && ready(&sm.k_empty[kp.st], k_ph)) {
                     if constexpr (kPaged) {
-                        const int box = lane % boxes, panel = lane / boxes, key = kt.key_of(kp.j) + rank * 64 + box * sub;
-                        const int page = panel < kPanels ? page_for(kt, key, sub) : 0;
+                        const int key = kt.key_of(kp.j) + rank * 64 + box * sub, page = page_for(kt, key, sub, entry);
+                        if (kp.j + 1 < kp.n) entry = entry_of(kt, kt.key_of(kp.j + 1) + rank * 64 + box * sub, sub);
                         if (rank == 0 && lane == 0) tc::mbar_arrive_expect_tx(&sm.k_full[kp.st], 2 * kTileBytes);
                         __syncwarp();
                         if (panel < kPanels)
@@ -738,13 +796,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                         }
                         if (lane < 2)                         // (keys of other sequences among them: the rows look for themselves)
                             asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"((lane ? odd1 : odd0) + (look.k % kPromptOddSlots) * 4), "r"(look.k + 1) : "memory");
+                        // (for the other CTA's memory alone, and dear: 1 us of every masked step, had it been outside)
+                        asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
                     }
                     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) {
-                        asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
-                        tc::mbar_arrive_release_cluster(v_bar0 + look.st * 8);
-                    }
+                    if (lane == 0) tc::mbar_arrive_cluster(v_bar0 + look.st * 8);
                     __syncwarp();
                     if (++look.st == kVStages) look.st = 0;
                     ++look.j;
@@ -782,9 +839,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
+            auto key_at = [&](int j) -> int { return t.key_of(j) + min(lane, boxes - 1) * sub; };
+            int entry = entry_of(t, key_at(0), sub);
             for (int j = 0; j < t.n_steps; ++j) {
-                const int key = t.key_of(j) + lane * sub, in = key & ((1 << g.pages.page_shift) - 1);
-                const int page = lane < boxes ? page_for(t, key, sub) : 0;
+                const int key = key_at(j), page = page_for(t, key, sub, entry), in = key & ((1 << g.pages.page_shift) - 1);
+                if (j + 1 < t.n_steps) entry = entry_of(t, key_at(j + 1), sub);
                 if (!(ok = tc::mbar_wait_warp(&sm.v_empty[st], ph, abort_flag))) break;
                 const bool masked = t.masked(j);              // K's warp looks for what is no number and says that it is there
                 if (lane == 0) {
@@ -829,14 +888,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             }
         }
     } else if (warp == kMmaWarp && rank == 1) {
-        // ------------------------------------------------------------ CTA 1: Q is there, said to the issuing warp of CTA 0
+        // ------------------------------------------------------------ CTA 1: Q is there, said to the issuing warp of CTA 0 (8-bit pages: by those that split it)
         if (lane == 0) {
             for (int k = 0;; ++k) {
                 const int slot = k % kPromptPlans;
                 if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit) || sm.tile[slot].n_steps == 0) break;
-                if (!tc::mbar_wait(&sm.q_full[k & 1], (k >> 1) & 1, abort_flag)) break;
-                asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
-                tc::mbar_arrive_cluster(cluster_address(&sm.q_peer[k & 1], 0));
+                if (!kCodes) {
+                    if (!tc::mbar_wait(&sm.q_full[k & 1], (k >> 1) & 1, abort_flag)) break;
+                    asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
+                    tc::mbar_arrive_cluster(cluster_address(&sm.q_peer[k & 1], 0));
+                }
                 tc::mbar_arrive(&sm.plan_empty[slot]);
             }
         }
@@ -844,7 +905,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
         // ------------------------------------------------------------ MMA issuer
         constexpr uint32_t kKStep = 32 >> 4;                                        // 16 elements of a 128-byte row
         constexpr uint32_t kQPanelStep = (128 * 128) >> 4, kKPanelStep = (64 * 128) >> 4, kVStep = (16 * kVRow) >> 4;
-        constexpr uint32_t kQSlotStep = (uint32_t)sizeof(sm.q[0]) >> 4, kStageStep = (uint32_t)sizeof(sm.k[0]) >> 4;
+        constexpr uint32_t kQSlotStep = (uint32_t)sizeof(sm.q[0]) >> 4, kKStageStep = (uint32_t)sizeof(sm.k[0]) >> 4, kStageStep = (uint32_t)sizeof(sm.v[0]) >> 4;
+        // codes of K: rows of D bytes with the 128- (64-) byte swizzle, 32 of them a step
+        constexpr uint32_t kIdescCodes = tc::make_idesc_e4m3(256, 128), kCodesDescHi = (uint32_t)((8 * D) >> 4) | (1u << 14) | ((D == 128 ? 2u : 4u) << 29);
         // V: rows of a key's 64 (D = 64: 32) values with the 128- (64-) byte swizzle, groups of 8 keys kVRow * 8 bytes apart
         constexpr uint32_t kVDescHi = (uint32_t)((8 * kVRow) >> 4) | (1u << 14) | ((D == 128 ? 2u : 4u) << 29);
         const uint32_t q_lo0 = __shfl_sync(0xffffffffu, tc::smem_desc_lo_sw128(smem_u32(&sm.q[0][0][0][0])), 0);
@@ -863,7 +926,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                     auto there = [&](uint64_t* bar, uint32_t phase) -> bool { return must ? (ok = tc::mbar_wait(bar, phase, abort_flag, plan_limit)) : tc::mbar_test(bar, phase); };
                     if (!there(&sm.plan_full[slot], (kn / kPromptPlans) & 1)) return false;
                     if ((ended = sm.tile[slot].n_steps == 0)) return false;
-                    if (!there(&sm.q_full[kn & 1], (kn >> 1) & 1) || !there(&sm.q_peer[kn & 1], (kn >> 1) & 1)) return false;
+                    if ((!kCodes && !there(&sm.q_full[kn & 1], (kn >> 1) & 1)) || !there(&sm.q_peer[kn & 1], (kn >> 1) & 1)) return false;
                     ks = kn;
                     n_steps2 = n_steps1;
                     n_steps1 = n_steps0;
@@ -872,11 +935,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 }
                 if (!(ok = tc::mbar_wait(&sm.k_full[kst], kph, abort_flag))) return false;
                 tc::tc_fence_after_sync();
-                const uint32_t qa = q_lo0 + (ks & 1) * kQSlotStep, kb = k_lo0 + kst * kStageStep, dst = tb + sbuf * 128;
+                const uint32_t qa = q_lo0 + (ks & 1) * kQSlotStep, kb = k_lo0 + kst * kKStageStep, dst = tb + sbuf * 128;
+                if constexpr (kCodes) {
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x)          // both parts of q, the products of 32 codes at a time
+                        tc::umma_ss_pair_e4m3(dst, tc::smem_desc_from_halves(qa + (x >> 2) * kQPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128),
+                                              tc::smem_desc_from_halves(kb + (x % (D / 32)) * kKStep, kCodesDescHi), kIdescCodes, x > 0);
+                } else {
 #pragma unroll
                 for (int x = 0; x < kQKSteps; ++x)
                     tc::umma_ss_pair(dst, tc::smem_desc_from_halves(qa + (x >> 2) * kQPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128),
                                      tc::smem_desc_from_halves(kb + (x >> 2) * kKPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128), kIdescS, x > 0);
+                }
                 tc::umma_commit_pair(&sm.s_full[sbuf]);
                 tc::umma_commit_pair(&sm.k_empty[kst]);
                 if (--s_left == 0) tc::umma_commit_pair(&sm.q_empty[ks & 1]);
@@ -949,6 +1019,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             const bool valid = tok < t.n_tok;                 // (the tile's last rows may be none, tokens behind the sequence not its own)
             const int first = kPaged && g.window > 0 ? max(last + 1 - g.window, 0) : 0;   // of those behind the first ones
             const bool idle = kPaged && !__any_sync(0xffffffffu, valid);   // no row of the warp is one: nothing is computed
+            [[maybe_unused]] float row_factor = 0.f;          // 8-bit pages: scores are products with codes times this and the key's power of two
+            if constexpr (kCodes) {
+                if (!tc::mbar_wait(&sm.row_factor_full[slot], (k / kPromptPlans) & 1, abort_flag)) ok = false;
+                row_factor = sm.row_factor[slot][row];
+            }
+            [[maybe_unused]] const unsigned long long row_factor2 = pack_f32x2(row_factor, row_factor);
+            // products of the two may leave 32 bits on the way, the score not: the key's first where the row's is large
+            [[maybe_unused]] const bool large = kCodes && __any_sync(0xffffffffu, valid && row_factor > 0x1p100f);
             const int j0 = (team + g0) & 1;
             const bool finishes = ((g0 + t.n_steps - 1) & 1) == team;
             float m_ref = 0.f, l_sum = 0.f;
@@ -964,8 +1042,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                     return below(last + 1 - k) & (~below(first - k) | below(g.sinks - k));
                 };
                 const int n_vis = masked ? last + 1 - j * 128 - half * 64 : 64;    // keys of the half step that the row sees (any number)
+                if constexpr (kCodes)
+                    if (!tc::mbar_wait(&sm.key_factor_full[gs % kPromptFactorSlots], (gs / kPromptFactorSlots) & 1, abort_flag)) ok = false;
                 if (!tc::mbar_wait(&sm.s_full[buf], (gs / kPromptBufs) & 1, abort_flag)) ok = false;
                 tc::tc_fence_after_sync();
+                // (the address as it is known behind the waits: the loads through it may go anywhere behind that)
+                [[maybe_unused]] uint32_t factors = 0u;
+                if constexpr (kCodes) asm volatile("add.u32 %0, %1, %2;\n" : "=r"(factors) : "r"(smem_u32(sm.key_factor[gs % kPromptFactorSlots])), "r"(half * 256) : "memory");
+                // 8-bit pages: four products with codes, times the row's factor and the keys' (i: the first of them / 4, of 32 keys from chunk c on)
+                [[maybe_unused]] auto scaled = [&](uint32_t (&s)[32], int c) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint4 f = load_shared_16_free(factors + c * 128 + i * 16);
+                        unsigned long long a = pack_f32x2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), b = pack_f32x2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3]));
+                        const unsigned long long fa = pack_f32x2(__uint_as_float(f.x), __uint_as_float(f.y)), fb = pack_f32x2(__uint_as_float(f.z), __uint_as_float(f.w));
+                        a = mul_f32x2(mul_f32x2(a, large ? fa : row_factor2), large ? row_factor2 : fa);
+                        b = mul_f32x2(mul_f32x2(b, large ? fb : row_factor2), large ? row_factor2 : fb);
+                        s[4 * i] = (uint32_t)a;
+                        s[4 * i + 1] = (uint32_t)(a >> 32);
+                        s[4 * i + 2] = (uint32_t)b;
+                        s[4 * i + 3] = (uint32_t)(b >> 32);
+                    }
+                };
                 auto hide = [&](uint32_t (&s)[32], int c) {
                     const int n = n_vis - c * 32;
                     const uint32_t seen = kPaged ? seen_of(c) : 0u;
@@ -1005,12 +1103,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                         uint32_t s[32];
                         tc::tmem_ld_32x32(s_addr + c * 32, s);
                         tc::tmem_wait_ld_for(s);
+                        if constexpr (kCodes) scaled(s, c);
                         if (!sees_all(c)) hide(s, c);
                         top = fmaxf(top, largest(s));
                     }
                     sm.other_ref[team][half][row] = top;
                     pair_sync();
-                    return fmaxf(fmaxf(top, sm.other_ref[team][half ^ 1][row]) * scale_log2, kPromptLowest);    // scale > 0
+                    return fmaxf(fmaxf(top, sm.other_ref[team][half ^ 1][row]) * (kCodes ? 1.f : scale_log2), kPromptLowest);    // scale > 0
                 };
                 if (j == 0) {
                     // ---- the reference of the tile: the largest of the first 128 scores
@@ -1049,20 +1148,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                     }
                     tc::tmem_ld_32x32(s_addr + c * 32, s);
                     tc::tmem_wait_ld_for(s);
-                    if (!sees_all(c)) hide(s, c);
+                    // (one loop for either order of the factors: a branch within would part its instructions)
+                    auto weigh = [&](auto key_first) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const unsigned long long x01 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), scale2, add2);
-                        const unsigned long long x23 = fma_f32x2(pack_f32x2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), scale2, add2);
-                        float x0, x1, x2, x3;
-                        unpack_f32x2(x01, x0, x1);
-                        unpack_f32x2(x23, x2, x3);
-                        const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = fast_exp2(x3);
-                        psA = add_f32x2(psA, pack_f32x2(p0, p1));
-                        psB = add_f32x2(psB, pack_f32x2(p2, p3));
-                        pk[2 * i] = pack_bf16x2(p0, p1);
-                        pk[2 * i + 1] = pack_bf16x2(p2, p3);
-                    }
+                        for (int i = 0; i < 8; ++i) {
+                            unsigned long long x01 = pack_f32x2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), x23 = pack_f32x2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3]));
+                            if constexpr (!kCodes) {
+                                x01 = fma_f32x2(x01, scale2, add2);
+                                x23 = fma_f32x2(x23, scale2, add2);
+                            } else {
+                                const uint4 f = load_shared_16_free(factors + c * 128 + i * 16);
+                                const unsigned long long f01 = pack_f32x2(__uint_as_float(f.x), __uint_as_float(f.y)), f23 = pack_f32x2(__uint_as_float(f.z), __uint_as_float(f.w));
+                                x01 = key_first.value ? fma_f32x2(mul_f32x2(x01, f01), row_factor2, add2) : fma_f32x2(mul_f32x2(x01, row_factor2), f01, add2);
+                                x23 = key_first.value ? fma_f32x2(mul_f32x2(x23, f23), row_factor2, add2) : fma_f32x2(mul_f32x2(x23, row_factor2), f23, add2);
+                            }
+                            float x0, x1, x2, x3;
+                            unpack_f32x2(x01, x0, x1);
+                            unpack_f32x2(x23, x2, x3);
+                            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = fast_exp2(x3);
+                            psA = add_f32x2(psA, pack_f32x2(p0, p1));
+                            psB = add_f32x2(psB, pack_f32x2(p2, p3));
+                            pk[2 * i] = pack_bf16x2(p0, p1);
+                            pk[2 * i + 1] = pack_bf16x2(p2, p3);
+                        }
+                    };
+                    if (!sees_all(c)) hide(s, c);
+                    if (kCodes && large) weigh(std::true_type());
+                    else weigh(std::false_type());
                     tc::tmem_st_32x16(s_addr + c * 16, pk);
                 }
                 float a0, a1, b0, b1;

@@ -411,7 +411,7 @@ adaspark_status_t adaspark_attn_paged_prompt(adaspark_attn_t* h, const adaspark_
     const bool e4m3 = c->pages.format == ADASPARK_PAGES_E4M3;
     CUtensorMap tmQ, tmK, tmV;
     if (!encode_bf16_rows(&tmQ, rq.p, c->n, g.Hq, D, rq.ts, rq.hs, 64, g.G, g.T) ||
-        !encode_page_boxes(&tmK, p.k, e4m3, p.n_pages, g.Hkv, page, D, p.page_stride, e4m3 ? D : 64, k_box, e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode_page_boxes(&tmK, p.k, e4m3, p.n_pages, g.Hkv, page, D, p.page_stride, e4m3 ? D : 64, k_box, e4m3 && D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B) ||
         !encode_page_boxes(&tmV, p.v, e4m3, p.n_pages, g.Hkv, page, D, p.page_stride, D / 2, v_box,
                            e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
         return fail(h, ADASPARK_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed", who);
