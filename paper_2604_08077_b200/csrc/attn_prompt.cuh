@@ -223,8 +223,10 @@ struct PromptSeq {
 // leaves its outputs, references and sums, and prompt_join_kernel puts them together.  There are at most 4/3 as many as pairs.
 constexpr int kPromptPairs = 74, kPromptMinUnit = 8;
 constexpr int kPromptParts = 100;
+constexpr int kPromptSlots = 2 * kPromptPairs;                // of parts (pages: two a pair, PromptLine)
+static_assert(kPromptParts <= kPromptSlots, "room for either");
 // Rows of the cut tiles' parts: outputs [part][CTA][128][D], then (reference, sum) [part][CTA][128]
-__host__ __device__ constexpr size_t prompt_partial_bytes(int D) { return (size_t)kPromptParts * 256 * (D + 2) * sizeof(float); }
+__host__ __device__ constexpr size_t prompt_partial_bytes(int D) { return (size_t)kPromptSlots * 256 * (D + 2) * sizeof(float); }
 // Could a call have tiles to cut?  (If not, there is nothing to join either: 36.1 against 37.9 us for 4301 tokens in 5 prompts, 16 heads of 64.)  More
 // tiles than 4 a pair: no one is long enough to matter.  Whole prompts: the n / W tiles of a prompt of n tokens, W to a tile, average half
 // of its n / 128 steps; that is 1.5 times what a pair has to do only up to n = 99 W / Hkv, and no tile of less than 12 steps is cut.
@@ -325,6 +327,152 @@ struct PromptWalk {
     // first token of CTA `rank` of the tile, and how many it has
     __device__ __forceinline__ int first_token(const PromptGeom& g, int rank) const { return (2 * tile + rank) * g.T; }
     __device__ __forceinline__ int tokens(const PromptGeom& g, int rank) const { return min(max(seq.nq - first_token(g, rank), 0), g.T); }
+};
+
+// What the rows of a tile see of pages: steps, and which are masked.
+struct PromptSpan {
+    int n;                                                    // steps
+    int hi, lo, sink_steps, jump, low_first, low_masked, first_masked;
+    __device__ __forceinline__ PromptSpan(const PromptGeom& g, const PromptSeq<true>& seq, int tile) {
+        const int tok0 = 2 * tile * g.T, m = min(seq.nq - tok0, 2 * g.T);
+        const int p0 = seq.off + tok0, p1 = p0 + m - 1;      // places of the tile's first and last token
+        hi = max(p1 + 1, 0);
+        n = max((hi + 127) >> 7, 1);
+        sink_steps = jump = lo = low_first = low_masked = 0;
+        if (g.window > 0) {
+            lo = max(p0 + 1 - g.window, 0);
+            sink_steps = min((g.sinks >> 7) + ((g.sinks & 127) != 0), n);
+            jump = max((lo >> 7) - sink_steps, 0);
+            n -= jump;
+            const int lo1 = max(p1 + 1 - g.window, 0);       // (the last row's)
+            if (lo1 > g.sinks) {
+                low_first = g.sinks >> 7;
+                low_masked = max(((lo1 + 127) >> 7) - jump, sink_steps);
+            }
+        }
+        first_masked = max((max(p0 + 1, 0) >> 7) - jump, 0);
+    }
+};
+
+// Few tiles over pages: all tiles, sequence by sequence, tile by tile, kv head by kv head, are one line, cut into equal runs, one a pair.
+// (Whole tiles dealt longest first left a pair 2072 of an average of 1602 steps, parts of about the average 257 of 171; and a planner that
+// walks levels finds its first tile 5 us later.)  Lengths are in keys: what the tile's last row sees, and in front of that kPromptAhead for what a
+// tile costs beside its steps.  A pair's first tile may have begun in an earlier run, its last may go on in the next: two parts a pair,
+// joined by prompt_join_kernel.  Nobody cuts off less than kPromptLeast steps.
+constexpr int kPromptAhead = 384, kPromptLeast = 3;
+struct PromptLine {
+    int chunk;                                                // first sequence of the lanes' 32
+    PromptSeq<true> mine;
+    // the tile
+    PromptSeq<true> seq;
+    int tile, gk;
+    long long place, cost;                                    // its beginning and length
+
+    static __device__ __forceinline__ long long limit(const PromptGeom& g) { return g.most_steps < 0x1000000 ? 128ll * g.most_steps : 0x7fffffffll; }
+    static __device__ __forceinline__ long long cost_of(const PromptGeom& g, const PromptSeq<true>& q, int t) {
+        return kPromptAhead + min(max((long long)q.off + 2ll * g.T * (t + 1), 0ll), limit(g));
+    }
+    // length of the first t tiles of one head
+    static __device__ __forceinline__ long long length(const PromptGeom& g, const PromptSeq<true>& q, int t) {
+        const long long W = 2 * g.T, most = limit(g);
+        const int none = q.off >= 0 ? 0 : min(g.div_w.div(-q.off), t);              // tiles that see nothing
+        // tiles of less than the limit: W (u + 1) + off < most
+        const long long room = most - q.off - 1;
+        const int rising = max(min(room < 0 ? 0 : room >= 0x7fffffffll ? t : g.div_w.div((int)room), t), none);
+        const long long m = rising - none;
+        return (long long)t * kPromptAhead + m * q.off + W * (m * none + m * (m + 1) / 2) + (t - rising) * most;
+    }
+    __device__ __forceinline__ bool load(const PromptGeom& g, int c, int lane) {
+        chunk = c;
+        mine.nt = 0;
+        return c + lane >= g.batch || mine.load(g, c + lane);
+    }
+    __device__ __forceinline__ long long mine_length(const PromptGeom& g) const { return mine.nt > 0 ? length(g, mine, mine.nt) * g.Hkv : 0; }
+    // length of the line; fine: no sequence leaves the tensors or its table
+    __device__ __forceinline__ long long begin(const PromptGeom& g, int lane, bool& fine) {
+        long long sum = 0;
+        fine = true;
+        for (int c = 0; c < g.batch; c += 32) {
+            fine = load(g, c, lane) && fine;
+            sum += mine_length(g);
+        }
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+        return sum;
+    }
+    __device__ __forceinline__ void take(const PromptGeom& g, int who) {
+        seq.q0 = __shfl_sync(0xffffffffu, mine.q0, who);
+        seq.nq = __shfl_sync(0xffffffffu, mine.nq, who);
+        seq.nk = __shfl_sync(0xffffffffu, mine.nk, who);
+        seq.off = seq.nk - seq.nq;
+        seq.nt = __shfl_sync(0xffffffffu, mine.nt, who);
+        seq.k0 = 0;
+        seq.b = chunk + who;
+    }
+    // the tile that holds place x of the line; false: there is none
+    __device__ __forceinline__ bool seek(const PromptGeom& g, long long x, int lane) {
+        long long before = 0;
+        for (int c = 0; c < g.batch; c += 32) {
+            if (c > 0 || chunk != 0) load(g, c, lane);
+            const long long own = mine_length(g);
+            long long upto = own;
+#pragma unroll
+            for (int y = 1; y < 32; y <<= 1) {
+                const long long z = __shfl_up_sync(0xffffffffu, upto, y);
+                if (lane >= y) upto += z;
+            }
+            const long long all = __shfl_sync(0xffffffffu, upto, 31);
+            if (x < before + all) {
+                const int who = __ffs(__ballot_sync(0xffffffffu, before + upto > x)) - 1;
+                const long long first = before + __shfl_sync(0xffffffffu, upto - own, who), rest = x - first;
+                take(g, who);
+                int lo = 0, hi = seq.nt;                      // length(lo) * Hkv <= rest < length(hi) * Hkv
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (length(g, seq, mid) * g.Hkv <= rest) lo = mid;
+                    else hi = mid;
+                }
+                tile = lo;
+                cost = cost_of(g, seq, tile);
+                place = first + length(g, seq, tile) * g.Hkv;
+                gk = (int)((x - place) / cost);
+                place += gk * cost;
+                return true;
+            }
+            before += all;
+        }
+        return false;
+    }
+    __device__ __forceinline__ bool next(const PromptGeom& g, int lane) {
+        place += cost;
+        if (++gk < g.Hkv) return true;
+        gk = 0;
+        if (++tile >= seq.nt) {
+            tile = 0;
+            int from = seq.b + 1 - chunk;
+            while (true) {
+                const uint32_t there = from < 32 ? __ballot_sync(0xffffffffu, mine.nt > 0) >> from << from : 0u;
+                if (there) {
+                    take(g, __ffs(there) - 1);
+                    break;
+                }
+                if (chunk + 32 >= g.batch) return false;
+                load(g, chunk + 32, lane);
+                from = 0;
+            }
+        }
+        cost = cost_of(g, seq, tile);
+        return true;
+    }
+    // steps of the tile's n that lie in front of place x
+    __device__ __forceinline__ int steps_before(long long x, int n) const {
+        const long long y = x - place - kPromptAhead;
+        if (y >= cost - kPromptAhead) return n;
+        if (y <= 0) return 0;
+        const int i = (int)(y * n / (cost - kPromptAhead));
+        return i < kPromptLeast ? 0 : n - i < kPromptLeast ? n : i;
+    }
+    static __device__ __forceinline__ long long run_begin(long long total, int n_pairs, int pair) { return total * pair / n_pairs; }
 };
 
 template <int D, int kKeys>
@@ -444,45 +592,66 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
     };
     if (warp == kPlanWarp) {
         // ------------------------------------------------------------ planner
+        // (pages) a tile's steps [begin, end)
+        [[maybe_unused]] auto tile_of_pages = [&](PromptTile& t, const PromptSeq<true>& seq, int tile, int gk, const PromptSpan& x, int begin, int end) {
+            const int tok = (2 * tile + rank) * g.T;
+            t.seq = seq.b;
+            t.q0 = seq.q0 + tok;
+            t.n_tok = min(max(seq.nq - tok, 0), g.T);
+            t.k0 = 0;
+            t.last0 = seq.off + tok;
+            t.gk = gk;
+            t.n_steps = end - begin;
+            t.step0 = begin;
+            t.hi = x.hi;
+            t.lo = x.lo;
+            t.sink_steps = x.sink_steps;
+            t.jump = x.jump;
+            t.first_masked = max(x.first_masked - begin, 0);
+            t.low_first = x.low_first - begin;
+            t.low_masked = x.low_masked - begin;
+        };
         PromptWalk<kPaged> w;
-        if (!w.begin(g, partial != nullptr, n_pairs, lane) && blockIdx.x == 0 && status != nullptr) atomicExch(status, 1);
+        [[maybe_unused]] PromptLine line;
+        const bool in_runs = kPaged && partial != nullptr;
+        bool fine, more = false;
+        long long run_end = 0, run_first = 0;
+        if (in_runs) {
+            const long long total = line.begin(g, lane, fine);
+            run_first = PromptLine::run_begin(total, n_pairs, pair);
+            run_end = PromptLine::run_begin(total, n_pairs, pair + 1);
+            more = run_first < run_end && line.seek(g, run_first, lane);
+        } else {
+            fine = w.begin(g, !kPaged && partial != nullptr, n_pairs, lane);
+        }
+        if (!fine && blockIdx.x == 0 && status != nullptr) atomicExch(status, 1);
         for (int k = 0;; ++k) {
             const int slot = k % kPromptPlans, qs = k & 1;
             if (!tc::mbar_wait(&sm.plan_empty[slot], ((k / kPromptPlans) & 1) ^ 1u, abort_flag)) break;
-            const int number = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
-            const bool found = w.find(g, number, lane);
+            bool found = false;
             PromptTile t;
-            if (kPaged && found) {
-                const int tok = w.first_token(g, rank), tok0 = w.first_token(g, 0), m = min(w.seq.nq - tok0, 2 * g.T);
-                const int p0 = w.seq.off + tok0, p1 = p0 + m - 1;          // places of the pair's first and last token
-                t.hi = max(p1 + 1, 0);
-                int n = max((t.hi + 127) >> 7, 1);
-                t.sink_steps = t.jump = t.lo = t.low_first = t.low_masked = 0;
-                if (g.window > 0) {
-                    t.lo = max(p0 + 1 - g.window, 0);
-                    t.sink_steps = min((g.sinks >> 7) + ((g.sinks & 127) != 0), n);
-                    t.jump = max((t.lo >> 7) - t.sink_steps, 0);
-                    n -= t.jump;
-                    const int lo1 = max(p1 + 1 - g.window, 0);             // (the last row's)
-                    if (lo1 > g.sinks) {
-                        t.low_first = g.sinks >> 7;
-                        t.low_masked = max(((lo1 + 127) >> 7) - t.jump, t.sink_steps);
+            if (in_runs) {
+                while (more && !found) {
+                    const PromptSpan x(g, line.seq, line.tile);
+                    const int begin = line.steps_before(run_first, x.n), end = line.steps_before(run_end, x.n);
+                    found = end > begin;
+                    if (found) {
+                        tile_of_pages(t, line.seq, line.tile, line.gk, x, begin, end);
+                        t.part = end - begin == x.n ? -1 : 2 * pair + (begin > 0 ? 0 : 1);
                     }
+                    more = line.place + line.cost < run_end && line.next(g, lane);
                 }
-                const int begin = w.part * n / w.parts;
-                t.seq = w.seq.b;
-                t.q0 = w.seq.q0 + tok;
-                t.n_tok = w.tokens(g, rank);
-                t.k0 = 0;
-                t.last0 = w.seq.off + tok;
-                t.gk = w.gk;
-                t.n_steps = (w.part + 1) * n / w.parts - begin;
-                t.step0 = begin;
-                t.first_masked = max((max(p0 + 1, 0) >> 7) - t.jump - begin, 0);
-                t.low_first -= begin;
-                t.low_masked -= begin;
-                t.part = w.parts > 1 ? number : -1;
-                if (lane == 0) sm.tile[slot] = t;
+                if (found && lane == 0) sm.tile[slot] = t;
+            } else {
+            const int number = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
+            found = w.find(g, number, lane);
+            if constexpr (kPaged) {
+                if (found) {
+                    const PromptSpan x(g, w.seq, w.tile);
+                    tile_of_pages(t, w.seq, w.tile, w.gk, x, 0, x.n);
+                    t.part = -1;
+                    if (lane == 0) sm.tile[slot] = t;
+                }
             } else if (found) {
                 const int tok = w.first_token(g, rank), begin = w.part * w.level / w.parts;
                 t.q0 = w.seq.q0 + tok;
@@ -494,6 +663,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 t.first_masked = max((max(w.seq.off + w.first_token(g, 0) + 1, 0) >> 7) - begin, 0);
                 t.part = w.parts > 1 ? number : -1;
                 if (lane == 0) sm.tile[slot] = t;
+            }
             }
             if (!found) {
                 if (lane == 0) {
@@ -1296,7 +1466,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 if (t.part >= 0) {
                     const size_t part_row = ((size_t)t.part * 2 + rank) * 128 + row;
                     part_o = partial + part_row * D + half * (D / 2);
-                    if (half == 0) reinterpret_cast<float2*>(partial + (size_t)kPromptParts * 256 * D)[part_row] = make_float2(m_ref, l_fin);
+                    if (half == 0) reinterpret_cast<float2*>(partial + (size_t)kPromptSlots * 256 * D)[part_row] = make_float2(m_ref, l_fin);
                 } else if (mine && half == 0 && lse != nullptr) lse[at] = (m_ref + log2f(l_fin)) * 0.6931471805599453f;
                 if (k > 0 && !tc::mbar_wait(&sm.out_free, (k - 1) & 1, abort_flag)) ok = false;
                 if (!tc::mbar_wait(&sm.o_full, k & 1, abort_flag)) ok = false;
@@ -1380,59 +1550,89 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
 }
 
 // Puts the parts of cut tiles together: grid (kPromptParts, 256 / kPromptJoinRows), CTA (i, y) kPromptJoinRows rows of the tile whose first
-// part is item i.
+// part is item i.  Pages: grid (runs - 1, ..), CTA (i, y) the tile that begins in run i and is cut by that run's end.
 constexpr int kPromptJoinThreads = 256, kPromptJoinRows = 16;
 
 template <int D, bool kPaged>
 __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptGeom g, int n_pairs, const float* partial, __nv_bfloat16* out, float* lse) {
     constexpr int kLanes = D / 4, kRows = 32 / kLanes;        // threads of a row, rows of a warp
-    __shared__ PromptWalk<kPaged> found;
-    __shared__ int mine;
+    __shared__ PromptSeq<kPaged> seq;
+    __shared__ int part_at[kPromptSlots], n_parts, tile, gk;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (warp == 0) {
-        PromptWalk<kPaged> w;
-        w.begin(g, true, n_pairs, lane);
-        const bool x = w.find(g, blockIdx.x, lane, true) && w.part == 0;
-        if (lane == 0) {
-            found = w;
-            mine = x;
+        int n = 0;
+        if constexpr (kPaged) {
+            PromptLine w;
+            bool fine;
+            const long long total = w.begin(g, lane, fine), cut = PromptLine::run_begin(total, n_pairs, blockIdx.x + 1);
+            if (cut < total && w.seek(g, cut, lane) && w.place < cut && w.place >= PromptLine::run_begin(total, n_pairs, blockIdx.x)) {
+                const PromptSpan x(g, w.seq, w.tile);
+                // a lane a run: of those that the tile lies in, the ones that hold steps of it
+                for (int r = blockIdx.x; r < n_pairs && PromptLine::run_begin(total, n_pairs, r) < w.place + w.cost; r += 32) {
+                    const int run = r + lane, begin = run < n_pairs ? w.steps_before(PromptLine::run_begin(total, n_pairs, run), x.n) : 0,
+                              end = run < n_pairs ? w.steps_before(PromptLine::run_begin(total, n_pairs, run + 1), x.n) : 0;
+                    const uint32_t holds = __ballot_sync(0xffffffffu, end > begin);
+                    if (end > begin) part_at[n + __popc(holds & ((1u << lane) - 1u))] = 2 * run + (begin > 0 ? 0 : 1);
+                    n += __popc(holds);
+                }
+                if (n == 1) n = 0;                            // whole after all
+                if (lane == 0) {
+                    seq = w.seq;
+                    tile = w.tile;
+                    gk = w.gk;
+                }
+            }
+        } else {
+            PromptWalk<false> w;
+            w.begin(g, true, n_pairs, lane);
+            if (w.find(g, blockIdx.x, lane, true) && w.part == 0) {
+                n = w.parts;
+                for (int i = lane; i < n; i += 32) part_at[i] = blockIdx.x + i;
+                if (lane == 0) {
+                    seq = w.seq;
+                    tile = w.tile;
+                    gk = w.gk;
+                }
+            }
         }
+        if (lane == 0) n_parts = n;
     }
     __syncthreads();
     launch_dependents();
     wait_for_previous_kernel();
-    if (!mine) return;
-    const PromptWalk<kPaged>& w = found;
-    const float2* stats = reinterpret_cast<const float2*>(partial + (size_t)kPromptParts * 256 * D);
+    const int parts = n_parts;
+    if (parts == 0) return;
+    auto first_token = [&](int rank) -> int { return (2 * tile + rank) * g.T; };
+    const float2* stats = reinterpret_cast<const float2*>(partial + (size_t)kPromptSlots * 256 * D);
     const int d4 = lane % kLanes;
     for (int r = warp * kRows + lane / kLanes; r < kPromptJoinRows; r += kRows * (kPromptJoinThreads / 32)) {
         const int row = blockIdx.y * kPromptJoinRows + r, rank = row >> 7;
         int tok, head;
         g.div_g.divmod(row & 127, tok, head);
-        if (tok >= w.tokens(g, rank)) continue;
+        if (tok >= min(max(seq.nq - first_token(rank), 0), g.T)) continue;
         // statistics and outputs of four parts are asked for together; more are joined to what these gave
         float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int p0 = 0; p0 < w.parts; p0 += 4) {
+        for (int p0 = 0; p0 < parts; p0 += 4) {
             float2 s[4];
             float4 o[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const size_t at = (size_t)(blockIdx.x + min(p0 + i, w.parts - 1)) * 256 + row;
+                const size_t at = (size_t)part_at[min(p0 + i, parts - 1)] * 256 + row;
                 s[i] = stats[at];
                 o[i] = *reinterpret_cast<const float4*>(partial + at * D + 4 * d4);
             }
             float top = m;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (p0 + i < w.parts && s[i].y != 0.f) top = fmaxf(top, s[i].x);      // (0: the row sees none of the part's keys)
+                if (p0 + i < parts && s[i].y != 0.f) top = fmaxf(top, s[i].x);      // (0: the row sees none of the part's keys)
             const MovedBy c(l != 0.f ? m - top : -INFINITY);
             l = c.of(l);
             acc = make_float4(c.of(acc.x), c.of(acc.y), c.of(acc.z), c.of(acc.w));
             m = top;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (p0 + i >= w.parts || s[i].y == 0.f) continue;
+                if (p0 + i >= parts || s[i].y == 0.f) continue;
                 const MovedBy f(s[i].x - m);
                 l = fmaf(s[i].y * f.b, f.a, l);
                 acc.x = fmaf(o[i].x * f.b, f.a, acc.x);
@@ -1442,7 +1642,7 @@ __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptG
             }
         }
         const float inv = l != 0.f ? 1.f / l : 0.f;
-        const long long at = (long long)(w.seq.q0 + w.first_token(g, rank) + tok) * g.Hq + w.gk * g.G + head;
+        const long long at = (long long)(seq.q0 + first_token(rank) + tok) * g.Hq + gk * g.G + head;
         *reinterpret_cast<uint2*>(out + at * D + 4 * d4) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
         if (d4 == 0 && lse != nullptr) lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
     }

@@ -182,8 +182,9 @@ adaspark_status_t launch_prompt(adaspark_attn* h, const PromptGeom& g, const CUt
     launch_kernel(true, kernel, dim3(2 * pairs), dim3(prompt_threads(kKeys)), bytes, st, g, tmQ, tmK, tmV, o.out, o.lse, o.partial, o.status);
     if (!launch_ok(h, "attn_prompt_kernel")) return ADASPARK_ERR_CUDA;
     if (!o.partial) return ADASPARK_OK;
-    launch_kernel(true, prompt_join_kernel<D, kKeys != kKeysPacked>, dim3(kPromptParts, 256 / kPromptJoinRows), dim3(kPromptJoinThreads), 0, st, g, pairs,
-                  (const float*)o.partial, o.out, o.lse);
+    if (kKeys != kKeysPacked && pairs == 1) return ADASPARK_OK;       // one run: nothing is cut
+    launch_kernel(true, prompt_join_kernel<D, kKeys != kKeysPacked>, dim3(kKeys == kKeysPacked ? kPromptParts : pairs - 1, 256 / kPromptJoinRows),
+                  dim3(kPromptJoinThreads), 0, st, g, pairs, (const float*)o.partial, o.out, o.lse);
     return launch_ok(h, "prompt_join_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
 }
 
