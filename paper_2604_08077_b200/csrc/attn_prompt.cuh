@@ -1306,7 +1306,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 const float ref = ref_now;
                 const unsigned long long add2 = pack_f32x2(-ref, -ref);
                 unsigned long long psA = 0ull, psB = 0ull;
-#pragma unroll
+                // (8-bit pages: their warps go so many ways that instructions are what they wait for most; rolled up 254 for 281 us of proposed tokens)
+                constexpr int kChunksAtOnce = kCodes ? 1 : 2;
+#pragma unroll kChunksAtOnce
                 for (int c = 0; c < 2; ++c) {
                     uint32_t s[32], pk[16];
                     if (sees_none(c)) {
