@@ -90,6 +90,8 @@ __device__ __forceinline__ uint32_t load_shared_byte(uint32_t at) {
 __device__ __forceinline__ void store_shared_16(uint32_t at, const uint4& v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+// sum += 0 * x, of two bf16 each
+__device__ __forceinline__ void add_times_zero(uint32_t& sum, uint32_t x) { asm("fma.rn.bf16x2 %0, %1, %2, %0;\n" : "+r"(sum) : "r"(x), "r"(0u)); }
 // Bit 7 of each byte: the code is no number (0x7f, 0xff)
 __device__ __forceinline__ uint32_t odd_codes(uint32_t c) { return (c & 0x7f7f7f7fu) + 0x01010101u; }
 // 8 codes that are numbers times 2^(s - 127), s in 8 .. 134, as bf16: exact.  A code's exponent and mantissa four bits below bf16's are the same number
@@ -846,15 +848,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                         const uint32_t s = min(load_shared_byte(scales + i * kRows), 254u);
                         const uint4 codes = load_shared_16(src + i * 512);
                         const uint4 lo = chunk_values(make_uint2(codes.x, codes.y), s), hi = chunk_values(make_uint2(codes.z, codes.w), s);
-                        // exponents of all ones: adding 0x80 to (x & 0x7f80) carries into bit 15
-                        any |= ((lo.x & 0x7f807f80u) + 0x00800080u) | ((lo.y & 0x7f807f80u) + 0x00800080u) | ((lo.z & 0x7f807f80u) + 0x00800080u) |
-                               ((lo.w & 0x7f807f80u) + 0x00800080u) | ((hi.x & 0x7f807f80u) + 0x00800080u) | ((hi.y & 0x7f807f80u) + 0x00800080u) |
-                               ((hi.z & 0x7f807f80u) + 0x00800080u) | ((hi.w & 0x7f807f80u) + 0x00800080u);
+                        const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                        for (int e = 0; e < 8; ++e) add_times_zero(any, w[e]);
                         store_shared_16(to0 + dst + i * (kRows * kRowBytes), lo);
                         store_shared_16(to1 + dst + i * (kRows * kRowBytes), hi);
                     }
                 }
-                if (t.masked(j) && __any_sync(0xffffffffu, (any & 0x80008000u) != 0u)) {
+                if (t.masked(j) && __any_sync(0xffffffffu, (any & 0x7fff7fffu) != 0u)) {
                     // zeros instead, and the rows add what they see (this warp's part of the keys, whole rows, as it has written them)
                     __syncwarp();
                     uint4* chunks = reinterpret_cast<uint4*>(sm.v[st]) + part * kPieces * 64;
@@ -946,16 +946,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 }
                 if (look.n > 0 && look.j < look.n && ready(&sm.v_raw[look.st], (raw_phases >> look.st) & 1)) {
                     raw_phases ^= 1u << look.st;
-                    // exponents of all ones: adding 0x80 to (x & 0x7f80) carries into bit 15
+                    // zero times what is infinite or no number is none, and stays that in a sum
                     uint4* chunks = reinterpret_cast<uint4*>(&sm.v[look.st][0]);
-                    uint32_t any = 0;
+                    uint32_t none[4] = {0u, 0u, 0u, 0u};
 #pragma unroll 8
                     for (int i = lane; i < (int)kTileBytes / 16; i += 32) {
-                        const uint4 x = chunks[i];
-                        any |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) | ((x.z & 0x7f807f80u) + 0x00800080u) |
-                               ((x.w & 0x7f807f80u) + 0x00800080u);
+                        const uint4 x = load_shared_16(smem_u32(chunks + i));
+                        add_times_zero(none[0], x.x);
+                        add_times_zero(none[1], x.y);
+                        add_times_zero(none[2], x.z);
+                        add_times_zero(none[3], x.w);
                     }
-                    if (__any_sync(0xffffffffu, (any & 0x80008000u) != 0u)) {
+                    if (__any_sync(0xffffffffu, ((none[0] | none[1] | none[2] | none[3]) & 0x7fff7fffu) != 0u)) {
                         for (int i = lane; i < (int)kTileBytes / 16; i += 32) {
                             uint32_t x[4] = {chunks[i].x, chunks[i].y, chunks[i].z, chunks[i].w};
                             for (int e = 0; e < 4; ++e) {

@@ -239,7 +239,11 @@ __global__ void __launch_bounds__(kRotateThreads, 3) rotate_kernel(const __grid_
                     for (int b = 1; b < kLanes; b <<= 1) s += __shfl_xor_sync(0xffffffffu, s, b);
                     return s;
                 };
-                float s = sum_of_squares(), f = rsqrtf(s * (1.f / D) + a.eps);
+                auto root = [](float v) -> float {            // 1 / sqrt(v), and what that leaves to first order
+                    const float r = rsqrtf(v);
+                    return fmaf(0.5f * r, fmaf(-v * r, r, 1.f), r);
+                };
+                float s = sum_of_squares(), f = root(s * (1.f / D) + a.eps);
                 if (__any_sync(0xffffffffu, !(s < 0x1p126f))) {   // rare: squares that leave 32 bits (eps is nothing beside them)
                     const float down = !(s < 0x1p126f) ? 0x1p-70f : 1.f;
                     const unsigned long long down2 = pack_f32x2(down, down);
@@ -249,7 +253,7 @@ __global__ void __launch_bounds__(kRotateThreads, 3) rotate_kernel(const __grid_
                         x[1][i] = mul_f32x2(x[1][i], down2);
                     }
                     s = sum_of_squares();
-                    if (down != 1.f) f = rsqrtf(s * (1.f / D));
+                    if (down != 1.f) f = root(s * (1.f / D));
                 }
                 const unsigned long long f2 = pack_f32x2(f, f);
 #pragma unroll
