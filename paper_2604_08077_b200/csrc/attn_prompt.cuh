@@ -428,17 +428,17 @@ struct PromptLine {
                 const int who = __ffs(__ballot_sync(0xffffffffu, before + upto > x)) - 1;
                 const long long first = before + __shfl_sync(0xffffffffu, upto - own, who), rest = x - first;
                 take(g, who);
-                int lo = 0, hi = seq.nt;                      // length(lo) * Hkv <= rest < length(hi) * Hkv
+                int lo = 0, hi = seq.nt;                      // length(lo) * Hkv <= rest < length(hi) * Hkv; a lane a place to look at
                 while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (length(g, seq, mid) * g.Hkv <= rest) lo = mid;
-                    else hi = mid;
+                    const int step = (hi - lo + 31) >> 5, at = lo + step * (lane + 1);
+                    const int below = __popc(__ballot_sync(0xffffffffu, at < hi && length(g, seq, at) * g.Hkv <= rest));
+                    lo += step * below;
+                    hi = min(lo + step, hi);
                 }
                 tile = lo;
                 cost = cost_of(g, seq, tile);
                 place = first + length(g, seq, tile) * g.Hkv;
-                gk = (int)((x - place) / cost);
-                place += gk * cost;
+                for (gk = 0; x - place >= cost; ++gk) place += cost;
                 return true;
             }
             before += all;
@@ -474,7 +474,13 @@ struct PromptLine {
         const int i = (int)(y * n / (cost - kPromptAhead));
         return i < kPromptLeast ? 0 : n - i < kPromptLeast ? n : i;
     }
-    static __device__ __forceinline__ long long run_begin(long long total, int n_pairs, int pair) { return total * pair / n_pairs; }
+};
+// The line's runs, of equal length but for a key
+struct PromptRuns {
+    long long length;
+    int longer;                                               // the first ones, by a key
+    __device__ __forceinline__ PromptRuns(long long total, int n_pairs) : length(total / n_pairs), longer((int)(total % n_pairs)) {}
+    __device__ __forceinline__ long long begin(int run) const { return length * run + min(run, longer); }
 };
 
 template <int D, int kKeys>
@@ -620,8 +626,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
         long long run_end = 0, run_first = 0;
         if (in_runs) {
             const long long total = line.begin(g, lane, fine);
-            run_first = PromptLine::run_begin(total, n_pairs, pair);
-            run_end = PromptLine::run_begin(total, n_pairs, pair + 1);
+            const PromptRuns runs(total, n_pairs);
+            run_first = runs.begin(pair);
+            run_end = runs.begin(pair + 1);
             more = run_first < run_end && line.seek(g, run_first, lane);
         } else {
             fine = w.begin(g, !kPaged && partial != nullptr, n_pairs, lane);
@@ -1568,13 +1575,15 @@ __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptG
         if constexpr (kPaged) {
             PromptLine w;
             bool fine;
-            const long long total = w.begin(g, lane, fine), cut = PromptLine::run_begin(total, n_pairs, blockIdx.x + 1);
-            if (cut < total && w.seek(g, cut, lane) && w.place < cut && w.place >= PromptLine::run_begin(total, n_pairs, blockIdx.x)) {
+            const long long total = w.begin(g, lane, fine);
+            const PromptRuns runs(total, n_pairs);
+            const long long cut = runs.begin(blockIdx.x + 1);
+            if (cut < total && w.seek(g, cut, lane) && w.place < cut && w.place >= runs.begin(blockIdx.x)) {
                 const PromptSpan x(g, w.seq, w.tile);
                 // a lane a run: of those that the tile lies in, the ones that hold steps of it
-                for (int r = blockIdx.x; r < n_pairs && PromptLine::run_begin(total, n_pairs, r) < w.place + w.cost; r += 32) {
-                    const int run = r + lane, begin = run < n_pairs ? w.steps_before(PromptLine::run_begin(total, n_pairs, run), x.n) : 0,
-                              end = run < n_pairs ? w.steps_before(PromptLine::run_begin(total, n_pairs, run + 1), x.n) : 0;
+                for (int r = blockIdx.x; r < n_pairs && runs.begin(r) < w.place + w.cost; r += 32) {
+                    const int run = r + lane, begin = run < n_pairs ? w.steps_before(runs.begin(run), x.n) : 0,
+                              end = run < n_pairs ? w.steps_before(runs.begin(run + 1), x.n) : 0;
                     const uint32_t holds = __ballot_sync(0xffffffffu, end > begin);
                     if (end > begin) part_at[n + __popc(holds & ((1u << lane) - 1u))] = 2 * run + (begin > 0 ? 0 : 1);
                     n += __popc(holds);
