@@ -457,12 +457,13 @@ adaspark_status_t adaspark_attn_paged_decode_window(adaspark_attn_t *handle, con
 
 /* Several new tokens per sequence, whose keys and values are in its pages already (adaspark_attn_paged_append, _paged_write): row
  * cu[b] + i of sequence b is token p = kv_len[b] - (cu[b+1] - cu[b]) + i and sees the tokens j <= p; with window > 0 those of them with j >
- * p - window or j < sinks.  Rows, masks, precision and what a row that sees nothing yields are those of adaspark_attn_prompt (what
- * 8-bit pages hold are bf16 numbers: the result is that of adaspark_attn_prompt over what adaspark_attn_paged_read gives).
+ * p - window or j < sinks.  Rows, masks, precision and what a row that sees nothing yields are those of adaspark_attn_prompt over what
+ * adaspark_attn_paged_read gives; with 8-bit pages a row of q is held to 2^-18 of its largest magnitude (what is smaller there loses bits), and a row
+ * of q that holds an infinity or no number yields no numbers.
  * Pages that hold nothing that a row of the sequence sees are not read, and their numbers may be any; a page number outside [0, n_pages) among the
  * others sets status 1, and what such a page would hold counts as zeros.  A sequence whose rows leave the tensors sets
  * status 1 and is left out; one whose kv_len is negative or more than the table holds sets status 1, and its rows become rows that see
- * nothing, as do rows in front of token 0 (kv_len[b] < cu[b+1] - cu[b], status 1). */
+ * nothing, as do rows in front of token 0 (kv_len[b] < cu[b+1] - cu[b], status 1).  Of a sequence without rows nothing is looked at. */
 typedef struct {
     adaspark_attn_pages_t pages;
     adaspark_attn_rows_t q;            /* n rows of Hq heads                                           */

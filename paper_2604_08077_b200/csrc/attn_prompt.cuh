@@ -168,7 +168,7 @@ struct PromptGeom {
     PageGeom pages;
     const int32_t* kv_len;
     int window, sinks;          // window 0: none
-    int most_steps;             // a bound on the steps of a tile that a window leaves
+    int most_steps;             // a bound on the steps of a tile (by the window, if there is one)
 };
 
 struct PromptTile {
@@ -236,6 +236,10 @@ inline bool prompt_may_cut(long long most_tiles, int n_k, bool whole, int W, int
     return most_tiles <= 4 * kPromptPairs && n_k > 128 * 3 * kPromptMinUnit / 2 && (!whole || W > 16 * Hkv);
 }
 
+// Steps of n keys; a table may have room for nearly 2^31.
+constexpr int kPromptMostSteps = 1 << 24;
+__host__ __device__ constexpr int prompt_steps(int n) { return ((n - 1) >> 7) + 1; }
+
 // The order of the items (tiles, or parts of them): levels from many steps to few, sequences in order, tiles, kv heads, parts.  A warp walks
 // it, with 32 sequences in its lanes.  Parts come first: an item's number is its part's.  (With a window a tile's level is the bound on its
 // steps where it would be more.)
@@ -260,7 +264,7 @@ struct PromptWalk {
             if (held * 32 + lane < g.batch) {
                 fine = mine.load(g, held * 32 + lane) && fine;
                 if (mine.nt > 0) {
-                    const int longest = max(1, (mine.nk + 127) >> 7);
+                    const int longest = max(1, prompt_steps(mine.nk));
                     const long long all = (long long)mine.nt * (max(mine.off, 0) / 128 + 2) + (long long)g.T * mine.nt * (mine.nt + 1) / 128;
                     level = max(level, kPaged ? min(longest, g.most_steps) : longest);
                     steps += kPaged ? min(all, (long long)mine.nt * g.most_steps) : all;
@@ -317,7 +321,7 @@ struct PromptWalk {
             }
             base += total;
             // the next level is that of the longest tile left: levels without a tile are passed over
-            if (first > 0) below = max(below, max((min(mine.off + 2 * g.T * first, mine.nk) + 127) >> 7, 1));   // (below `level`, whatever bounds that)
+            if (first > 0) below = max(below, max(prompt_steps(min(mine.off + 2 * g.T * first, mine.nk)), 1));   // (below `level`, whatever bounds that)
             if (++chunk * 32 >= g.batch) {
                 chunk = 0;
                 level = min((int)__reduce_max_sync(0xffffffffu, (unsigned)below), level - 1);   // (down in any case: the walk ends)
@@ -339,17 +343,17 @@ struct PromptSpan {
         const int tok0 = 2 * tile * g.T, m = min(seq.nq - tok0, 2 * g.T);
         const int p0 = seq.off + tok0, p1 = p0 + m - 1;      // places of the tile's first and last token
         hi = max(p1 + 1, 0);
-        n = max((hi + 127) >> 7, 1);
+        n = max(prompt_steps(hi), 1);
         sink_steps = jump = lo = low_first = low_masked = 0;
         if (g.window > 0) {
             lo = max(p0 + 1 - g.window, 0);
-            sink_steps = min((g.sinks >> 7) + ((g.sinks & 127) != 0), n);
+            sink_steps = min(prompt_steps(g.sinks), n);
             jump = max((lo >> 7) - sink_steps, 0);
             n -= jump;
             const int lo1 = max(p1 + 1 - g.window, 0);       // (the last row's)
             if (lo1 > g.sinks) {
                 low_first = g.sinks >> 7;
-                low_masked = max(((lo1 + 127) >> 7) - jump, sink_steps);
+                low_masked = max(prompt_steps(lo1) - jump, sink_steps);
             }
         }
         first_masked = max((max(p0 + 1, 0) >> 7) - jump, 0);
@@ -370,7 +374,7 @@ struct PromptLine {
     int tile, gk;
     long long place, cost;                                    // its beginning and length
 
-    static __device__ __forceinline__ long long limit(const PromptGeom& g) { return g.most_steps < 0x1000000 ? 128ll * g.most_steps : 0x7fffffffll; }
+    static __device__ __forceinline__ long long limit(const PromptGeom& g) { return g.most_steps < kPromptMostSteps ? 128ll * g.most_steps : 0x7fffffffll; }
     static __device__ __forceinline__ long long cost_of(const PromptGeom& g, const PromptSeq<true>& q, int t) {
         return kPromptAhead + min(max((long long)q.off + 2ll * g.T * (t + 1), 0ll), limit(g));
     }

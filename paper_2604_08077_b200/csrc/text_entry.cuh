@@ -406,8 +406,8 @@ adaspark_status_t adaspark_attn_paged_prompt(adaspark_attn_t* h, const adaspark_
     g.window = c->window;
     g.sinks = c->window ? c->sinks : 0;
     // first ones and window, each rounded outwards by a step at most, and the 2 T tokens of a tile
-    const long long most = c->window ? (long long)c->sinks / 128 + ((long long)c->window + 2 * g.T) / 128 + 3 : 0x7fffffff;
-    g.most_steps = (int)(most < 0x7fffffff ? most : 0x7fffffff);
+    const long long most = c->window ? (long long)c->sinks / 128 + ((long long)c->window + 2 * g.T) / 128 + 3 : kPromptMostSteps;
+    g.most_steps = (int)std::min(most, (long long)kPromptMostSteps);
     const int D = h->cfg.head_dim, page = c->pages.page_size, k_box = page < 64 ? page : 64, v_box = page < 128 ? page : 128;
     const bool e4m3 = c->pages.format == ADASPARK_PAGES_E4M3;
     CUtensorMap tmQ, tmK, tmV;

@@ -383,3 +383,100 @@ def test_decode_window_is_a_chunk_of_one():
     _, _, _, tol, ltol = chunk_reference(q, [0, 1, 2, 3], kv_len, lambda b, m: sequence_values(cache, table, b, m), 1500, 4, D ** -0.5)
     assert_close(out, out2.double(), 2 * tol, "out")
     assert_lse(lse, lse2.double(), 2 * ltol)
+
+
+# ---------------------------------------------------------------------------------------------------------------- 8-bit pages as the tensor cores take them
+
+def one_sequence(g, n, page, Hkv, D):
+    table, cache = pool(g, [n], page, Hkv, D, True)
+    return table, cache, sequence_values(cache, table, 0, n)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("q_power,k_power", [(110, -105), (-105, 100), (60, -60), (0, 0)])
+def test_powers_of_two_at_opposite_ends(D, q_power, k_power):
+    """Queries and keys whose powers of two cancel: the scores are ordinary ones."""
+    g = torch.Generator().manual_seed(30)
+    Hq, Hkv, page, n, r = 8, 2, 16, 700, 20
+    eng = engine(Hq, Hkv, D)
+    table, cache = pool(g, [n], page, Hkv, D, True)
+    cache.k_scale.copy_((cache.k_scale.to(torch.int32) + k_power).clamp(0, 247).to(torch.uint8))
+    q = (0.02 * torch.randn(r, Hq, D, generator=g) * 2.0 ** q_power).to(torch.bfloat16).cuda()
+    run_and_check(eng, cache, table, q, [0, r], [n])
+
+
+def test_queries_with_large_elements():
+    """One value of a row 2^12 times the others: those are held to 2^-18 of it, which moves a score by 2^-18 max|q| sum|k| at most, on top of
+    what the bounds have."""
+    g = torch.Generator().manual_seed(31)
+    Hq, Hkv, D, page, n, r = 8, 2, 128, 64, 900, 30
+    eng = engine(Hq, Hkv, D)
+    table, cache, (k, v) = one_sequence(g, n, page, Hkv, D)
+    q = rand(g, r, Hq, D)
+    q[..., 17] *= 64
+    q[::3, :, 17] *= 64
+    for x in (cache.k_pages.view(torch.uint8),):
+        x[..., 17] &= 0x87                                       # the keys are small where the queries are large
+    k, v = sequence_values(cache, table, 0, n)
+    out, lse = eng.paged_prompt(q, cache, ints([0, r]), table, ints([n]), want_lse=True)
+    want, wl, tol, ltol = attend_masked(q, k, v, hidden_from(n - r, r, n, 0, 0), D ** -0.5)
+    e = q.double().abs().amax(-1) * 2.0 ** -18 * k.abs().sum(-1).amax() * D ** -0.5
+    size = v.abs().amax()
+    assert_close(out, want, tol + (2 * e * size)[..., None], "out")
+    assert_lse(lse, wl, ltol + e)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_code_with_every_power_of_two(D):
+    """A token that sees itself alone gives its value back, whatever code and power of two it has."""
+    eng = engine(1, 1, D)
+    per = 256 // D if D < 256 else 1
+    codes = torch.arange(256, dtype=torch.uint8).repeat(255).view(-1, D)
+    s = torch.arange(255, dtype=torch.uint8).repeat_interleave(per)
+    n = codes.shape[0]
+    kp, vp = torch.zeros(n, 1, 16, D, dtype=torch.uint8, device="cuda"), torch.zeros(n, 1, 16, D, dtype=torch.uint8, device="cuda")
+    vs = torch.full((n, 1, 16), 127, dtype=torch.uint8, device="cuda")
+    vp[:, 0, 0], vs[:, 0, 0] = codes.cuda(), s.cuda()
+    cache = binding.PagedCache(kp.view(torch.float8_e4m3fn), vp.view(torch.float8_e4m3fn), torch.full_like(vs, 127), vs)
+    table, one, cu = torch.arange(n, dtype=torch.int32, device="cuda")[:, None].contiguous(), ints([1] * n), torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    q = torch.ones(n, 1, D, dtype=torch.bfloat16, device="cuda")
+    out, _ = eng.paged_prompt(q, cache, cu, table, one)
+    want, k = torch.empty_like(out), torch.empty_like(out)
+    eng.paged_read(cache, cu, table, one, k, want)
+    assert eng.text_status() == 0
+    assert torch.equal(out.isnan(), want.isnan()) and torch.equal(out.nan_to_num(), want.nan_to_num())
+
+
+def test_keys_and_queries_that_are_no_numbers():
+    g = torch.Generator().manual_seed(33)
+    Hq, Hkv, D, page, n, r = 8, 2, 128, 16, 500, 40
+    eng = engine(Hq, Hkv, D)
+    table, cache = pool(g, [n], page, Hkv, D, True)
+    q = rand(g, r, Hq, D)
+    want, _ = run_and_check(eng, cache, table, q, [0, r], [n])
+    at = n - 10                                                  # a key that the last ten rows see
+    kept = cache.k_pages.view(torch.uint8)[int(table[0, at // page]), 1, at % page, 5].clone()
+    cache.k_pages.view(torch.uint8)[int(table[0, at // page]), 1, at % page, 5] = 0x7f
+    out, _ = eng.paged_prompt(q, cache, ints([0, r]), table, ints([n]))
+    assert torch.equal(out[:r - 10], want[:r - 10]) and torch.equal(out[:, :4], want[:, :4]) and out[r - 10:, 4:].isnan().all()
+    cache.k_pages.view(torch.uint8)[int(table[0, at // page]), 1, at % page, 5] = kept
+    q[3, 2, 7], q[20, 5, 0] = math.nan, math.inf
+    out, _ = eng.paged_prompt(q, cache, ints([0, r]), table, ints([n]))
+    assert out[3, 2].isnan().all() and out[20, 5].isnan().all()
+    out[3, 2], out[20, 5] = want[3, 2], want[20, 5]
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (3000, 10)])
+def test_runs_that_end_anywhere(window, sinks, e4m3):
+    """Sequences that the pairs' runs cut at any place, one that is a run of many, ones without rows between them."""
+    g = torch.Generator().manual_seed(34)
+    Hq, Hkv, D, page = 16, 4, 64, 32
+    eng = engine(Hq, Hkv, D)
+    new, kv_len = [1, 0, 33, 5, 64, 130, 0, 7, 2], [9000, 500, 2000, 12345, 1600, 130, 0, 4100, 2]
+    table, cache = pool(g, kv_len, page, Hkv, D, e4m3)
+    q = rand(g, sum(new), Hq, D)
+    first = run_and_check(eng, cache, table, q, cumulative(new), kv_len, window, sinks)
+    again = run_and_check(eng, cache, table, q, cumulative(new), kv_len, window, sinks)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
