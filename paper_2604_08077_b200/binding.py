@@ -36,6 +36,7 @@ class Layout(ctypes.Structure):
 
 
 PAGES_BF16, PAGES_E4M3 = 0, 1
+_BF16, _INT32 = torch.bfloat16, torch.int32
 
 # The arguments of the text calls, packed as the header's structs lay them out (one bytes object per call: a quarter of the time that
 # ctypes takes for two dozen arguments).  A row argument is (pointer, token stride, head stride).
@@ -628,15 +629,18 @@ class AdaSAttn:
     def _rows(self, t, heads: int, what: str):
         """(pointer, token stride, head stride) of a bf16 tensor [rows, heads, head_dim] on this device, and its rows."""
         shape, strides = t.shape, t.stride()
-        if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[1] != heads or shape[2] != self._head_dim:
+        if len(shape) == 3:                                    # (in one go: what is wrong is worked out below)
+            n, h, d = shape
+            s0, s1, s2 = strides
+            if h == heads and d == self._head_dim and s2 == 1 and t.dtype is _BF16 and t.get_device() == self._index and \
+                    (s0 >= d or n <= 1) and (s1 >= d or heads == 1):
+                # (the stride of an axis of one entry says nothing)
+                return (t.data_ptr(), s0 if n > 1 else 0, s1 if heads > 1 else 0), n
+        if t.dtype is not _BF16 or len(shape) != 3 or shape[1] != heads or shape[2] != self._head_dim:
             _refuse(f"{what}: {t.dtype} {tuple(shape)} is not bfloat16 [rows, {heads}, {self._head_dim}]")
-        n = shape[0]
-        if strides[2] != 1 or (n > 1 and strides[0] < shape[2]) or (heads > 1 and strides[1] < shape[2]):    # (0 would say dense)
-            _refuse(f"{what}: the values of a row have to lie side by side, and rows apart (strides {tuple(strides)})")
         if t.get_device() != self._index:
             _refuse(f"{what} is on {t.device}, not on {self.device}")
-        # (the stride of an axis of one entry says nothing)
-        return (t.data_ptr(), strides[0] if n > 1 else 0, strides[1] if heads > 1 else 0), n
+        _refuse(f"{what}: the values of a row have to lie side by side, and rows apart (strides {tuple(strides)})")   # (0 would say dense)
 
     def _dense(self, t, shape, dtype, what: str) -> int:
         if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != self._index:
@@ -663,47 +667,57 @@ class AdaSAttn:
     def _turn(self, rotary, positions, n: int, q_norm, k_norm):
         """(positions, rotary, weights of the norms) of n tokens as pointers."""
         where = turned = None
+        axes = 1
         if rotary is not None:
             if rotary.head_dim != self._head_dim:
                 _refuse(f"rotary is one of heads of {rotary.head_dim}")
-            turned = rotary.address
+            turned, axes = rotary.address, rotary.axes
         if positions is not None:
-            if positions.dtype is not torch.int32 or positions.numel() != n * (rotary.axes if rotary is not None else 1) or positions.shape[-1:] != (n,) or \
-                    positions.dim() > 2 or not positions.is_contiguous() or positions.get_device() != self._index:
-                _refuse(f"positions: {positions.dtype} {tuple(positions.shape)} on {positions.device} is not dense int32 [axes, {n}] on {self.device}")
+            shape = positions.shape
+            if positions.dtype is not _INT32 or (shape != (axes, n) and (axes != 1 or shape != (n,))) or not positions.is_contiguous() or \
+                    positions.get_device() != self._index:
+                _refuse(f"positions: {positions.dtype} {tuple(shape)} on {positions.device} is not dense int32 [{axes}, {n}] on {self.device}")
             where = positions.data_ptr()
-        D = self._head_dim
-        return where, turned, *(None if w is None else self._dense(w, (D,), torch.bfloat16, what) for w, what in ((q_norm, "q_norm"), (k_norm, "k_norm")))
+        if q_norm is not None:
+            q_norm = self._dense(q_norm, (self._head_dim,), _BF16, "q_norm")
+        if k_norm is not None:
+            k_norm = self._dense(k_norm, (self._head_dim,), _BF16, "k_norm")
+        return where, turned, q_norm, k_norm
 
     def rotate(self, q, k, positions=None, rotary: Optional[Rotary] = None, *, q_norm=None, k_norm=None, eps: float = 1e-6, q_out=None, k_out=None, stream=None):
         """Queries [n, Hq, D] and keys [n, Hkv, D] (either may be None), each head with its norm (q_norm, k_norm: bf16 [D]) and turned by its
         positions, int32 [n] or [axes, n].  Outputs may be the inputs themselves.  Returns (q_out, k_out)."""
-        got, rows, n = [], [], None
-        for x, out, heads, what in ((q, q_out, self._n_q_heads, "q"), (k, k_out, self._n_kv_heads, "k")):
-            if x is None:
-                if out is not None:
-                    _refuse(f"{what}_out without {what}")
-                got.append(None)
-                rows.append((_NO_ROWS, _NO_ROWS))
-                continue
-            r, m = self._rows(x, heads, what)
-            if n is not None and m != n:
-                _refuse(f"q has {n} rows, k {m}")
-            n = m
-            if out is None:
-                out = self._empty((n, heads, self._head_dim), torch.bfloat16, stream)
-            o, m = self._rows(out, heads, what + "_out")
-            if m != n:
-                _refuse(f"{what}_out has {m} rows, {what} {n}")
-            got.append(out)
-            rows.append((r, o))
-        if n is None:
+        Hq, Hkv = self._n_q_heads, self._n_kv_heads
+        qr = qo = kr = ko = _NO_ROWS
+        if q is not None:
+            qr, n = self._rows(q, Hq, "q")
+            if q_out is None:
+                q_out = self._empty((n, Hq, self._head_dim), _BF16, stream)
+            qo, n_q = self._rows(q_out, Hq, "q_out")
+        elif q_out is not None:
+            _refuse("q_out without q")
+        if k is not None:
+            kr, n_k = self._rows(k, Hkv, "k")
+            if k_out is None:
+                k_out = self._empty((n_k, Hkv, self._head_dim), _BF16, stream)
+            ko, n_o = self._rows(k_out, Hkv, "k_out")
+            if n_o != n_k:
+                _refuse(f"k_out has {n_o} rows, k {n_k}")
+            if q is None:
+                n = n_q = n_k
+            elif n_k != n:
+                _refuse(f"q has {n} rows, k {n_k}")
+        elif k_out is not None:
+            _refuse("k_out without k")
+        elif q is None:
             _refuse("rotate: neither q nor k")
-        if rotary is not None and rotary.pairs and positions is None:
+        if n_q != n:
+            _refuse(f"q_out has {n_q} rows, q {n}")
+        if rotary is not None and positions is None and rotary.pairs:
             _refuse("rotate: a rotation needs positions")
-        (qr, qo), (kr, ko) = rows
-        adaspark_attn_rotate(self.handle, qr, kr, qo, ko, *self._turn(rotary, positions, n, q_norm, k_norm), eps, n, _raw_stream(self._index) if stream is None else stream.cuda_stream)
-        return tuple(got)
+        where, turned, q_norm, k_norm = self._turn(rotary, positions, n, q_norm, k_norm)
+        adaspark_attn_rotate(self.handle, qr, kr, qo, ko, where, turned, q_norm, k_norm, eps, n, _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        return q_out, k_out
 
     def paged_append(self, cache: PagedCache, q, k, v, cu, block_table, kv_len, rotary: Optional[Rotary] = None, *, positions=None, q_norm=None, k_norm=None,
                      eps: float = 1e-6, q_out=None, stream=None):

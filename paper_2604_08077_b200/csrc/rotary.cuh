@@ -161,7 +161,10 @@ __global__ void __launch_bounds__(kRotateThreads, 3) rotate_kernel(const __grid_
 #pragma unroll 1
     for (int i = 0; i < kRotateRing - 1; ++i) load_row(i);
     if (kPages) {
-        if (tid < kTokens) place[tid] = place_of<D>(p, a.cu, a.kv_len, a.batch, a.n, t0 + tid, a.status);
+        if (tid < 32) {
+            const TokenPlace x = place_of_lane<D, kTokens>(p, a.cu, a.kv_len, a.batch, a.n, t0, tid, a.status);
+            if (tid < kTokens) place[tid] = x;
+        }
         if (a.positions == nullptr) __syncthreads();
     }
     for (int i = tid; i < kTokens * a.pairs; i += kRotateThreads) {
