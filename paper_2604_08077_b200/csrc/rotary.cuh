@@ -127,7 +127,7 @@ template <int D, int kPages, int kTokens>
 __global__ void __launch_bounds__(kRotateThreads, 3) rotate_kernel(const __grid_constant__ RotateCall a, const __grid_constant__ PageGeom p) {
     constexpr int kLanes = D / 16, kGroups = kRotateThreads / kLanes / kTokens;     // of a token
     __shared__ uint4 ring[kRotateRing][2][kRotateThreads];
-    __shared__ float2 turn[kTokens][kRotaryPairs + 2];        // (the tokens of a warp on banks of their own)
+    __shared__ float2 turn[kTokens][D / 2 + 2];               // (the tokens of a warp on banks of their own)
     __shared__ TokenPlace place[kTokens];
     const int tid = threadIdx.x, t0 = blockIdx.x * kTokens;
     const int group = tid / kLanes, l = tid % kLanes, t = group / kGroups, at = t0 + t, g = group % kGroups;

@@ -12,7 +12,7 @@
 namespace {
 
 constexpr int kCacheManyTokens = 16384;
-constexpr int kRotateFew = 300, kRotateMany = 2400;   // tokens
+constexpr int kRotateFew = 300, kRotateMany = 2400, kRotateMost = 32768;   // tokens
 
 // The handle's device for the length of a call; the caller's is current again afterwards.
 struct DeviceScope {
@@ -306,12 +306,16 @@ adaspark_status_t launch_rotate(adaspark_attn* h, const RotateCall& a, const Pag
     auto launch = [&](auto kernel, int tokens) {
         launch_kernel(true, kernel, dim3((unsigned)((a.n + tokens - 1) / tokens)), dim3(kRotateThreads), 0, (cudaStream_t)cuda_stream, a, p);
     };
-    // as many tokens a CTA as leave every SM two
-    const int step = a.n >= kRotateMany ? 2 : a.n >= kRotateFew ? 1 : 0;
+    // As many tokens a CTA as leave every SM a few: what is worked out once for a token or a group is shared by more rows, against CTAs that an SM
+    // ends up without.  Measured with 28 + 4 heads of 128 (1 / 4 / 8 / 16 a CTA): 16 tokens 4.2 / 5.3 / 7.3 / - us, 300 5.5 / 5.6 / 7.5 / -,
+    // 1500 16.0 / 9.6 / 11.5 / -, 4096 40 / 20.7 / 18.8 / 23.3, 16512 - / - / 52.8 / 57.5; 65536 into pages - / - / 200 / 197, in 8 bits 251 / 236
+    const int step = a.n >= kRotateMost ? 3 : a.n >= kRotateMany ? 2 : a.n >= kRotateFew ? 1 : 0;
     if (h->cfg.head_dim == 128)
-        step == 2 ? launch(rotate_kernel<128, kPages, 8>, 8) : step == 1 ? launch(rotate_kernel<128, kPages, 4>, 4) : launch(rotate_kernel<128, kPages, 1>, 1);
+        step == 3 ? launch(rotate_kernel<128, kPages, 16>, 16) : step == 2 ? launch(rotate_kernel<128, kPages, 8>, 8)
+        : step == 1 ? launch(rotate_kernel<128, kPages, 4>, 4) : launch(rotate_kernel<128, kPages, 1>, 1);
     else
-        step == 2 ? launch(rotate_kernel<64, kPages, 16>, 16) : step == 1 ? launch(rotate_kernel<64, kPages, 4>, 4) : launch(rotate_kernel<64, kPages, 1>, 1);
+        step == 3 ? launch(rotate_kernel<64, kPages, 32>, 32) : step == 2 ? launch(rotate_kernel<64, kPages, 16>, 16)
+        : step == 1 ? launch(rotate_kernel<64, kPages, 4>, 4) : launch(rotate_kernel<64, kPages, 1>, 1);
     return launch_ok(h, "rotate_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
 }
 

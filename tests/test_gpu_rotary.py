@@ -99,6 +99,24 @@ def test_own_frequencies_and_interleaved_axes():
     check(ko, k, None, pos, freq, axis, False, "k")
 
 
+@pytest.mark.parametrize("D,adjacent", [(128, False), (64, True)])
+def test_as_many_tokens_as_a_long_video_has(D, adjacent):
+    g = torch.Generator().manual_seed(15)
+    Hq, Hkv, n, page = 2, 1, 33001, 64
+    eng = engine(Hq, Hkv, D)
+    r, freq, axis = turn(D, [8, 8, 8], adjacent)
+    q, k, v, w = rand(g, n, Hq, D), rand(g, n, Hkv, D), rand(g, n, Hkv, D), rand(g, D)
+    pos = torch.randint(0, 1000, (3, n), generator=g, dtype=torch.int32).cuda()
+    qo, ko = eng.rotate(q, k, pos, r, q_norm=w)
+    check(qo, q, w, pos, freq, axis, adjacent, "q")
+    check(ko, k, None, pos, freq, axis, adjacent, "k")
+    table, cache = pool(g, [n], page, Hkv, D, False)
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    qa = eng.paged_append(cache, q, k, v, cumulative([n]), table, lens, r, positions=pos, q_norm=w)
+    got = [x[table[0].long()].transpose(1, 2).reshape(-1, Hkv, D)[:n] for x in (cache.k_pages, cache.v_pages)]
+    assert torch.equal(qa, qo) and torch.equal(got[0], ko) and torch.equal(got[1], v)
+
+
 def test_norm_alone_and_sizes_whose_squares_leave_32_bits():
     g = torch.Generator().manual_seed(9)
     eng = engine(4, 4, 128)
