@@ -92,18 +92,24 @@ __device__ __forceinline__ void store_shared_16(uint32_t at, const uint4& v) {
 }
 // sum += 0 * x, of two bf16 each
 __device__ __forceinline__ void add_times_zero(uint32_t& sum, uint32_t x) { asm("fma.rn.bf16x2 %0, %1, %2, %0;\n" : "+r"(sum) : "r"(x), "r"(0u)); }
-// Bit 7 of each byte: the code is no number (0x7f, 0xff)
-__device__ __forceinline__ uint32_t odd_codes(uint32_t c) { return (c & 0x7f7f7f7fu) + 0x01010101u; }
 // 8 codes that are numbers times 2^(s - 127), s in 8 .. 134, as bf16: exact.  A code's exponent and mantissa four bits below bf16's are the same number
-// times 2^-120, subnormal ones too; f is 2^(s - 7) twice.  (Codes to f16, to f32, multiplied and rounded: as many instructions, but a chain
-// of conversions.)
-__device__ __forceinline__ uint4 codes_to_bf16x8(uint32_t a, uint32_t b, uint32_t f) {
-    const uint32_t p[4] = {__byte_perm(a, 0u, 0x1404), __byte_perm(a, 0u, 0x3424), __byte_perm(b, 0u, 0x1404), __byte_perm(b, 0u, 0x3424)};
+// times 2^-120, subnormal ones too; f is 2^(s - 7) twice.  Bytes are made four at a time: the low ones of the bf16 numbers, the high ones, then
+// these beside those.  top: the largest magnitudes so far, before f; a code that is no number shows as 0x7f0 and is 480 here.  (Codes to f16, to f32, multiplied and
+// rounded: as many instructions, but a chain of conversions.)
+constexpr uint32_t kNoNumberTop = 0x07f0u;
+__device__ __forceinline__ uint4 codes_to_bf16x8(uint32_t a, uint32_t b, uint32_t f, uint32_t& top) {
     uint32_t r[4];
+    const uint32_t w[2] = {a, b};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t low = (w[i] << 4) & 0xf0f0f0f0u, high = ((w[i] >> 4) & 0x07070707u) | (w[i] & 0x80808080u);
+        r[2 * i] = __byte_perm(low, high, 0x5140);
+        r[2 * i + 1] = __byte_perm(low, high, 0x7362);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t x = ((p[i] >> 4) & 0x07f007f0u) | (p[i] & 0x80008000u);
-        asm("mul.rn.bf16x2 %0, %1, %2;\n" : "=r"(r[i]) : "r"(x), "r"(f));
+        asm("max.xorsign.abs.bf16x2 %0, %0, %1;\n" : "+r"(top) : "r"(r[i]));
+        asm("mul.rn.bf16x2 %0, %0, %1;\n" : "+r"(r[i]) : "r"(f));
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
@@ -828,7 +834,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 if (lane == 0) tc::mbar_arrive(&sm.key_factor_full[gs % kPromptFactorSlots]);
                 const uint32_t src = raw0 + raw * (64 * D), scales = scale0 + raw * 128, dst = st * (64 * D * 2);
                 if (!(ok = tc::mbar_wait_warp(&sm.v_empty[st], ph, abort_flag))) break;
-                uint32_t odd = 0u, any = 0u;
+                uint32_t top = 0u, far = 0u, any = 0u;
 #pragma unroll 1
                 for (int i = 0; i < kPieces; i += 2) {
                     uint4 x[2];
@@ -842,9 +848,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const uint32_t f = (sc[y] + 120u) * 0x00800080u;      // 2^(s - 7) twice
-                        odd |= odd_codes(x[y].x) | odd_codes(x[y].y) | odd_codes(x[y].z) | odd_codes(x[y].w) | (sc[y] - 8u <= 126u ? 0u : 0x80u);
-                        r[y][0] = codes_to_bf16x8(x[y].x, x[y].y, f);
-                        r[y][1] = codes_to_bf16x8(x[y].z, x[y].w, f);
+                        far = max(far, sc[y] - 8u);
+                        r[y][0] = codes_to_bf16x8(x[y].x, x[y].y, f, top);
+                        r[y][1] = codes_to_bf16x8(x[y].z, x[y].w, f, top);
                     }
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
@@ -852,7 +858,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                         store_shared_16(to1 + dst + (i + y) * (kRows * kRowBytes), r[y][1]);
                     }
                 }
-                if (__any_sync(0xffffffffu, (odd & 0x80808080u) != 0u)) {
+                if (__any_sync(0xffffffffu, (top & 0x7fffu) >= kNoNumberTop || (top >> 16 & 0x7fffu) >= kNoNumberTop || far > 126u)) {
                     // rare: codes that are no numbers, powers of two far out
 #pragma unroll 1
                     for (int i = 0; i < kPieces; ++i) {
