@@ -37,6 +37,20 @@
 // A weight of zero does not hide a value that is no number: 0 * inf is one too.  Steps in which a row of the tile does not see a key
 // (the last one to three of a tile) therefore go over V in shared memory before the tensor core reads it: what is infinite or no
 // number is replaced by zero, and if it belongs to the sequence, the rows that do see it get it added at the end.
+//
+// Keys and values in the pages of a cache (kKeysPages): several new tokens a sequence, all of its tokens or a window of the last ones and the first few.
+// The steps of a tile are those of the first ones and those from the window's beginning on; what only some of its rows see is masked by 32 bits a
+// row and chunk.  A row whose first steps show it nothing begins with the first that does.  Boxes that no row sees are read as zeros, whatever
+// the table says of them.  A page's number is asked for a step ahead.  With few tiles a pair (PromptLine) they are one line cut into
+// equal runs: 2048 tokens over 65536 2.64 -> 2.13 ms, a mixed batch of chunks and single tokens 105 -> 88 us against tiles dealt longest first.
+//
+// Pages of e4m3 (kKeysPages8): K goes to the tensor cores as it lies in the pages (kind::f8f6f4), against q in two parts of four bits each whose sum
+// q is; the products are multiplied by the row's power of two and, four keys a load, by the keys' before they are weighed.  V is brought to bf16 in
+// shared memory by four more warps (20-23), with its powers of two in it: the weights need more bits than an 8-bit operand has.  (K brought to
+// bf16, too: 2.89 against 2.75 ms of 2048 tokens over 65536 then.)  What bounds it is issue and fetch of instructions: 5300 instructions of warps a
+// step and CTA against 3100 of bf16 pages, and the stall that leads is that none is there (2.4 of 9.9 cycles an instruction; bf16 1.1); loops
+// that are rolled up are faster than the same unrolled.  Tried without gain: rows of few tokens twice, each copy with half of the keys; 8 warps for
+// the codes and registers moved between warpgroups (spills); more or fewer stages of K, V and codes; the keys' powers of two a step ahead.
 #pragma once
 #include <type_traits>
 
