@@ -385,6 +385,7 @@ struct PromptSpan {
 // walks levels finds its first tile 5 us later.)  Lengths are in keys: what the tile's last row sees, and in front of that kPromptAhead for what a
 // tile costs beside its steps.  A pair's first tile may have begun in an earlier run, its last may go on in the next: two parts a pair,
 // joined by prompt_join_kernel.  Nobody cuts off less than kPromptLeast steps.
+// (Not with more than four tiles a pair, prompt_may_cut: 456 tiles of 270 steps on average gain 5 %, of 17 steps lose 17.)
 constexpr int kPromptAhead = 384, kPromptLeast = 3;
 struct PromptLine {
     int chunk;                                                // first sequence of the lanes' 32

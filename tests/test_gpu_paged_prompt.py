@@ -480,3 +480,85 @@ def test_runs_that_end_anywhere(window, sinks, e4m3):
     first = run_and_check(eng, cache, table, q, cumulative(new), kv_len, window, sinks)
     again = run_and_check(eng, cache, table, q, cumulative(new), kv_len, window, sinks)
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_many_long_tiles(e4m3):
+    """More tiles than four a pair, dealt longest first: long ones alike, and ones of two lengths."""
+    g = torch.Generator().manual_seed(35)
+    Hq, Hkv, D, page = 16, 8, 64, 64
+    eng = engine(Hq, Hkv, D)
+    for new, kv_len in (([40] * 45, [13000] * 45), ([300, 129] * 10, [1800, 130] * 10)):
+        order = torch.randperm(64 * -(-max(kv_len) // page) // 4, generator=g).to(torch.int32)
+        width = -(-max(kv_len) // page)
+        table = torch.stack([order[torch.randint(0, order.numel(), (width,), generator=g)] for _ in kv_len]).cuda()   # (sequences may share what nobody writes)
+        k, v = rand(g, order.numel(), Hkv, page, D), rand(g, order.numel(), Hkv, page, D)
+        if e4m3:
+            k, v = (x.float().mul(16).to(torch.float8_e4m3fn) for x in (k, v))
+            cache = binding.PagedCache(k, v, *(torch.full(k.shape[:3], 123, dtype=torch.uint8, device="cuda") for _ in range(2)))
+        else:
+            cache = binding.PagedCache(k, v)
+        q = rand(g, sum(new), Hq, D)
+        out, lse = eng.paged_prompt(q, cache, cumulative(new), table, ints(kv_len), want_lse=True)
+        assert eng.text_status() == 0
+        at = 0
+        for b, (r, n) in enumerate(zip(new, kv_len)):
+            rows, at = slice(at, at + r), at + r
+            if b % 9:
+                continue
+            keys, values = sequence_values(cache, table, b, n)
+            want, wl, tol, ltol = attend_masked(q[rows], keys, values, hidden_from(n - r, r, n, 0, 0), D ** -0.5)
+            if e4m3:                                             # q in two parts: 2^-18 of its largest magnitude, as a score
+                e = q[rows].double().abs().amax(-1) * 2.0 ** -18 * keys.abs().sum(-1).amax() * D ** -0.5
+                tol, ltol = tol + (2 * e * values.abs().amax())[..., None], ltol + e
+            assert_close(out[rows], want, tol, f"out {b}")
+            assert_lse(lse[rows], wl, ltol)
+
+
+def test_pages_far_apart():
+    """A pool of more than 2^31 values: what lies at its end is written and read there."""
+    g = torch.Generator().manual_seed(36)
+    Hq, Hkv, D, page, n_pages = 8, 4, 128, 64, 70000
+    eng = engine(Hq, Hkv, D)
+    cache = binding.PagedCache(*(torch.empty(n_pages, Hkv, page, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    assert cache.k_pages.numel() > 2 ** 31
+    n, r = 500, 500
+    table = (n_pages - 1 - torch.randperm(8, generator=g).to(torch.int32) * 100).cuda()[None].contiguous()
+    q, k, v = rand(g, r, Hq, D), rand(g, r, Hkv, D), rand(g, r, Hkv, D)
+    eng.paged_append(cache, None, k, v, ints([0, r]), table, ints([n]))
+    at = torch.arange(n, device="cuda")
+    assert torch.equal(cache.k_pages[table[0].long()[at // page], :, at % page], k) and torch.equal(cache.v_pages[table[0].long()[at // page], :, at % page], v)
+    out, _ = eng.paged_prompt(q[-40:], cache, ints([0, 40]), table, ints([n]), window=300, sinks=3)
+    want, _, tol, _ = attend_masked(q[-40:], k, v, hidden_from(n - 40, 40, n, 300, 3), D ** -0.5)
+    assert_close(out, want, tol, "out")
+    one, _ = eng.paged_decode(q[-1:], None, None, cache, table, ints([n]), window=300, sinks=3)
+    assert_close(one, want[-1:], tol[-1:], "decode")
+    assert eng.text_status() == 0
+
+
+def test_refusals_of_the_binding():
+    eng = engine(4, 2, 64)
+    cache = eng.paged_cache(4, 16)
+    other = engine(4, 4, 64).paged_cache(4, 16)
+    q, k, table, lens, cu = torch.zeros(5, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(5, 2, 64, dtype=torch.bfloat16, device="cuda"), ints([[0], [1]]), ints([5, 0]), ints([0, 5, 5])
+    rope, wide = binding.Rotary(64, sections=[8, 8, 8]), binding.Rotary(128)
+    pos = torch.zeros(3, 5, dtype=torch.int32, device="cuda")
+
+    def refused(fn, *a, **kw):
+        with pytest.raises(binding.AdasparkError) as e:
+            fn(*a, **kw)
+        return e.value.status == binding.ERR_INVALID_ARG
+    assert refused(eng.paged_prompt, q, other, cu, table, lens) and refused(eng.paged_prompt, q.half(), cache, cu, table, lens)
+    assert refused(eng.paged_prompt, k, cache, cu, table, lens) and refused(eng.paged_prompt, q, cache, cu[:2], table, lens)
+    assert refused(eng.paged_prompt, q, cache, cu, table, lens, window=-1) and refused(eng.paged_prompt, q, cache, cu, table, lens, window=4, sinks=-2)
+    assert refused(eng.paged_prompt, q, cache, cu, table.cpu(), lens) and refused(eng.paged_prompt, q, cache, cu, table, lens, out=q[:4])
+    assert refused(eng.paged_prompt, q, cache, cu.long(), table, lens) and refused(eng.paged_prompt, q, cache, cu, table, lens, lse=torch.zeros(5, 4, dtype=torch.float64, device="cuda"))
+    assert refused(eng.paged_decode, q[:2], None, None, cache, table, lens, window=-3) and refused(eng.paged_decode, q[:2], None, None, cache, table, lens, sinks=-1)
+    assert refused(eng.rotate, q, k, pos, wide) and refused(eng.rotate, q, k, None, rope) and refused(eng.rotate, None, None)
+    assert refused(eng.rotate, q, k, pos[:2], rope) and refused(eng.rotate, q, k, pos.long(), rope) and refused(eng.rotate, q, k[:4], pos, rope)
+    assert refused(eng.rotate, q, k, pos.cpu(), rope) and refused(eng.rotate, q, None, pos, rope, k_out=k) and refused(eng.rotate, q, k, pos, rope, q_out=q[:3])
+    assert refused(eng.rotate, q, k, q_norm=torch.zeros(128, dtype=torch.bfloat16, device="cuda")) and refused(eng.rotate, q, k, eps=-1.0)
+    assert refused(eng.rotate, q.expand(5, 4, 64)[:, :1].expand(5, 4, 64), k)                # one row for all heads
+    assert refused(eng.paged_append, cache, q, k, k[:4], cu, table, lens) and refused(eng.paged_append, cache, None, k, k, cu, table, lens, q_out=q)
+    assert refused(eng.paged_append, cache, q, k, k, cu, table, lens, rope, positions=pos[0].contiguous())
+    assert eng.text_status() == 0

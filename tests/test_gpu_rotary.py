@@ -271,3 +271,22 @@ def test_values_that_are_no_numbers_in_8_bits():
         a, b = a.float(), b.float()
         assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num())
     assert torch.equal(cache.k_scale, ref.k_scale) and torch.equal(cache.v_scale, ref.v_scale)
+
+
+@pytest.mark.parametrize("batch", [31, 32, 100])
+def test_append_of_many_sequences(batch):
+    """Places found by the lanes of a warp, and by a search; sequences without rows among them."""
+    g = torch.Generator().manual_seed(batch)
+    Hq, Hkv, D, page = 4, 2, 64, 16
+    eng = engine(Hq, Hkv, D)
+    new = [int(x) for x in torch.randint(0, 40, (batch,), generator=g)]
+    kv_len = [a + int(x) for a, x in zip(new, torch.randint(0, 50, (batch,), generator=g))]
+    table, cache = pool(g, kv_len, page, Hkv, D, False)
+    n = sum(new)
+    q, k, v = rand(g, n, Hq, D), rand(g, n, Hkv, D), rand(g, n, Hkv, D)
+    cu = cumulative(new)
+    eng.paged_append(cache, q, k, v, cu, table, torch.tensor(kv_len, dtype=torch.int32, device="cuda"))
+    assert eng.text_status() == 0
+    where = places(table, kv_len, cu.tolist(), page)
+    rows, pages, slots = (torch.tensor([x[i] for x in where], device="cuda") for i in range(3))
+    assert torch.equal(cache.k_pages[pages, :, slots], k[rows]) and torch.equal(cache.v_pages[pages, :, slots], v[rows])
