@@ -181,9 +181,10 @@ __device__ __forceinline__ void find_tokens(const PageGeom& p, const int32_t* cu
 // A sequence with bad bounds may have no row in the tensors (all of it behind them): the CTAs share the batch out among them and look at every
 // sequence's.  (Behind the copies: in front of them it took registers that left room for a CTA less, 157 instead of 146 us for 131072 tokens
 // written and read in 8 bits; hence the bound of 4 CTAs on both kernels, too.)
+template <int kThreads = kCacheThreads>
 __device__ __forceinline__ void report_bounds(const int32_t* cu, int batch, int n, int32_t* status) {
     if (status == nullptr || blockIdx.y != 0) return;
-    for (long long b = blockIdx.x * (long long)kCacheThreads + threadIdx.x; b < batch; b += gridDim.x * (long long)kCacheThreads)
+    for (long long b = blockIdx.x * (long long)kThreads + threadIdx.x; b < batch; b += gridDim.x * (long long)kThreads)
         if (!bounds_fit(cu[b], cu[b + 1], n)) atomicExch(status, 1);
 }
 

@@ -119,12 +119,12 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float* x) {
     return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
 
-constexpr int kRotateThreads = kCacheThreads;
+constexpr int kRotateThreads = 128;                           // (256: 52 for 49 us of 16512 tokens, 236 for 222 of 65536 into 8-bit pages)
 constexpr int kRotateRing = 4;                                // rows of a group under way, and one in work
 
 // kPages: 0 rows out; 1, 2 keys and values into pages of bf16, e4m3.  grid (tokens / kTokens).
 template <int D, int kPages, int kTokens>
-__global__ void __launch_bounds__(kRotateThreads, 3) rotate_kernel(const __grid_constant__ RotateCall a, const __grid_constant__ PageGeom p) {
+__global__ void __launch_bounds__(kRotateThreads, 6) rotate_kernel(const __grid_constant__ RotateCall a, const __grid_constant__ PageGeom p) {
     constexpr int kLanes = D / 16, kGroups = kRotateThreads / kLanes / kTokens;     // of a token
     __shared__ uint4 ring[kRotateRing][2][kRotateThreads];
     __shared__ float2 turn[kTokens][D / 2 + 2];               // (the tokens of a warp on banks of their own)
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kRotateThreads, 3) rotate_kernel(const __grid_
     rows_of(std::integral_constant<int, 1>());
     if (kPages) rows_of(std::integral_constant<int, 2>());
     cp_async_wait<0>();
-    if (kPages) report_bounds(a.cu, a.batch, a.n, a.status);
+    if (kPages) report_bounds<kRotateThreads>(a.cu, a.batch, a.n, a.status);
 }
 
 }  // namespace adaspark

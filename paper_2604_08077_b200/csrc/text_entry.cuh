@@ -307,15 +307,15 @@ adaspark_status_t launch_rotate(adaspark_attn* h, const RotateCall& a, const Pag
         launch_kernel(true, kernel, dim3((unsigned)((a.n + tokens - 1) / tokens)), dim3(kRotateThreads), 0, (cudaStream_t)cuda_stream, a, p);
     };
     // As many tokens a CTA as leave every SM a few: what is worked out once for a token or a group is shared by more rows, against CTAs that an SM
-    // ends up without.  Measured with 28 + 4 heads of 128 (1 / 4 / 8 / 16 a CTA): 16 tokens 4.2 / 5.3 / 7.3 / - us, 300 5.5 / 5.6 / 7.5 / -,
-    // 1500 16.0 / 9.6 / 11.5 / -, 4096 40 / 20.7 / 18.8 / 23.3, 16512 - / - / 52.8 / 57.5; 65536 into pages - / - / 200 / 197, in 8 bits 251 / 236
+    // ends up without.  Measured with 28 + 4 heads of 128 and CTAs of 256 threads (twice the tokens): 2 / 4 / 8 / 16 a CTA at 16 tokens 4.2 / 5.3 / 7.3 / - us,
+    // 300 5.5 / 5.6 / 7.5 / -, 1500 16.0 / 9.6 / 11.5 / -, 4096 40 / 20.7 / 18.8 / 23.3, 16512 - / - / 52.8 / 57.5; 65536 into pages - / - / 200 / 197
     const int step = a.n >= kRotateMost ? 3 : a.n >= kRotateMany ? 2 : a.n >= kRotateFew ? 1 : 0;
     if (h->cfg.head_dim == 128)
-        step == 3 ? launch(rotate_kernel<128, kPages, 16>, 16) : step == 2 ? launch(rotate_kernel<128, kPages, 8>, 8)
-        : step == 1 ? launch(rotate_kernel<128, kPages, 4>, 4) : launch(rotate_kernel<128, kPages, 1>, 1);
+        step == 3 ? launch(rotate_kernel<128, kPages, 8>, 8) : step == 2 ? launch(rotate_kernel<128, kPages, 4>, 4)
+        : step == 1 ? launch(rotate_kernel<128, kPages, 2>, 2) : launch(rotate_kernel<128, kPages, 1>, 1);
     else
-        step == 3 ? launch(rotate_kernel<64, kPages, 32>, 32) : step == 2 ? launch(rotate_kernel<64, kPages, 16>, 16)
-        : step == 1 ? launch(rotate_kernel<64, kPages, 4>, 4) : launch(rotate_kernel<64, kPages, 1>, 1);
+        step == 3 ? launch(rotate_kernel<64, kPages, 16>, 16) : step == 2 ? launch(rotate_kernel<64, kPages, 8>, 8)
+        : step == 1 ? launch(rotate_kernel<64, kPages, 2>, 2) : launch(rotate_kernel<64, kPages, 1>, 1);
     return launch_ok(h, "rotate_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
 }
 
