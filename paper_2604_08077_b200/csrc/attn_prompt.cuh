@@ -390,6 +390,7 @@ constexpr int kPromptAhead = 384, kPromptLeast = 3;
 struct PromptLine {
     int chunk;                                                // first sequence of the lanes' 32
     PromptSeq<true> mine;
+    long long own;                                            // its length
     // the tile
     PromptSeq<true> seq;
     int tile, gk;
@@ -412,16 +413,17 @@ struct PromptLine {
     __device__ __forceinline__ bool load(const PromptGeom& g, int c, int lane) {
         chunk = c;
         mine.nt = 0;
-        return c + lane >= g.batch || mine.load(g, c + lane);
+        const bool fine = c + lane >= g.batch || mine.load(g, c + lane);
+        own = mine.nt > 0 ? length(g, mine, mine.nt) * g.Hkv : 0;
+        return fine;
     }
-    __device__ __forceinline__ long long mine_length(const PromptGeom& g) const { return mine.nt > 0 ? length(g, mine, mine.nt) * g.Hkv : 0; }
     // length of the line; fine: no sequence leaves the tensors or its table
     __device__ __forceinline__ long long begin(const PromptGeom& g, int lane, bool& fine) {
         long long sum = 0;
         fine = true;
         for (int c = 0; c < g.batch; c += 32) {
             fine = load(g, c, lane) && fine;
-            sum += mine_length(g);
+            sum += own;
         }
 #pragma unroll
         for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
@@ -441,7 +443,6 @@ struct PromptLine {
         long long before = 0;
         for (int c = 0; c < g.batch; c += 32) {
             if (c > 0 || chunk != 0) load(g, c, lane);
-            const long long own = mine_length(g);
             long long upto = own;
 #pragma unroll
             for (int y = 1; y < 32; y <<= 1) {
@@ -496,16 +497,17 @@ struct PromptLine {
         const long long y = x - place - kPromptAhead;
         if (y >= cost - kPromptAhead) return n;
         if (y <= 0) return 0;
-        const int i = (int)(y * n / (cost - kPromptAhead));
+        // (in 32 bits: it has to grow with y and to be the same for whoever asks, no more)
+        const int i = (int)((float)(int)y / (float)(int)(cost - kPromptAhead) * (float)n);
         return i < kPromptLeast ? 0 : n - i < kPromptLeast ? n : i;
     }
 };
-// The line's runs, of equal length but for a key
+// The line's runs, of equal length but for the last one's few keys more
 struct PromptRuns {
-    long long length;
-    int longer;                                               // the first ones, by a key
-    __device__ __forceinline__ PromptRuns(long long total, int n_pairs) : length(total / n_pairs), longer((int)(total % n_pairs)) {}
-    __device__ __forceinline__ long long begin(int run) const { return length * run + min(run, longer); }
+    long long total, length;
+    int n_pairs;
+    __device__ __forceinline__ PromptRuns(long long total_, int n) : total(total_), length(total_ >> 32 ? total_ / n : (uint32_t)total_ / (uint32_t)n), n_pairs(n) {}
+    __device__ __forceinline__ long long begin(int run) const { return run == n_pairs ? total : length * run; }
 };
 
 template <int D, int kKeys>
