@@ -474,7 +474,8 @@ typedef struct {
     int64_t workspace_bytes;
     int32_t *status;
     int32_t batch, n, table_width;
-    int32_t window, sinks;             /* window 0: none (sinks says nothing then)                     */
+    int32_t window, sinks;             /* window 0: none (sinks says nothing then).  With a window a table may hold
+                                          2^31 - 256 tokens                                            */
     int32_t reserved;
 } adaspark_attn_paged_prompt_t;
 adaspark_status_t adaspark_attn_paged_prompt(adaspark_attn_t *handle, const adaspark_attn_paged_prompt_t *call, void *cuda_stream);

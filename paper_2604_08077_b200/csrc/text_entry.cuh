@@ -402,6 +402,8 @@ adaspark_status_t adaspark_attn_paged_prompt(adaspark_attn_t* h, const adaspark_
     ADASPARK_TRY(check_rows(h, who, "q", c->q, h->cfg.n_q_heads, rq));
     if (!c->cu || !c->kv_len || !c->out) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: NULL pointer", who);
     if ((uintptr_t)c->out % 16) return fail(h, ADASPARK_ERR_INVALID_ARG, "%s: out is not 16-byte aligned", who);
+    if (c->window && ((long long)c->table_width << p.page_shift) > 0x7fffff00ll)      // (a window's steps begin anywhere: the last one ends up to 127 tokens further)
+        return fail(h, ADASPARK_ERR_UNSUPPORTED, "%s: %d pages a sequence hold more than 2^31 - 256 tokens", who, c->table_width);
     ADASPARK_TRY(check_workspace(h, who, c->workspace, c->workspace_bytes));
     DeviceScope scope;
     ADASPARK_TRY(scope.enter(h, who));

@@ -51,7 +51,7 @@ SHAPES = [
     # new tokens, tokens before them, page, window, sinks
     ([41], [503], 16, 0, 0), ([1], [0], 16, 0, 0), ([5, 4, 1], [1000, 2047, 0], 64, 0, 0), ([130, 0, 1, 300], [77, 40, 128, 0], 32, 0, 0),
     ([17, 1, 64], [300, 128, 1000], 16, 100, 4), ([200], [900], 128, 128, 0), ([40, 3], [2000, 700], 64, 1, 0), ([33, 70], [1000, 0], 256, 257, 130),
-    ([256, 5], [0, 640], 16, 37, 1), ([9], [4000], 64, 4000, 16), ([9], [4000], 32, 5000, 5000), ([100], [1500], 16, 64, 700)]
+    ([77, 3], [1111, 333], 16, 200, 0), ([77, 3], [1111, 333], 32, 131, 40), ([77], [1111], 64, 100, 129), ([150], [1111], 128, 300, 4), ([256, 5], [0, 640], 16, 37, 1), ([9], [4000], 64, 4000, 16), ([9], [4000], 32, 5000, 5000), ([100], [1500], 16, 64, 700)]
 
 
 @pytest.mark.parametrize("e4m3", [False, True])

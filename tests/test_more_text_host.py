@@ -140,6 +140,7 @@ def test_attention_refusals(handle, call, bad, status):
 
 def test_other_refusals(handle):
     assert code(lambda: chunk(handle, cu=None)) == INVALID and code(lambda: chunk(handle, n=-1)) == INVALID
+    assert code(lambda: chunk(handle, table_width=(1 << 27) - 1, window=7)) == UNSUPPORTED
     assert code(lambda: decode(handle, window=0)) == INVALID and code(lambda: decode(handle, k_new=ROW)) == INVALID
     for name in ("paged_decode_window", "paged_prompt", "rotate", "paged_append"):
         assert getattr(binding.load(), "adaspark_attn_" + name)(None, b"", None) == INVALID
