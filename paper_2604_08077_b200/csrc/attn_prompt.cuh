@@ -366,12 +366,12 @@ struct PromptSpan {
         n = max(prompt_steps(hi), 1);
         sink_steps = base = lo = low_first = low_masked = 0;
         if (g.window > 0) {
-            lo = max(p0 + 1 - g.window, 0);
+            lo = max(max(p0, 0) + 1 - g.window, 0);          // (rows in front of token 0: a window may be 2^31 - 1)
             sink_steps = min(prompt_steps(g.sinks), n);
             // the window's steps begin with the box that holds its first key, or go on where the first ones' end
             base = max(lo & -min(1 << g.pages.page_shift, 128), sink_steps << 7);
             n = max(sink_steps + prompt_steps(max(hi - base, 0)), 1);
-            const int lo1 = max(p1 + 1 - g.window, 0);       // (the last row's)
+            const int lo1 = max(hi - g.window, 0);           // (the last row's)
             if (lo1 > g.sinks) {
                 low_first = g.sinks >> 7;
                 low_masked = sink_steps + prompt_steps(max(lo1 - base, 0));
@@ -1225,7 +1225,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             if (t.n_steps == 0) break;
             const int last = t.last0 + tok;                   // the last key that the row sees
             const bool valid = tok < t.n_tok;                 // (the tile's last rows may be none, tokens behind the sequence not its own)
-            const int first = kPaged && g.window > 0 ? max(last + 1 - g.window, 0) : 0;   // of those behind the first ones
+            const int first = kPaged && g.window > 0 ? max(max(last, 0) + 1 - g.window, 0) : 0;   // of those behind the first ones
             const bool idle = kPaged && !__any_sync(0xffffffffu, valid);   // no row of the warp is one: nothing is computed
             [[maybe_unused]] float row_factor = 0.f;          // 8-bit pages: scores are products with codes times this and the key's power of two
             if constexpr (kCodes) {
@@ -1542,7 +1542,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 if (kPaged && odd && mine) {                  // rare: values that are no numbers and that this row sees
                     __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(srow);
                     for (int j = t.next_masked(0); j < t.n_steps; j = t.next_masked(j + 1))
-                        for (int key = t.key_of(j), end = min(key + 128, last + 1); key < end; ++key) {
+                        for (int key = t.key_of(j), end = key + min(128, last + 1 - key); key < end; ++key) {
                             if (key < first && key >= g.sinks) continue;
                             for (int c = 0; c < D / 16; ++c) {
                                 const uint4 chunk = paged_chunk<D, kCodes>(g.pages, g.pages.v, g.pages.vs, t.seq, t.gk, key, half * (D / 16) + c);

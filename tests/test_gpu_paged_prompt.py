@@ -240,6 +240,22 @@ def test_lengths_bounds_and_pages_out_of_range(e4m3):
     assert_lse(lse, wl, ltol)
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (28, 4, 128)])
+def test_rows_in_front_of_the_first_token_with_a_window_of_any_length(Hq, Hkv, D, e4m3):
+    g = torch.Generator().manual_seed(80)
+    eng = engine(Hq, Hkv, D)
+    table, cache = pool(g, [144], 16, Hkv, D, e4m3)
+    q = rand(g, 90, Hq, D)
+    out, lse = eng.paged_prompt(q, cache, ints([0, 90]), table, ints([60]), window=2 ** 31 - 1, sinks=5, want_lse=True)
+    assert eng.text_status() == 1
+    assert (out[:30] == 0).all() and (lse[:30] == -math.inf).all()
+    k, v = sequence_values(cache, table, 0, 60)
+    want, wl, tol, ltol = attend_masked(q[30:], k, v, hidden_from(0, 60, 60, 0, 0), D ** -0.5)
+    assert_close(out[30:], want, tol, "out")
+    assert_lse(lse[30:], wl, ltol)
+
+
 def test_empty_calls():
     eng = engine(4, 2, 64)
     cache = eng.paged_cache(2, 16)
