@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kRotateThreads, 6) rotate_kernel(const __grid_
                         x[1][i] = mul_f32x2(x[1][i], down2);
                     }
                     s = sum_of_squares();
-                    if (down != 1.f) f = root(s * (1.f / D));
+                    if (down != 1.f) f = s == INFINITY ? 0.f : root(s * (1.f / D));   // (beside an infinity what is finite becomes zeros)
                 }
                 const unsigned long long f2 = pack_f32x2(f, f);
 #pragma unroll

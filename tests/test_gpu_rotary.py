@@ -131,6 +131,21 @@ def test_norm_alone_and_sizes_whose_squares_leave_32_bits():
     assert torch.equal(zeros, torch.zeros_like(q))
 
 
+def test_norm_beside_values_that_are_no_numbers():
+    g = torch.Generator().manual_seed(91)
+    eng = engine(4, 4, 64)
+    w, q = rand(g, 64), rand(g, 3, 4, 64)
+    q[0, 1, 5], q[1, 0, 63], q[1, 0, 2], q[2, 3, 7] = float("inf"), float("-inf"), float("inf"), float("nan")
+    qo, _ = eng.rotate(q, None, q_norm=w)
+    x = q.double()
+    want = x / torch.sqrt(x.square().mean(-1, keepdim=True) + 1e-6) * w.double()
+    assert torch.equal(qo.isnan(), want.isnan()) and want.isnan().sum() == 67
+    assert (qo[0, 1][torch.arange(64) != 5] == 0).all()
+    rest = torch.ones(3, 4, dtype=torch.bool)
+    rest[0, 1] = rest[1, 0] = rest[2, 3] = False
+    check(qo[rest][None], q[rest][None], w, None, [], [], False, "rows beside them", eps=1e-6)
+
+
 def test_no_rows():
     eng = engine(4, 2, 64)
     r, _, _ = turn(64, [32], False)
