@@ -12,7 +12,7 @@
 namespace {
 
 constexpr int kCacheManyTokens = 16384;
-constexpr int kRotateFew = 300, kRotateMany = 2400, kRotateMost = 32768;   // tokens
+constexpr int kRotateFew = 300, kRotateMany = 2400, kRotateMost = 32768, kRotateFew64 = 600, kRotateMany64 = 3500;   // tokens
 
 // The handle's device for the length of a call; the caller's is current again afterwards.
 struct DeviceScope {
@@ -307,15 +307,17 @@ adaspark_status_t launch_rotate(adaspark_attn* h, const RotateCall& a, const Pag
         launch_kernel(true, kernel, dim3((unsigned)((a.n + tokens - 1) / tokens)), dim3(kRotateThreads), 0, (cudaStream_t)cuda_stream, a, p);
     };
     // As many tokens a CTA as leave every SM a few: what is worked out once for a token or a group is shared by more rows, against CTAs that an SM
-    // ends up without.  Measured with 28 + 4 heads of 128 and CTAs of 256 threads (twice the tokens): 2 / 4 / 8 / 16 a CTA at 16 tokens 4.2 / 5.3 / 7.3 / - us,
-    // 300 5.5 / 5.6 / 7.5 / -, 1500 16.0 / 9.6 / 11.5 / -, 4096 40 / 20.7 / 18.8 / 23.3, 16512 - / - / 52.8 / 57.5; 65536 into pages - / - / 200 / 197
-    const int step = a.n >= kRotateMost ? 3 : a.n >= kRotateMany ? 2 : a.n >= kRotateFew ? 1 : 0;
-    if (h->cfg.head_dim == 128)
-        step == 3 ? launch(rotate_kernel<128, kPages, 8>, 8) : step == 2 ? launch(rotate_kernel<128, kPages, 4>, 4)
-        : step == 1 ? launch(rotate_kernel<128, kPages, 2>, 2) : launch(rotate_kernel<128, kPages, 1>, 1);
-    else
-        step == 3 ? launch(rotate_kernel<64, kPages, 16>, 16) : step == 2 ? launch(rotate_kernel<64, kPages, 8>, 8)
-        : step == 1 ? launch(rotate_kernel<64, kPages, 2>, 2) : launch(rotate_kernel<64, kPages, 1>, 1);
+    // ends up without.  Measured, us at 1 / 2 / 4 / 8 tokens a CTA, 28 + 4 heads of 128 with norms: 300 tokens 5.3 / 5.5 / 6.6 / 10.3, 1200 9.9 / 9.2 / 9.9 / 11.6,
+    // 2400 17.1 / 13.8 / 13.5 / 15.7, 16512 85 / 62 / 49.6 / 55.5; into bf16 pages 65536 384 / 255 / 184 / 193; into 8-bit ones 33000 232 / 156 / 122 / 122,
+    // 65536 452 / 302 / 231 / 222.  16 + 4 heads of 64 into bf16 pages and read back, at 2 / 4 / 8 / 16: 400 5.2 / 5.0 / 6.3 / 9.1, 701 6.0 / 5.6 / 6.4 / 9.1,
+    // 2400 10.0 / 8.8 / 8.7 / 10.2 (8-bit pages 14.0 / 13.3 / 14.8 / 18.6), 9000 27.8 / 19.4 / 17.6 / 22.1, 33000 85 / 53 / 42 / 43; at 4682 calls one behind the
+    // other take 17.9 us with 4 (1.3 waves of CTAs) and 16.5 with 8
+    if (h->cfg.head_dim == 128) {
+        if (kPages == 2 && a.n >= kRotateMost) launch(rotate_kernel<128, 2, 8>, 8);
+        else a.n >= kRotateMany ? launch(rotate_kernel<128, kPages, 4>, 4) : a.n >= kRotateFew ? launch(rotate_kernel<128, kPages, 2>, 2) : launch(rotate_kernel<128, kPages, 1>, 1);
+    } else {
+        a.n >= kRotateMany64 ? launch(rotate_kernel<64, kPages, 8>, 8) : a.n >= kRotateFew64 ? launch(rotate_kernel<64, kPages, 4>, 4) : launch(rotate_kernel<64, kPages, 2>, 2);
+    }
     return launch_ok(h, "rotate_kernel") ? ADASPARK_OK : ADASPARK_ERR_CUDA;
 }
 

@@ -146,6 +146,11 @@ def test_norm_beside_values_that_are_no_numbers():
     check(qo[rest][None], q[rest][None], w, None, [], [], False, "rows beside them", eps=1e-6)
 
 
+def pages_of(cache):
+    """Pages and powers of two as bytes."""
+    return [x.view(torch.uint8) for x in (cache.k_pages, cache.v_pages, cache.k_scale, cache.v_scale) if x is not None]
+
+
 def test_no_rows():
     eng = engine(4, 2, 64)
     r, _, _ = turn(64, [32], False)
@@ -246,6 +251,34 @@ def test_bf16_pages_are_rotate_and_write(D, n):
     used = table[0, :-(-n // page)].long()
     got = [x[used].transpose(1, 2).reshape(-1, Hkv, D)[:n] for x in (a.k_pages, c.k_pages)]
     assert torch.equal(*got)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("D,n,pieces", [(128, 32800, [200, 299, 301, 2000, 30000]), (64, 6200, [100, 599, 601, 4900]), (128, 2500, [1, 2499])])
+def test_in_one_call_or_in_several(D, n, pieces, e4m3):
+    """The same rows whatever number of tokens a call has."""
+    g = torch.Generator().manual_seed(n)
+    Hq, Hkv, page = 3, 1, 32
+    assert sum(pieces) == n
+    eng = engine(Hq, Hkv, D)
+    r, _, _ = turn(D, [8, 16], True)
+    q, k, v, w = rand(g, n, Hq, D), rand(g, n, Hkv, D), rand(g, n, Hkv, D), rand(g, D)
+    pos = torch.randint(0, 100000, (2, n), generator=g, dtype=torch.int32).cuda()
+    table, one = pool(g, [n], page, Hkv, D, e4m3)
+    other = binding.PagedCache(*(x.clone() for x in (one.k_pages, one.v_pages, one.k_scale, one.v_scale) if x is not None))
+    got = eng.paged_append(one, q, k, v, cumulative([n]), table, torch.tensor([n], dtype=torch.int32, device="cuda"), r, positions=pos, q_norm=w, k_norm=w)
+    turned, _ = eng.rotate(q, None, pos, r, q_norm=w)
+    assert torch.equal(got, turned)
+    at = 0
+    for m in pieces:
+        rows = slice(at, at + m)
+        at += m
+        part = eng.paged_append(other, q[rows], k[rows], v[rows], cumulative([m]), table, torch.tensor([at], dtype=torch.int32, device="cuda"), r,
+                                positions=pos[:, rows].contiguous(), q_norm=w, k_norm=w)
+        assert torch.equal(part, got[rows])
+    assert eng.text_status() == 0
+    for a, b in zip(pages_of(one), pages_of(other)):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
