@@ -319,6 +319,57 @@ def test_a_captured_step_with_new_lengths():
         assert eng.text_status() == 0
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 31 - 1), (2 ** 30, 2 ** 30)])
+def test_windows_that_hide_nothing(window, sinks, e4m3):
+    g = torch.Generator().manual_seed(141)
+    Hq, Hkv, D, page = 8, 2, 128, 32
+    eng = engine(Hq, Hkv, D)
+    new, kv_len = [3, 40, 0, 1], [3, 1700, 0, 900]
+    table, cache = pool(g, kv_len, page, Hkv, D, e4m3)
+    q, cu = rand(g, 44, Hq, D), cumulative(new)
+    run_and_check(eng, cache, table, q, cu, kv_len, window, sinks)
+    got = eng.paged_decode(q[:4], None, None, cache, table, ints(kv_len), window=window, sinks=sinks, want_lse=True)
+    want = eng.paged_decode(q[:4], None, None, cache, table, ints(kv_len), want_lse=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert eng.text_status() == 0
+
+
+def test_two_captured_steps_in_turn():
+    """Graphs of one object, replayed one behind the other in any order: they share its workspace."""
+    g = torch.Generator().manual_seed(142)
+    Hq, Hkv, D, page = 28, 4, 128, 64
+    eng = engine(Hq, Hkv, D)
+    table, cache = pool(g, [9000, 5000], page, Hkv, D, True)
+    cu, lens, rotary = ints([0, 4, 5]), ints([9000, 5000]), binding.Rotary(D)
+    q, k, v, pos = rand(g, 5, Hq, D), rand(g, 5, Hkv, D), rand(g, 5, Hkv, D), ints([1, 2, 3, 4, 5])
+
+    def chunk():
+        return eng.paged_prompt(eng.rotate(q, None, pos, rotary)[0], cache, cu, table, lens)[0]
+
+    def token():
+        return eng.paged_decode(q[:2], k[:2], v[:2], cache, table, lens, window=4000, sinks=4)[0]
+    want = []
+    graphs, outs = [], []
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        token()
+        for f in (chunk, token):
+            want.append(f().clone())
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                outs.append(f())
+            graphs.append(graph)
+    torch.cuda.synchronize()
+    for i in (0, 1, 1, 0, 0, 1):
+        outs[i].fill_(7.0)
+        graphs[i].replay()
+        graphs[1 - i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
 def test_another_stream():
     g = torch.Generator().manual_seed(14)
     Hq, Hkv, D, page, n = 8, 2, 128, 32, 3000

@@ -281,6 +281,30 @@ def test_in_one_call_or_in_several(D, n, pieces, e4m3):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,n", [(28, 4, 128, 77), (16, 4, 64, 4100)])
+def test_append_of_a_fused_projection_in_place(Hq, Hkv, D, n):
+    """q, k and v are slices of one tensor, and q comes back where it was."""
+    g = torch.Generator().manual_seed(121)
+    eng = engine(Hq, Hkv, D)
+    r, _, _ = turn(D, [D // 2], False)
+    qkv, w = rand(g, n, Hq + 2 * Hkv, D), rand(g, D)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    table, a = pool(g, [n], 16, Hkv, D, False)
+    b = binding.PagedCache(a.k_pages.clone(), a.v_pages.clone())
+    cu, lens, before = cumulative([n]), torch.tensor([n], dtype=torch.int32, device="cuda"), qkv.clone()
+    want = eng.paged_append(a, q, k, v, cu, table, lens, r, q_norm=w, k_norm=w)
+    assert torch.equal(qkv, before)
+    assert eng.paged_append(b, q, k, v, cu, table, lens, r, q_norm=w, k_norm=w, q_out=q) is q
+    assert torch.equal(q, want) and torch.equal(qkv[:, Hq:], before[:, Hq:])
+    assert torch.equal(a.k_pages, b.k_pages) and torch.equal(a.v_pages, b.v_pages)
+    # heads in front of tokens
+    c = binding.PagedCache(torch.zeros_like(a.k_pages), torch.zeros_like(a.v_pages))
+    qt, kt, vt = (before[:, x].transpose(0, 1).contiguous().transpose(0, 1) for x in (slice(0, Hq), slice(Hq, Hq + Hkv), slice(Hq + Hkv, None)))
+    assert torch.equal(eng.paged_append(c, qt, kt, vt, cu, table, lens, r, q_norm=w, k_norm=w), want)
+    used = table[0].long()
+    assert torch.equal(c.k_pages[used].transpose(1, 2).reshape(-1, Hkv, D)[:n], a.k_pages[used].transpose(1, 2).reshape(-1, Hkv, D)[:n])
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_append_of_rows_without_a_place(e4m3):
     """Bad pages, lengths and bounds: reported, not followed; everything else is done."""
