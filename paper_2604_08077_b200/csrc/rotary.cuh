@@ -121,7 +121,7 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float* x) {
 
 constexpr int kRotateThreads = 128;                           // (256: 52 for 49 us of 16512 tokens, 236 for 222 of 65536 into 8-bit pages)
 constexpr int kRotateRing = 4;                                // rows of a group under way, and one in work
-// (CTAs an SM, ring: 6, 4 take 49.3 us for 16512 tokens rotated and 183.5 for 65536 into pages; 5, 4 51.1 and 201; 7, 4 50.7 and 190; 8, 4 55 and 200, spilling;
+// (CTAs an SM, ring: 6, 4 take 49.3 us for 16512 tokens rotated and 183.5 for 65536 into pages; 5, 4 51.1 and 201; 7, 4 50.7 and 190; 8, 4 55 and 200;
 // 6, 3 51 and 186; 6, 6 51 and 185)
 
 // kPages: 0 rows out; 1, 2 keys and values into pages of bf16, e4m3.  grid (tokens / kTokens).
