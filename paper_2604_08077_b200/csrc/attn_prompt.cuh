@@ -207,8 +207,8 @@ struct PromptTile {
     __device__ __forceinline__ bool masked(int j) const { return j >= first_masked || (j >= low_first && j < low_masked); }
     // the first masked step from step j on (n_steps: none)
     __device__ __forceinline__ int next_masked(int j) const {
-        const int low = max(j, low_first);
-        return min(low < low_masked ? low : max(j, first_masked), n_steps);
+        const int low = max(j, low_first), tail = max(j, first_masked);      // (a tile that begins among the first tokens: its tail in front of the border)
+        return min(low < low_masked ? min(low, tail) : tail, n_steps);
     }
 };
 
