@@ -576,8 +576,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             tc::mbar_init(&sm.k_empty[i], 1);
         }
         for (int i = 0; i < kVStages; ++i) {
-            tc::mbar_init(&sm.v_full[i], kCodes ? 2 * kPromptCodeWarps : 2);   // of both CTAs
-            tc::mbar_init(&sm.v_raw[i], 1);
+            tc::mbar_init(&sm.v_full[i], kCodes ? kPromptCodeWarps + 1 : 2);   // CTA 0's own, and CTA 1
+            tc::mbar_init(&sm.v_raw[i], kCodes ? kPromptCodeWarps : 1);
             tc::mbar_init(&sm.v_empty[i], 1);
         }
         for (int i = 0; i < kRawStages; ++i) {
@@ -823,7 +823,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             __syncwarp();
             if (lane == 0) {
                 tc::mbar_arrive(&sm.row_factor_full[slot]);
-                tc::mbar_arrive_cluster(q_peer0 + qs * 8);
+                tc::mbar_arrive_release_cluster(q_peer0 + qs * 8);
             }
             __syncwarp();
             return true;
@@ -835,7 +835,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
         auto place = [&](int chunk) -> uint32_t { return D == 128 ? sw128(row0, chunk) : row0 * 64 + ((chunk ^ ((row0 >> 1) & 3)) << 4); };
         const uint32_t to0 = smem_u32(sm.v[0]) + place(2 * c), to1 = smem_u32(sm.v[0]) + place(2 * c + 1);
         const uint32_t raw0 = smem_u32(sm.raw_v[0]) + (part * kPieces * 32 + lane) * 16, scale0 = smem_u32(sm.raw_vs[0]) + row0;
-        const uint32_t full0 = cluster_address(sm.v_full, 0);
+        uint64_t* const full = rank == 0 ? sm.v_full : sm.v_raw;   // (CTA 1's are passed on to CTA 0's issuing warp)
         const uint32_t odd0 = cluster_address(sm.odd_tile, 0), odd1 = cluster_address(sm.odd_tile, 1);
         int st = 0, ph = 1, raw = 0, raw_ph = 0, gs = 0;
         bool ok = split_q(0);
@@ -908,7 +908,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    tc::mbar_arrive_cluster(full0 + st * 8);  // (what was written is this SM's own to read)
+                    tc::mbar_arrive(&full[st]);
                     tc::mbar_arrive(&sm.rv_empty[raw]);
                 }
                 __syncwarp();
@@ -1004,12 +1004,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                         }
                         if (lane < 2)                         // (keys of other sequences among them: the rows look for themselves)
                             asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"((lane ? odd1 : odd0) + (look.k % kPromptOddSlots) * 4), "r"(look.k + 1) : "memory");
-                        // (for the other CTA's memory alone, and dear: 1 us of every masked step, had it been outside)
                         asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
                     }
                     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) tc::mbar_arrive_cluster(v_bar0 + look.st * 8);
+                    if (lane == 0) tc::mbar_arrive_release_cluster(v_bar0 + look.st * 8);
                     __syncwarp();
                     if (++look.st == kVStages) look.st = 0;
                     ++look.j;
@@ -1096,17 +1095,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             }
         }
     } else if (warp == kMmaWarp && rank == 1) {
-        // ------------------------------------------------------------ CTA 1: Q is there, said to the issuing warp of CTA 0 (8-bit pages: by those that split it)
+        // ------------------------------------------------------------ CTA 1: Q is there, said to the issuing warp of CTA 0 (8-bit pages: by those that
+        // split it).  8-bit pages: V is there, too.  (What a thread of this CTA has written is visible to one of the other's behind a release of the
+        // cluster's scope.  It is this thread's, which has written nothing: by the four warps that write V, 350 for 268 us of proposed tokens)
         if (lane == 0) {
-            for (int k = 0;; ++k) {
+            [[maybe_unused]] const uint32_t v_bar0 = cluster_address(sm.v_full, 0);
+            [[maybe_unused]] int st = 0, ph = 0;
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
                 const int slot = k % kPromptPlans;
-                if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit) || sm.tile[slot].n_steps == 0) break;
+                if (!tc::mbar_wait(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit)) break;
+                const int n_steps = sm.tile[slot].n_steps;
+                if (n_steps == 0) break;
                 if (!kCodes) {
                     if (!tc::mbar_wait(&sm.q_full[k & 1], (k >> 1) & 1, abort_flag)) break;
                     asm volatile("fence.acq_rel.cluster;\n" ::: "memory");
                     tc::mbar_arrive_cluster(cluster_address(&sm.q_peer[k & 1], 0));
                 }
                 tc::mbar_arrive(&sm.plan_empty[slot]);
+                for (int j = 0; kCodes && j < n_steps; ++j) {
+                    if (!(ok = tc::mbar_wait(&sm.v_raw[st], ph, abort_flag))) break;
+                    tc::mbar_arrive_release_cluster(v_bar0 + st * 8);
+                    if (++st == kVStages) { st = 0; ph ^= 1; }
+                }
             }
         }
     } else if (warp == kMmaWarp) {
@@ -1131,10 +1142,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 if (s_left == 0) {
                     if (ended) return false;
                     const int kn = ks + 1, slot = kn % kPromptPlans;
-                    auto there = [&](uint64_t* bar, uint32_t phase) -> bool { return must ? (ok = tc::mbar_wait(bar, phase, abort_flag, plan_limit)) : tc::mbar_test(bar, phase); };
-                    if (!there(&sm.plan_full[slot], (kn / kPromptPlans) & 1)) return false;
+                    auto there = [&](uint64_t* bar, uint32_t phase, auto pair) -> bool {
+                        return must ? (ok = tc::mbar_wait<pair.value>(bar, phase, abort_flag, plan_limit)) : tc::mbar_test<pair.value>(bar, phase);
+                    };
+                    const std::false_type own;
+                    const std::true_type both;                // (both CTAs' threads arrive)
+                    if (!there(&sm.plan_full[slot], (kn / kPromptPlans) & 1, own)) return false;
                     if ((ended = sm.tile[slot].n_steps == 0)) return false;
-                    if ((!kCodes && !there(&sm.q_full[kn & 1], (kn >> 1) & 1)) || !there(&sm.q_peer[kn & 1], (kn >> 1) & 1)) return false;
+                    if ((!kCodes && !there(&sm.q_full[kn & 1], (kn >> 1) & 1, own)) || !there(&sm.q_peer[kn & 1], (kn >> 1) & 1, both)) return false;
                     ks = kn;
                     n_steps2 = n_steps1;
                     n_steps1 = n_steps0;
@@ -1170,7 +1185,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                     while (ahead < kPromptBufs && next_scores(ahead == 0)) {}
                     if (!ok || ahead == 0) { ok = false; break; }  // no more
                     if (j == 0) steps = ks == k ? n_steps0 : ks == k + 1 ? n_steps1 : n_steps2;
-                    if (!(ok = tc::mbar_wait(&sm.v_full[vst], vph, abort_flag))) break;
+                    if (!(ok = tc::mbar_wait<true>(&sm.v_full[vst], vph, abort_flag))) break;
                     if (j == 0 && k > 0 && !(ok = tc::mbar_wait(&sm.o_free, (k - 1) & 1, abort_flag))) break;
                     if (!(ok = tc::mbar_wait(&sm.p_full[buf], buf_ph, abort_flag))) break;
                     tc::tc_fence_after_sync();
