@@ -844,6 +844,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             if (!(ok = tc::mbar_wait_warp(&sm.plan_full[slot], (k / kPromptPlans) & 1, abort_flag, plan_limit))) break;
             const PromptTile t = sm.tile[slot];
             if (t.n_steps == 0) break;
+            bool split = false;
             for (int j = 0; j < t.n_steps; ++j, ++gs) {
                 if (!(ok = tc::mbar_wait_warp(&sm.rv_full[raw], raw_ph, abort_flag))) break;
                 // the keys' powers of two.  (Their slot's last readers, kPromptFactorSlots steps ago, are through: the step before this has found its
@@ -914,7 +915,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 __syncwarp();
                 if (++st == kVStages) { st = 0; ph ^= 1; }
                 if (++raw == kRawStages) { raw = 0; raw_ph ^= 1; }
-                if (j == 0 && !(ok = split_q(k + 1))) break;  // beside the first steps of this tile
+                // the next tile's Q beside the first steps of this one, or where it is planned: no step waits for a plan
+                if (!split && (j == t.n_steps - 1 || __all_sync(0xffffffffu, tc::mbar_test(&sm.plan_full[(k + 1) % kPromptPlans], ((k + 1) / kPromptPlans) & 1)))) {
+                    if (!(ok = split_q(k + 1))) break;
+                    split = true;
+                }
             }
             if (lane == 0) tc::mbar_arrive(&sm.plan_empty[slot]);
         }
