@@ -248,18 +248,26 @@ __global__ void __launch_bounds__(kRotateThreads, 6) rotate_kernel(const __grid_
                     const float r = rsqrtf(v);
                     return fmaf(0.5f * r, fmaf(-v * r, r, 1.f), r);
                 };
-                float s = sum_of_squares(), f = root(s * (1.f / D) + a.eps);
-                if (__any_sync(0xffffffffu, !(s < 0x1p126f))) {   // rare: squares that leave 32 bits (eps is nothing beside them)
-                    const float down = !(s < 0x1p126f) ? 0x1p-70f : 1.f;
-                    const unsigned long long down2 = pack_f32x2(down, down);
+                float v = sum_of_squares() * (1.f / D) + a.eps;
+                // rare: squares that leave 32 bits at either end, or an eps that nearly does.  (2^-100 <= v < 2^118 by v's bits, one comparison)
+                if (__any_sync(0xffffffffu, __float_as_uint(v) - 0x0d800000u >= 0x7a800000u - 0x0d800000u)) {
+                    const float by = v < 0x1p-100f ? 0x1p100f : !(v < 0x1p118f) ? 0x1p-70f : 1.f;
+                    auto times = [&](float y) {
+                        const unsigned long long y2 = pack_f32x2(y, y);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[0][i] = mul_f32x2(x[0][i], down2);
-                        x[1][i] = mul_f32x2(x[1][i], down2);
+                        for (int i = 0; i < 4; ++i) {
+                            x[0][i] = mul_f32x2(x[0][i], y2);
+                            x[1][i] = mul_f32x2(x[1][i], y2);
+                        }
+                    };
+                    times(by);
+                    v = sum_of_squares() * (1.f / D) + a.eps * by * by;
+                    if (v == INFINITY) {                      // beside an infinity what is finite becomes zeros
+                        times(0.f);
+                        v = 1.f;
                     }
-                    s = sum_of_squares();
-                    if (down != 1.f) f = s == INFINITY ? 0.f : root(s * (1.f / D));   // (beside an infinity what is finite becomes zeros)
                 }
+                const float f = root(v);
                 const unsigned long long f2 = pack_f32x2(f, f);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
