@@ -261,11 +261,11 @@ constexpr int kPromptMostSteps = 1 << 24;
 __host__ __device__ constexpr int prompt_steps(int n) { return ((n - 1) >> 7) + 1; }
 
 // The order of the items (tiles, or parts of them): levels from many steps to few, sequences in order, tiles, kv heads, parts.  A warp walks
-// it, with 32 sequences in its lanes.  Parts come first: an item's number is its part's.  (With a window a tile's level is the bound on its
-// steps where it would be more.)
+// it, with 32 sequences in its lanes.  Parts come first: an item's number is its part's.  (Pages: whole tiles alone, cut ones are PromptLine's; with a
+// window a tile's level is the bound on its steps where it would be more.)
 template <bool kPaged>
 struct PromptWalk {
-    int level, unit;                                          // unit 0: nothing is cut
+    int level, unit;                                          // unit 0: nothing is cut (packed rows alone, as part and parts are)
     int below;                                                // most steps of a tile of fewer than `level`, among the sequences seen so far
     int chunk, base;                                          // number of the first item of (level, chunk)
     int held;                                                 // chunk of `mine`, this lane's sequence
@@ -275,9 +275,9 @@ struct PromptWalk {
     int tile, gk, part, parts;
 
     // false: a sequence leaves the tensors
-    __device__ __forceinline__ bool begin(const PromptGeom& g, bool cut, int n_pairs, int lane) {
+    __device__ __forceinline__ bool begin(const PromptGeom& g, [[maybe_unused]] bool cut, [[maybe_unused]] int n_pairs, int lane) {
         bool fine = true;
-        long long steps = 0;                                  // at least as many as there are
+        [[maybe_unused]] long long steps = 0;                 // at least as many as there are
         level = chunk = base = below = 0;
         for (held = 0; held * 32 < g.batch; ++held) {
             mine.nt = 0;
@@ -285,28 +285,30 @@ struct PromptWalk {
                 fine = mine.load(g, held * 32 + lane) && fine;
                 if (mine.nt > 0) {
                     const int longest = max(1, prompt_steps(mine.nk));
-                    const long long all = (long long)mine.nt * (max(mine.off, 0) / 128 + 2) + (long long)g.T * mine.nt * (mine.nt + 1) / 128;
                     level = max(level, kPaged ? min(longest, g.most_steps) : longest);
-                    steps += kPaged ? min(all, (long long)mine.nt * g.most_steps) : all;
+                    if constexpr (!kPaged) steps += (long long)mine.nt * (max(mine.off, 0) / 128 + 2) + (long long)g.T * mine.nt * (mine.nt + 1) / 128;
                 }
             }
         }
         --held;
         level = (int)__reduce_max_sync(0xffffffffu, (unsigned)level);
-        unit = 0;
-        if (cut) {
+        if constexpr (!kPaged) {
+            unit = 0;
+            if (cut) {
 #pragma unroll
-            for (int x = 16; x > 0; x >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, x);
-            unit = (int)max((steps * g.Hkv + n_pairs - 1) / n_pairs, (long long)kPromptMinUnit);
+                for (int x = 16; x > 0; x >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, x);
+                unit = (int)max((steps * g.Hkv + n_pairs - 1) / n_pairs, (long long)kPromptMinUnit);
+            }
         }
         return fine;
     }
-    __device__ __forceinline__ int parts_of(int steps) const { return unit > 0 ? max((2 * steps + unit) / (2 * unit), 1) : 1; }
+    __device__ __forceinline__ int parts_of(int steps) const { return !kPaged && unit > 0 ? max((2 * steps + unit) / (2 * unit), 1) : 1; }
     // item `number`, which is no smaller than the one before; false: there are not so many (of cut tiles)
     __device__ __forceinline__ bool find(const PromptGeom& g, int number, int lane, bool cut_only = false) {
         while (level > 0) {
-            parts = parts_of(level);
-            if (cut_only && parts == 1) return false;
+            const int n_parts = parts_of(level);              // (pages: 1)
+            if constexpr (!kPaged) parts = n_parts;
+            if (cut_only && n_parts == 1) return false;
             if (held != chunk) {                              // (up to 32 sequences: never)
                 held = chunk;
                 mine.nt = 0;
@@ -315,7 +317,7 @@ struct PromptWalk {
             int first = 0, n = 0;
             if (mine.nt > 0) {
                 first = level == 1 ? 0 : mine.tiles_up_to(g, 128 * (level - 1));
-                n = ((kPaged && level == g.most_steps ? mine.nt : mine.tiles_up_to(g, 128 * level)) - first) * g.Hkv * parts;
+                n = ((kPaged && level == g.most_steps ? mine.nt : mine.tiles_up_to(g, 128 * level)) - first) * g.Hkv * n_parts;
             }
             int upto = n;
 #pragma unroll
@@ -333,8 +335,10 @@ struct PromptWalk {
                 seq.nk = __shfl_sync(0xffffffffu, mine.nk, who);
                 seq.off = __shfl_sync(0xffffffffu, mine.off, who);
                 if (kPaged) seq.b = chunk * 32 + who;
-                part = i % parts;
-                i /= parts;
+                if constexpr (!kPaged) {
+                    part = i % n_parts;
+                    i /= n_parts;
+                }
                 g.div_kv.divmod(i, tile, gk);
                 tile += __shfl_sync(0xffffffffu, first, who);
                 return true;
@@ -660,7 +664,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
             run_end = runs.begin(pair + 1);
             more = run_first < run_end && line.seek(g, run_first, lane);
         } else {
-            fine = w.begin(g, !kPaged && partial != nullptr, n_pairs, lane);
+            fine = w.begin(g, partial != nullptr, n_pairs, lane);
         }
         if (!fine && blockIdx.x == 0 && status != nullptr) atomicExch(status, 1);
         for (int k = 0;; ++k) {
@@ -681,27 +685,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                 }
                 if (found && lane == 0) sm.tile[slot] = t;
             } else {
-            const int number = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
-            found = w.find(g, number, lane);
-            if constexpr (kPaged) {
-                if (found) {
-                    const PromptSpan x(g, w.seq, w.tile);
-                    tile_of_pages(t, w.seq, w.tile, w.gk, x, 0, x.n);
-                    t.part = -1;
+                const int number = k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair);
+                found = w.find(g, number, lane);
+                if constexpr (kPaged) {
+                    if (found) {
+                        const PromptSpan x(g, w.seq, w.tile);
+                        tile_of_pages(t, w.seq, w.tile, w.gk, x, 0, x.n);
+                        t.part = -1;
+                        if (lane == 0) sm.tile[slot] = t;
+                    }
+                } else if (found) {
+                    const int tok = w.first_token(g, rank), begin = w.part * w.level / w.parts;
+                    t.q0 = w.seq.q0 + tok;
+                    t.n_tok = w.tokens(g, rank);
+                    t.k0 = w.seq.k0 + begin * 128;                // a part counts its keys from its own first one
+                    t.last0 = w.seq.off + tok - begin * 128;
+                    t.gk = w.gk;
+                    t.n_steps = (w.part + 1) * w.level / w.parts - begin;
+                    t.first_masked = max((max(w.seq.off + w.first_token(g, 0) + 1, 0) >> 7) - begin, 0);
+                    t.part = w.parts > 1 ? number : -1;
                     if (lane == 0) sm.tile[slot] = t;
                 }
-            } else if (found) {
-                const int tok = w.first_token(g, rank), begin = w.part * w.level / w.parts;
-                t.q0 = w.seq.q0 + tok;
-                t.n_tok = w.tokens(g, rank);
-                t.k0 = w.seq.k0 + begin * 128;                // a part counts its keys from its own first one
-                t.last0 = w.seq.off + tok - begin * 128;
-                t.gk = w.gk;
-                t.n_steps = (w.part + 1) * w.level / w.parts - begin;
-                t.first_masked = max((max(w.seq.off + w.first_token(g, 0) + 1, 0) >> 7) - begin, 0);
-                t.part = w.parts > 1 ? number : -1;
-                if (lane == 0) sm.tile[slot] = t;
-            }
             }
             if (!found) {
                 if (lane == 0) {
@@ -1171,9 +1175,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(prompt_threads(kKeys
                                               tc::smem_desc_from_halves(kb + (x % (D / 32)) * kKStep, kCodesDescHi), kIdescCodes, x > 0);
                 } else {
 #pragma unroll
-                for (int x = 0; x < kQKSteps; ++x)
-                    tc::umma_ss_pair(dst, tc::smem_desc_from_halves(qa + (x >> 2) * kQPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128),
-                                     tc::smem_desc_from_halves(kb + (x >> 2) * kKPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128), kIdescS, x > 0);
+                    for (int x = 0; x < kQKSteps; ++x)
+                        tc::umma_ss_pair(dst, tc::smem_desc_from_halves(qa + (x >> 2) * kQPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128),
+                                         tc::smem_desc_from_halves(kb + (x >> 2) * kKPanelStep + (x & 3) * kKStep, tc::kSmemDescHiSw128), kIdescS, x > 0);
                 }
                 tc::umma_commit_pair(&sm.s_full[sbuf]);
                 tc::umma_commit_pair(&sm.k_empty[kst]);
