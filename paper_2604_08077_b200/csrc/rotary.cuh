@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kRotateThreads, 6) rotate_kernel(const __grid_
     const bool rotated = l < pc, adjacent = a.adjacent != 0;
     const int c0 = rotated ? l : 2 * l, c1 = rotated ? l + pc : 2 * l + 1;
     // The rows ahead: heads g, g + kGroups, ... of q, of k, of v.
-    int kind_ahead = -1, left_ahead = 0, head_ahead = 0;      // (left: heads of the kind from the first group's on)
+    int kind_ahead = -1, left_ahead = 0;                      // (left: heads of the kind from the first group's on)
     const __nv_bfloat16* ahead = nullptr;
     long long step_ahead = 0;
     auto load_row = [&](int slot) {
@@ -146,7 +146,6 @@ __global__ void __launch_bounds__(kRotateThreads, 6) rotate_kernel(const __grid_
             ++kind_ahead;
             const RowsIn& src = kind_ahead == 0 ? a.q : kind_ahead == 1 ? a.k : a.v;
             left_ahead = kind_ahead == 0 ? a.Hq : a.Hkv;
-            head_ahead = g;
             ahead = src.p + (long long)min(at, a.n - 1) * src.ts + g * src.hs;
             step_ahead = kGroups * src.hs;
         }
