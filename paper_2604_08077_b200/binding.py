@@ -429,6 +429,10 @@ class PagedCache:
                                   v_scale.data_ptr() if fmt else None, self.page_stride, stride_of(k_scale, v_scale) if fmt else 0,
                                   self.n_pages, self.page_size, fmt)
 
+    def __reduce__(self):                                      # (a copy has the addresses of its own tensors)
+        return type(self), (self.k_pages, self.v_pages, self.k_scale, self.v_scale)
+
+
 class Rotary:
     """A rotation of a head's pairs by the positions of its token (see adaspark_attn_rotary_t).  sections: how many pairs follow each axis of
     the positions, one axis behind the other (default: all head_dim / 2 on one), pair i turning by theta^(-i / pairs) per position; frequencies and
@@ -456,7 +460,11 @@ class Rotary:
         if 2 * len(frequencies) > head_dim:
             _refuse(f"Rotary: {len(frequencies)} pairs in a head of {head_dim}")
         self.struct = adaspark_attn_rotary_init(frequencies, axis, axes, adjacent)
-        self.address, self.axes, self.pairs, self.head_dim = ctypes.addressof(self.struct), axes, len(frequencies), head_dim
+        self.axes, self.pairs, self.head_dim = axes, len(frequencies), head_dim
+
+    @property
+    def address(self) -> int:                                  # (worked out anew: a copy has a struct of its own)
+        return ctypes.addressof(self.struct)
 
 
 class AdaSAttn:
