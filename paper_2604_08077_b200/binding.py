@@ -329,17 +329,24 @@ def adaspark_attn_paged_decode(handle: int, q, k_new, v_new, pages: bytes, block
 
 def adaspark_attn_paged_decode_window(handle: int, q, k_new, v_new, pages: bytes, block_table, table_width: int, kv_len, batch: int, out, lse,
                                       workspace, workspace_bytes: int, status, window: int, sinks: int, stream: Optional[int]):
-    st = (_lib or load()).adaspark_attn_paged_decode_window(handle, pages + _PAGED_DECODE.pack(
-        *q, *k_new, *v_new, kv_len or 0, block_table or 0, out or 0, lse or 0, workspace or 0, workspace_bytes, status or 0, batch, table_width) +
-        _WINDOW.pack(window, sinks), stream)
+    try:
+        call = pages + _PAGED_DECODE.pack(*q, *k_new, *v_new, kv_len or 0, block_table or 0, out or 0, lse or 0, workspace or 0, workspace_bytes, status or 0, batch,
+                                          table_width) + _WINDOW.pack(window, sinks)
+    except struct.error as e:
+        _refuse(f"paged_decode_window: window {window}, sinks {sinks}: {e}")
+    st = (_lib or load()).adaspark_attn_paged_decode_window(handle, call, stream)
     if st != OK:
         _check(handle, st)
 
 
 def adaspark_attn_paged_prompt(handle: int, q, pages: bytes, cu, batch: int, n: int, block_table, table_width: int, kv_len, window: int, sinks: int,
                                out, lse, workspace, workspace_bytes: int, status, stream: Optional[int]):
-    st = (_lib or load()).adaspark_attn_paged_prompt(handle, pages + _PAGED_PROMPT.pack(
-        *q, cu or 0, kv_len or 0, block_table or 0, out or 0, lse or 0, workspace or 0, workspace_bytes, status or 0, batch, n, table_width, window, sinks, 0), stream)
+    try:
+        call = pages + _PAGED_PROMPT.pack(*q, cu or 0, kv_len or 0, block_table or 0, out or 0, lse or 0, workspace or 0, workspace_bytes, status or 0, batch, n, table_width,
+                                          window, sinks, 0)
+    except struct.error as e:
+        _refuse(f"paged_prompt: window {window}, sinks {sinks}: {e}")
+    st = (_lib or load()).adaspark_attn_paged_prompt(handle, call, stream)
     if st != OK:
         _check(handle, st)
 
@@ -356,15 +363,23 @@ def adaspark_attn_rotary_init(radians, axis, axes: int, adjacent: bool) -> Rotar
 
 def adaspark_attn_rotate(handle: int, q, k, q_out, k_out, positions, rotary: Optional[int], q_norm, k_norm, eps: float, n: int, stream: Optional[int]):
     """rotary: address of a RotaryStruct, or None."""
-    st = (_lib or load()).adaspark_attn_rotate(handle, _ROTATE.pack(*q, *k, *q_out, *k_out, positions or 0, rotary or 0, q_norm or 0, k_norm or 0, eps, n), stream)
+    try:
+        call = _ROTATE.pack(*q, *k, *q_out, *k_out, positions or 0, rotary or 0, q_norm or 0, k_norm or 0, eps, n)
+    except (struct.error, OverflowError) as e:
+        _refuse(f"rotate: eps {eps}: {e}")
+    st = (_lib or load()).adaspark_attn_rotate(handle, call, stream)
     if st != OK:
         _check(handle, st)
 
 
 def adaspark_attn_paged_append(handle: int, q, k, v, q_out, pages: bytes, cu, batch: int, n: int, block_table, table_width: int, kv_len, positions,
                                rotary: Optional[int], q_norm, k_norm, eps: float, status, stream: Optional[int]):
-    st = (_lib or load()).adaspark_attn_paged_append(handle, pages + _PAGED_APPEND.pack(
-        *q, *k, *v, *q_out, cu or 0, kv_len or 0, block_table or 0, positions or 0, rotary or 0, q_norm or 0, k_norm or 0, status or 0, eps, batch, n, table_width), stream)
+    try:
+        call = pages + _PAGED_APPEND.pack(*q, *k, *v, *q_out, cu or 0, kv_len or 0, block_table or 0, positions or 0, rotary or 0, q_norm or 0, k_norm or 0, status or 0, eps, batch,
+                                          n, table_width)
+    except (struct.error, OverflowError) as e:
+        _refuse(f"paged_append: eps {eps}: {e}")
+    st = (_lib or load()).adaspark_attn_paged_append(handle, call, stream)
     if st != OK:
         _check(handle, st)
 
