@@ -1621,7 +1621,7 @@ template <int D, bool kPaged>
 __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptGeom g, int n_pairs, const float* partial, __nv_bfloat16* out, float* lse) {
     constexpr int kLanes = D / 4, kRows = 32 / kLanes;        // threads of a row, rows of a warp
     __shared__ PromptSeq<kPaged> seq;
-    __shared__ int part_at[kPromptSlots], n_parts, tile, gk;
+    __shared__ int part_at[kPaged ? kPromptSlots : 1], n_parts, tile, gk;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (warp == 0) {
         int n = 0;
@@ -1653,7 +1653,6 @@ __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptG
             w.begin(g, true, n_pairs, lane);
             if (w.find(g, blockIdx.x, lane, true) && w.part == 0) {
                 n = w.parts;
-                for (int i = lane; i < n; i += 32) part_at[i] = blockIdx.x + i;
                 if (lane == 0) {
                     seq = w.seq;
                     tile = w.tile;
@@ -1684,7 +1683,8 @@ __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptG
             float4 o[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const size_t at = (size_t)part_at[min(p0 + i, parts - 1)] * 256 + row;
+                const int p = min(p0 + i, parts - 1);
+                const size_t at = (size_t)(kPaged ? part_at[p] : (int)blockIdx.x + p) * 256 + row;
                 s[i] = stats[at];
                 o[i] = *reinterpret_cast<const float4*>(partial + at * D + 4 * d4);
             }
@@ -1692,19 +1692,26 @@ __global__ void __launch_bounds__(kPromptJoinThreads) prompt_join_kernel(PromptG
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (p0 + i < parts && s[i].y != 0.f) top = fmaxf(top, s[i].x);      // (0: the row sees none of the part's keys)
-            const MovedBy c(l != 0.f ? m - top : -INFINITY);
-            l = c.of(l);
-            acc = make_float4(c.of(acc.x), c.of(acc.y), c.of(acc.z), c.of(acc.w));
+            if (p0 > 0) {
+                const MovedBy c(l != 0.f ? m - top : -INFINITY);
+                l = c.of(l);
+                acc = make_float4(c.of(acc.x), c.of(acc.y), c.of(acc.z), c.of(acc.w));
+            }
             m = top;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (p0 + i >= parts || s[i].y == 0.f) continue;
-                const MovedBy f(s[i].x - m);
-                l = fmaf(s[i].y * f.b, f.a, l);
-                acc.x = fmaf(o[i].x * f.b, f.a, acc.x);
-                acc.y = fmaf(o[i].y * f.b, f.a, acc.y);
-                acc.z = fmaf(o[i].z * f.b, f.a, acc.z);
-                acc.w = fmaf(o[i].w * f.b, f.a, acc.w);
+                const float d = s[i].x - m, f = fast_exp2(fmaxf(d, -120.f));
+                if (d < -120.f) {                             // rare (two factors, as MovedBy; for every part: 0.9 us more)
+                    const float b = fast_exp2(d + 120.f);
+                    s[i].y *= b;
+                    o[i] = make_float4(o[i].x * b, o[i].y * b, o[i].z * b, o[i].w * b);
+                }
+                l = fmaf(s[i].y, f, l);
+                acc.x = fmaf(o[i].x, f, acc.x);
+                acc.y = fmaf(o[i].y, f, acc.y);
+                acc.z = fmaf(o[i].z, f, acc.z);
+                acc.w = fmaf(o[i].w, f, acc.w);
             }
         }
         const float inv = l != 0.f ? 1.f / l : 0.f;
