@@ -431,7 +431,8 @@ adaspark_status_t adaspark_attn_paged_read(adaspark_attn_t *handle, const adaspa
  * not there (the new token is written if its own is, whatever the other pages); the row becomes zeros (lse: -infinity), as it does
  * with kv_len 0, and where every score is -infinity.
  * Two sequences may share pages that neither of them appends to.
- * With 8-bit pages a row of q is held to 2^-28 of its largest magnitude: what is smaller there loses bits. */
+ * With 8-bit pages a row of q is held to 2^-28 of its largest magnitude: what is smaller there loses bits, as does a token's weight times its value's
+ * power of two below 2^-28 of the row's largest such product. */
 typedef struct {
     adaspark_attn_pages_t pages;
     adaspark_attn_rows_t q;            /* batch rows of Hq heads                                       */
@@ -458,8 +459,8 @@ adaspark_status_t adaspark_attn_paged_decode_window(adaspark_attn_t *handle, con
 /* Several new tokens per sequence, whose keys and values are in its pages already (adaspark_attn_paged_append, _paged_write): row
  * cu[b] + i of sequence b is token p = kv_len[b] - (cu[b+1] - cu[b]) + i and sees the tokens j <= p; with window > 0 those of them with j >
  * p - window or j < sinks.  Rows, masks, precision and what a row that sees nothing yields are those of adaspark_attn_prompt over what
- * adaspark_attn_paged_read gives; with 8-bit pages a row of q is held to 2^-18 of its largest magnitude (what is smaller there loses bits), and a row
- * of q that holds an infinity or no number yields no numbers.
+ * adaspark_attn_paged_read gives; with 8-bit pages a row of q is held to 2^-18 of its largest magnitude (what is smaller there loses bits: below 2^-10 of it;
+ * adaspark_attn_prompt over what is read back keeps all of them), and a row of q that holds an infinity or no number yields no numbers.
  * Pages that hold nothing that a row of the sequence sees are not read, and their numbers may be any; a page number outside [0, n_pages) among the
  * others sets status 1, and what such a page would hold counts as zeros.  A sequence whose rows leave the tensors sets
  * status 1 and is left out; one whose kv_len is negative or more than the table holds sets status 1, and its rows become rows that see
@@ -495,7 +496,8 @@ adaspark_status_t adaspark_attn_rotary_init(adaspark_attn_rotary_t *rotary, cons
                                             int32_t axes, int32_t adjacent);
 
 /* Queries and keys between the projection and the attention: every head is divided by the root of its mean square plus eps and multiplied by
- * the norm's weights (where they are given), then rotated (where a rotation is given).  In 32 bits, rounded once.
+ * the norm's weights (where they are given), then rotated (where a rotation is given).  In 32 bits, rounded once.  Rows of any magnitude: what a square
+ * or eps would lose at either end of the range is kept; zeros with an eps of 0 yield no numbers, and beside an infinity finite values become zeros.
  * An output may be the very rows of its input; otherwise it must not overlap them. */
 typedef struct {
     adaspark_attn_rows_t q, k;         /* n rows of Hq, Hkv heads; data NULL: none                     */

@@ -21,7 +21,7 @@
 // the present one:
 //   warps 0-15  softmax, two teams of two warpgroups that take the steps of 128 keys in turn; a row's keys are shared by two threads
 //   warp  16    TMA producer of K; masked steps: looks for values that are no numbers (below)
-//   warp  17    MMA issuer (CTA 0): S = Q K^T, O += P V (P in TMEM, V with its rows along d); CTA 1: passes on that its Q is there
+//   warp  17    MMA issuer (CTA 0): S = Q K^T, O += P V (P in TMEM, V with its rows along d); CTA 1: passes on that its Q (8-bit pages: its V) is there
 //   warp  18    TMA producer of V
 //   warp  19    planner: the next tiles and their Q
 // TMEM (512 columns): three score tiles of 128 columns, each with the weights (bf16 pairs) over the first 32 of either half, and O.  The
@@ -49,7 +49,8 @@
 // shared memory by four more warps (20-23), with its powers of two in it: the weights need more bits than an 8-bit operand has.  (K brought to
 // bf16, too: 2.89 against 2.75 ms of 2048 tokens over 65536 then.)  What bounds it is issue and fetch of instructions: 5300 instructions of warps a
 // step and CTA against 3100 of bf16 pages, and the stall that leads is that none is there (2.4 of 9.9 cycles an instruction; bf16 1.1); loops
-// that are rolled up are faster than the same unrolled.  Tried without gain: rows of few tokens twice, each copy with half of the keys; 8 warps for
+// that are rolled up are faster than the same unrolled.  24 warps leave a thread 80 registers: 94 bytes of it are spilled with heads of 64, 86 with heads of
+// 128 (bf16 pages, 20 warps and 96 registers: 18 bytes; packed rows: none).  Tried without gain: rows of few tokens twice, each copy with half of the keys; 8 warps for
 // the codes and registers moved between warpgroups (spills); more or fewer stages of K, V and codes; the keys' powers of two a step ahead.
 #pragma once
 #include <type_traits>

@@ -311,7 +311,10 @@ adaspark_status_t launch_rotate(adaspark_attn* h, const RotateCall& a, const Pag
     // 2400 17.1 / 13.8 / 13.5 / 15.7, 16512 85 / 62 / 49.6 / 55.5; into bf16 pages 65536 384 / 255 / 184 / 193; into 8-bit ones 33000 232 / 156 / 122 / 122,
     // 65536 452 / 302 / 231 / 222.  16 + 4 heads of 64 into bf16 pages and read back, at 2 / 4 / 8 / 16: 400 5.2 / 5.0 / 6.3 / 9.1, 701 6.0 / 5.6 / 6.4 / 9.1,
     // 2400 10.0 / 8.8 / 8.7 / 10.2 (8-bit pages 14.0 / 13.3 / 14.8 / 18.6), 9000 27.8 / 19.4 / 17.6 / 22.1, 33000 85 / 53 / 42 / 43; at 4682 calls one behind the
-    // other take 17.9 us with 4 (1.3 waves of CTAs) and 16.5 with 8
+    // other take 17.9 us with 4 (1.3 waves of CTAs) and 16.5 with 8.  The rule goes by tokens alone; other numbers of heads, with norms, us on the device: 8 + 2 of 128
+    // 300 tokens 4.5 / 4.2 / 4.7 / 6.3, 2400 12.9 / 9.4 / 9.1 / 9.6, 33000 140 / 78 / 61 / 53 (bf16 pages 157 / 84 / 62 / 54, 8-bit ones 178 / 107 / 72 / 59); 32 + 8 of 128
+    // 300 5.2 / 5.3 / 7.1 / 11.5, 2400 15.4 / 12.9 / 15.3 / 18.4, 33000 168 / 120 / 107 / 114; 8 + 1 of 64, at 2 / 4 / 8, 600 4.5 / 4.0 / 4.7, 3500 9.3 / 6.4 / 7.0, 9000
+    // 20.8 / 13.4 / 12.4: up to 14 % lie between the rule's choice and the best one with few heads and many tokens, 18 % with 32 + 8 at 2400
     if (h->cfg.head_dim == 128) {
         if (kPages == 2 && a.n >= kRotateMost) launch(rotate_kernel<128, 2, 8>, 8);
         else a.n >= kRotateMany ? launch(rotate_kernel<128, kPages, 4>, 4) : a.n >= kRotateFew ? launch(rotate_kernel<128, kPages, 2>, 2) : launch(rotate_kernel<128, kPages, 1>, 1);
